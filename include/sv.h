@@ -18,6 +18,9 @@
  *   sv_kv_append      commit of the accepted draft tokens to the cache, with
  *                     the representatives of the grown blocks refreshed (Section 2.1)
  *   sv_accept         acceptance of the draft tokens after verification (Eq. 2-3)
+ *   sv_rope_append, sv_chunk_attn, sv_sample   the serving loop around a verification
+ *                     step: new tokens rotated and written to the cache, their
+ *                     attention over it, and distributions and tokens from logits
  *   sv_anchor_jaccard / sv_pick_anchors   anchor-layer calibration       (Eq. 7-8)
  *   sv_select_blocks_global / _tokens, sv_token_overlap, sv_block_reps_bf16,
  *   sv_select_blocks_bf16reps   retrieval variants the paper discusses but does
@@ -466,6 +469,77 @@ SV_API sv_status sv_verify_step_from_host_direct(const sv_geom *geom, const sv_l
                                                  int32_t n_sink, int32_t n_local, int32_t *idx, int32_t *cnt, int32_t max_sel, void *out,
                                                  void *out_host, void *workspace, size_t workspace_bytes, int32_t *status_word,
                                                  int32_t refresh_tail, const uint8_t *refresh_which, void *stream);
+
+/*
+ * New tokens (a prompt, chunks of several prompts, single tokens, in one ragged batch): rotary positions applied to their queries
+ * and keys, keys and values written to the paged cache behind what it holds, representatives of the grown blocks refreshed.
+ *
+ * The batch is N = n_tokens rows; rows q_start[s] .. q_start[s + 1] - 1 are sequence s's (q_start[0] = 0, ascending, empty sequences
+ * allowed; rows from q_start[S] on belong to nobody and are left alone).  Row i of sequence s is the token at position p = seq_lens[s] + i.
+ * A rotated head x has, for j < rot_dim / 2, the pair (a, b) = (x[j], x[j + rot_dim / 2]) (interleaved == 0) or (x[2 j], x[2 j + 1])
+ * replaced by (a cos - b sin, b cos + a sin), cos = rope[p][j], sin = rope[p][rot_dim / 2 + j]; dims from rot_dim on are copied.  Products
+ * and sums are rounded to fp32 one by one, the result once to bf16.
+ *   q, k, v         dev bf16 rows [N][Hq][D], [N][Hkv][D]; the heads of a token are contiguous, tokens q_stride / k_stride / v_stride
+ *                   elements apart (multiples of 8), so that all three may be parts of one projection's output.  q may be NULL (then
+ *                   q_out too): the cache only
+ *   rope            dev fp32 [rope_rows][rot_dim] or NULL (no rotation; q_out is then a copy).  rot_dim: a multiple of 16, at most D.  A
+ *                   position outside the table takes its nearest row and sets SV_STATUS_INDEX
+ *   q_out           dev bf16 [N][Hq][D] contiguous; may be q itself
+ *   k_pool, v_pool  as in sv_kv_append, modified in place; block_table must hold pages for the blocks that are entered: tokens behind the
+ *                   last page of the table, or from a block on whose entry is not a page of the pool, are dropped
+ *   seq_lens_out    dev int32 [S], a different buffer than seq_lens: the lengths with the tokens that were written
+ *   reps            dev fp32 [S][Hkv][NBmax][D] or NULL: the representatives of the blocks that received tokens, bit for bit those of
+ *                   sv_block_reps
+ * geom->n_draft is not read.  One launch.
+ */
+SV_API sv_status sv_rope_append(const sv_geom *geom, void *k_pool, void *v_pool, int32_t n_pages, const int32_t *block_table,
+                                const int32_t *seq_lens, const void *q, const void *k, const void *v, int64_t q_stride,
+                                int64_t k_stride, int64_t v_stride, const int32_t *q_start, int32_t n_tokens, const float *rope,
+                                int32_t rope_rows, int32_t rot_dim, int32_t interleaved, void *q_out, int32_t *seq_lens_out,
+                                float *reps, int32_t *status_word, void *stream);
+
+/*
+ * Attention of such a batch over the cache that holds its own keys and values already (sv_rope_append): kv->seq_lens counts the new
+ * tokens too, so that row i of sequence s, of n rows, is at position p = seq_lens[s] - n + i and sees the cached tokens 0 .. p:
+ * softmax(softmax_scale * q . k) . v.  fp32 softmax and accumulation; probabilities are rounded to bf16 for the PV product.  A row that
+ * sees nothing (p < 0) has an output of zeros and an lse of -infinity.  Single tokens, chunks and whole prompts may share a batch: the
+ * keys of long sequences are split over the SMs and merged, so that a batch costs what its tokens cost however they are distributed.
+ *   q               dev bf16 [N][Hq][D] contiguous
+ *   q_start         dev int32 [S + 1], as above
+ *   softmax_scale   0 selects 1/sqrt(D)
+ *   out             dev bf16 [N][Hq][D]; lse: dev fp32 [N][Hq] or NULL.  Rows from q_start[S] on are left alone
+ *   workspace       dev scratch of sv_chunk_workspace_bytes bytes, 16-byte aligned.  Calls that may overlap need distinct ones
+ *   status_word     as in sv_verify_attn
+ * Lengths beyond the block table are cut to it; page ids outside the pool are clamped into it and set SV_STATUS_INDEX.  geom->n_draft is
+ * not read; G = Hq / Hkv <= 128.
+ */
+SV_API size_t sv_chunk_workspace_bytes(const sv_geom *geom, int32_t n_tokens);
+SV_API sv_status sv_chunk_attn(const sv_geom *geom, const void *q, const sv_kv *kv, const int32_t *q_start, int32_t n_tokens,
+                               float softmax_scale, void *out, float *lse, void *workspace, size_t workspace_bytes,
+                               int32_t *status_word, void *stream);
+
+/*
+ * From logits to distributions and tokens, by row: the first token of a prompt, a draft model's tokens and the distributions they were
+ * drawn from, the target's distributions that sv_accept takes.
+ *
+ * With e(x) = exp((logit(x) - max) / temperature) and the entries in descending order of their logits (equal ones: the smaller index
+ * first): the first top_k entries stay; of these, those whose predecessors have less than top_p of the mass of all of them; of these,
+ * those with e >= min_p.  The first entry always stays.  probs = e / sum of e over the entries that stayed, zero elsewhere; the token is
+ * the smallest x that stayed with sum_{y <= x} e(y) >= u * sum_y e(y), both sums over the entries that stayed in the order of the
+ * vocabulary.  temperature 0: the first entry alone.  A logit of -infinity or NaN is that of an entry that is not there; +infinity
+ * leaves the entries at +infinity, with equal shares.  A row without an entry has the token -1 and zeros.
+ *   logits          dev fp32 or (logits_bf16 != 0) bf16, rows row_stride elements apart, row_stride >= vocab
+ *   temperature, top_k, top_p, min_p   dev fp32 / int32, one entry for each rows_per_param rows (n_rows a multiple of it), or NULL: 1, and no
+ *                   restriction.  A negative or NaN temperature counts as 0; top_k <= 0, top_p >= 1 or NaN and min_p <= 0 or NaN
+ *                   restrict nothing
+ *   u               dev fp32 [n_rows] in [0, 1), from the caller; may be NULL when tokens is
+ *   tokens          dev int32 [n_rows] or NULL; probs: dev fp32 [n_rows][vocab] or NULL (not both NULL).  probs is what sv_accept takes
+ * Masses are summed as multiples of 2^-40 of the largest entry's, so sums do not depend on their order and results are reproducible.
+ * vocab <= 2^20 (SV_ERR_UNSUPPORTED).  One launch.
+ */
+SV_API sv_status sv_sample(int32_t n_rows, int32_t vocab, const void *logits, int32_t logits_bf16, int64_t row_stride,
+                           int32_t rows_per_param, const float *temperature, const int32_t *top_k, const float *top_p,
+                           const float *min_p, const float *u, int32_t *tokens, float *probs, void *stream);
 
 /* Number of KV splits (CTAs per (sequence, KV head)) that the workspace of this geometry has room for.  sv_verify_attn uses as many, or
  * fewer where the CTAs of a thread-block cluster merge their splits themselves (the workspace is then not written). */

@@ -31,7 +31,8 @@ EXPORTS = ("sv_strerror", "sv_status_word_check", "sv_budget_blocks", "sv_worksp
            "sv_select_blocks_tokens", "sv_token_overlap", "sv_select_blocks_global", "sv_accept",
            "sv_block_reps_bf16", "sv_select_blocks_bf16reps", "sv_layer_table_bytes", "sv_layer_table", "sv_workspace_bytes_layers",
            "sv_block_reps_layers", "sv_select_blocks_layers", "sv_verify_attn_layers", "sv_kv_append_layers", "sv_host_step_create",
-           "sv_host_step_destroy", "sv_verify_step_from_host", "sv_verify_step_from_host_direct", "sv_workspace_bytes_host_step")
+           "sv_host_step_destroy", "sv_verify_step_from_host", "sv_verify_step_from_host_direct", "sv_workspace_bytes_host_step",
+           "sv_rope_append", "sv_chunk_workspace_bytes", "sv_chunk_attn", "sv_sample")
 SV_MAX_LAYERS = 256
 SV_STACK_STATE_BYTES = 256   # what a stack's launches keep at the start of their workspace
 
@@ -97,6 +98,14 @@ def _load() -> ctypes.CDLL:
     lib.sv_block_reps_bf16.argtypes = [gp, kp, i32, i32, vp, vp]
     lib.sv_select_blocks_bf16reps.restype = ctypes.c_int
     lib.sv_select_blocks_bf16reps.argtypes = [gp, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, i32, vp, vp]
+    lib.sv_rope_append.restype = ctypes.c_int
+    lib.sv_rope_append.argtypes = [gp, vp, vp, i32, vp, vp, vp, vp, vp, i64, i64, i64, vp, i32, vp, i32, i32, i32, vp, vp, vp, vp, vp]
+    lib.sv_chunk_workspace_bytes.restype = sz
+    lib.sv_chunk_workspace_bytes.argtypes = [gp, i32]
+    lib.sv_chunk_attn.restype = ctypes.c_int
+    lib.sv_chunk_attn.argtypes = [gp, vp, kp, vp, i32, f32, vp, vp, vp, sz, vp, vp]
+    lib.sv_sample.restype = ctypes.c_int
+    lib.sv_sample.argtypes = [i32, i32, vp, i32, i64, i32, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.sv_accept.restype = ctypes.c_int
     lib.sv_accept.argtypes = [i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.sv_verify_attn_noalloc.restype = ctypes.c_int
@@ -272,6 +281,40 @@ def sv_accept(p_target, p_draft, tokens, parent, u_accept, u_next, path, n_path,
         raise ValueError("sv_accept: shapes disagree")
     _check(_native.accept(p_target, p_draft, tokens, parent, u_accept, u_next, path, n_path, next_token, alpha, stream),
            "sv_accept")
+
+
+def sv_rope_append(geom: sv_geom, k_pool, v_pool, block_table, seq_lens, q, k, v, q_start, q_out, seq_lens_out, rope=None,
+                   interleaved: bool = False, reps=None, status_word=None, stream=None) -> None:
+    """New tokens of a ragged batch: rotary positions on q (into q_out, which may be q) and k, k and v into the paged cache behind
+    the seq_lens tokens it holds, the new lengths to seq_lens_out (a different tensor), the representatives of the grown blocks.
+
+    q bfloat16 [N][Hq][128], k, v [N][Hkv][128]: tokens may be any multiple of 8 elements apart (slices of one projection's
+    output); q and q_out may be None.  q_start int32 [S + 1]: sequence s has rows q_start[s] .. q_start[s + 1] - 1.  rope float32
+    [positions][rot_dim], cos then sin; interleaved: pairs are neighbouring dims, else halves of the rotated ones."""
+    _check(_native.rope_append(geom, k_pool, v_pool, block_table, seq_lens, q, k, v, q_start, q_out, seq_lens_out, rope, interleaved,
+                               reps, status_word, stream), "sv_rope_append")
+
+
+def sv_chunk_workspace_bytes(geom: sv_geom, n_tokens: int) -> int:
+    """Scratch that sv_chunk_attn needs for a batch of this many new tokens, however they are distributed over the sequences."""
+    return int(_lib.sv_chunk_workspace_bytes(ctypes.byref(geom), n_tokens))
+
+
+def sv_chunk_attn(geom: sv_geom, q, kv: sv_kv, q_start, out, lse=None, workspace=None, softmax_scale: float = 0.0, status_word=None,
+                  stream=None) -> None:
+    """Causal attention of a ragged batch of new tokens over the paged cache that holds them (kv's seq_lens counts them: the
+    seq_lens_out of sv_rope_append).  q, out bfloat16 [N][Hq][128]; q_start int32 [S + 1]; lse optional float32 [N][Hq];
+    workspace of sv_chunk_workspace_bytes bytes."""
+    _check(_native.chunk_attn(geom, q, kv, q_start, out, lse, workspace, softmax_scale, status_word, stream), "sv_chunk_attn")
+
+
+def sv_sample(logits, u, tokens, probs=None, temperature=None, top_k=None, top_p=None, min_p=None, stream=None) -> None:
+    """Distributions and tokens from logits: temperature, then top-k, top-p and min-p; the token by inversion with the given u.
+
+    logits float32 or bfloat16 [R][V] or [S][T][V] (rows may be padded); u float32 [R]; outputs tokens int32 [R] (or None), probs
+    float32 [R][V] (or None; [S][T][V] is what sv_accept takes).  temperature, top_p, min_p float32 and top_k int32: one entry for
+    each of the R rows, or of the S sequences, or None."""
+    _check(_native.sample(logits, u, tokens, probs, temperature, top_k, top_p, min_p, stream), "sv_sample")
 
 
 def sv_pick_anchors(inter, uni, n_anchors: int):

@@ -554,10 +554,145 @@ PyObject *accept_new(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// Rows of heads: a CUDA tensor [tokens][heads][head_dim] whose heads are contiguous, tokens any number of elements apart.
+const at::Tensor &head_rows(PyObject *o, int64_t heads, int64_t dim, const char *name)
+{
+    if (THPVariable_Check(o)) {
+        const at::Tensor &t = THPVariable_Unpack(o);
+        if (t.is_cuda() && t.scalar_type() == at::kBFloat16 && t.dim() == 3 && t.size(1) == heads && t.size(2) == dim && t.stride(2) == 1 &&
+            (t.stride(1) == dim || heads == 1))
+            return t;
+    }
+    PyErr_Format(PyExc_TypeError, "%s: expected a CUDA tensor [tokens][%lld][%lld] of torch.bfloat16 with contiguous heads", name,
+                 (long long)heads, (long long)dim);
+    throw ArgError{};
+}
+[[noreturn]] void shapes_disagree(const char *call)
+{
+    PyErr_Format(PyExc_ValueError, "%s: shapes disagree", call);
+    throw ArgError{};
+}
+// Sizes that the library cannot see behind a pointer.
+void has(const at::Tensor &t, int64_t numel, const char *call)
+{
+    if (t.numel() != numel) shapes_disagree(call);
+}
+
+// geom, k_pool, v_pool, block_table, seq_lens, q, k, v, q_start, q_out, seq_lens_out, rope, interleaved, reps, status_word, stream
+PyObject *rope_append(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return checked(n, 16, [&] {
+        constexpr const char *call = "sv_rope_append";
+        const sv_geom g = geometry(a[0]);
+        const at::Tensor &kp = tensor(a[1], at::kBFloat16, "k_pool"), &vp = tensor(a[2], at::kBFloat16, "v_pool");
+        const at::Tensor &k = head_rows(a[6], g.n_kv_heads, g.head_dim, "k"), &v = head_rows(a[7], g.n_kv_heads, g.head_dim, "v");
+        const int64_t N = k.size(0);
+        has(tensor(a[3], at::kInt, "block_table"), (int64_t)g.n_seq * g.max_blocks, call);
+        has(tensor(a[4], at::kInt, "seq_lens"), g.n_seq, call);
+        has(tensor(a[8], at::kInt, "q_start"), (int64_t)g.n_seq + 1, call);
+        has(tensor(a[10], at::kInt, "seq_lens_out"), g.n_seq, call);
+        if (v.size(0) != N || N > INT32_MAX || !vp.sizes().equals(kp.sizes()) || kp.dim() != 4 || kp.size(1) != g.n_kv_heads || kp.size(2) != g.block_size)
+            shapes_disagree(call);
+        const void *q = nullptr;
+        int64_t q_stride = 0;
+        if (a[5] != Py_None) {
+            const at::Tensor &t = head_rows(a[5], g.n_q_heads, g.head_dim, "q");
+            if (t.size(0) != N || a[9] == Py_None) shapes_disagree(call);
+            has(tensor(a[9], at::kBFloat16, "q_out"), N * g.n_q_heads * g.head_dim, call);
+            q = t.data_ptr(), q_stride = t.stride(0);
+        }
+        void *const q_out = bf16(a[9], "q_out");
+        const float *rope = nullptr;
+        int32_t rope_rows = 0, rot = 0;
+        if (a[11] != Py_None) {
+            const at::Tensor &t = tensor(a[11], at::kFloat, "rope");
+            if (t.dim() != 2 || t.size(0) > INT32_MAX || t.size(1) > g.head_dim) shapes_disagree(call);
+            rope = t.data_ptr<float>(), rope_rows = (int32_t)t.size(0), rot = (int32_t)t.size(1);
+        }
+        const int32_t pairs = truth(a[12]) ? 1 : 0;
+        if (a[13] != Py_None) has(tensor(a[13], at::kFloat, "reps"), (int64_t)g.n_seq * g.n_kv_heads * g.max_blocks * g.head_dim, call);
+        float *const reps = f32(a[13], "reps");
+        int32_t *const word = i32(a[14], "status_word"), *const lens_out = i32(a[10], "seq_lens_out");
+        const int32_t *const table = i32(a[3], "block_table"), *const lens = i32(a[4], "seq_lens"), *const start = i32(a[8], "q_start");
+        void *const s = stream(a[15]);
+        return status(unlocked([&] {
+            return sv_rope_append(&g, kp.data_ptr(), vp.data_ptr(), (int32_t)kp.size(0), table, lens, q, k.data_ptr(), v.data_ptr(), q_stride,
+                                  k.stride(0), v.stride(0), start, (int32_t)N, rope, rope_rows, rot, pairs, q_out, lens_out, reps, word, s);
+        }));
+    });
+}
+
+// geom, q, kv, q_start, out, lse, workspace, softmax_scale, status_word, stream
+PyObject *chunk_attn(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return checked(n, 10, [&] {
+        constexpr const char *call = "sv_chunk_attn";
+        const sv_geom g = geometry(a[0]);
+        const at::Tensor &q = tensor(a[1], at::kBFloat16, "q"), &out = tensor(a[4], at::kBFloat16, "out");
+        const sv_kv kv = cache(a[2]);
+        const int64_t N = q.dim() ? q.size(0) : 0;
+        if (N > INT32_MAX || q.numel() != N * g.n_q_heads * g.head_dim || !out.sizes().equals(q.sizes())) shapes_disagree(call);
+        has(tensor(a[3], at::kInt, "q_start"), (int64_t)g.n_seq + 1, call);
+        if (a[5] != Py_None) has(tensor(a[5], at::kFloat, "lse"), N * g.n_q_heads, call);
+        const int32_t *const start = i32(a[3], "q_start");
+        float *const lse = f32(a[5], "lse");
+        const Scratch ws = scratch(a[6]);
+        const double scale = PyFloat_AsDouble(a[7]);
+        if (scale == -1.0 && PyErr_Occurred()) throw ArgError{};
+        int32_t *const word = i32(a[8], "status_word");
+        void *const s = stream(a[9]);
+        return status(unlocked([&] {
+            return sv_chunk_attn(&g, q.data_ptr(), &kv, start, (int32_t)N, (float)scale, out.data_ptr(), lse, ws.p, ws.bytes, word, s);
+        }));
+    });
+}
+
+// logits, u, tokens, probs, temperature, top_k, top_p, min_p, stream
+PyObject *sample(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return checked(n, 9, [&] {
+        constexpr const char *call = "sv_sample";
+        if (!THPVariable_Check(a[0])) {
+            PyErr_SetString(PyExc_TypeError, "logits: expected a CUDA tensor");
+            throw ArgError{};
+        }
+        const at::Tensor &x = THPVariable_Unpack(a[0]);
+        const bool half = x.scalar_type() == at::kBFloat16;
+        // rows a fixed distance apart: [rows][vocab] or [sequences][rows][vocab], the vocabulary contiguous
+        if (!x.is_cuda() || !(half || x.scalar_type() == at::kFloat) || (x.dim() != 2 && x.dim() != 3) || (x.size(-1) > 1 && x.stride(-1) != 1) ||
+            (x.dim() == 3 && x.size(0) > 1 && x.size(1) > 1 && x.stride(0) != x.size(1) * x.stride(1))) {
+            PyErr_SetString(PyExc_TypeError, "logits: expected a CUDA tensor of torch.float32 or torch.bfloat16 whose rows are contiguous and evenly spaced");
+            throw ArgError{};
+        }
+        const int64_t V = x.size(-1), per = x.dim() == 3 ? x.size(1) : 1, S = x.size(0), R = S * per;
+        const int64_t stride = R < 2 ? V : per > 1 ? x.stride(1) : x.stride(0);
+        if (V > INT32_MAX || R > INT32_MAX) shapes_disagree(call);
+        if (a[1] != Py_None) has(tensor(a[1], at::kFloat, "u"), R, call);
+        if (a[2] != Py_None) has(tensor(a[2], at::kInt, "tokens"), R, call);
+        if (a[3] != Py_None) has(tensor(a[3], at::kFloat, "probs"), R * V, call);
+        if (a[4] != Py_None) has(tensor(a[4], at::kFloat, "temperature"), S, call);
+        if (a[5] != Py_None) has(tensor(a[5], at::kInt, "top_k"), S, call);
+        if (a[6] != Py_None) has(tensor(a[6], at::kFloat, "top_p"), S, call);
+        if (a[7] != Py_None) has(tensor(a[7], at::kFloat, "min_p"), S, call);
+        const float *const u = f32(a[1], "u"), *const temperature = f32(a[4], "temperature"), *const top_p = f32(a[6], "top_p"),
+                    *const min_p = f32(a[7], "min_p");
+        int32_t *const tokens = i32(a[2], "tokens");
+        const int32_t *const top_k = i32(a[5], "top_k");
+        float *const probs = f32(a[3], "probs");
+        const void *const logits = x.data_ptr();
+        void *const s = stream(a[8]);
+        return status(unlocked([&] {
+            return sv_sample((int32_t)R, (int32_t)V, logits, half ? 1 : 0, stride, (int32_t)(per > 0 ? per : 1), temperature, top_k, top_p, min_p, u,
+                             tokens, probs, s);
+        }));
+    });
+}
+
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(block_reps), METHOD(select_blocks), METHOD(verify_attn), METHOD(kv_append), METHOD(accept),
                          METHOD(verify_layer), METHOD(layer_row), METHOD(workspace_bytes_layers), METHOD(workspace_bytes_host_step), METHOD(block_reps_layers),
-                         METHOD(verify_layers), METHOD(kv_append_layers), METHOD(accept_new), METHOD(host_step), METHOD(verify_step_from_host), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(verify_layers), METHOD(kv_append_layers), METHOD(accept_new), METHOD(host_step), METHOD(verify_step_from_host), METHOD(rope_append),
+                         METHOD(chunk_attn), METHOD(sample), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Argument marshalling for the entry points of sv.h.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

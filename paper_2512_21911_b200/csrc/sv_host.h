@@ -44,6 +44,20 @@ inline sv_status check_geom(const sv_geom *g)
     return SV_OK;
 }
 
+// Geometry of the calls on ragged batches of new tokens: those of check_geom that do not concern the draft.
+inline sv_status check_ragged(const sv_geom *g, int32_t n_tokens)
+{
+    if (!g) return SV_ERR_NULL;
+    if (g->n_seq < 1 || g->n_q_heads < 1 || g->n_kv_heads < 1 || g->max_blocks < 1 || n_tokens < 0) return SV_ERR_SHAPE;
+    if (g->n_q_heads % g->n_kv_heads) return SV_ERR_SHAPE;
+    if (g->head_dim != kHeadDim) return SV_ERR_UNSUPPORTED;
+    if (g->block_size != 64 && g->block_size != 128) return SV_ERR_UNSUPPORTED;
+    if (g->n_q_heads / g->n_kv_heads > kMaxRows) return SV_ERR_UNSUPPORTED;
+    if (g->n_seq > 65535 || g->n_kv_heads > 65535) return SV_ERR_SHAPE;
+    if ((int64_t)n_tokens * g->n_q_heads >= (int64_t)1 << 31 || (int64_t)g->max_blocks * g->block_size >= (int64_t)1 << 31) return SV_ERR_SHAPE;
+    return SV_OK;
+}
+
 inline sv_status check_kv(const sv_geom *g, const sv_kv *kv, bool need_v)
 {
     if (!kv || !kv->k_pool || !kv->block_table || !kv->seq_lens || (need_v && !kv->v_pool)) return SV_ERR_NULL;
