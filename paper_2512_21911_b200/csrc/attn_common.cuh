@@ -103,4 +103,8 @@ cudaError_t launch_attn_tc(const CUtensorMap &tm_k, const CUtensorMap &tm_v, con
 cudaError_t launch_attn_tc_handed(const CUtensorMap &tm_k, const CUtensorMap &tm_v, const StackAttnParams &p, dim3 grid, cudaStream_t stream);
 cudaError_t launch_attn_tc_stack(const StackAttnParams &p, dim3 grid, cudaStream_t stream);
 
+// Tensor maps of sv_chunk_attn (verify_attn.cu, where the encoding function is looked up); false: not encoded.
+bool half_rows_tensor_map(const void *pool, int64_t n_rows, int halves, CUtensorMap *out);
+bool rows_tensor_map(const void *q, int64_t tokens, int heads, int group, int box_tokens, CUtensorMap *out);
+
 }  // namespace svk

@@ -1,84 +1,603 @@
-// sv_chunk_attn: causal attention of a ragged batch of new tokens over the paged cache that holds them.
+// sv_chunk_attn: causal attention of a ragged batch of new tokens over the paged cache that holds them, on the 5th-generation tensor
+// cores (tcgen05 + TMEM).
 //
-// Mathematics, for a row q at position p: running maximum m and sum l of 2^(s_t - m), s_t = q . k_t * scale * log2 e over the keys t <= p,
-// and o = sum_t 2^(s_t - m) v_t, rescaled when m grows; the output is o / l.  Simple form: a warp per row (token, query head), four dims a
-// lane, one pass over the keys.
+// Mathematics, for a row q at position p and its keys t <= p: s_t = q . k_t * scale * log2 e, a reference m not far below their running
+// maximum, l = sum 2^(s_t - m), o = sum 2^(s_t - m) v_t; the output is o / l.  When the maximum outgrows the reference by more than 8,
+// m moves and l and o are multiplied by 2^(old - new); o / l does not depend on m, and bf16 and fp32 have the same exponents.
+//
+// A row tile is 128 of the G * n rows (token-major: token r / G, head r % G) of a (sequence, KV head); an item is two neighbouring row tiles
+// of TT = 128 / G tokens each, or the one that is left (always the case for single tokens).  A CTA runs two streams, each with a softmax
+// warpgroup, an issuing warp and S and O of its own in TMEM (4 x 128 columns), over units of 128 keys:
+//   two tiles   stream g has tile g and takes every unit; K and V of a unit are fetched once for both
+//   one tile    the streams take the units in turn and add their sums at the end
+//   S[128 x 128] = Q . K^T      8 x tcgen05.mma (M128 N128 K16), both operands from shared memory (TMA, 128-byte swizzle)
+//   P = 2^(s - m)               a thread per row (tcgen05.ld 32x32b), rounded to bf16 into the columns of S
+//   O[128 x 128] += P . V       8 x tcgen05.mma, P from TMEM, V MN-major as TMA stored it
+// A stream's chain is S, softmax, PV, S, ...; while one stream is in its softmax the tensor cores work for the other.
+//
+// The batch is ragged and its lengths are on the device, so the work is divided there: all items of the batch in a row, an item as long as
+// the keys it sees plus kItemCost, are cut into equal shares, a CTA each (chunk_shares.h).  An item that is cut is written as partial sums to the workspace
+// and merged by a second kernel; a CTA has at most two cuts.  That balances a prompt's triangle of items, single tokens over long
+// caches and any mixture of the two without a case of its own.
+// All waits are on mbarriers and bounded; one that gives up sets the status word, the CTA drains its copies and MMAs, frees TMEM and returns.
+#include <cuda.h>
 #include <cuda_bf16.h>
 
+#include <algorithm>
+
 #include "attn_common.cuh"
+#include "chunk_shares.h"
 #include "sv_host.h"
 #include "sv_ptx.cuh"
 
 namespace {
 
-constexpr int kThreads = 256;
+using namespace svk;
+
+constexpr int kThreads = 384;
+constexpr int kUnit = kChunkUnit;             // keys of a unit
+constexpr int kHalf = 16384;                 // [128 rows][64 bf16]: half of a Q, K or V tile
+constexpr int kTileBytes = 2 * kHalf;
+constexpr int kStages = 5;                   // ring of K and V tiles, in turn
+constexpr int kOffQ = kStages * kTileBytes;
+constexpr int kOffMisc = kOffQ + 2 * kTileBytes;
+constexpr int kSmemBytes = 1024 + kOffMisc + 2048;
+static_assert(kSmemBytes <= 232448, "shared memory budget");
+constexpr int kRegsMany = 208, kRegsFew = 88;
+static_assert((2 * kRegsMany + kRegsFew) * 128 <= 168 * kThreads, "registers of the launch");
+constexpr float kLag = 8.f;                  // what the maximum may exceed the reference by (log2)
+
+enum Bar {
+    kFull = 0,                   // [kStages] a K or V tile has landed
+    kEmpty = kFull + kStages,    // [kStages] both streams are through with it
+    kQFull = kEmpty + kStages,   // the item's Q has landed
+    kQFree,                      // all S of the item are through
+    kS,                          // [2] S of the stream's unit is in TMEM
+    kP0 = kS + 2,                // [2] P of the first 64 keys is
+    kP1 = kP0 + 2,               // [2] ... of the others
+    kO = kP1 + 2,                // [2] the stream's last PV of the item is through
+    kX = kO + 2,                 // (one tile) the second stream's sums are there
+    kXFree,                      // ... and have been taken
+    kDone,                       // all MMAs are through
+    kNumBars
+};
+__device__ __forceinline__ int arrivals(int bar)
+{
+    if (bar >= kEmpty && bar < kEmpty + kStages) return 2;
+    if (bar == kQFree || bar == kDone) return 2;
+    return (bar >= kP0 && bar < kO) || bar == kX || bar == kXFree ? 4 : 1;   // (one lane of each warp of a warpgroup)
+}
 
 struct Params {
-    const uint2 *q, *k_pool, *v_pool;
-    const int32_t *block_table, *seq_lens, *q_start;
-    uint2 *out;
+    ChunkBatch batch;
+    const int32_t *block_table;
+    __nv_bfloat16 *out;
     float *lse;
+    float *ws_o;      // [2 * gridDim.x][slot_rows][128]: of a CTA, the share of an item that began before and of one that goes on behind
+    float2 *ws_ml;    // [2 * gridDim.x][slot_rows]
+    int4 *cuts;       // [gridDim.x] the cut item that begins in a CTA's share: first row, tokens, KV head, parts (0: none)
     int32_t *status;
-    int S, N, Hq, Hkv, B, NBmax, n_pages;
+    int Hq, Hkv, G, TT, B, NBmax, n_pages, slot_rows;
     float scale_log2;
 };
 
-__device__ __forceinline__ float4 four(uint2 w)
+// The share of this CTA, found by all of its threads together; scratch: 16 words of shared memory.  False: none.
+__device__ bool begin_walk(const Params &p, ChunkWalk &walk, long long *scratch)
 {
-    const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&w.x)), b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&w.y));
-    return make_float4(a.x, a.y, b.x, b.y);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    long long mine = 0, first = 0;
+    for (int i = tid; i < p.batch.S; i += kThreads) {
+        walk.load(i);
+        mine += walk.per_head();
+        if (i == tid) first = mine;
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, d);
+    if (lane == 0) scratch[warp] = mine;
+    __syncthreads();
+    long long total = 0;
+    for (int w = 0; w < kThreads / 32; ++w) total += scratch[w];
+    if (!walk.divide(total * p.batch.Hkv, gridDim.x, blockIdx.x)) return false;
+    long long ahead = 0;   // the sequence that the share begins in, by sums over the ones before
+    for (int base = 0; base < p.batch.S && ahead <= walk.lo; base += kThreads) {
+        const int i = base + tid;
+        long long cost = first;
+        if (base) {
+            cost = 0;
+            if (i < p.batch.S) walk.load(i), cost = walk.per_head();
+        }
+        cost *= p.batch.Hkv;
+        long long upto = cost;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const long long o = __shfl_up_sync(0xffffffffu, upto, d);
+            if (lane >= d) upto += o;
+        }
+        __syncthreads();
+        if (lane == 31) scratch[warp] = upto;
+        __syncthreads();
+        upto += ahead;
+        for (int w = 0; w < kThreads / 32; ++w) {
+            if (w < warp) upto += scratch[w];
+            ahead += scratch[w];
+        }
+        if (i < p.batch.S && cost > 0 && upto - cost <= walk.lo && walk.lo < upto) scratch[14] = i, scratch[15] = upto - cost;
+        __syncthreads();
+    }
+    walk.enter((int)scratch[14], scratch[15]);
+    return true;
 }
 
-__global__ void __launch_bounds__(kThreads) chunk_attn_kernel(const Params p)
+__device__ __forceinline__ void load_box_3d(uint32_t dst, const void *map, int x, int y, int z, uint32_t bar)
 {
-    svk::grid_dependency_wait();
-    svk::grid_launch_dependents();
-    const int token = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const auto start = [&](int s) { return min(max(p.q_start[s], 0), p.N); };
-    int s = 0, hi = p.S - 1;   // the last sequence that starts at or before the token
-    while (s < hi) {
-        const int mid = (s + hi + 1) / 2;
-        if (start(mid) <= token) s = mid;
-        else hi = mid - 1;
-    }
-    if (token < start(s) || token >= start(s + 1)) return;
-    const int len = (int)min((long long)p.seq_lens[s], (long long)p.NBmax * p.B);
-    const int pos = min(p.seq_lens[s] - start(s + 1) + token, len - 1);
-    const int G = p.Hq / p.Hkv;
-    for (int hq = warp; hq < p.Hq; hq += kThreads / 32) {
-        const int h = hq / G;
-        const size_t row = (size_t)token * p.Hq + hq;
-        const float4 q = four(p.q[row * 32 + lane]);
-        float m = -INFINITY, l = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int t = 0; t <= pos; ++t) {
-            int page = p.block_table[(size_t)s * p.NBmax + t / p.B];
-            if ((unsigned)page >= (unsigned)p.n_pages) {
-                if (lane == 0 && p.status) atomicOr(p.status, svk::kStatusIndex);
-                page = page < 0 ? 0 : p.n_pages - 1;
-            }
-            const size_t at = (((size_t)page * p.Hkv + h) * p.B + t % p.B) * 32 + lane;
-            const float4 k = four(p.k_pool[at]);
-            float x = q.x * k.x + q.y * k.y + q.z * k.z + q.w * k.w;
-#pragma unroll
-            for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-            x *= p.scale_log2;
-            const float m_new = fmaxf(m, x), c = svk::fast_exp2(m - m_new), w = svk::fast_exp2(x - m_new);
-            const float4 v = four(p.v_pool[at]);
-            o.x = o.x * c + w * v.x, o.y = o.y * c + w * v.y, o.z = o.z * c + w * v.z, o.w = o.w * c + w * v.w;
-            l = l * c + w, m = m_new;
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+                 "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void load_box_4d(uint32_t dst, const void *map, int x, int y, int z, int w, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+                 "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
+                 : "memory");
+}
+
+// What the warps of a CTA share: barriers, and whether one of their waits gave up.
+struct Shared {
+    uint32_t bars;
+    volatile int *abort_flag;
+    volatile int *landed;   // [2] the last ring slot that the issuing warp of a stream has seen full
+    int32_t *status;
+    __device__ uint32_t bar(int i) const { return bars + i * 8; }
+    __device__ bool wait(int i, uint32_t parity, int bit) const
+    {
+        for (int round = 0; round < 64; ++round) {   // (looks at the flag between polls of a limited number)
+            if (mbar_wait_bounded(bar(i), parity, 1u << 13)) return true;
+            if (*abort_flag) return false;
         }
-        const float inv = l > 0.f ? 1.f / l : 0.f;
-        p.out[row * 32 + lane] = make_uint2(svk::pack_bf16(o.x * inv, o.y * inv), svk::pack_bf16(o.z * inv, o.w * inv));
-        if (p.lse && lane == 0) p.lse[row] = l > 0.f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+        *abort_flag = 1;
+        if (status) atomicOr(status, bit);
+        return false;
     }
+    // until the stream's issuing warp has seen this slot full
+    __device__ bool wait_landed(int stream, int slot, int bit) const
+    {
+        for (int i = 0; i < 1 << 22; ++i) {
+            if (landed[stream] >= slot) return true;
+            if (*abort_flag) return false;
+        }
+        *abort_flag = 1;
+        if (status) atomicOr(status, bit);
+        return false;
+    }
+    // the same for a converged warp: true if every lane has seen the phase
+    __device__ bool warp_wait(int i, uint32_t parity, int bit) const { return __all_sync(0xffffffffu, wait(i, parity, bit)); }
+};
+
+// ---------------------------------------------------------------------- warp 8: copies
+__device__ __forceinline__ void produce(const Params &p, ChunkWalk &walk, const Shared &sh, uint32_t smem0, const CUtensorMap &tm_q, const CUtensorMap &tm_k,
+                                        const CUtensorMap &tm_v)
+{
+    const int lane = threadIdx.x & 31;
+    const int per_unit = kUnit / p.B;   // pages of a unit
+    int slot = 0, items = 0;            // ring slots and items so far
+    bool dead = false, clamped = false;
+    ChunkItem it;
+    while (!dead && walk.next(it)) {
+        if (it.units == 0) continue;
+        const int *pages = p.block_table + (size_t)it.s * p.NBmax;
+        const int last_page = (it.kv_end - 1) / p.B;
+        // Q: both halves of one or two tiles, as soon as the S of the item before are through
+        if (items > 0 && !sh.warp_wait(kQFree, (items - 1) & 1, 1)) break;
+        const int n_tiles = it.tokens > p.TT ? 2 : 1;
+        if (elect_one()) {
+            mbar_arrive_expect_tx(sh.bar(kQFull), (uint32_t)(n_tiles * 2 * p.G * p.TT * 128));
+            for (int i = 0; i < 2 * n_tiles; ++i)
+                load_box_4d(smem0 + kOffQ + (i >> 1) * kTileBytes + (i & 1) * kHalf, &tm_q, 0, it.h * p.G, it.row0 + (i >> 1) * p.TT, i & 1, sh.bar(kQFull));
+        }
+        __syncwarp();
+        ++items;
+        int known = 0, batch0 = -1;   // a page number a lane, 32 pages from batch0 on
+        for (int u = it.u0; u < it.u1 && !dead; ++u) {
+            const int first = u * per_unit;
+            if (batch0 < 0 || first >= batch0 + 32) {   // (32 is a multiple of per_unit)
+                batch0 = first;
+                known = first + lane <= last_page ? __ldg(pages + first + lane) : 0;
+                if ((unsigned)known >= (unsigned)p.n_pages) clamped = true, known = known < 0 ? 0 : p.n_pages - 1;
+            }
+            // rows of the pools, seen as [pages * Hkv * B][128], where the two halves of the unit begin
+            const int keys = min(kUnit, it.kv_end - u * kUnit);
+            const int page0 = __shfl_sync(0xffffffffu, known, first - batch0);
+            const int page1 = __shfl_sync(0xffffffffu, known, (first - batch0 + 1) & 31);
+            const int y0 = (page0 * p.Hkv + it.h) * p.B, y1 = per_unit == 2 ? (page1 * p.Hkv + it.h) * p.B : y0 + 64;
+            const int halves = keys > 64 ? 2 : 1;
+            for (int v = 0; v < 2; ++v, ++slot) {
+                const int stage = slot % kStages, turn = slot / kStages;
+                if (turn > 0 && !sh.warp_wait(kEmpty + stage, (turn - 1) & 1, 2)) {
+                    dead = true;
+                    break;
+                }
+                if (elect_one()) {
+                    const uint32_t dst = smem0 + stage * kTileBytes, full = sh.bar(kFull + stage);
+                    mbar_arrive_expect_tx(full, halves * kHalf);
+                    for (int i = 0; i < halves; ++i) {
+                        const int y = i ? y1 : y0;
+                        if (v) {   // V: [64 keys] of both halves of the dims
+                            load_box_3d(dst + i * kHalf, &tm_v, 0, y, 0, full);
+                        } else {   // K: either half of the dims, [128 keys]
+                            load_box_3d(dst + i * (kHalf / 2), &tm_k, 0, y, 0, full);
+                            load_box_3d(dst + kHalf + i * (kHalf / 2), &tm_k, 0, y, 1, full);
+                        }
+                    }
+                }
+                __syncwarp();
+            }
+        }
+    }
+    if (clamped && p.status) atomicOr(p.status, kStatusIndex);
+    // Copies in flight write to this CTA's memory: it stays until they have arrived (all of them have, unless somebody gave up).
+    for (int stage = 0; stage < kStages; ++stage) {
+        const int n = slot > stage ? (slot - stage + kStages - 1) / kStages : 0;   // copies requested into the stage
+        if (n > 0 && !__all_sync(0xffffffffu, mbar_wait_bounded(sh.bar(kFull + stage), (n - 1) & 1)) && p.status) atomicOr(p.status, 1);
+    }
+    if (items > 0 && !__all_sync(0xffffffffu, mbar_wait_bounded(sh.bar(kQFull), (items - 1) & 1)) && p.status) atomicOr(p.status, 1);
+}
+
+// ---------------------------------------------------------------------- warps 9 and 10: the MMAs of stream g
+// A wait on a parity cannot tell a phase from the one two before it, so a stage's phase may only be waited for when the one before is known
+// to be complete.  Of a stage that the other stream had last, this one knows that from the other's word (Shared::landed).
+__device__ __forceinline__ void issue(const Params &p, ChunkWalk &walk, const Shared &sh, uint32_t smem0, uint32_t tmem, int g)
+{
+    constexpr uint32_t idesc_s = umma_idesc_bf16(128, kUnit, false), idesc_pv = umma_idesc_bf16(128, 128, true);
+    const uint64_t dq = umma_desc_sw128(smem0 + kOffQ, 16, 1024), dk = umma_desc_sw128(smem0, 16, 1024);
+    const uint64_t dv = umma_desc_sw128(smem0, kHalf / 2, 1024);
+    const uint32_t dq_lo = (uint32_t)dq, dk_lo = (uint32_t)dk, dv_lo = (uint32_t)dv;
+    const uint64_t d_hi = dk & 0xFFFFFFFF00000000ull, dv_hi = dv & 0xFFFFFFFF00000000ull;
+    const uint32_t t_s = tmem + g * 128, t_o = tmem + 256 + g * 128;
+    int unit0 = 0, mine = 0, items = 0;   // units of the CTA before this item; units of this stream, items so far
+    uint32_t foreign = 0;                 // the stages that the other stream alone had last
+    bool dead = false;
+    const auto full = [&](int slot) {
+        const int stage = slot % kStages;
+        if (foreign >> stage & 1) {
+            if (!__all_sync(0xffffffffu, sh.wait_landed(1 - g, slot - kStages, 4))) return false;
+            foreign &= ~(1u << stage);
+        }
+        if (!sh.warp_wait(kFull + stage, (slot / kStages) & 1, 4)) return false;
+        if ((threadIdx.x & 31) == 0) sh.landed[g] = slot;
+        return true;
+    };
+    const auto pass = [&](int unit) { foreign |= 1u << (2 * unit) % kStages | 1u << (2 * unit + 1) % kStages; };
+    ChunkItem it;
+    while (!dead && walk.next(it)) {
+        if (it.units == 0) continue;
+        const bool two = it.tokens > p.TT;
+        const int n_units = it.u1 - it.u0, step = two ? 1 : 2, begin = two ? 0 : g;
+        if (!sh.warp_wait(kQFull, items & 1, 4)) break;
+        ++items;
+        if (begin >= n_units && elect_one()) mbar_arrive(sh.bar(kQFree));
+        __syncwarp();
+        if (begin) pass(unit0);
+        for (int j = begin; j < n_units && !dead; j += step, ++mine) {
+            const int slot = 2 * (unit0 + j), sk = slot % kStages, sv = (slot + 1) % kStages;
+            const bool last = j + step >= n_units;
+            if (!full(slot)) {
+                dead = true;
+                break;
+            }
+            tc_fence_after_sync();
+            if (elect_one()) {
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks) {
+                    const uint32_t o = (uint32_t)(((ks >> 2) * kHalf + (ks & 3) * 32) >> 4);
+                    tc_mma_bf16(t_s, d_hi | (dq_lo + (uint32_t)((two ? g * kTileBytes : 0) >> 4) + o), d_hi | (dk_lo + (uint32_t)((sk * kTileBytes) >> 4) + o),
+                                idesc_s, ks > 0);
+                }
+                tc_commit(sh.bar(kS + g));
+                tc_commit(sh.bar(kEmpty + sk));
+                if (!two) tc_commit(sh.bar(kEmpty + sk));   // (a stage has two readers)
+                if (last) tc_commit(sh.bar(kQFree));
+            }
+            __syncwarp();
+            if (!full(slot + 1)) {
+                dead = true;
+                break;
+            }
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                if (!sh.warp_wait((half ? kP1 : kP0) + g, mine & 1, 8)) {
+                    dead = true;
+                    break;
+                }
+                tc_fence_after_sync();
+                if (elect_one()) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        tc_mma_bf16_ta(t_o, t_s + (half * 4 + i) * 8, dv_hi | (dv_lo + (uint32_t)((sv * kTileBytes + half * kHalf + i * 2048) >> 4)), idesc_pv,
+                                       j > begin || half > 0 || i > 0);
+                    if (half) {
+                        tc_commit(sh.bar(kEmpty + sv));
+                        if (!two) tc_commit(sh.bar(kEmpty + sv));
+                        if (last) tc_commit(sh.bar(kO + g));
+                    }
+                }
+                __syncwarp();
+            }
+            if (!two && j + 1 < n_units) pass(unit0 + j + 1);
+        }
+        unit0 += n_units;
+    }
+    if (elect_one()) tc_commit(sh.bar(kDone));
+    __syncwarp();
+}
+
+// ---------------------------------------------------------------------- warps 0-3 and 4-7: the softmax of stream g, a thread per row
+__device__ __forceinline__ void softmax(const Params &p, ChunkWalk &walk, const Shared &sh, uint8_t *smem, uint32_t tmem, int g, float2 *exchange)
+{
+    const int r = threadIdx.x & 127, lane = threadIdx.x & 31;
+    const uint32_t t_lane = tmem + ((uint32_t)((r >> 5) * 32) << 16), t_s = t_lane + g * 128, t_o = t_lane + 256 + g * 128;
+    int unit0 = 0, mine = 0, ends = 0, meets = 0;   // units of the CTA and of the stream, items that it had units of, items of both streams
+    ChunkItem it;
+    while (walk.next(it)) {
+        const bool two = it.tokens > p.TT;
+        const int n_units = it.u1 - it.u0, step = two ? 1 : 2, begin = two ? 0 : g;
+        const int first_token = two ? g * p.TT : 0, token = first_token + r / p.G;
+        const bool real = r < p.G * p.TT && token < it.tokens;
+        const int last_key = min(it.pos0 + token, it.kv_end - 1);   // of this row
+        float m = -INFINITY, l = 0.f;
+        for (int j = begin; j < n_units; j += step, ++mine) {
+            const int key0 = (it.u0 + j) * kUnit;
+            if (!sh.warp_wait(kS + g, mine & 1, 16)) return;
+            tc_fence_after_sync();
+            uint32_t x[4][32];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_ld_x32(t_s + c * 32, x[c]);
+            tmem_ld_wait();
+            if (key0 + kUnit - 1 > min(it.pos0 + first_token, it.kv_end - 1)) {   // some row of the tile does not see all of the unit
+                const int seen = last_key - key0;
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (c * 32 + i > seen) x[c][i] = 0xff800000u;
+            }
+            float mx[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                mx[c] = fmaxf(__uint_as_float(x[c][0]), __uint_as_float(x[c][1]));
+#pragma unroll
+                for (int i = 2; i < 32; i += 2) mx[c] = max3f(mx[c], __uint_as_float(x[c][i]), __uint_as_float(x[c][i + 1]));
+            }
+            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2;
+            const bool move = top > m + kLag;
+            if (__any_sync(0xffffffffu, move)) {
+                const float c = move ? fast_exp2(m - top) : 1.f;
+                if (move) m = top;
+                l *= c;
+                if (j > begin) {   // (S of this unit was issued behind the PV of the one before: O is at rest)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        uint32_t o[32];
+                        tmem_ld_x32(t_o + q * 32, o);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * c);
+                        tmem_st_x32(t_o + q * 32, o);
+                    }
+                    tmem_st_wait();
+                }
+            }
+            // V rows behind the last key are another tile's or nobody's: zero, so that 0 * V is 0
+            if (key0 + kUnit > it.kv_end) {
+                const int slot = 2 * (unit0 + j) + 1, stage = slot % kStages;
+                if (!sh.warp_wait(kFull + stage, (slot / kStages) & 1, 16)) return;
+                uint8_t *tile = smem + stage * kTileBytes;
+                for (int i = (it.kv_end - key0) * 16 + r; i < kUnit * 16; i += 128) {
+                    const int row = i >> 4, c = i & 15;
+                    *reinterpret_cast<uint4 *>(tile + (row >> 6) * kHalf + (c >> 3) * (kHalf / 2) + swz128(row & 63, c & 7)) = make_uint4(0u, 0u, 0u, 0u);
+                }
+                fence_proxy_async();
+            }
+            const float m_use = m == -INFINITY ? 0.f : m;
+            const unsigned long long scale2 = f2_pack(p.scale_log2, p.scale_log2), ref2 = f2_pack(-m_use, -m_use);
+            unsigned long long sum2[2] = {0ull, 0ull};
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                uint32_t w[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    const uint32_t *at = x[half * 2 + (i >> 4)] + (i & 15) * 2;
+                    float a, b;
+                    f2_unpack(f2_fma(f2_pack(__uint_as_float(at[0]), __uint_as_float(at[1])), scale2, ref2), a, b);
+                    a = fast_exp2(a), b = fast_exp2(b);
+                    sum2[i & 1] = f2_add(sum2[i & 1], f2_pack(a, b));
+                    w[i] = pack_bf16(a, b);
+                }
+                tmem_st_x32(t_s + half * 32, w);
+                tmem_st_wait();
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(sh.bar((half ? kP1 : kP0) + g));
+            }
+            float a, b;
+            f2_unpack(f2_add(sum2[0], sum2[1]), a, b);
+            l += a + b;
+        }
+        const bool had = begin < n_units, both = !two && n_units > 1;
+        if (had) {
+            if (!sh.warp_wait(kO + g, ends & 1, 16)) return;
+            ++ends;
+            tc_fence_after_sync();
+        }
+        unit0 += n_units;
+        // the rows: of two tiles each stream's own; of one tile those of both streams, added by the first
+        if (both && g) {
+            exchange[r] = make_float2(m, l);
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(sh.bar(kX));
+            if (!sh.warp_wait(kXFree, meets & 1, 32)) return;
+            ++meets;
+            tc_fence_after_sync();
+        }
+        if (!two && g) continue;
+        float w0 = 1.f, w1 = 0.f;
+        if (both) {
+            if (!sh.warp_wait(kX, meets & 1, 32)) return;
+            ++meets;
+            tc_fence_after_sync();
+            const float2 o = exchange[r];
+            const float top = fmaxf(m, o.x), use = top == -INFINITY ? 0.f : top;
+            w0 = fast_exp2(m - use), w1 = fast_exp2(o.x - use);
+            l = l * w0 + o.y * w1, m = top;
+        }
+        const bool whole = it.whole();
+        const size_t row = (size_t)(it.row0 + token) * p.Hq + it.h * p.G + r % p.G;
+        const size_t part = ((size_t)blockIdx.x * 2 + (it.u0 == 0)) * p.slot_rows + (two ? g * 128 : 0) + r;
+        const float inv = !whole ? 1.f : l > 0.f ? 1.f / l : 0.f;
+        w0 *= inv, w1 *= inv;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            float o[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] = 0.f;
+            if (had) {
+                uint32_t x[32];
+                tmem_ld_x32(t_o + c * 32, x);
+                tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = __uint_as_float(x[i]) * w0;
+            }
+            if (both) {
+                uint32_t x[32];
+                tmem_ld_x32(t_o + 128 + c * 32, x);
+                tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] += __uint_as_float(x[i]) * w1;
+            }
+            if (real && whole) {
+                uint4 *to = reinterpret_cast<uint4 *>(p.out + row * 128 + c * 32);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    to[i] = l > 0.f ? make_uint4(pack_bf16(o[i * 8], o[i * 8 + 1]), pack_bf16(o[i * 8 + 2], o[i * 8 + 3]), pack_bf16(o[i * 8 + 4], o[i * 8 + 5]),
+                                                 pack_bf16(o[i * 8 + 6], o[i * 8 + 7]))
+                                    : make_uint4(0u, 0u, 0u, 0u);
+            } else if (real) {
+                float4 *to = reinterpret_cast<float4 *>(p.ws_o + part * 128 + c * 32);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) to[i] = make_float4(o[i * 4], o[i * 4 + 1], o[i * 4 + 2], o[i * 4 + 3]);
+            }
+        }
+        if (real && whole && p.lse) p.lse[row] = l > 0.f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+        if (real && !whole) p.ws_ml[part] = make_float2(m, l);
+        if (threadIdx.x == 0 && it.parts) p.cuts[blockIdx.x] = make_int4(it.row0, it.tokens, it.h, it.parts);
+        tc_fence_before_sync();
+        if (both) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(sh.bar(kXFree));
+        }
+    }
+}
+
+__global__ void __launch_bounds__(kThreads, 1)
+    chunk_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                      const __grid_constant__ Params p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t smem0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t *smem = smem_raw + (smem0 - smem_u32(smem_raw));
+    uint8_t *misc = smem + kOffMisc;
+    const Shared sh{smem0 + kOffMisc, reinterpret_cast<volatile int *>(misc + 256), reinterpret_cast<volatile int *>(misc + 264), p.status};
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(misc + 260);
+    long long *scratch = reinterpret_cast<long long *>(misc + 384);
+    float2 *exchange = reinterpret_cast<float2 *>(misc + 512);
+    static_assert(kNumBars * 8 <= 256 && 512 + 128 * sizeof(float2) <= 2048, "");
+    const int tid = threadIdx.x, warp = tid >> 5;
+
+    if (tid == 0) {
+        for (int i = 0; i < kNumBars; ++i) mbar_init(sh.bar(i), arrivals(i));
+        mbar_fence_init();
+        *sh.abort_flag = 0;
+        sh.landed[0] = sh.landed[1] = -1;
+    }
+    if (warp == 8 && (tid & 31) == 0) tma_prefetch_desc(&tm_q), tma_prefetch_desc(&tm_k), tma_prefetch_desc(&tm_v);
+    if (warp == 9) tmem_alloc(smem_u32(tmem_slot), 512);
+    grid_dependency_wait();
+    if (tid == 0) p.cuts[blockIdx.x] = make_int4(0, 0, 0, 0);
+    ChunkWalk walk(p.batch);
+    const bool some = begin_walk(p, walk, scratch);
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = *tmem_slot;
+    if (some) {
+        if (warp >= 8) {
+            reg_dealloc<kRegsFew>();
+            if (warp == 8) produce(p, walk, sh, smem0, tm_q, tm_k, tm_v);
+            else if (warp < 11) issue(p, walk, sh, smem0, tmem, warp - 9);
+        } else {
+            reg_alloc<kRegsMany>();
+            softmax(p, walk, sh, smem, tmem, warp >> 2, exchange);
+        }
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    if (warp == 9) {
+        // (MMAs that nobody waited for, when a wait gave up)
+        if (some && !__all_sync(0xffffffffu, mbar_wait_bounded(sh.bar(kDone), 0)) && p.status) atomicOr(p.status, 4);
+        __syncwarp();
+        tmem_dealloc(tmem, 512);
+    }
+    grid_launch_dependents();
+}
+
+// A cut item: the partial sums of its shares, which are numbered from the CTA that it begins in.  A warp per row, four dims a lane.
+constexpr int kMergeRows = 32;   // rows of a CTA
+__global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant__ Params p)
+{
+    grid_dependency_wait();
+    const int cta = blockIdx.x, lane = threadIdx.x & 31;
+    const int4 cut = p.cuts[cta];
+    if (cut.w == 0) return;
+    const bool two = cut.y > p.TT;
+    for (int i = threadIdx.x >> 5; i < kMergeRows; i += 8) {
+        const int at = blockIdx.y * kMergeRows + i;
+        if (at >= p.slot_rows) return;
+        const int r = at & 127, token = (two ? (at >> 7) * p.TT : 0) + r / p.G;
+        if (r >= p.G * p.TT || token >= cut.y || (!two && at >= 128)) continue;
+        SplitSum sum;
+        constexpr int U = 4;
+        for (int base = 0; base < cut.w; base += U) {
+            float2 ml[U];
+            float4 o[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const size_t part = ((size_t)(cta + base + k) * 2 + (base + k == 0)) * p.slot_rows + at;
+                const bool in = base + k < cut.w;
+                ml[k] = in ? __ldcg(p.ws_ml + part) : make_float2(-INFINITY, 0.f);
+                o[k] = in ? __ldcg(reinterpret_cast<const float4 *>(p.ws_o + part * 128) + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+            sum.add(ml, o);
+        }
+        const size_t row = (size_t)(cut.x + token) * p.Hq + cut.z * p.G + r % p.G;
+        reinterpret_cast<uint2 *>(p.out + row * 128)[lane] = sum.l > 0.f ? sum.out() : make_uint2(0u, 0u);
+        if (p.lse && lane == 0) p.lse[row] = sum.l > 0.f ? sum.lse() : -INFINITY;
+    }
+}
+
+// Rows of a partial: the rows of the batch where these are one tile at most.
+int slot_rows(const sv_geom *g, int32_t n_tokens)
+{
+    const int64_t rows = (int64_t)(g->n_q_heads / g->n_kv_heads) * n_tokens;
+    return rows <= 128 ? (int)std::max<int64_t>(rows, 1) : 256;
 }
 
 }  // namespace
 
 extern "C" size_t sv_chunk_workspace_bytes(const sv_geom *geom, int32_t n_tokens)
 {
-    return svh::check_ragged(geom, n_tokens) == SV_OK ? 16 : 0;
+    if (svh::check_ragged(geom, n_tokens) != SV_OK) return 0;
+    return (size_t)svh::sm_count() * (sizeof(int4) + 2 * (size_t)slot_rows(geom, n_tokens) * 130 * sizeof(float));
 }
 
 extern "C" sv_status sv_chunk_attn(const sv_geom *geom, const void *q, const sv_kv *kv, const int32_t *q_start, int32_t n_tokens,
@@ -90,24 +609,45 @@ extern "C" sv_status sv_chunk_attn(const sv_geom *geom, const void *q, const sv_
     st = svh::check_kv(geom, kv, true);
     if (st != SV_OK) return st;
     if (!q_start || (n_tokens > 0 && (!q || !out))) return SV_ERR_NULL;
+    if (!(softmax_scale >= 0.f && softmax_scale < INFINITY)) return SV_ERR_SHAPE;
     if (!svh::aligned(q, 16) || !svh::aligned(out, 16) || !svh::aligned(workspace, 16)) return SV_ERR_ALIGN;
     if (workspace_bytes < sv_chunk_workspace_bytes(geom, n_tokens)) return SV_ERR_WORKSPACE;
     if (!workspace) return SV_ERR_NULL;
     if (n_tokens == 0) return SV_OK;
+    const int ctas = svh::sm_count();
     Params p = {};
-    p.q = static_cast<const uint2 *>(q), p.k_pool = static_cast<const uint2 *>(kv->k_pool), p.v_pool = static_cast<const uint2 *>(kv->v_pool);
-    p.block_table = kv->block_table, p.seq_lens = kv->seq_lens, p.q_start = q_start;
-    p.out = static_cast<uint2 *>(out), p.lse = lse, p.status = status_word;
-    p.S = geom->n_seq, p.N = n_tokens, p.Hq = geom->n_q_heads, p.Hkv = geom->n_kv_heads, p.B = geom->block_size, p.NBmax = geom->max_blocks;
-    p.n_pages = kv->n_pages;
+    p.Hq = geom->n_q_heads, p.Hkv = geom->n_kv_heads, p.B = geom->block_size, p.NBmax = geom->max_blocks;
+    p.G = p.Hq / p.Hkv, p.TT = 128 / p.G;
+    p.batch = {q_start, kv->seq_lens, geom->n_seq, n_tokens, p.Hkv, p.TT, (long long)p.NBmax * p.B};
+    p.n_pages = kv->n_pages, p.slot_rows = slot_rows(geom, n_tokens);
+    p.block_table = kv->block_table;
+    p.out = static_cast<__nv_bfloat16 *>(out), p.lse = lse, p.status = status_word;
+    p.cuts = static_cast<int4 *>(workspace);
+    p.ws_o = reinterpret_cast<float *>(p.cuts + ctas);
+    p.ws_ml = reinterpret_cast<float2 *>(p.ws_o + (size_t)2 * ctas * p.slot_rows * 128);
     p.scale_log2 = (softmax_scale == 0.f ? 0.08838834764831845f : softmax_scale) * 1.4426950408889634f;
+    CUtensorMap tm_q, tm_k, tm_v;
+    const int64_t pool_rows = (int64_t)p.n_pages * p.Hkv * p.B;
+    if (!rows_tensor_map(q, n_tokens, p.Hq, p.G, p.TT, &tm_q) || !half_rows_tensor_map(kv->k_pool, pool_rows, 1, &tm_k) ||
+        !half_rows_tensor_map(kv->v_pool, pool_rows, 2, &tm_v))
+        return SV_ERR_CUDA;
+    static svh::OncePerDevice once;
+    if (once.run([] { return cudaFuncSetAttribute(chunk_attn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes); }) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return SV_ERR_CUDA;
+    }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)n_tokens);
+    cfg.gridDim = dim3(ctas);
     cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmemBytes;
     cfg.stream = static_cast<cudaStream_t>(stream);
     cudaLaunchAttribute attr[1];
     svh::pdl_attribute(attr);
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, chunk_attn_kernel, p) == cudaSuccess ? svh::launch_status() : SV_ERR_CUDA;
+    if (cudaLaunchKernelEx(&cfg, chunk_attn_kernel, tm_q, tm_k, tm_v, p) != cudaSuccess) return SV_ERR_CUDA;
+    cfg.gridDim = dim3(ctas, (p.slot_rows + kMergeRows - 1) / kMergeRows);
+    cfg.blockDim = dim3(256);
+    cfg.dynamicSmemBytes = 0;
+    return cudaLaunchKernelEx(&cfg, chunk_merge_kernel, p) == cudaSuccess ? svh::launch_status() : SV_ERR_CUDA;
 }

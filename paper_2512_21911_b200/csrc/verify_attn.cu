@@ -106,6 +106,36 @@ bool encode_pool_map(const void *pool, int64_t n_rows, CUtensorMap *out)
            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+}  // namespace
+
+// For sv_chunk_attn (chunk_attn.cu).  A pool as above; box = 64 rows of one half or of both halves.
+bool svk::half_rows_tensor_map(const void *pool, int64_t n_rows, int halves, CUtensorMap *out)
+{
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {64, (cuuint64_t)n_rows, 2};
+    const cuuint64_t strides[2] = {256, 128};
+    const cuuint32_t box[3] = {64, kUnit, (cuuint32_t)halves};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(pool), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Queries [tokens][heads][128]; box = one half of `group` heads of `box_tokens` tokens.  Tokens behind the last one are zero.
+bool svk::rows_tensor_map(const void *q, int64_t tokens, int heads, int group, int box_tokens, CUtensorMap *out)
+{
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[4] = {64, (cuuint64_t)heads, (cuuint64_t)tokens, 2};
+    const cuuint64_t strides[3] = {256, (cuuint64_t)heads * 256, 128};
+    const cuuint32_t box[4] = {64, (cuuint32_t)group, (cuuint32_t)box_tokens, 1};
+    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    return fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(q), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+namespace {
+
 // Encoding costs microseconds of host time, so the maps of single layers are kept in a small fixed table keyed by
 // (pool, rows) (no heap use; a full table is overwritten round-robin).
 bool pool_tensor_map(const void *pool, int64_t n_rows, CUtensorMap *out)

@@ -120,6 +120,25 @@ def test_long_caches_split_over_the_device():
 
 
 @pytest.mark.gpu
+def test_many_units_per_cta_and_calls_one_behind_the_other():
+    """Long loops at the speed of HBM, single tokens (both streams on one tile) and a chunk mixed: every call gives the same bits."""
+    import paper_2512_21911_b200 as sv
+    for lens, new, Hq, Hkv in (([10439, 5106, 16227, 9001, 12000, 15041], [1, 1, 1, 1, 1, 1], 32, 8), ([15000, 9000, 3000], [1, 200, 1], 28, 4)):
+        t = _batch(sv, lens, new, Hq, Hkv, 64)
+        out, lse, status = _run(sv, t)
+        _check(t, out, lse, lens, new)
+        outs = [torch.empty_like(out) for _ in range(3)]
+        ws = torch.empty(sv.sv_chunk_workspace_bytes(t["geom"], t["q"].shape[0]), dtype=torch.uint8, device="cuda")
+        word = torch.zeros(1, dtype=torch.int32, device="cuda")
+        kv = sv.make_kv(t["k"], t["v"], t["table"], t["lens"])
+        for i in range(300):
+            sv.sv_chunk_attn(t["geom"], t["q"], kv, t["start"], outs[i % 3], workspace=ws, status_word=word)
+        torch.cuda.synchronize()
+        assert int(word) == 0 and status == 0
+        assert all(torch.equal(o, out) for o in outs)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("sigma", [0.0, 1.0, 8.0])
 def test_flat_and_sharp_scores_and_a_scale(sigma):
     """Equal scores; scores whose maximum moves by hundreds from key to key."""
