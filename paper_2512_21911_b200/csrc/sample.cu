@@ -1,16 +1,21 @@
 // sv_sample: temperature, top-k, top-p and min-p on rows of logits, the kept entries' distribution and a token drawn from it.
 //
-// Mathematics: e(x) = 2^((x - max) log2 e / temperature).  Masses are whole multiples of 2^-40 (e <= 1, at most 2^20 entries: 60 bits), so
-// every sum is exact and no order of adding changes a result.  The entries are never sorted: what stays is everything up to one entry, the
-// boundary (key, index), in the order "larger logit first, then smaller index".  Search for the boundary by count (top-k) or mass (top-p):
+// Mathematics: e(x) = 2^((x - max) log2 e / temperature).  The entries are never sorted: what stays is everything up to one entry, the
+// boundary (logit, index), in the order "larger logit first, then smaller index".  Search for the boundary by count (top-k) or mass (top-p):
 // a histogram of the entries by their distance from the maximum, the bin in which the goal is reached, and the few entries of that bin,
-// ranked exactly.  A bin with too many of them is divided again by the bits of its keys; entries that are all equal are
-// counted off by index.  With a short top-k all entries up to the bin are ranked at once and top-p, min-p and the token follow from the list.
+// ranked exactly.  A bin with too many of them is divided again by the bits of its keys; entries that are all equal are counted off by
+// index.  For a short top-k the histogram holds the threads' maxima only: the k-th largest of these bounds the k-th entry
+// from below, all entries up to its bin are ranked at once, and top-p, min-p and the token follow from that list.
+//
+// Sums of masses are sums of whole numbers, exact in any order.  Of the nucleus: multiples of 2^-32 of the largest entry's mass, so that a bin is
+// two 32-bit words that shared-memory atomics add to (2^-32 is less than fp32 sums keep; what is lost are entries below 2^-33 of
+// the largest, 2^-16 of its mass if there were 2^17 of them).  Of the draw: multiples of 2^-40, added in registers.
 //
 // A cluster of 1 to 8 CTAs per row; a CTA keeps its part of the row in shared memory, so the logits are read once from HBM.  Warps
 // own contiguous parts: a token is found by sums per CTA, warp and lane.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
+#include <float.h>
 
 #include <algorithm>
 
@@ -23,12 +28,15 @@ namespace cg = cooperative_groups;
 
 constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
-constexpr int kMaxVocab = 1 << 20;
 constexpr int kMaxCluster = 8;
 constexpr int kBins = 2048;
-constexpr float kBinsPerBit = 2048.f / 44.f;   // bins of the first histogram: 44 powers of two below the maximum, beyond what has a mass
+constexpr float kBinsPerBit = 2048.f / 36.f;   // bins of the first histogram: 36 powers of two below the maximum, beyond what has a mass
 constexpr int kList = 1024;                    // entries that are ranked one against another
 constexpr int kGrain = kWarps * 128;           // a CTA's part of a row is a multiple of this: 32 lanes x 4 entries for each warp
+constexpr int kMostPart = 24 * kGrain;         // entries that fit in shared memory
+constexpr int kPart = 8 * kGrain;              // ... and leave room for a second CTA on the SM
+constexpr int kMaxVocab = kMaxCluster * kMostPart;
+static_assert((1ll << 16) * kMostPart < 1ll << 32 && (1ll << 15) * kMostPart < 1ll << 31, "words of a bin");
 
 using Mass = unsigned long long;
 
@@ -43,46 +51,62 @@ struct Params {
     int part;   // entries of a CTA
 };
 
-// Ascending in the logit; -0 equals +0.  0: an entry that is not there (-infinity; a NaN is taken as one when it is read).
+// Ascending in the logit; -0 equals +0.  (Not for -infinity, which stands for an entry that is not there.)
 __device__ __forceinline__ uint32_t key_of(float x)
 {
     const uint32_t b = __float_as_uint(x) == 0x80000000u ? 0u : __float_as_uint(x);
-    return x == -INFINITY ? 0u : b & 0x80000000u ? ~b : b | 0x80000000u;
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
+// What a logit counts as: a NaN as -infinity, +infinity as the largest number.
+__device__ __forceinline__ float taken(float x) { return fminf(fmaxf(x, -INFINITY), FLT_MAX); }
 
-// e * 2^40 to the nearest integer as high * 2^20 + low, by adding numbers whose last place is 1 (0 <= e <= 1).
+// e * 2^(2 N) to the nearest integer as high * 2^N + low, by adding numbers whose last place is 1 (0 <= e <= 1).
 struct Parts {
-    uint32_t high;   // <= 2^20
-    int low;         // at most 2^19 either way
+    uint32_t high;   // <= 2^N
+    int low;         // at most 2^(N - 1) either way
 };
+template <int N>
 __device__ __forceinline__ Parts parts_of(float e)
 {
-    const float f = __fmul_rn(e, 1048576.f), t = __fadd_rn(f, 8388608.f);
+    constexpr float kOne = (float)(1 << N);
+    const float f = __fmul_rn(e, kOne), t = __fadd_rn(f, 8388608.f);
     const float rest = __fsub_rn(f, __fsub_rn(t, 8388608.f));
-    return {__float_as_uint(t) - 0x4b000000u, (int)(__float_as_uint(__fmaf_rn(rest, 1048576.f, 12582912.f)) - 0x4b400000u)};
+    return {__float_as_uint(t) - 0x4b000000u, (int)(__float_as_uint(__fmaf_rn(rest, kOne, 12582912.f)) - 0x4b400000u)};
 }
-__device__ __forceinline__ Mass mass_of(Parts p) { return ((Mass)p.high << 20) + (long long)p.low; }
+template <int N>
+__device__ __forceinline__ Mass whole(uint32_t high, int low) { return ((Mass)high << N) + (long long)low; }
+template <int N>
+__device__ __forceinline__ Mass mass_of(float e)
+{
+    const Parts p = parts_of<N>(e);
+    return whole<N>(p.high, p.low);
+}
+constexpr int kNucleus = 16, kDraw = 20;   // halves of the bits of a mass
 
 struct Boundary {
-    uint32_t key, index;   // the last entry that stays; (1, any): all of them
-    __device__ bool keeps(uint32_t k, uint32_t i) const { return k > key || (k == key && i <= index); }
+    float x;
+    uint32_t index;   // the last entry that stays
+    __device__ bool keeps(float y, uint32_t i) const { return y > x || (y == x && i <= index); }
 };
 
 struct Smem {
-    Mass bins[kBins];
+    uint32_t high[kBins];     // histogram: sums of masses in two words, or counts in the first;
+    int low[kBins];           // the first CTA also sorts its list into the one and keeps masses in the other
     uint64_t list[kList];     // key << 32 | ~index: descending is the order of the rule
-    uint64_t sorted[kList];
     Mass sums[kWarps], scan[kWarps];
     Mass of_cta[2][kMaxCluster];   // written by all CTAs of the cluster; two in turn, so that no CTA writes what another still reads
-    uint32_t top_of_cta[kMaxCluster], count_of_cta[kMaxCluster];
+    float top_of_cta[kMaxCluster], of_warp[kWarps];
+    uint32_t count_of_cta[kMaxCluster];
     uint32_t range[kMaxCluster][2];
-    Mass found_ahead;           // written by the CTA that finds it
+    Mass found_ahead;              // written by the CTA that finds it
     int found_bin, token;
     Boundary boundary;
     uint32_t n_list;
-    uint32_t words[kWarps];
+    __device__ uint64_t *sorted() { return reinterpret_cast<uint64_t *>(low); }
+    __device__ Mass *masses() { return reinterpret_cast<Mass *>(high); }
 };
+static_assert(kBins * 4 >= kList * 8 && sizeof(Smem) % 16 == 0, "");
 
 template <class T, class Op>
 __device__ __forceinline__ T over_warp(T v, Op op)
@@ -92,78 +116,34 @@ __device__ __forceinline__ T over_warp(T v, Op op)
     return v;
 }
 __device__ __forceinline__ Mass sum_over_warp(Mass v) { return over_warp(v, [](Mass a, Mass b) { return a + b; }); }
+template <class T>
+__device__ __forceinline__ T scan_warp(T v)   // inclusive
+{
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const T o = __shfl_up_sync(0xffffffffu, v, d);
+        if ((threadIdx.x & 31) >= d) v += o;
+    }
+    return v;
+}
 
-// kHeld: the CTA's part of the row is in shared memory; else (parts that do not fit) every pass reads it again.
-template <bool kHalf, bool kHeld>
-struct Row {
-    const void *row;
-    float *held;
-    int V, part, rank, warp, lane;
-    bool wide;   // rows start on 16 bytes
-
-    __device__ float at(int i) const
-    {
-        const float x = kHalf ? __bfloat162float(static_cast<const __nv_bfloat16 *>(row)[i]) : __ldg(static_cast<const float *>(row) + i);
-        return x == x ? x : -INFINITY;
-    }
-    __device__ float4 read(int i) const
-    {
-        float4 v;
-        if (wide && i + 4 <= V) {
-            if constexpr (kHalf) {
-                const uint2 w = __ldg(reinterpret_cast<const uint2 *>(static_cast<const __nv_bfloat16 *>(row) + i));
-                v = make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u));
-            } else {
-                v = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(row) + i));
-            }
-            v.x = v.x == v.x ? v.x : -INFINITY, v.y = v.y == v.y ? v.y : -INFINITY;
-            v.z = v.z == v.z ? v.z : -INFINITY, v.w = v.w == v.w ? v.w : -INFINITY;
-        } else {
-            v.x = i < V ? at(i) : -INFINITY, v.y = i + 1 < V ? at(i + 1) : -INFINITY;
-            v.z = i + 2 < V ? at(i + 2) : -INFINITY, v.w = i + 3 < V ? at(i + 3) : -INFINITY;
-        }
-        return v;
-    }
-    __device__ int words() const { return part / kGrain; }   // of a lane
-    __device__ int first(int j) const { return warp * (part / kWarps) + (j * 32 + lane) * 4; }   // entry of a lane's word, in the CTA's part
-    __device__ float4 word(int j) const
-    {
-        const int i = first(j);
-        if constexpr (kHeld) return *reinterpret_cast<const float4 *>(held + i);
-        else return read(rank * part + i);
-    }
-    template <class F>
-    __device__ void each(F f) const   // f(index, logit), all entries of this thread in ascending order
-    {
-        for (int j = 0; j < words(); ++j) {
-            const float4 v = word(j);
-            const int i = rank * part + first(j);
-            f(i, v.x), f(i + 1, v.y), f(i + 2, v.z), f(i + 3, v.w);
-        }
-    }
-};
-
-template <bool kHalf, bool kHeld>
-__global__ void __launch_bounds__(kThreads) sample_kernel(const Params p)
+template <bool kHalf>
+__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_constant__ Params p)
 {
     extern __shared__ __align__(16) uint8_t raw[];
     Smem &sm = *reinterpret_cast<Smem *>(raw);
-    static_assert(sizeof(Smem) % 16 == 0, "");
+    float *const held = reinterpret_cast<float *>(raw + sizeof(Smem));
     const cg::cluster_group cluster = cg::this_cluster();
     const int CL = (int)cluster.num_blocks(), rank = (int)cluster.block_rank(), r = blockIdx.x / CL, g = r / p.rows_per_param;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int first = rank * p.part, n_here = min(p.part, p.V - first);   // entries of this CTA (possibly none), from `first` on
+    const int words = p.part / kGrain, w0 = warp * (p.part / kWarps) + lane * 4;   // a lane's words of four entries: w0, w0 + 128, ...
     const auto everywhere = [&](auto *at, auto v) {   // (one warp) the same word of every CTA's shared memory
         if (lane < CL) *cluster.map_shared_rank(at, lane) = v;
     };
     svk::grid_dependency_wait();
     svk::grid_launch_dependents();
-    Row<kHalf, kHeld> row;
-    row.row = static_cast<const char *>(p.logits) + r * p.stride * (kHalf ? 2 : 4);
-    row.held = reinterpret_cast<float *>(raw + sizeof(Smem));
-    row.V = p.V, row.part = p.part, row.rank = rank, row.warp = warp, row.lane = lane;
-    row.wide = (reinterpret_cast<uintptr_t>(row.row) & 15) == 0;
 
-    // the row, and its maximum
     const float T = p.temperature ? p.temperature[g] : 1.f;
     const bool greedy = !(T > 0.f);
     const int k = greedy ? 1 : p.top_k ? p.top_k[g] : 0;
@@ -171,46 +151,98 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const Params p)
     float min_e = p.min_p && !greedy ? p.min_p[g] : 0.f;
     if (!(min_e > 0.f)) min_e = 0.f;
     const float u = p.tokens ? fminf(fmaxf(p.u[r], 0.f), 1.f) : 0.f;
+
+    // the row, its maximum, and the maximum of the entries that this thread has read
     float most = -INFINITY;
-    for (int j = 0; j < row.words(); ++j) {
-        const float4 v = row.read(rank * p.part + row.first(j));
-        if constexpr (kHeld) *reinterpret_cast<float4 *>(row.held + row.first(j)) = v;
-        most = fmaxf(most, fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)));
+    {
+        const char *row = static_cast<const char *>(p.logits) + (r * p.stride + first) * (kHalf ? 2 : 4);
+        const auto keep4 = [&](int at, float4 v) {
+            v = make_float4(taken(v.x), taken(v.y), taken(v.z), taken(v.w));
+            *reinterpret_cast<float4 *>(held + at) = v;
+            most = fmaxf(most, fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)));
+        };
+        const int n_wide = (reinterpret_cast<uintptr_t>(row) & 15) == 0 ? max(0, n_here) / 8 * 8 : 0;   // read 16 bytes at a time
+        constexpr int kAhead = 4;
+        for (int base = 0; base < n_wide; base += kAhead * kThreads * (kHalf ? 8 : 4)) {
+            uint4 v[kAhead];
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a) {
+                const int at = base + (a * kThreads + tid) * (kHalf ? 8 : 4);
+                if (at < n_wide) v[a] = __ldg(reinterpret_cast<const uint4 *>(row + at * (kHalf ? 2 : 4)));
+            }
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a) {
+                const int at = base + (a * kThreads + tid) * (kHalf ? 8 : 4);
+                if (at >= n_wide) continue;
+                const auto lo = [](uint32_t w) { return __uint_as_float(w << 16); };
+                const auto hi = [](uint32_t w) { return __uint_as_float(w & 0xffff0000u); };
+                if constexpr (kHalf) {
+                    keep4(at, make_float4(lo(v[a].x), hi(v[a].x), lo(v[a].y), hi(v[a].y)));
+                    keep4(at + 4, make_float4(lo(v[a].z), hi(v[a].z), lo(v[a].w), hi(v[a].w)));
+                } else {
+                    keep4(at, make_float4(__uint_as_float(v[a].x), __uint_as_float(v[a].y), __uint_as_float(v[a].z), __uint_as_float(v[a].w)));
+                }
+            }
+        }
+        // what is left, an entry at a time; entries behind the end are not there
+        constexpr int kSingles = 8;
+        for (int base = n_wide; base < p.part; base += kSingles * kThreads) {
+            float v[kSingles];
+#pragma unroll
+            for (int a = 0; a < kSingles; ++a) {
+                const int at = base + a * kThreads + tid;
+                v[a] = at >= n_here ? -INFINITY
+                     : kHalf ? __bfloat162float(__ldg(reinterpret_cast<const __nv_bfloat16 *>(row) + at)) : __ldg(reinterpret_cast<const float *>(row) + at);
+            }
+#pragma unroll
+            for (int a = 0; a < kSingles; ++a) {
+                const int at = base + a * kThreads + tid;
+                if (at >= p.part) continue;
+                held[at] = taken(v[a]);
+                most = fmaxf(most, held[at]);
+            }
+        }
     }
-    most = over_warp(most, [](float a, float b) { return fmaxf(a, b); });
-    if (lane == 0) sm.words[warp] = key_of(most);
-    for (int i = tid; i < kBins; i += kThreads) sm.bins[i] = 0;
+    const float top_here = over_warp(most, [](float a, float b) { return fmaxf(a, b); });
+    if (lane == 0) sm.of_warp[warp] = top_here;
+    for (int i = tid; i < kBins; i += kThreads) sm.high[i] = 0, sm.low[i] = 0;
     if (tid == 0) sm.n_list = 0;
     __syncthreads();
     if (warp == 0) {
-        const uint32_t top = __reduce_max_sync(0xffffffffu, lane < kWarps ? sm.words[lane] : 0u);
+        const float top = over_warp(sm.of_warp[lane & (kWarps - 1)], [](float a, float b) { return fmaxf(a, b); });
         everywhere(&sm.top_of_cta[rank], top);
     }
     cluster.sync();
-    const uint32_t top = __reduce_max_sync(0xffffffffu, lane < CL ? sm.top_of_cta[lane] : 0u);
-    const float peak = logit_of(top), rate = fmaxf(1.4426950408889634f / (greedy ? 1.f : T), 1.2e-38f);   // (an infinite T: all alike)
-    const auto bits_of = [&](float x) { return x == peak ? 0.f : (x - peak) * rate; };   // log2 e
-    const auto e_of = [&](float x) { return x == peak ? 1.f : svk::fast_exp2((x - peak) * rate); };
-    if (top == 0) {   // no entry
+    const float peak = over_warp(sm.top_of_cta[lane < CL ? lane : 0], [](float a, float b) { return fmaxf(a, b); });
+    if (peak == -INFINITY) {   // no entry
         if (p.probs)
-            for (int i = rank * p.part + tid; i < min(p.V, (rank + 1) * p.part); i += kThreads) p.probs[(size_t)r * p.V + i] = 0.f;
+            for (int i = tid; i < n_here; i += kThreads) p.probs[(size_t)r * p.V + first + i] = 0.f;
         if (p.tokens && rank == 0 && tid == 0) p.tokens[r] = -1;
         return;
     }
+    const float rate = fmaxf(1.4426950408889634f / (greedy ? 1.f : T), 1.2e-38f);   // (an infinite temperature: all alike)
+    const auto bits_of = [&](float x) { return __fmul_rn(__fsub_rn(peak, x), rate); };   // -log2 e
+    const auto e_of = [&](float x) { return svk::fast_exp2(-bits_of(x)); };
+    constexpr float kPlace = 8388608.f;   // (the last place of a sum with it is 1)
+    const auto place_of = [&](float bits) { return __fadd_rn(fminf(__fmul_rn(bits, kBinsPerBit), (float)(kBins - 1)), kPlace); };
+    const auto bin_at = [](float place) { return __float_as_uint(place) & (kBins - 1); };
+    const auto each = [&](auto f) {   // f(index, logit), all entries of this lane in ascending order
+        for (int j = 0; j < words; ++j) {
+            const int at = w0 + j * 128;
+            const float4 v = *reinterpret_cast<const float4 *>(held + at);
+            f(first + at, v.x), f(first + at + 1, v.y), f(first + at + 2, v.z), f(first + at + 3, v.w);
+        }
+    };
 
     // exclusive prefix and total over the CTA, in thread order
     const auto scan_block = [&](Mass v, Mass &total) {
-        Mass upto = v;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const Mass o = __shfl_up_sync(0xffffffffu, upto, d);
-            if (lane >= d) upto += o;
-        }
+        const Mass upto = scan_warp(v);
         __syncthreads();
         if (lane == 31) sm.scan[warp] = upto;
         __syncthreads();
         Mass before = upto - v;
         total = 0;
+#pragma unroll
         for (int w = 0; w < kWarps; ++w) {
             if (w < warp) before += sm.scan[w];
             total += sm.scan[w];
@@ -218,7 +250,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const Params p)
         return before;
     };
     int turn = 0;
-    // total over the cluster of a value of each thread; of_cta[turn] keeps the CTAs' totals
+    // total over the cluster of a value of each thread; sums keeps the warps' totals, of_cta[turn] the CTAs'
     const auto sum_cluster = [&](Mass v) {
         turn ^= 1;
         v = sum_over_warp(v);
@@ -228,6 +260,12 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const Params p)
         if (warp == 0) everywhere(&sm.of_cta[turn][rank], sum_over_warp(lane < kWarps ? sm.sums[lane] : 0));
         cluster.sync();
         return sum_over_warp(lane < CL ? sm.of_cta[turn][lane] : 0);
+    };
+    const auto before_warp = [&] {   // ... of the CTAs and warps before this one
+        Mass before = 0;
+        for (int c = 0; c < rank; ++c) before += sm.of_cta[turn][c];
+        for (int w = 0; w < warp; ++w) before += sm.sums[w];
+        return before;
     };
     // The bin in which the sums over the cluster's histograms reach the goal, and what is in the bins ahead of it.  A CTA adds up its share of the
     // bins of all CTAs; the CTA in whose share the goal lies finds the bin.  goal <= the sum of all.
@@ -240,7 +278,8 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const Params p)
             v[i] = 0;
             const int b = tid * per + i;
             if (i < per && b < share)
-                for (int c = 0; c < CL; ++c) v[i] += *cluster.map_shared_rank(&sm.bins[rank * share + b], c);
+                for (int c = 0; c < CL; ++c)
+                    v[i] += whole<kNucleus>(*cluster.map_shared_rank(&sm.high[rank * share + b], c), *cluster.map_shared_rank(&sm.low[rank * share + b], c));
             mine += v[i];
         }
         Mass total;
@@ -267,17 +306,18 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const Params p)
     };
     const auto clear = [&] {
         __syncthreads();
-        for (int i = tid; i < kBins; i += kThreads) sm.bins[i] = 0;
+        for (int i = tid; i < kBins; i += kThreads) sm.high[i] = 0, sm.low[i] = 0;
         if (tid == 0) sm.n_list = 0;
         __syncthreads();
     };
-    // Entries for which `in` holds, into the first CTA's list; their number (over kList: the list is not complete).
+    // Counts are kept in units that make them masses of the nucleus' kind.
+    const auto add_one = [&](uint32_t bin) { atomicAdd(&sm.low[bin], 1); };
+    // Entries for which `in` holds, sorted by the first CTA; their number (over kList: there is no list).
     const auto gather = [&](auto in) {
-        row.each([&](int i, float x) {
-            const uint32_t key = key_of(x);
-            if (key && in(key, x, (uint32_t)i)) {
+        each([&](int i, float x) {
+            if (in(x, (uint32_t)i)) {
                 const uint32_t at = atomicAdd(&sm.n_list, 1u);
-                if (at < kList) sm.list[at] = (uint64_t)key << 32 | (uint32_t)~i;
+                if (at < kList) sm.list[at] = (uint64_t)key_of(x) << 32 | (uint32_t)~i;
             }
         });
         __syncthreads();
@@ -285,7 +325,9 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const Params p)
         cluster.sync();
         uint32_t n = 0;
         for (int c = 0; c < CL; ++c) n += sm.count_of_cta[c];
-        if (rank == 0 && n <= kList) {
+        if (n > kList) {
+            cluster.sync();   // (the counts may be written again)
+        } else if (rank == 0) {
             uint32_t at = sm.count_of_cta[0];
             for (int c = 1; c < CL; ++c) {
                 for (uint32_t i = tid; i < sm.count_of_cta[c]; i += kThreads) sm.list[at + i] = *cluster.map_shared_rank(&sm.list[i], c);
@@ -296,59 +338,84 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const Params p)
                 const uint64_t me = sm.list[i];
                 int place = 0;
                 for (uint32_t o = 0; o < n; ++o) place += sm.list[o] > me;
-                sm.sorted[place] = me;
+                sm.sorted()[place] = me;
             }
             __syncthreads();
         }
-        if (n > kList) cluster.sync();   // (the counts may be written again)
         return n;
     };
-    const auto bin_of = [&](float x) { return max(0, min(kBins - 1, (int)(-bits_of(x) * kBinsPerBit))); };
 
-    Boundary last{1u, 0xffffffffu};
+    Boundary last{-FLT_MAX, 0xffffffffu};   // all of them
     const bool by_count = k > 0 && k < p.V, by_mass = top_p < 1.f;
     bool listed = false;   // the first CTA's sorted list begins with all entries that stay
     uint32_t n_listed = 0;
     for (int step = 0; step < 2 && !listed; ++step) {
         if (!(step ? by_mass : by_count)) continue;
+        Mass ahead;
+        if (step == 0) {
+            // the k-th largest of the threads' maxima
+            if (most > -INFINITY) add_one(bin_at(place_of(bits_of(most))));
+            const Mass maxima = sum_cluster(most > -INFINITY ? 1 : 0);
+            if (maxima >= (Mass)k) {
+                const float place = kPlace + find_bin((Mass)k, ahead);
+                const uint32_t n = gather([&](float x, uint32_t) { return x > -INFINITY && place_of(bits_of(x)) <= place; });
+                if (n <= kList) {
+                    listed = true, n_listed = n;
+                    break;
+                }
+            }
+        }
         const Boundary within = last;
-        const auto weight = [&](uint32_t key, float x) { return step ? mass_of(parts_of(e_of(x))) : 1ull; };
+        const auto weight = [&](float x) { return step ? mass_of<kNucleus>(e_of(x)) : 1ull; };
+        const auto add = [&](uint32_t bin, float bits) {
+            if (step == 0) {
+                add_one(bin);
+                return;
+            }
+            const Parts q = parts_of<kNucleus>(svk::fast_exp2(-bits));
+            if (q.high) atomicAdd(&sm.high[bin], q.high);
+            if (q.low) atomicAdd(&sm.low[bin], q.low);
+        };
         // first histogram: by the distance from the maximum
-        Mass all = 0;
         clear();
-        row.each([&](int i, float x) {
-            const uint32_t key = key_of(x);
-            if (!key || !within.keeps(key, i)) return;
-            const Mass w = weight(key, x);
-            all += w;
-            if (w) atomicAdd(&sm.bins[bin_of(x)], w);
-        });
+        Mass all = 0;
+        if (step == 0) {
+            each([&](int, float x) {
+                if (x > -INFINITY) add_one(bin_at(place_of(bits_of(x)))), ++all;
+            });
+        } else {
+            uint32_t high = 0;   // (a lane has at most 96 entries)
+            int low = 0;
+            each([&](int i, float x) {
+                if (!within.keeps(x, i)) return;
+                const float bits = bits_of(x);
+                const Parts q = parts_of<kNucleus>(svk::fast_exp2(-bits));
+                const uint32_t bin = bin_at(place_of(bits));
+                high += q.high, low += q.low;
+                if (q.high) atomicAdd(&sm.high[bin], q.high);
+                if (q.low) atomicAdd(&sm.low[bin], q.low);
+            });
+            all = whole<kNucleus>(high, low);
+        }
         all = sum_cluster(all);
         const Mass goal = step ? max((Mass)1, (Mass)ceil((double)fmaxf(top_p, 0.f) * (double)all)) : (Mass)k;
         if (goal > all) continue;   // (fewer entries than k)
-        Mass ahead;
-        const int bin = find_bin(goal, ahead);
-        if (step == 0) {
-            const uint32_t n = gather([&](uint32_t, float x, uint32_t) { return bin_of(x) <= bin; });
-            if (n <= kList) {
-                listed = true, n_listed = n;
-                break;
-            }
-            clear();
-        }
-        uint32_t n = gather([&](uint32_t key, float x, uint32_t i) { return bin_of(x) == bin && within.keeps(key, i); });
+        const float place = kPlace + find_bin(goal, ahead);
+        __syncthreads();
+        if (tid == 0) sm.n_list = 0;
+        __syncthreads();
+        uint32_t n = gather([&](float x, uint32_t i) { return place_of(bits_of(x)) == place && within.keeps(x, i); });
         // too many: the keys of the bin, then of a part of them, divided evenly
-        uint32_t lo = 1, hi = 0xffffffffu;
+        uint32_t lo = 0, hi = 0;
         if (n > kList) {
-            uint32_t least = 0xffffffffu, greatest = 0;
-            row.each([&](int i, float x) {
-                const uint32_t key = key_of(x);
-                if (key && bin_of(x) == bin && within.keeps(key, i)) least = min(least, key), greatest = max(greatest, key);
+            lo = 0xffffffffu;
+            each([&](int i, float x) {
+                if (place_of(bits_of(x)) == place && within.keeps(x, i)) lo = min(lo, key_of(x)), hi = max(hi, key_of(x));
             });
-            least = __reduce_min_sync(0xffffffffu, least), greatest = __reduce_max_sync(0xffffffffu, greatest);
+            lo = __reduce_min_sync(0xffffffffu, lo), hi = __reduce_max_sync(0xffffffffu, hi);
             if (tid == 0) sm.range[rank][0] = 0xffffffffu, sm.range[rank][1] = 0;
             __syncthreads();
-            if (lane == 0) atomicMin(&sm.range[rank][0], least), atomicMax(&sm.range[rank][1], greatest);
+            if (lane == 0) atomicMin(&sm.range[rank][0], lo), atomicMax(&sm.range[rank][1], hi);
             __syncthreads();
             if (warp == 0) {
                 const uint32_t a = sm.range[rank][0], b = sm.range[rank][1];
@@ -360,60 +427,55 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const Params p)
         }
         while (n > kList && lo < hi) {
             const int shift = max(0, 32 - __clz(hi - lo) - 11);   // (hi - lo) >> shift < kBins
+            const auto in = [&](float x, uint32_t i) { return x > -INFINITY && key_of(x) >= lo && key_of(x) <= hi && within.keeps(x, i); };
             clear();
-            row.each([&](int i, float x) {
-                const uint32_t key = key_of(x);
-                if (key < lo || key > hi || !within.keeps(key, i)) return;
-                const Mass w = weight(key, x);
-                if (w) atomicAdd(&sm.bins[(hi - key) >> shift], w);
+            each([&](int i, float x) {
+                if (in(x, i)) add((hi - key_of(x)) >> shift, bits_of(x));
             });
             const int b = find_bin(goal - ahead, all);
             ahead += all;
             const uint32_t below = (uint32_t)(((Mass)(b + 1) << shift) - 1);
             lo = hi - lo < below ? lo : hi - below, hi -= (uint32_t)b << shift;
-            clear();
-            n = gather([&](uint32_t key, float, uint32_t i) { return key >= lo && key <= hi && within.keeps(key, i); });
+            __syncthreads();
+            if (tid == 0) sm.n_list = 0;
+            __syncthreads();
+            n = gather(in);
         }
+        const auto found = [&](float x, uint32_t i) {
+            for (int c = 0; c < CL; ++c) *cluster.map_shared_rank(&sm.boundary, c) = Boundary{x, i};
+        };
         if (n <= kList) {   // ranked by the first CTA
             if (rank == 0) {
                 Mass sum = ahead;
                 for (uint32_t base = 0; base < n; base += kThreads) {
                     const bool in = base + tid < n;
-                    const uint64_t me = in ? sm.sorted[base + tid] : 0;
-                    const Mass w = in ? weight((uint32_t)(me >> 32), logit_of((uint32_t)(me >> 32))) : 0;
+                    const uint64_t me = in ? sm.sorted()[base + tid] : 0;
+                    const Mass w = in ? weight(logit_of((uint32_t)(me >> 32))) : 0;
                     Mass total;
                     const Mass before = sum + scan_block(w, total);
-                    if (in && before < goal && before + w >= goal) {
-                        for (int c = 0; c < CL; ++c) *cluster.map_shared_rank(&sm.boundary, c) = Boundary{(uint32_t)(me >> 32), ~(uint32_t)me};
-                    }
+                    if (in && before < goal && before + w >= goal) found(logit_of((uint32_t)(me >> 32)), ~(uint32_t)me);
                     sum += total;
                 }
             }
         } else {   // all equal: counted off in the order of the vocabulary
-            const Mass each = weight(hi, logit_of(hi)), nth = (goal - ahead + each - 1) / each;   // >= 1; the nth of them is the last
+            const float x_all = logit_of(hi);
+            const Mass one = weight(x_all), nth = (goal - ahead + one - 1) / one;   // the nth of them (from 1) is the last
             uint32_t mine = 0;
-            row.each([&](int i, float x) { mine += key_of(x) == hi && within.keeps(hi, i); });
-            mine = __reduce_add_sync(0xffffffffu, mine);
-            (void)sum_cluster(lane == 0 ? mine : 0);
-            Mass before = 0;
-            for (int c = 0; c < rank; ++c) before += sm.of_cta[turn][c];
-            for (int w = 0; w < warp; ++w) before += sm.sums[w];
-            for (int j = 0; j < row.words() && before < nth; ++j) {   // (uniform over a warp)
-                const float4 v = row.word(j);
+            each([&](int i, float x) { mine += x == x_all && within.keeps(x, i); });
+            (void)sum_cluster(mine);
+            Mass before = before_warp();
+            for (int j = 0; j < words && before < nth; ++j) {   // (uniform over a warp)
+                const int at = w0 + j * 128;
+                const float4 v = *reinterpret_cast<const float4 *>(held + at);
                 const float x[4] = {v.x, v.y, v.z, v.w};
-                const int i = rank * p.part + row.first(j);
                 uint32_t m = 0;
-                for (int e = 0; e < 4; ++e) m += key_of(x[e]) == hi && within.keeps(hi, i + e);
-                uint32_t upto = m;
 #pragma unroll
-                for (int d = 1; d < 32; d <<= 1) {
-                    const uint32_t o = __shfl_up_sync(0xffffffffu, upto, d);
-                    if (lane >= d) upto += o;
-                }
-                Mass at = before + upto - m;
+                for (int e = 0; e < 4; ++e) m += x[e] == x_all && within.keeps(x[e], first + at + e);
+                const uint32_t upto = scan_warp(m);
+                Mass place_in = before + upto - m;
+#pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (key_of(x[e]) == hi && within.keeps(hi, i + e) && ++at == nth)
-                        for (int c = 0; c < CL; ++c) *cluster.map_shared_rank(&sm.boundary, c) = Boundary{hi, (uint32_t)(i + e)};
+                    if (x[e] == x_all && within.keeps(x[e], first + at + e) && ++place_in == nth) found(x_all, first + at + e);
                 before += __shfl_sync(0xffffffffu, upto, 31);
             }
         }
@@ -421,50 +483,53 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const Params p)
         last = sm.boundary;
     }
 
+    Mass total;   // of the draw
     if (listed) {
         if (rank == 0) {
             // of the sorted list: the first k, their nucleus, those that are likely enough; at most two entries a thread
+            uint64_t *const sorted = sm.sorted();
             const uint32_t n_k = min(n_listed, (uint32_t)k);
-            Mass w[kList / kThreads], ahead[kList / kThreads], whole = 0;
+            float e[kList / kThreads];
+            Mass ahead[kList / kThreads], all = 0;
 #pragma unroll
             for (int i = 0; i < kList / kThreads; ++i) {
                 const uint32_t at = i * kThreads + tid;
-                w[i] = at < n_k ? mass_of(parts_of(e_of(logit_of((uint32_t)(sm.sorted[at] >> 32))))) : 0;
-                Mass total;
-                ahead[i] = whole + scan_block(w[i], total);
-                whole += total;
+                e[i] = at < n_k ? e_of(logit_of((uint32_t)(sorted[at] >> 32))) : 0.f;
+                Mass sum;
+                ahead[i] = all + scan_block(mass_of<kNucleus>(e[i]), sum);
+                all += sum;
             }
-            const Mass goal = by_mass ? max((Mass)1, (Mass)ceil((double)fmaxf(top_p, 0.f) * (double)whole)) : whole + 1;
+            const Mass goal = by_mass ? max((Mass)1, (Mass)ceil((double)fmaxf(top_p, 0.f) * (double)all)) : all + 1;
             uint32_t n_keep = 0;
 #pragma unroll
             for (int i = 0; i < kList / kThreads; ++i) {
                 const uint32_t at = i * kThreads + tid;
-                const uint32_t key = at < n_k ? (uint32_t)(sm.sorted[at] >> 32) : 0;
-                n_keep += __syncthreads_count(at < n_k && (at == 0 || (ahead[i] < goal && (key == top || e_of(logit_of(key)) >= min_e))));
+                n_keep += __syncthreads_count(at < n_k && (at == 0 || (ahead[i] < goal && (e[i] >= min_e || logit_of((uint32_t)(sorted[at] >> 32)) == peak))));
             }
-            Mass total = 0;
+            Mass kept = 0;
 #pragma unroll
-            for (int i = 0; i < kList / kThreads; ++i) total += i * kThreads + tid < n_keep ? w[i] : 0;
-            Mass sum;
-            (void)scan_block(total, sum);
+            for (int i = 0; i < kList / kThreads; ++i) kept += i * kThreads + tid < n_keep ? mass_of<kDraw>(e[i]) : 0;
+            (void)scan_block(kept, total);
             if (tid == 0) {
-                const uint64_t at = sm.sorted[n_keep - 1];
+                const uint64_t at = sorted[n_keep - 1];
                 for (int c = 0; c < CL; ++c) {
-                    *cluster.map_shared_rank(&sm.boundary, c) = Boundary{(uint32_t)(at >> 32), ~(uint32_t)at};
-                    *cluster.map_shared_rank(&sm.found_ahead, c) = sum;
+                    *cluster.map_shared_rank(&sm.boundary, c) = Boundary{logit_of((uint32_t)(at >> 32)), ~(uint32_t)at};
+                    *cluster.map_shared_rank(&sm.found_ahead, c) = total;
                 }
                 sm.token = 0x7fffffff;
             }
             __syncthreads();
             if (p.tokens) {   // the first entry in the order of the vocabulary up to which the masses reach the target
-                const Mass target = max((Mass)1, min(sum, (Mass)ceil((double)u * (double)sum)));
-                Mass *of = sm.bins;
-                for (uint32_t i = tid; i < n_keep; i += kThreads) of[i] = mass_of(parts_of(e_of(logit_of((uint32_t)(sm.sorted[i] >> 32)))));
+                const Mass target = max((Mass)1, min(total, (Mass)ceil((double)u * (double)total)));
+                Mass *const of = sm.masses();
+#pragma unroll
+                for (int i = 0; i < kList / kThreads; ++i)
+                    if (i * kThreads + tid < n_keep) of[i * kThreads + tid] = mass_of<kDraw>(e[i]);
                 __syncthreads();
                 for (uint32_t i = tid; i < n_keep; i += kThreads) {
-                    const uint32_t me = (uint32_t)sm.sorted[i];   // (complement of the index)
+                    const uint32_t me = (uint32_t)sorted[i];   // (complement of the index)
                     Mass upto = 0;
-                    for (uint32_t o = 0; o < n_keep; ++o) upto += (uint32_t)sm.sorted[o] >= me ? of[o] : 0;
+                    for (uint32_t o = 0; o < n_keep; ++o) upto += (uint32_t)sorted[o] >= me ? of[o] : 0;
                     if (of[i] && upto >= target) atomicMin(&sm.token, (int)~me);
                 }
                 __syncthreads();
@@ -473,108 +538,65 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const Params p)
         }
         cluster.sync();   // (nobody leaves while the first CTA reads its list)
         if (!p.probs) return;
-        last = sm.boundary;
-        const float inv = 1099511627776.f / (float)sm.found_ahead;
-        for (int j = 0; j < row.words(); ++j) {
-            const float4 v = row.word(j);
-            const float x[4] = {v.x, v.y, v.z, v.w};
-            const int i = rank * p.part + row.first(j);
-            float *to = p.probs + (size_t)r * p.V + i;
-            float o[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t key = key_of(x[e]);
-                o[e] = key && last.keeps(key, i + e) ? e_of(x[e]) * inv : 0.f;
-            }
-            if (i + 4 <= p.V && (reinterpret_cast<uintptr_t>(to) & 15) == 0) *reinterpret_cast<float4 *>(to) = make_float4(o[0], o[1], o[2], o[3]);
-            else
-                for (int e = 0; e < 4; ++e)
-                    if (i + e < p.V) to[e] = o[e];
-        }
-        return;
-    }
-
-    // the mass that stays, by CTA and warp
-    const auto kept = [&](int i, float x, float &e) {
-        const uint32_t key = key_of(x);
-        e = e_of(x);
-        return key && last.keeps(key, i) && (e >= min_e || key == top);
-    };
-    uint32_t high = 0;
-    int low = 0;
-    Mass mine = 0;
-    int since = 0;
-    row.each([&](int i, float x) {
-        float e;
-        if (kept(i, x, e)) {
-            const Parts q = parts_of(e);
+        last = sm.boundary, total = sm.found_ahead, min_e = 0.f;
+    } else {
+        // the mass that stays, by CTA and warp
+        const auto mass = [&](float x, uint32_t i) {
+            if (!last.keeps(x, i)) return Parts{0u, 0};
+            const float e = e_of(x);
+            return e >= min_e || x == peak ? parts_of<kDraw>(e) : Parts{0u, 0};
+        };
+        uint32_t high = 0;   // (a lane has at most 96 entries)
+        int low = 0;
+        each([&](int i, float x) {
+            const Parts q = mass(x, i);
             high += q.high, low += q.low;
+        });
+        total = sum_cluster(whole<kDraw>(high, low));
+        if (p.tokens) {
+            const Mass target = max((Mass)1, min(total, (Mass)ceil((double)u * (double)total)));
+            Mass before = before_warp();
+            if (before < target && before + sm.sums[warp] >= target) {   // this warp has it
+                for (int j = 0; j < words && before < target; ++j) {
+                    const int at = w0 + j * 128;
+                    const float4 v = *reinterpret_cast<const float4 *>(held + at);
+                    const float x[4] = {v.x, v.y, v.z, v.w};
+                    Mass w[4], m = 0;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const Parts q = mass(x[e], first + at + e);
+                        w[e] = whole<kDraw>(q.high, q.low);
+                        m += w[e];
+                    }
+                    const Mass upto = scan_warp(m);
+                    Mass sum = before + upto - m;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (sum < target && sum + w[e] >= target) p.tokens[r] = first + at + e;
+                        sum += w[e];
+                    }
+                    before += __shfl_sync(0xffffffffu, upto, 31);
+                }
+            }
         }
-        if (++since == 1024) mine += ((Mass)high << 20) + (long long)low, high = 0, low = 0, since = 0;   // (before 32 bits overflow)
-    });
-    mine += ((Mass)high << 20) + (long long)low;
-    const Mass total = sum_cluster(mine);
-    const Mass target = max((Mass)1, min(total, (Mass)ceil((double)u * (double)total)));
+        if (!p.probs) return;
+    }
+
     const float inv = 1099511627776.f / (float)total;
-    if (p.tokens) {
-        Mass before = 0;
-        for (int c = 0; c < rank; ++c) before += sm.of_cta[turn][c];
-        for (int w = 0; w < warp; ++w) before += sm.sums[w];
-        if (before < target && before + sm.sums[warp] >= target) {   // this warp has it
-            for (int j = 0; j < row.words(); ++j) {
-                const float4 v = row.word(j);
-                const float x[4] = {v.x, v.y, v.z, v.w};
-                const int i = rank * p.part + row.first(j);
-                Mass w[4], m = 0;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float ex;
-                    w[e] = kept(i + e, x[e], ex) ? mass_of(parts_of(ex)) : 0;
-                    m += w[e];
-                }
-                Mass upto = m;
-#pragma unroll
-                for (int d = 1; d < 32; d <<= 1) {
-                    const Mass o = __shfl_up_sync(0xffffffffu, upto, d);
-                    if (lane >= d) upto += o;
-                }
-                Mass at = before + upto - m;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (at < target && at + w[e] >= target) p.tokens[r] = i + e;
-                    at += w[e];
-                }
-                before += __shfl_sync(0xffffffffu, upto, 31);
-                if (before >= target) break;
-            }
-        }
+    const auto prob = [&](float x, uint32_t i) {
+        if (!last.keeps(x, i)) return 0.f;
+        const float e = e_of(x);
+        return e >= min_e || x == peak ? e * inv : 0.f;
+    };
+    float *const to = p.probs + (size_t)r * p.V + first;
+    const int n_wide = (reinterpret_cast<uintptr_t>(to) & 15) == 0 ? max(0, n_here) / 4 * 4 : 0;
+#pragma unroll 2
+    for (int at = tid * 4; at < n_wide; at += kThreads * 4) {
+        const float4 v = *reinterpret_cast<const float4 *>(held + at);
+        *reinterpret_cast<float4 *>(to + at) = make_float4(prob(v.x, first + at), prob(v.y, first + at + 1), prob(v.z, first + at + 2), prob(v.w, first + at + 3));
     }
-    if (p.probs) {
-        for (int j = 0; j < row.words(); ++j) {
-            const float4 v = row.word(j);
-            const float x[4] = {v.x, v.y, v.z, v.w};
-            const int i = rank * p.part + row.first(j);
-            float *to = p.probs + (size_t)r * p.V + i;
-            float o[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float ex;
-                o[e] = kept(i + e, x[e], ex) ? ex * inv : 0.f;
-            }
-            if (i + 4 <= p.V && (reinterpret_cast<uintptr_t>(to) & 15) == 0) *reinterpret_cast<float4 *>(to) = make_float4(o[0], o[1], o[2], o[3]);
-            else
-                for (int e = 0; e < 4; ++e)
-                    if (i + e < p.V) to[e] = o[e];
-        }
-    }
-}
-
-constexpr int kMostSmem = 227 * 1024;
-
-const void *kernel_for(bool half, bool held)
-{
-    return half ? held ? (const void *)sample_kernel<true, true> : (const void *)sample_kernel<true, false>
-                : held ? (const void *)sample_kernel<false, true> : (const void *)sample_kernel<false, false>;
+#pragma unroll 4
+    for (int at = n_wide + tid; at < n_here; at += kThreads) to[at] = prob(held[at], first + at);
 }
 
 int part_for(int vocab, int cluster) { return ((vocab + cluster - 1) / cluster + kGrain - 1) / kGrain * kGrain; }
@@ -591,24 +613,25 @@ extern "C" sv_status sv_sample(int32_t n_rows, int32_t vocab, const void *logits
     if (!svh::aligned(logits, logits_bf16 ? 2 : 4) || !svh::aligned(probs, 4)) return SV_ERR_ALIGN;
     if (n_rows == 0) return SV_OK;
     if ((int64_t)n_rows * kMaxCluster > INT32_MAX) return SV_ERR_SHAPE;
-    // the smallest cluster that holds a row, and larger ones while they find SMs
+    // the smallest cluster whose CTAs share an SM by two, and larger ones while they find SMs
     int cluster = 1;
-    while (cluster < kMaxCluster && (part_for(vocab, cluster) * sizeof(float) + sizeof(Smem) > kMostSmem || 2 * cluster * n_rows <= svh::sm_count()) &&
-           part_for(vocab, cluster) > kGrain)
+    while (cluster < kMaxCluster && part_for(vocab, cluster) > kGrain &&
+           (part_for(vocab, cluster) > kPart || 2ll * cluster * n_rows <= svh::sm_count()))
         cluster *= 2;
     const int part = part_for(vocab, cluster);
-    const bool held = part * sizeof(float) + sizeof(Smem) <= kMostSmem;
     const Params p = {logits, row_stride, temperature, top_p, min_p, u, top_k, tokens, probs, vocab, rows_per_param, part};
-    const void *fn = kernel_for(logits_bf16, held);
-    static svh::OncePerDevice once[2][2];
-    if (once[logits_bf16 != 0][held].run([&] { return cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem); }) != cudaSuccess) {
+    const auto kernel = logits_bf16 ? sample_kernel<true> : sample_kernel<false>;
+    static svh::OncePerDevice once[2];
+    if (once[logits_bf16 != 0].run([&] {
+            return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(sizeof(Smem) + kMostPart * sizeof(float)));
+        }) != cudaSuccess) {
         (void)cudaGetLastError();
         return SV_ERR_CUDA;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(n_rows * cluster));
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = sizeof(Smem) + (held ? part * sizeof(float) : 0);
+    cfg.dynamicSmemBytes = sizeof(Smem) + part * sizeof(float);
     cfg.stream = static_cast<cudaStream_t>(stream);
     cudaLaunchAttribute attr[2];
     svh::pdl_attribute(attr);
@@ -616,6 +639,5 @@ extern "C" sv_status sv_sample(int32_t n_rows, int32_t vocab, const void *logits
     attr[1].val.clusterDim.x = cluster, attr[1].val.clusterDim.y = 1, attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    void *args[] = {const_cast<Params *>(&p)};
-    return cudaLaunchKernelExC(&cfg, fn, args) == cudaSuccess ? svh::launch_status() : SV_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, kernel, p) == cudaSuccess ? svh::launch_status() : SV_ERR_CUDA;
 }
