@@ -59,12 +59,16 @@ enum Bar {
     kX = kO + 2,                 // (one tile) the second stream's sums are there
     kXFree,                      // ... and have been taken
     kDone,                       // all MMAs are through
-    kNumBars
+    kItem,                       // [2] the next item is in shared memory (items take the two places in turn)
+    kItemTaken = kItem + 2,      // [2] ... and has been read by all roles
+    kNumBars = kItemTaken + 2
 };
+constexpr int kReaders = 11;     // warps that read the items
 __device__ __forceinline__ int arrivals(int bar)
 {
     if (bar >= kEmpty && bar < kEmpty + kStages) return 2;
     if (bar == kQFree || bar == kDone) return 2;
+    if (bar >= kItemTaken) return kReaders;
     return (bar >= kP0 && bar < kO) || bar == kX || bar == kXFree ? 4 : 1;   // (one lane of each warp of a warpgroup)
 }
 
@@ -144,13 +148,14 @@ __device__ __forceinline__ void load_box_4d(uint32_t dst, const void *map, int x
 // What the warps of a CTA share: barriers, and whether one of their waits gave up.
 struct Shared {
     uint32_t bars;
+    ChunkItem *items;       // [2]
     volatile int *abort_flag;
     volatile int *landed;   // [2] the last ring slot that the issuing warp of a stream has seen full
     int32_t *status;
     __device__ uint32_t bar(int i) const { return bars + i * 8; }
-    __device__ bool wait(int i, uint32_t parity, int bit) const
+    __device__ bool wait(int i, uint32_t parity, int bit, int rounds = 64) const
     {
-        for (int round = 0; round < 64; ++round) {   // (looks at the flag between polls of a limited number)
+        for (int round = 0; round < rounds; ++round) {   // (looks at the flag between polls of a limited number)
             if (mbar_wait_bounded(bar(i), parity, 1u << 13)) return true;
             if (*abort_flag) return false;
         }
@@ -173,8 +178,36 @@ struct Shared {
     __device__ bool warp_wait(int i, uint32_t parity, int bit) const { return __all_sync(0xffffffffu, wait(i, parity, bit)); }
 };
 
+// ---------------------------------------------------------------------- warp 11: the items, two ahead of the roles that read them
+// (A walk of their own in every role cost the softmax its registers: spills of 17 loads a unit, two thirds of them from L2, were most of
+// the time of a prompt of 8K.)
+__device__ __forceinline__ void hand_out(ChunkWalk &walk, const Shared &sh)
+{
+    for (int n = 0;; ++n) {
+        if (n > 1 && !__all_sync(0xffffffffu, sh.wait(kItemTaken + (n & 1), ((n >> 1) - 1) & 1, 64, 1 << 13))) return;   // (as long as an item)
+        ChunkItem it;
+        const bool more = walk.next(it);
+        if (!more) it.units = -1;
+        if ((threadIdx.x & 31) == 0) {
+            sh.items[n & 1] = it;
+            mbar_arrive(sh.bar(kItem + (n & 1)));
+        }
+        __syncwarp();
+        if (!more) return;
+    }
+}
+// The item of this number, by a whole warp; false: there are no more, or a wait gave up.
+__device__ __forceinline__ bool take(const Shared &sh, int n, ChunkItem &it)
+{
+    if (!sh.warp_wait(kItem + (n & 1), (n >> 1) & 1, 64)) return false;
+    it = sh.items[n & 1];
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(sh.bar(kItemTaken + (n & 1)));
+    return it.units >= 0;
+}
+
 // ---------------------------------------------------------------------- warp 8: copies
-__device__ __forceinline__ void produce(const Params &p, ChunkWalk &walk, const Shared &sh, uint32_t smem0, const CUtensorMap &tm_q, const CUtensorMap &tm_k,
+__device__ __forceinline__ void produce(const Params &p, const Shared &sh, uint32_t smem0, const CUtensorMap &tm_q, const CUtensorMap &tm_k,
                                         const CUtensorMap &tm_v)
 {
     const int lane = threadIdx.x & 31;
@@ -182,7 +215,7 @@ __device__ __forceinline__ void produce(const Params &p, ChunkWalk &walk, const 
     int slot = 0, items = 0;            // ring slots and items so far
     bool dead = false, clamped = false;
     ChunkItem it;
-    while (!dead && walk.next(it)) {
+    for (int n = 0; !dead && take(sh, n, it); ++n) {
         if (it.units == 0) continue;
         const int *pages = p.block_table + (size_t)it.s * p.NBmax;
         const int last_page = (it.kv_end - 1) / p.B;
@@ -245,7 +278,7 @@ __device__ __forceinline__ void produce(const Params &p, ChunkWalk &walk, const 
 // ---------------------------------------------------------------------- warps 9 and 10: the MMAs of stream g
 // A wait on a parity cannot tell a phase from the one two before it, so a stage's phase may only be waited for when the one before is known
 // to be complete.  Of a stage that the other stream had last, this one knows that from the other's word (Shared::landed).
-__device__ __forceinline__ void issue(const Params &p, ChunkWalk &walk, const Shared &sh, uint32_t smem0, uint32_t tmem, int g)
+__device__ __forceinline__ void issue(const Params &p, const Shared &sh, uint32_t smem0, uint32_t tmem, int g)
 {
     constexpr uint32_t idesc_s = umma_idesc_bf16(128, kUnit, false), idesc_pv = umma_idesc_bf16(128, 128, true);
     const uint64_t dq = umma_desc_sw128(smem0 + kOffQ, 16, 1024), dk = umma_desc_sw128(smem0, 16, 1024);
@@ -268,7 +301,7 @@ __device__ __forceinline__ void issue(const Params &p, ChunkWalk &walk, const Sh
     };
     const auto pass = [&](int unit) { foreign |= 1u << (2 * unit) % kStages | 1u << (2 * unit + 1) % kStages; };
     ChunkItem it;
-    while (!dead && walk.next(it)) {
+    for (int n = 0; !dead && take(sh, n, it); ++n) {
         if (it.units == 0) continue;
         const bool two = it.tokens > p.TT;
         const int n_units = it.u1 - it.u0, step = two ? 1 : 2, begin = two ? 0 : g;
@@ -331,13 +364,13 @@ __device__ __forceinline__ void issue(const Params &p, ChunkWalk &walk, const Sh
 }
 
 // ---------------------------------------------------------------------- warps 0-3 and 4-7: the softmax of stream g, a thread per row
-__device__ __forceinline__ void softmax(const Params &p, ChunkWalk &walk, const Shared &sh, uint8_t *smem, uint32_t tmem, int g, float2 *exchange)
+__device__ __forceinline__ void softmax(const Params &p, const Shared &sh, uint8_t *smem, uint32_t tmem, int g, float2 *exchange)
 {
     const int r = threadIdx.x & 127, lane = threadIdx.x & 31;
     const uint32_t t_lane = tmem + ((uint32_t)((r >> 5) * 32) << 16), t_s = t_lane + g * 128, t_o = t_lane + 256 + g * 128;
     int unit0 = 0, mine = 0, ends = 0, meets = 0;   // units of the CTA and of the stream, items that it had units of, items of both streams
     ChunkItem it;
-    while (walk.next(it)) {
+    for (int n = 0; take(sh, n, it); ++n) {
         const bool two = it.tokens > p.TT;
         const int n_units = it.u1 - it.u0, step = two ? 1 : 2, begin = two ? 0 : g;
         const int first_token = two ? g * p.TT : 0, token = first_token + r / p.G;
@@ -506,11 +539,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t smem0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *smem = smem_raw + (smem0 - smem_u32(smem_raw));
     uint8_t *misc = smem + kOffMisc;
-    const Shared sh{smem0 + kOffMisc, reinterpret_cast<volatile int *>(misc + 256), reinterpret_cast<volatile int *>(misc + 264), p.status};
+    const Shared sh{smem0 + kOffMisc, reinterpret_cast<ChunkItem *>(misc + 1536), reinterpret_cast<volatile int *>(misc + 256), reinterpret_cast<volatile int *>(misc + 264), p.status};
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(misc + 260);
     long long *scratch = reinterpret_cast<long long *>(misc + 384);
     float2 *exchange = reinterpret_cast<float2 *>(misc + 512);
-    static_assert(kNumBars * 8 <= 256 && 512 + 128 * sizeof(float2) <= 2048, "");
+    static_assert(kNumBars * 8 <= 256 && 512 + 128 * sizeof(float2) <= 1536 && 1536 + 2 * sizeof(ChunkItem) <= 2048, "");
     const int tid = threadIdx.x, warp = tid >> 5;
 
     if (tid == 0) {
@@ -532,11 +565,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (some) {
         if (warp >= 8) {
             reg_dealloc<kRegsFew>();
-            if (warp == 8) produce(p, walk, sh, smem0, tm_q, tm_k, tm_v);
-            else if (warp < 11) issue(p, walk, sh, smem0, tmem, warp - 9);
+            if (warp == 8) produce(p, sh, smem0, tm_q, tm_k, tm_v);
+            else if (warp < 11) issue(p, sh, smem0, tmem, warp - 9);
+            else hand_out(walk, sh);
         } else {
             reg_alloc<kRegsMany>();
-            softmax(p, walk, sh, smem, tmem, warp >> 2, exchange);
+            softmax(p, sh, smem, tmem, warp >> 2, exchange);
         }
     }
     tc_fence_before_sync();
