@@ -61,14 +61,15 @@ enum Bar {
     kDone,                       // all MMAs are through
     kItem,                       // [2] the next item is in shared memory (items take the two places in turn)
     kItemTaken = kItem + 2,      // [2] ... and has been read by all roles
-    kNumBars = kItemTaken + 2
+    kTurn = kItemTaken + 2,      // [2][4] the stream's warp of a lane quarter has its turn at the exponentials
+    kNumBars = kTurn + 8
 };
 constexpr int kReaders = 11;     // warps that read the items
 __device__ __forceinline__ int arrivals(int bar)
 {
     if (bar >= kEmpty && bar < kEmpty + kStages) return 2;
     if (bar == kQFree || bar == kDone) return 2;
-    if (bar >= kItemTaken) return kReaders;
+    if (bar >= kItemTaken && bar < kTurn) return kReaders;
     return (bar >= kP0 && bar < kO) || bar == kX || bar == kXFree ? 4 : 1;   // (one lane of each warp of a warpgroup)
 }
 
@@ -369,6 +370,15 @@ __device__ __forceinline__ void softmax(const Params &p, const Shared &sh, uint8
     const int r = threadIdx.x & 127, lane = threadIdx.x & 31;
     const uint32_t t_lane = tmem + ((uint32_t)((r >> 5) * 32) << 16), t_s = t_lane + g * 128, t_o = t_lane + 256 + g * 128;
     int unit0 = 0, mine = 0, ends = 0, meets = 0;   // units of the CTA and of the stream, items that it had units of, items of both streams
+    // The warps of both streams that share a scheduler take their exponentials in turns, the first stream first.  Left alone, the streams fall
+    // into step: both wait for the tensor cores, then both share the special-function unit (4750 cycles a unit of a prompt).
+    int turns = 0;
+    const int quad = threadIdx.x >> 5 & 3;
+    const auto my_turn = [&] { return (!g && turns == 0) || sh.warp_wait(kTurn + g * 4 + quad, (g ? turns : turns - 1) & 1, 32); };
+    const auto next_turn = [&] {
+        ++turns;
+        if (lane == 0) mbar_arrive(sh.bar(kTurn + (1 - g) * 4 + quad));
+    };
     ChunkItem it;
     for (int n = 0; take(sh, n, it); ++n) {
         const bool two = it.tokens > p.TT;
@@ -433,6 +443,7 @@ __device__ __forceinline__ void softmax(const Params &p, const Shared &sh, uint8
             const float m_use = m == -INFINITY ? 0.f : m;
             const unsigned long long scale2 = f2_pack(p.scale_log2, p.scale_log2), ref2 = f2_pack(-m_use, -m_use);
             unsigned long long sum2[2] = {0ull, 0ull};
+            if (!my_turn()) return;
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 uint32_t w[32];
@@ -445,6 +456,7 @@ __device__ __forceinline__ void softmax(const Params &p, const Shared &sh, uint8
                     sum2[i & 1] = f2_add(sum2[i & 1], f2_pack(a, b));
                     w[i] = pack_bf16(a, b);
                 }
+                if (half) next_turn();
                 tmem_st_x32(t_s + half * 32, w);
                 tmem_st_wait();
                 tc_fence_before_sync();
@@ -454,6 +466,10 @@ __device__ __forceinline__ void softmax(const Params &p, const Shared &sh, uint8
             float a, b;
             f2_unpack(f2_add(sum2[0], sum2[1]), a, b);
             l += a + b;
+        }
+        if (!two && g && (n_units & 1)) {   // (the first stream had one unit more)
+            if (!my_turn()) return;
+            next_turn();
         }
         const bool had = begin < n_units, both = !two && n_units > 1;
         if (had) {
@@ -539,11 +555,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t smem0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *smem = smem_raw + (smem0 - smem_u32(smem_raw));
     uint8_t *misc = smem + kOffMisc;
-    const Shared sh{smem0 + kOffMisc, reinterpret_cast<ChunkItem *>(misc + 1536), reinterpret_cast<volatile int *>(misc + 256), reinterpret_cast<volatile int *>(misc + 264), p.status};
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(misc + 260);
-    long long *scratch = reinterpret_cast<long long *>(misc + 384);
-    float2 *exchange = reinterpret_cast<float2 *>(misc + 512);
-    static_assert(kNumBars * 8 <= 256 && 512 + 128 * sizeof(float2) <= 1536 && 1536 + 2 * sizeof(ChunkItem) <= 2048, "");
+    const Shared sh{smem0 + kOffMisc, reinterpret_cast<ChunkItem *>(misc + 1552), reinterpret_cast<volatile int *>(misc + 384), reinterpret_cast<volatile int *>(misc + 392), p.status};
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(misc + 388);
+    long long *scratch = reinterpret_cast<long long *>(misc + 400);
+    float2 *exchange = reinterpret_cast<float2 *>(misc + 528);
+    static_assert(kNumBars * 8 <= 384 && 528 + 128 * sizeof(float2) <= 1552 && 1552 + 2 * sizeof(ChunkItem) <= 2048, "");
     const int tid = threadIdx.x, warp = tid >> 5;
 
     if (tid == 0) {
