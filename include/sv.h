@@ -506,7 +506,7 @@ SV_API sv_status sv_rope_append(const sv_geom *geom, void *k_pool, void *v_pool,
  * keys of long sequences are split over the SMs and merged, so that a batch costs what its tokens cost however they are distributed.
  *   q               dev bf16 [N][Hq][D] contiguous
  *   q_start         dev int32 [S + 1], as above
- *   softmax_scale   0 selects 1/sqrt(D)
+ *   softmax_scale   0 selects 1/sqrt(D); not negative (SV_ERR_SHAPE)
  *   out             dev bf16 [N][Hq][D]; lse: dev fp32 [N][Hq] or NULL.  Rows from q_start[S] on are left alone
  *   workspace       dev scratch of sv_chunk_workspace_bytes bytes, 16-byte aligned.  Calls that may overlap need distinct ones
  *   status_word     as in sv_verify_attn

@@ -6,12 +6,12 @@
 // m moves and l and o are multiplied by 2^(old - new); o / l does not depend on m, and bf16 and fp32 have the same exponents.
 //
 // A row tile is 128 of the G * n rows (token-major: token r / G, head r % G) of a (sequence, KV head); an item is two neighbouring row tiles
-// of TT = 128 / G tokens each, or the one that is left (always the case for single tokens).  A CTA runs two streams, each with a softmax
-// warpgroup, an issuing warp and S and O of its own in TMEM (4 x 128 columns), over units of 128 keys:
+// of TT = 128 / G tokens each, or the one that is left (always the case for single tokens).  A CTA runs two streams, each with eight
+// softmax warps, an issuing warp and S and O of its own in TMEM (4 x 128 columns), over units of 128 keys:
 //   two tiles   stream g has tile g and takes every unit; K and V of a unit are fetched once for both
 //   one tile    the streams take the units in turn and add their sums at the end
 //   S[128 x 128] = Q . K^T      8 x tcgen05.mma (M128 N128 K16), both operands from shared memory (TMA, 128-byte swizzle)
-//   P = 2^(s - m)               a thread per row (tcgen05.ld 32x32b), rounded to bf16 into the columns of S
+//   P = 2^(s - m)               four lanes per row (tcgen05.ld 16x256b), rounded to bf16 into the columns of S
 //   O[128 x 128] += P . V       8 x tcgen05.mma, P from TMEM, V MN-major as TMA stored it
 // A stream's chain is S, softmax, PV, S, ...; while one stream is in its softmax the tensor cores work for the other.
 //
@@ -22,6 +22,8 @@
 // All waits are on mbarriers and bounded; one that gives up sets the status word, the CTA drains its copies and MMAs, frees TMEM and returns.
 #include <cuda.h>
 #include <cuda_bf16.h>
+
+#include <stddef.h>
 
 #include <algorithm>
 
@@ -34,7 +36,8 @@ namespace {
 
 using namespace svk;
 
-constexpr int kThreads = 384;
+constexpr int kSoftmax = 16;                  // warps of the softmax, eight for either stream
+constexpr int kThreads = (kSoftmax + 4) * 32;
 constexpr int kUnit = kChunkUnit;             // keys of a unit
 constexpr int kHalf = 16384;                 // [128 rows][64 bf16]: half of a Q, K or V tile
 constexpr int kTileBytes = 2 * kHalf;
@@ -43,8 +46,9 @@ constexpr int kOffQ = kStages * kTileBytes;
 constexpr int kOffMisc = kOffQ + 2 * kTileBytes;
 constexpr int kSmemBytes = 1024 + kOffMisc + 2048;
 static_assert(kSmemBytes <= 232448, "shared memory budget");
-constexpr int kRegsMany = 208, kRegsFew = 88;
-static_assert((2 * kRegsMany + kRegsFew) * 128 <= 168 * kThreads, "registers of the launch");
+constexpr int kRegsMany = 104, kRegsFew = 64;
+static_assert((4 * kRegsMany + kRegsFew) * 128 <= 96 * kThreads, "registers of the launch");
+constexpr int kPoly = 0;                      // of every four pairs of exponentials, those computed without the special-function unit
 constexpr float kLag = 8.f;                  // what the maximum may exceed the reference by (log2)
 
 enum Bar {
@@ -61,16 +65,19 @@ enum Bar {
     kDone,                       // all MMAs are through
     kItem,                       // [2] the next item is in shared memory (items take the two places in turn)
     kItemTaken = kItem + 2,      // [2] ... and has been read by all roles
-    kTurn = kItemTaken + 2,      // [2][4] the stream's warp of a lane quarter has its turn at the exponentials
+    kTurn = kItemTaken + 2,      // [2][4] the stream's two warps of a lane quarter have their turn at the exponentials
     kNumBars = kTurn + 8
 };
-constexpr int kReaders = 11;     // warps that read the items
+constexpr int kReaders = kSoftmax + 3;   // warps that read the items
+enum ItemWord { kSeq, kHead, kRow0, kTokens, kPos0, kKvEnd, kU0, kU1, kUnits, kParts };   // of a ChunkItem
+static_assert(sizeof(ChunkItem) == 10 * 4 && offsetof(ChunkItem, units) == kUnits * 4 && offsetof(ChunkItem, kv_end) == kKvEnd * 4, "");
 __device__ __forceinline__ int arrivals(int bar)
 {
     if (bar >= kEmpty && bar < kEmpty + kStages) return 2;
     if (bar == kQFree || bar == kDone) return 2;
     if (bar >= kItemTaken && bar < kTurn) return kReaders;
-    return (bar >= kP0 && bar < kO) || bar == kX || bar == kXFree ? 4 : 1;   // (one lane of each warp of a warpgroup)
+    if (bar >= kTurn) return 2;
+    return (bar >= kP0 && bar < kO) || bar == kX || bar == kXFree ? kSoftmax / 2 : 1;   // (one lane of each warp of a stream)
 }
 
 struct Params {
@@ -86,11 +93,13 @@ struct Params {
     float scale_log2;
 };
 
-// The share of this CTA, found by all of its threads together; scratch: 16 words of shared memory.  False: none.
+constexpr int kFound = kThreads / 32;
+// The share of this CTA, found by all of its threads together; scratch: kFound + 2 words of shared memory.  False: none.
 __device__ bool begin_walk(const Params &p, ChunkWalk &walk, long long *scratch)
 {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     long long mine = 0, first = 0;
+#pragma unroll 1
     for (int i = tid; i < p.batch.S; i += kThreads) {
         walk.load(i);
         mine += walk.per_head();
@@ -101,9 +110,11 @@ __device__ bool begin_walk(const Params &p, ChunkWalk &walk, long long *scratch)
     if (lane == 0) scratch[warp] = mine;
     __syncthreads();
     long long total = 0;
+#pragma unroll 1
     for (int w = 0; w < kThreads / 32; ++w) total += scratch[w];
     if (!walk.divide(total * p.batch.Hkv, gridDim.x, blockIdx.x)) return false;
     long long ahead = 0;   // the sequence that the share begins in, by sums over the ones before
+#pragma unroll 1
     for (int base = 0; base < p.batch.S && ahead <= walk.lo; base += kThreads) {
         const int i = base + tid;
         long long cost = first;
@@ -122,14 +133,15 @@ __device__ bool begin_walk(const Params &p, ChunkWalk &walk, long long *scratch)
         if (lane == 31) scratch[warp] = upto;
         __syncthreads();
         upto += ahead;
+#pragma unroll 1
         for (int w = 0; w < kThreads / 32; ++w) {
             if (w < warp) upto += scratch[w];
             ahead += scratch[w];
         }
-        if (i < p.batch.S && cost > 0 && upto - cost <= walk.lo && walk.lo < upto) scratch[14] = i, scratch[15] = upto - cost;
+        if (i < p.batch.S && cost > 0 && upto - cost <= walk.lo && walk.lo < upto) scratch[kFound] = i, scratch[kFound + 1] = upto - cost;
         __syncthreads();
     }
-    walk.enter((int)scratch[14], scratch[15]);
+    walk.enter((int)scratch[kFound], scratch[kFound + 1]);
     return true;
 }
 
@@ -146,68 +158,95 @@ __device__ __forceinline__ void load_box_4d(uint32_t dst, const void *map, int x
                  : "memory");
 }
 
-// What the warps of a CTA share: barriers, and whether one of their waits gave up.
+__device__ __forceinline__ void store_zero(uint32_t at) { asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory"); }
+__device__ __forceinline__ void store_pair(uint32_t at, float a, float b) { asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(a), "f"(b) : "memory"); }
+__device__ __forceinline__ float2 load_pair(uint32_t at)
+{
+    float2 v;
+    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
+    return v;
+}
+
+// What the warps of a CTA share, by its address in shared memory: barriers, and whether one of their waits gave up.
 struct Shared {
-    uint32_t bars;
-    ChunkItem *items;       // [2]
-    volatile int *abort_flag;
-    volatile int *landed;   // [2] the last ring slot that the issuing warp of a stream has seen full
-    int32_t *status;
-    __device__ uint32_t bar(int i) const { return bars + i * 8; }
-    __device__ bool wait(int i, uint32_t parity, int bit, int rounds = 64) const
+    uint32_t at;
+    static constexpr uint32_t kAbort = 384, kTmem = 388, kLanded = 392, kScratch = 400, kExchange = 576, kItems = 1600;
+    __device__ uint32_t bar(int i) const { return at + i * 8; }
+    __device__ static int load(uint32_t a)
     {
-        for (int round = 0; round < rounds; ++round) {   // (looks at the flag between polls of a limited number)
-            if (mbar_wait_bounded(bar(i), parity, 1u << 13)) return true;
-            if (*abort_flag) return false;
-        }
-        *abort_flag = 1;
+        int v;
+        asm volatile("ld.volatile.shared.b32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+        return v;
+    }
+    __device__ static void store(uint32_t a, int v) { asm volatile("st.volatile.shared.b32 [%0], %1;" ::"r"(a), "r"(v) : "memory"); }
+    __device__ void give_up(int32_t *status, int bit) const
+    {
+        store(at + kAbort, 1);
         if (status) atomicOr(status, bit);
+    }
+    // (Loops that are not unrolled: with the waits of all roles unrolled four by four the kernel had 158 KB of code, and its instruction fetches
+    // made every step of a hand-over 400 cycles.)
+    __device__ bool wait(int i, uint32_t parity, int32_t *status, int bit, int polls = 1 << 19) const
+    {
+#pragma unroll 1
+        for (int n = 0; n < polls; ++n) {
+            if (mbar_try_wait(bar(i), parity)) return true;
+            if ((n & 8191) == 8191 && load(at + kAbort)) return false;
+        }
+        give_up(status, bit);
         return false;
     }
     // until the stream's issuing warp has seen this slot full
-    __device__ bool wait_landed(int stream, int slot, int bit) const
+    __device__ bool wait_landed(int stream, int slot, int32_t *status, int bit) const
     {
+#pragma unroll 1
         for (int i = 0; i < 1 << 22; ++i) {
-            if (landed[stream] >= slot) return true;
-            if (*abort_flag) return false;
+            if (load(at + kLanded + stream * 4) >= slot) return true;
+            if (load(at + kAbort)) return false;
         }
-        *abort_flag = 1;
-        if (status) atomicOr(status, bit);
+        give_up(status, bit);
         return false;
     }
     // the same for a converged warp: true if every lane has seen the phase
-    __device__ bool warp_wait(int i, uint32_t parity, int bit) const { return __all_sync(0xffffffffu, wait(i, parity, bit)); }
+    __device__ bool warp_wait(int i, uint32_t parity, int32_t *status, int bit) const { return __all_sync(0xffffffffu, wait(i, parity, status, bit)); }
+    // words of an item (ChunkItem)
+    __device__ int item(int n, int word) const { return load(at + kItems + (n & 1) * (uint32_t)sizeof(ChunkItem) + word * 4); }
 };
+static_assert(kNumBars * 8 <= Shared::kAbort && Shared::kScratch + (kFound + 2) * 8 <= Shared::kExchange && Shared::kExchange + 128 * 8 <= Shared::kItems &&
+                  Shared::kItems + 2 * sizeof(ChunkItem) <= 2048,
+              "");
 
-// ---------------------------------------------------------------------- warp 11: the items, two ahead of the roles that read them
+// ---------------------------------------------------------------------- warp 19: the items, two ahead of the roles that read them
 // (A walk of their own in every role cost the softmax its registers: spills of 17 loads a unit, two thirds of them from L2, were most of
 // the time of a prompt of 8K.)
-__device__ __forceinline__ void hand_out(ChunkWalk &walk, const Shared &sh)
+__device__ __forceinline__ void hand_out(ChunkWalk &walk, const Shared &sh, ChunkItem *items, int32_t *status)
 {
+#pragma unroll 1
     for (int n = 0;; ++n) {
-        if (n > 1 && !__all_sync(0xffffffffu, sh.wait(kItemTaken + (n & 1), ((n >> 1) - 1) & 1, 64, 1 << 13))) return;   // (as long as an item)
+        if (n > 1 && !__all_sync(0xffffffffu, sh.wait(kItemTaken + (n & 1), ((n >> 1) - 1) & 1, status, 64, 1 << 26))) return;   // (as long as an item)
         ChunkItem it;
         const bool more = walk.next(it);
         if (!more) it.units = -1;
         if ((threadIdx.x & 31) == 0) {
-            sh.items[n & 1] = it;
+            items[n & 1] = it;
             mbar_arrive(sh.bar(kItem + (n & 1)));
         }
         __syncwarp();
         if (!more) return;
     }
 }
-// The item of this number, by a whole warp; false: there are no more, or a wait gave up.
-__device__ __forceinline__ bool take(const Shared &sh, int n, ChunkItem &it)
+// The item of this number is there, for a whole warp, until it says that it is through with it; false: there are no more, or a wait gave up.
+__device__ __forceinline__ bool take(const Shared &sh, int n, int32_t *status)
 {
-    if (!sh.warp_wait(kItem + (n & 1), (n >> 1) & 1, 64)) return false;
-    it = sh.items[n & 1];
+    return sh.warp_wait(kItem + (n & 1), (n >> 1) & 1, status, 64) && sh.item(n, kUnits) >= 0;
+}
+__device__ __forceinline__ void taken(const Shared &sh, int n)
+{
     __syncwarp();
     if ((threadIdx.x & 31) == 0) mbar_arrive(sh.bar(kItemTaken + (n & 1)));
-    return it.units >= 0;
 }
 
-// ---------------------------------------------------------------------- warp 8: copies
+// ---------------------------------------------------------------------- warp 16: copies
 __device__ __forceinline__ void produce(const Params &p, const Shared &sh, uint32_t smem0, const CUtensorMap &tm_q, const CUtensorMap &tm_k,
                                         const CUtensorMap &tm_v)
 {
@@ -215,16 +254,20 @@ __device__ __forceinline__ void produce(const Params &p, const Shared &sh, uint3
     const int per_unit = kUnit / p.B;   // pages of a unit
     int slot = 0, items = 0;            // ring slots and items so far
     bool dead = false, clamped = false;
-    ChunkItem it;
-    for (int n = 0; !dead && take(sh, n, it); ++n) {
+    const auto wait = [&](int bar, uint32_t parity, int bit) { return sh.warp_wait(bar, parity, p.status, bit); };
+    for (int n = 0; !dead && take(sh, n, p.status); ++n) {
+        const struct { int s, h, row0, tokens, kv_end, u0, u1, units; } it = {sh.item(n, kSeq), sh.item(n, kHead), sh.item(n, kRow0), sh.item(n, kTokens),
+                                                                         sh.item(n, kKvEnd), sh.item(n, kU0), sh.item(n, kU1), sh.item(n, kUnits)};
+        taken(sh, n);
         if (it.units == 0) continue;
         const int *pages = p.block_table + (size_t)it.s * p.NBmax;
         const int last_page = (it.kv_end - 1) / p.B;
         // Q: both halves of one or two tiles, as soon as the S of the item before are through
-        if (items > 0 && !sh.warp_wait(kQFree, (items - 1) & 1, 1)) break;
+        if (items > 0 && !wait(kQFree, (items - 1) & 1, 1)) break;
         const int n_tiles = it.tokens > p.TT ? 2 : 1;
         if (elect_one()) {
             mbar_arrive_expect_tx(sh.bar(kQFull), (uint32_t)(n_tiles * 2 * p.G * p.TT * 128));
+#pragma unroll 1
             for (int i = 0; i < 2 * n_tiles; ++i)
                 load_box_4d(smem0 + kOffQ + (i >> 1) * kTileBytes + (i & 1) * kHalf, &tm_q, 0, it.h * p.G, it.row0 + (i >> 1) * p.TT, i & 1, sh.bar(kQFull));
         }
@@ -244,9 +287,10 @@ __device__ __forceinline__ void produce(const Params &p, const Shared &sh, uint3
             const int page1 = __shfl_sync(0xffffffffu, known, (first - batch0 + 1) & 31);
             const int y0 = (page0 * p.Hkv + it.h) * p.B, y1 = per_unit == 2 ? (page1 * p.Hkv + it.h) * p.B : y0 + 64;
             const int halves = keys > 64 ? 2 : 1;
+#pragma unroll 1
             for (int v = 0; v < 2; ++v, ++slot) {
                 const int stage = slot % kStages, turn = slot / kStages;
-                if (turn > 0 && !sh.warp_wait(kEmpty + stage, (turn - 1) & 1, 2)) {
+                if (turn > 0 && !wait(kEmpty + stage, (turn - 1) & 1, 2)) {
                     dead = true;
                     break;
                 }
@@ -269,6 +313,7 @@ __device__ __forceinline__ void produce(const Params &p, const Shared &sh, uint3
     }
     if (clamped && p.status) atomicOr(p.status, kStatusIndex);
     // Copies in flight write to this CTA's memory: it stays until they have arrived (all of them have, unless somebody gave up).
+#pragma unroll 1
     for (int stage = 0; stage < kStages; ++stage) {
         const int n = slot > stage ? (slot - stage + kStages - 1) / kStages : 0;   // copies requested into the stage
         if (n > 0 && !__all_sync(0xffffffffu, mbar_wait_bounded(sh.bar(kFull + stage), (n - 1) & 1)) && p.status) atomicOr(p.status, 1);
@@ -276,9 +321,9 @@ __device__ __forceinline__ void produce(const Params &p, const Shared &sh, uint3
     if (items > 0 && !__all_sync(0xffffffffu, mbar_wait_bounded(sh.bar(kQFull), (items - 1) & 1)) && p.status) atomicOr(p.status, 1);
 }
 
-// ---------------------------------------------------------------------- warps 9 and 10: the MMAs of stream g
+// ---------------------------------------------------------------------- warps 17 and 18: the MMAs of stream g
 // A wait on a parity cannot tell a phase from the one two before it, so a stage's phase may only be waited for when the one before is known
-// to be complete.  Of a stage that the other stream had last, this one knows that from the other's word (Shared::landed).
+// to be complete.  Of a stage that the other stream had last, this one knows that from the other's word (Shared::kLanded).
 __device__ __forceinline__ void issue(const Params &p, const Shared &sh, uint32_t smem0, uint32_t tmem, int g)
 {
     constexpr uint32_t idesc_s = umma_idesc_bf16(128, kUnit, false), idesc_pv = umma_idesc_bf16(128, 128, true);
@@ -293,20 +338,21 @@ __device__ __forceinline__ void issue(const Params &p, const Shared &sh, uint32_
     const auto full = [&](int slot) {
         const int stage = slot % kStages;
         if (foreign >> stage & 1) {
-            if (!__all_sync(0xffffffffu, sh.wait_landed(1 - g, slot - kStages, 4))) return false;
+            if (!__all_sync(0xffffffffu, sh.wait_landed(1 - g, slot - kStages, p.status, 4))) return false;
             foreign &= ~(1u << stage);
         }
-        if (!sh.warp_wait(kFull + stage, (slot / kStages) & 1, 4)) return false;
-        if ((threadIdx.x & 31) == 0) sh.landed[g] = slot;
+        if (!sh.warp_wait(kFull + stage, (slot / kStages) & 1, p.status, 4)) return false;
+        if ((threadIdx.x & 31) == 0) Shared::store(sh.at + Shared::kLanded + g * 4, slot);
         return true;
     };
     const auto pass = [&](int unit) { foreign |= 1u << (2 * unit) % kStages | 1u << (2 * unit + 1) % kStages; };
-    ChunkItem it;
-    for (int n = 0; !dead && take(sh, n, it); ++n) {
-        if (it.units == 0) continue;
-        const bool two = it.tokens > p.TT;
-        const int n_units = it.u1 - it.u0, step = two ? 1 : 2, begin = two ? 0 : g;
-        if (!sh.warp_wait(kQFull, items & 1, 4)) break;
+    for (int n = 0; !dead && take(sh, n, p.status); ++n) {
+        const int n_units = sh.item(n, kU1) - sh.item(n, kU0);
+        const bool two = sh.item(n, kTokens) > p.TT, none = sh.item(n, kUnits) == 0;
+        taken(sh, n);
+        if (none) continue;
+        const int step = two ? 1 : 2, begin = two ? 0 : g;
+        if (!sh.warp_wait(kQFull, items & 1, p.status, 4)) break;
         ++items;
         if (begin >= n_units && elect_one()) mbar_arrive(sh.bar(kQFree));
         __syncwarp();
@@ -338,7 +384,7 @@ __device__ __forceinline__ void issue(const Params &p, const Shared &sh, uint32_
             }
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                if (!sh.warp_wait((half ? kP1 : kP0) + g, mine & 1, 8)) {
+                if (!sh.warp_wait((half ? kP1 : kP0) + g, mine & 1, p.status, 8)) {
                     dead = true;
                     break;
                 }
@@ -364,186 +410,299 @@ __device__ __forceinline__ void issue(const Params &p, const Shared &sh, uint32_
     __syncwarp();
 }
 
-// ---------------------------------------------------------------------- warps 0-3 and 4-7: the softmax of stream g, a thread per row
-__device__ __forceinline__ void softmax(const Params &p, const Shared &sh, uint8_t *smem, uint32_t tmem, int g, float2 *exchange)
+// ---------------------------------------------------------------------- warps 0-7 and 8-15: the softmax of stream g
+// 2^x of two numbers, none above 2^7, without the special-function unit: x = n + f with n whole and |f| <= 1/2, 2^f as a polynomial, n added to
+// the exponent.  The polynomial is 1 at 0 (minimax under that condition, off by 2.8e-6 of itself at most), so that -127, which stands for
+// everything below, -infinity included, gives 0.
+__device__ __forceinline__ unsigned long long exp2_pair(unsigned long long x2)
 {
-    const int r = threadIdx.x & 127, lane = threadIdx.x & 31;
-    const uint32_t t_lane = tmem + ((uint32_t)((r >> 5) * 32) << 16), t_s = t_lane + g * 128, t_o = t_lane + 256 + g * 128;
-    int unit0 = 0, mine = 0, ends = 0, meets = 0;   // units of the CTA and of the stream, items that it had units of, items of both streams
+    const auto both = [](float v) { return f2_pack(v, v); };
+    float a, b;
+    f2_unpack(x2, a, b);
+    x2 = f2_pack(fmaxf(a, -127.f), fmaxf(b, -127.f));
+    const unsigned long long z = f2_add(x2, both(12582912.f));   // n in the last places
+    const unsigned long long f = f2_fma(f2_add(z, both(-12582912.f)), both(-1.f), x2);
+    unsigned long long y = f2_fma(both(0.009582553f), f, both(0.055906326f));
+    y = f2_fma(y, f, both(0.24024104f));
+    y = f2_fma(y, f, both(0.69312423f));
+    y = f2_fma(y, f, both(1.f));
+    float ya, yb, za, zb;
+    f2_unpack(y, ya, yb);
+    f2_unpack(z, za, zb);
+    return f2_pack(__uint_as_float(__float_as_uint(ya) + (__float_as_uint(za) << 23)), __uint_as_float(__float_as_uint(yb) + (__float_as_uint(zb) << 23)));
+}
+// P of two rows of 8 scores each, from x (four words of the fragment of tcgen05.ld 16x256b for either eight keys): rounded to one word a row and
+// eight keys, the unrounded ones added to the sums.  Of every four such steps kPoly go by exp2_pair: the special-function unit has a quarter
+// of the rate of the other pipes.
+__device__ __forceinline__ void exponentials(const uint32_t *x, uint32_t *w, unsigned long long scale2, const unsigned long long (&ref2)[2],
+                                             unsigned long long (&sum2)[2], bool poly)
+{
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        unsigned long long v = f2_fma(f2_pack(__uint_as_float(x[2 * h]), __uint_as_float(x[2 * h + 1])), scale2, ref2[h]);
+        float a, b;
+        if (poly) {
+            v = exp2_pair(v);
+            f2_unpack(v, a, b);
+        } else {
+            f2_unpack(v, a, b);
+            a = fast_exp2(a), b = fast_exp2(b);
+            v = f2_pack(a, b);
+        }
+        sum2[h] = f2_add(sum2[h], v);
+        w[h] = pack_bf16(a, b);
+    }
+}
+template <class T>
+__device__ __forceinline__ T over_row(T v, T (*op)(T, T))   // over the four lanes that share a row
+{
+    v = op(v, __shfl_xor_sync(0xffffffffu, v, 1));
+    return op(v, __shfl_xor_sync(0xffffffffu, v, 2));
+}
+__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ float sum_of(float a, float b) { return a + b; }
+// Word i of lane q of every four lanes becomes word q of lane i.
+__device__ __forceinline__ void transpose_4(uint32_t (&w)[4], int q)
+{
+    const bool odd = q & 1, high = q & 2;
+    uint32_t a = __shfl_xor_sync(0xffffffffu, odd ? w[0] : w[1], 1), b = __shfl_xor_sync(0xffffffffu, odd ? w[2] : w[3], 1);
+    if (odd) w[0] = a, w[2] = b;
+    else w[1] = a, w[3] = b;
+    a = __shfl_xor_sync(0xffffffffu, high ? w[0] : w[2], 2), b = __shfl_xor_sync(0xffffffffu, high ? w[1] : w[3], 2);
+    if (high) w[0] = a, w[1] = b;
+    else w[2] = a, w[3] = b;
+}
+
+// The eight warps of a stream: a lane quarter has two, for 16 rows each; a thread has rows i and i + 8 of these and every fourth pair of keys.
+__device__ __forceinline__ void softmax(const Params &p, const Shared sh, uint32_t smem0, uint32_t tmem, int g)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, q = lane & 3;
+    const int r0 = (warp & 3) * 32 + (warp >> 2 & 1) * 16 + (lane >> 2);   // first of the thread's rows of the tile
+    const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32 + (warp >> 2 & 1) * 16) << 16), t_s = t_lane + g * 128, t_o = t_lane + 256 + g * 128;
+    uint32_t phases = 0;   // parities of what this warp has waited for
+    constexpr uint32_t kOfS = 1, kOfTurn = 2, kOfO = 4, kOfX = 8;
+    const auto wait = [&](int bar, uint32_t of, int bit) {
+        const bool ok = sh.warp_wait(bar, (phases & of) != 0, p.status, bit);
+        phases ^= of;
+        return ok;
+    };
     // The warps of both streams that share a scheduler take their exponentials in turns, the first stream first.  Left alone, the streams fall
     // into step: both wait for the tensor cores, then both share the special-function unit (4750 cycles a unit of a prompt).
-    int turns = 0;
-    const int quad = threadIdx.x >> 5 & 3;
-    const auto my_turn = [&] { return (!g && turns == 0) || sh.warp_wait(kTurn + g * 4 + quad, (g ? turns : turns - 1) & 1, 32); };
-    const auto next_turn = [&] {
-        ++turns;
-        if (lane == 0) mbar_arrive(sh.bar(kTurn + (1 - g) * 4 + quad));
+    const uint32_t turn_bar = kTurn + (warp & 3);
+    bool first_turn = g == 0;
+    const auto my_turn = [&] {
+        if (first_turn) {
+            first_turn = false;
+            return true;
+        }
+        return wait(turn_bar + g * 4, kOfTurn, 32);
     };
-    ChunkItem it;
-    for (int n = 0; take(sh, n, it); ++n) {
-        const bool two = it.tokens > p.TT;
-        const int n_units = it.u1 - it.u0, step = two ? 1 : 2, begin = two ? 0 : g;
-        const int first_token = two ? g * p.TT : 0, token = first_token + r / p.G;
-        const bool real = r < p.G * p.TT && token < it.tokens;
-        const int last_key = min(it.pos0 + token, it.kv_end - 1);   // of this row
-        float m = -INFINITY, l = 0.f;
-        for (int j = begin; j < n_units; j += step, ++mine) {
-            const int key0 = (it.u0 + j) * kUnit;
-            if (!sh.warp_wait(kS + g, mine & 1, 16)) return;
+    const auto next_turn = [&] {
+        if (lane == 0) mbar_arrive(sh.bar(turn_bar + (1 - g) * 4));
+    };
+    const auto arrive = [&](int bar) {
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(sh.bar(bar));
+    };
+    int v_slot = 1;   // ring slot of the V of the item's first unit
+    for (int n = 0; take(sh, n, p.status); ++n) {
+        const bool two = sh.item(n, kTokens) > p.TT;
+        const int n_units = sh.item(n, kU1) - sh.item(n, kU0), step = two ? 1 : 2, begin = two ? 0 : g;
+        // keys counted from the share's first: behind the last one that any row sees, that every row of the tile sees, and these rows
+        const int begins = sh.item(n, kU0) * kUnit, kv_end = sh.item(n, kKvEnd) - begins;
+        const int pos0 = sh.item(n, kPos0) + (two ? g * p.TT : 0) - begins;
+        const int all_see = min(pos0 + 1, kv_end);
+        int sees[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) sees[h] = min(pos0 + (r0 + 8 * h) / p.G + 1, kv_end) - 2 * q;   // (less the thread's first key)
+        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+        for (int j = begin; j < n_units; j += step) {
+            if (!wait(kS + g, kOfS, 16)) return;
             tc_fence_after_sync();
-            uint32_t x[4][32];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld_x32(t_s + c * 32, x[c]);
+            uint32_t x[64];   // word 4 i + 2 h + e: row h, key 8 i + 2 q + e
+            tmem_ld_16x256b_x16(t_s, x);
             tmem_ld_wait();
-            if (key0 + kUnit - 1 > min(it.pos0 + first_token, it.kv_end - 1)) {   // some row of the tile does not see all of the unit
-                const int seen = last_key - key0;
+            if ((j + 1) * kUnit > all_see) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
+                for (int h = 0; h < 2; ++h) {
+                    const int seen = sees[h] - j * kUnit;
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (c * 32 + i > seen) x[c][i] = 0xff800000u;
+                    for (int i = 0; i < 16; ++i) {
+                        if (8 * i >= seen) x[4 * i + 2 * h] = 0xff800000u;
+                        if (8 * i + 1 >= seen) x[4 * i + 2 * h + 1] = 0xff800000u;
+                    }
+                }
             }
-            float mx[4];
+            float top[2];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                mx[c] = fmaxf(__uint_as_float(x[c][0]), __uint_as_float(x[c][1]));
+            for (int h = 0; h < 2; ++h) {
+                float mx[2];
 #pragma unroll
-                for (int i = 2; i < 32; i += 2) mx[c] = max3f(mx[c], __uint_as_float(x[c][i]), __uint_as_float(x[c][i + 1]));
+                for (int c = 0; c < 2; ++c) {
+                    mx[c] = fmaxf(__uint_as_float(x[32 * c + 2 * h]), __uint_as_float(x[32 * c + 2 * h + 1]));
+#pragma unroll
+                    for (int i = 1; i < 8; ++i) mx[c] = max3f(mx[c], __uint_as_float(x[32 * c + 4 * i + 2 * h]), __uint_as_float(x[32 * c + 4 * i + 2 * h + 1]));
+                }
+                top[h] = over_row(fmaxf(mx[0], mx[1]), larger) * p.scale_log2;
             }
-            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2;
-            const bool move = top > m + kLag;
-            if (__any_sync(0xffffffffu, move)) {
-                const float c = move ? fast_exp2(m - top) : 1.f;
-                if (move) m = top;
-                l *= c;
+            // Each row goes by its own: a warp's other rows may be nobody's, of whatever the queries' tile holds there.
+            if (__any_sync(0xffffffffu, top[0] > m[0] + kLag || top[1] > m[1] + kLag)) {
+                float c[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const bool move = top[h] > m[h] + kLag;
+                    c[h] = move ? fast_exp2(m[h] - top[h]) : 1.f;
+                    if (move) m[h] = top[h];
+                    l[h] *= c[h];
+                }
                 if (j > begin) {   // (S of this unit was issued behind the PV of the one before: O is at rest)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        uint32_t o[32];
-                        tmem_ld_x32(t_o + q * 32, o);
+#pragma unroll 1
+                    for (int o0 = 0; o0 < 128; o0 += 32) {
+                        uint32_t o[16];
+                        tmem_ld_16x256b_x4(t_o + o0, o);
                         tmem_ld_wait();
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * c);
-                        tmem_st_x32(t_o + q * 32, o);
+                        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * c[i >> 1 & 1]);
+                        tmem_st_16x256b_x4(t_o + o0, o);
                     }
                     tmem_st_wait();
                 }
             }
             // V rows behind the last key are another tile's or nobody's: zero, so that 0 * V is 0
-            if (key0 + kUnit > it.kv_end) {
-                const int slot = 2 * (unit0 + j) + 1, stage = slot % kStages;
-                if (!sh.warp_wait(kFull + stage, (slot / kStages) & 1, 16)) return;
-                uint8_t *tile = smem + stage * kTileBytes;
-                for (int i = (it.kv_end - key0) * 16 + r; i < kUnit * 16; i += 128) {
+            if ((j + 1) * kUnit > kv_end) {
+                const int slot = v_slot + 2 * j, stage = slot % kStages;
+                if (!sh.warp_wait(kFull + stage, (slot / kStages) & 1, p.status, 16)) return;
+#pragma unroll 1
+                for (int i = (kv_end - j * kUnit) * 16 + (int)(threadIdx.x & 255); i < kUnit * 16; i += 256) {
                     const int row = i >> 4, c = i & 15;
-                    *reinterpret_cast<uint4 *>(tile + (row >> 6) * kHalf + (c >> 3) * (kHalf / 2) + swz128(row & 63, c & 7)) = make_uint4(0u, 0u, 0u, 0u);
+                    store_zero(smem0 + stage * kTileBytes + (row >> 6) * kHalf + (c >> 3) * (kHalf / 2) + swz128(row & 63, c & 7));
                 }
                 fence_proxy_async();
             }
-            const float m_use = m == -INFINITY ? 0.f : m;
-            const unsigned long long scale2 = f2_pack(p.scale_log2, p.scale_log2), ref2 = f2_pack(-m_use, -m_use);
-            unsigned long long sum2[2] = {0ull, 0ull};
-            if (!my_turn()) return;
+            const unsigned long long scale2 = f2_pack(p.scale_log2, p.scale_log2);
+            unsigned long long ref2[2], sum2[2] = {0ull, 0ull};
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                uint32_t w[32];
-#pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    const uint32_t *at = x[half * 2 + (i >> 4)] + (i & 15) * 2;
-                    float a, b;
-                    f2_unpack(f2_fma(f2_pack(__uint_as_float(at[0]), __uint_as_float(at[1])), scale2, ref2), a, b);
-                    a = fast_exp2(a), b = fast_exp2(b);
-                    sum2[i & 1] = f2_add(sum2[i & 1], f2_pack(a, b));
-                    w[i] = pack_bf16(a, b);
-                }
-                if (half) next_turn();
-                tmem_st_x32(t_s + half * 32, w);
-                tmem_st_wait();
-                tc_fence_before_sync();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(sh.bar((half ? kP1 : kP0) + g));
+            for (int h = 0; h < 2; ++h) {
+                const float use = m[h] == -INFINITY ? 0.f : -m[h];
+                ref2[h] = f2_pack(use, use);
             }
-            float a, b;
-            f2_unpack(f2_add(sum2[0], sum2[1]), a, b);
-            l += a + b;
+            if (!my_turn()) return;
+            const auto quarter = [&](int c) {
+                uint32_t w[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) exponentials(x + 16 * c + 4 * i, w + 2 * i, scale2, ref2, sum2, i >= 4 - kPoly);
+                tmem_st_16x128b_x4(t_s + c * 16, w);
+            };
+            quarter(0);
+            quarter(1);
+            tmem_st_wait();
+            arrive(kP0 + g);
+            quarter(2);
+            quarter(3);
+            next_turn();
+            tmem_st_wait();
+            arrive(kP1 + g);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float a, b;
+                f2_unpack(sum2[h], a, b);
+                l[h] += a + b;
+            }
         }
+        v_slot += 2 * n_units;
         if (!two && g && (n_units & 1)) {   // (the first stream had one unit more)
             if (!my_turn()) return;
             next_turn();
         }
         const bool had = begin < n_units, both = !two && n_units > 1;
         if (had) {
-            if (!sh.warp_wait(kO + g, ends & 1, 16)) return;
-            ++ends;
+            if (!wait(kO + g, kOfO, 16)) return;
             tc_fence_after_sync();
         }
-        unit0 += n_units;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) l[h] = over_row(l[h], sum_of);
         // the rows: of two tiles each stream's own; of one tile those of both streams, added by the first
         if (both && g) {
-            exchange[r] = make_float2(m, l);
-            tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(sh.bar(kX));
-            if (!sh.warp_wait(kXFree, meets & 1, 32)) return;
-            ++meets;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (q == 0) store_pair(sh.at + Shared::kExchange + (r0 + 8 * h) * 8, m[h], l[h]);
+            arrive(kX);
+            if (!wait(kXFree, kOfX, 32)) return;
             tc_fence_after_sync();
         }
-        if (!two && g) continue;
-        float w0 = 1.f, w1 = 0.f;
-        if (both) {
-            if (!sh.warp_wait(kX, meets & 1, 32)) return;
-            ++meets;
-            tc_fence_after_sync();
-            const float2 o = exchange[r];
-            const float top = fmaxf(m, o.x), use = top == -INFINITY ? 0.f : top;
-            w0 = fast_exp2(m - use), w1 = fast_exp2(o.x - use);
-            l = l * w0 + o.y * w1, m = top;
-        }
-        const bool whole = it.whole();
-        const size_t row = (size_t)(it.row0 + token) * p.Hq + it.h * p.G + r % p.G;
-        const size_t part = ((size_t)blockIdx.x * 2 + (it.u0 == 0)) * p.slot_rows + (two ? g * 128 : 0) + r;
-        const float inv = !whole ? 1.f : l > 0.f ? 1.f / l : 0.f;
-        w0 *= inv, w1 *= inv;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            float o[32];
-#pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] = 0.f;
-            if (had) {
-                uint32_t x[32];
-                tmem_ld_x32(t_o + c * 32, x);
-                tmem_ld_wait();
-#pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] = __uint_as_float(x[i]) * w0;
-            }
+        if (two || !g) {
+            float w0[2] = {1.f, 1.f}, w1[2] = {0.f, 0.f};
             if (both) {
-                uint32_t x[32];
-                tmem_ld_x32(t_o + 128 + c * 32, x);
-                tmem_ld_wait();
+                if (!wait(kX, kOfX, 32)) return;
+                tc_fence_after_sync();
 #pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] += __uint_as_float(x[i]) * w1;
+                for (int h = 0; h < 2; ++h) {
+                    const float2 o = load_pair(sh.at + Shared::kExchange + (r0 + 8 * h) * 8);
+                    const float most = fmaxf(m[h], o.x), use = most == -INFINITY ? 0.f : most;
+                    w0[h] = fast_exp2(m[h] - use), w1[h] = fast_exp2(o.x - use);
+                    l[h] = l[h] * w0[h] + o.y * w1[h], m[h] = most;
+                }
             }
-            if (real && whole) {
-                uint4 *to = reinterpret_cast<uint4 *>(p.out + row * 128 + c * 32);
+            const int tokens = sh.item(n, kTokens), u0 = sh.item(n, kU0);
+            const bool whole = u0 == 0 && sh.item(n, kU1) == sh.item(n, kUnits);
+            bool real[2];
+            size_t row[2], part[2];
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    to[i] = l > 0.f ? make_uint4(pack_bf16(o[i * 8], o[i * 8 + 1]), pack_bf16(o[i * 8 + 2], o[i * 8 + 3]), pack_bf16(o[i * 8 + 4], o[i * 8 + 5]),
-                                                 pack_bf16(o[i * 8 + 6], o[i * 8 + 7]))
-                                    : make_uint4(0u, 0u, 0u, 0u);
-            } else if (real) {
-                float4 *to = reinterpret_cast<float4 *>(p.ws_o + part * 128 + c * 32);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) to[i] = make_float4(o[i * 4], o[i * 4 + 1], o[i * 4 + 2], o[i * 4 + 3]);
+            for (int h = 0; h < 2; ++h) {
+                const int r = r0 + 8 * h, token = (two ? g * p.TT : 0) + r / p.G;
+                real[h] = r < p.G * p.TT && token < tokens;
+                row[h] = (size_t)(sh.item(n, kRow0) + token) * p.Hq + sh.item(n, kHead) * p.G + r % p.G;
+                part[h] = ((size_t)blockIdx.x * 2 + (u0 == 0)) * p.slot_rows + (two ? g * 128 : 0) + r;
+                const float inv = !whole ? 1.f : l[h] > 0.f ? 1.f / l[h] : 0.f;
+                w0[h] *= inv, w1[h] *= inv;
             }
+#pragma unroll 1
+            for (int o0 = 0; o0 < 128; o0 += 32) {
+                float o[16];   // of O as of S: word 4 i + 2 h + e is row h, dim o0 + 8 i + 2 q + e
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[i] = 0.f;
+                if (had) {
+                    uint32_t x[16];
+                    tmem_ld_16x256b_x4(t_o + o0, x);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[i] = __uint_as_float(x[i]) * w0[i >> 1 & 1];
+                }
+                if (both) {
+                    uint32_t x[16];
+                    tmem_ld_16x256b_x4(t_o + 128 + o0, x);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[i] += __uint_as_float(x[i]) * w1[i >> 1 & 1];
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (whole) {   // 16 bytes a lane, 64 consecutive ones a row
+                        uint32_t w[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) w[i] = l[h] > 0.f ? pack_bf16(o[4 * i + 2 * h], o[4 * i + 2 * h + 1]) : 0u;
+                        transpose_4(w, q);
+                        if (real[h]) *reinterpret_cast<uint4 *>(p.out + row[h] * 128 + o0 + 8 * q) = make_uint4(w[0], w[1], w[2], w[3]);
+                    } else if (real[h]) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            *reinterpret_cast<float2 *>(p.ws_o + part[h] * 128 + o0 + 8 * i + 2 * q) = make_float2(o[4 * i + 2 * h], o[4 * i + 2 * h + 1]);
+                    }
+                }
+            }
+            if (both) arrive(kXFree);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (q || !real[h]) continue;
+                if (!whole) p.ws_ml[part[h]] = make_float2(m[h], l[h]);
+                else if (p.lse) p.lse[row[h]] = l[h] > 0.f ? (m[h] + log2f(l[h])) * 0.69314718055994531f : -INFINITY;
+            }
+            const int parts = sh.item(n, kParts);
+            if (threadIdx.x == 0 && parts) p.cuts[blockIdx.x] = make_int4(sh.item(n, kRow0), tokens, sh.item(n, kHead), parts);
         }
-        if (real && whole && p.lse) p.lse[row] = l > 0.f ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
-        if (real && !whole) p.ws_ml[part] = make_float2(m, l);
-        if (threadIdx.x == 0 && it.parts) p.cuts[blockIdx.x] = make_int4(it.row0, it.tokens, it.h, it.parts);
         tc_fence_before_sync();
-        if (both) {
-            __syncwarp();
-            if (lane == 0) mbar_arrive(sh.bar(kXFree));
-        }
+        taken(sh, n);
     }
 }
 
@@ -553,46 +712,42 @@ __global__ void __launch_bounds__(kThreads, 1)
 {
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    uint8_t *smem = smem_raw + (smem0 - smem_u32(smem_raw));
-    uint8_t *misc = smem + kOffMisc;
-    const Shared sh{smem0 + kOffMisc, reinterpret_cast<ChunkItem *>(misc + 1552), reinterpret_cast<volatile int *>(misc + 384), reinterpret_cast<volatile int *>(misc + 392), p.status};
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(misc + 388);
-    long long *scratch = reinterpret_cast<long long *>(misc + 400);
-    float2 *exchange = reinterpret_cast<float2 *>(misc + 528);
-    static_assert(kNumBars * 8 <= 384 && 528 + 128 * sizeof(float2) <= 1552 && 1552 + 2 * sizeof(ChunkItem) <= 2048, "");
+    uint8_t *misc = smem_raw + (smem0 - smem_u32(smem_raw)) + kOffMisc;
+    const Shared sh{smem0 + kOffMisc};
     const int tid = threadIdx.x, warp = tid >> 5;
 
     if (tid == 0) {
+#pragma unroll 1
         for (int i = 0; i < kNumBars; ++i) mbar_init(sh.bar(i), arrivals(i));
         mbar_fence_init();
-        *sh.abort_flag = 0;
-        sh.landed[0] = sh.landed[1] = -1;
+        Shared::store(sh.at + Shared::kAbort, 0);
+        Shared::store(sh.at + Shared::kLanded, -1), Shared::store(sh.at + Shared::kLanded + 4, -1);
     }
-    if (warp == 8 && (tid & 31) == 0) tma_prefetch_desc(&tm_q), tma_prefetch_desc(&tm_k), tma_prefetch_desc(&tm_v);
-    if (warp == 9) tmem_alloc(smem_u32(tmem_slot), 512);
+    if (warp == kSoftmax && (tid & 31) == 0) tma_prefetch_desc(&tm_q), tma_prefetch_desc(&tm_k), tma_prefetch_desc(&tm_v);
+    if (warp == kSoftmax + 1) tmem_alloc(sh.at + Shared::kTmem, 512);
     grid_dependency_wait();
     if (tid == 0) p.cuts[blockIdx.x] = make_int4(0, 0, 0, 0);
     ChunkWalk walk(p.batch);
-    const bool some = begin_walk(p, walk, scratch);
+    const bool some = begin_walk(p, walk, reinterpret_cast<long long *>(misc + Shared::kScratch));
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
-    const uint32_t tmem = *tmem_slot;
+    const uint32_t tmem = Shared::load(sh.at + Shared::kTmem);
     if (some) {
-        if (warp >= 8) {
+        if (warp >= kSoftmax) {
             reg_dealloc<kRegsFew>();
-            if (warp == 8) produce(p, sh, smem0, tm_q, tm_k, tm_v);
-            else if (warp < 11) issue(p, sh, smem0, tmem, warp - 9);
-            else hand_out(walk, sh);
+            if (warp == kSoftmax) produce(p, sh, smem0, tm_q, tm_k, tm_v);
+            else if (warp < kSoftmax + 3) issue(p, sh, smem0, tmem, warp - kSoftmax - 1);
+            else hand_out(walk, sh, reinterpret_cast<ChunkItem *>(misc + Shared::kItems), p.status);
         } else {
             reg_alloc<kRegsMany>();
-            softmax(p, sh, smem, tmem, warp >> 2, exchange);
+            softmax(p, sh, smem0, tmem, warp >> 3);
         }
     }
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
-    if (warp == 9) {
+    if (warp == kSoftmax + 1) {
         // (MMAs that nobody waited for, when a wait gave up)
         if (some && !__all_sync(0xffffffffu, mbar_wait_bounded(sh.bar(kDone), 0)) && p.status) atomicOr(p.status, 4);
         __syncwarp();

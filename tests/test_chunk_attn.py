@@ -309,7 +309,7 @@ def test_refusals_without_a_device():
     assert call(kv=b.sv_kv(0x1000, None, 0x3000, 0x4000, 8)) == 1
     assert call(n=-1) == 2 and call(kv=b.sv_kv(0x1000, 0x2000, 0x3000, 0x4000, 0)) == 2
     assert call(geom=b.make_geom(2, 8, 3, 128, 64, 16, 1)) == 2
-    assert call(q=0x5008) == 3 and call(kv=b.sv_kv(0x1040, 0x2000, 0x3000, 0x4000, 8)) == 3 and call(ws=0x8004) == 3
+    assert call(q=0x5008) == 3 and call(kv=b.sv_kv(0x1040, 0x2000, 0x3000, 0x4000, 8)) == 3 and call(ws=0x8004) == 3 and call(out=0x7008) == 3
     assert call(size=0) == 5
     assert call(geom=b.make_geom(2, 8, 2, 64, 64, 16, 1)) == 6 and call(geom=b.make_geom(2, 129, 1, 128, 64, 16, 1)) == 6
     assert b.sv_chunk_workspace_bytes(b.make_geom(2, 8, 3, 128, 64, 16, 1), 10) == 0
