@@ -184,14 +184,34 @@ struct Shared {
         store(at + kAbort, 1);
         if (status) atomicOr(status, bit);
     }
-    // (Loops that are not unrolled: with the waits of all roles unrolled four by four the kernel had 158 KB of code, and its instruction fetches
-    // made every step of a hand-over 400 cycles.)
-    __device__ bool wait(int i, uint32_t parity, int32_t *status, int bit, int polls = 1 << 19) const
+    // As few instructions as it takes: the code of a hand-over is cold when it is reached (the softmax has run through the instruction caches
+    // meanwhile), and is fetched line by line.  With the waits unrolled four by four the kernel had 158 KB of code, and every step of a
+    // hand-over took 400 cycles.
+    __device__ static bool poll(uint32_t bar, uint32_t parity)   // 2^13 times
+    {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\t"
+            "mov.u32 n, 8192;\n"
+            "POLL%=:\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+            "@p bra DONE%=;\n\t"
+            "add.u32 n, n, -1;\n\t"
+            "setp.ne.u32 q, n, 0;\n\t"
+            "@q bra POLL%=;\n"
+            "DONE%=:\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity)
+            : "memory");
+        return ok != 0;
+    }
+    __device__ bool wait(int i, uint32_t parity, int32_t *status, int bit, int rounds = 64) const
     {
 #pragma unroll 1
-        for (int n = 0; n < polls; ++n) {
-            if (mbar_try_wait(bar(i), parity)) return true;
-            if ((n & 8191) == 8191 && load(at + kAbort)) return false;
+        for (int n = 0; n < rounds; ++n) {   // (looks at the flag between polls of a limited number)
+            if (poll(bar(i), parity)) return true;
+            if (load(at + kAbort)) return false;
         }
         give_up(status, bit);
         return false;
@@ -223,7 +243,7 @@ __device__ __forceinline__ void hand_out(ChunkWalk &walk, const Shared &sh, Chun
 {
 #pragma unroll 1
     for (int n = 0;; ++n) {
-        if (n > 1 && !__all_sync(0xffffffffu, sh.wait(kItemTaken + (n & 1), ((n >> 1) - 1) & 1, status, 64, 1 << 26))) return;   // (as long as an item)
+        if (n > 1 && !__all_sync(0xffffffffu, sh.wait(kItemTaken + (n & 1), ((n >> 1) - 1) & 1, status, 64, 1 << 13))) return;   // (as long as an item)
         ChunkItem it;
         const bool more = walk.next(it);
         if (!more) it.units = -1;
@@ -329,85 +349,87 @@ __device__ __forceinline__ void issue(const Params &p, const Shared &sh, uint32_
     constexpr uint32_t idesc_s = umma_idesc_bf16(128, kUnit, false), idesc_pv = umma_idesc_bf16(128, 128, true);
     const uint64_t dq = umma_desc_sw128(smem0 + kOffQ, 16, 1024), dk = umma_desc_sw128(smem0, 16, 1024);
     const uint64_t dv = umma_desc_sw128(smem0, kHalf / 2, 1024);
-    const uint32_t dq_lo = (uint32_t)dq, dk_lo = (uint32_t)dk, dv_lo = (uint32_t)dv;
-    const uint64_t d_hi = dk & 0xFFFFFFFF00000000ull, dv_hi = dv & 0xFFFFFFFF00000000ull;
     const uint32_t t_s = tmem + g * 128, t_o = tmem + 256 + g * 128;
-    int unit0 = 0, mine = 0, items = 0;   // units of the CTA before this item; units of this stream, items so far
+    const auto wait = [&](int bar, uint32_t parity, int bit) { return sh.wait(bar, parity, p.status, bit); };
+    int slot = 0, stage = 0, items = 0;   // ring slots and items so far, slot % kStages
+    uint32_t turn = 0, of_p = 0;          // parity of slot / kStages and of the units of this stream
     uint32_t foreign = 0;                 // the stages that the other stream alone had last
-    bool dead = false;
-    const auto full = [&](int slot) {
-        const int stage = slot % kStages;
+    const auto next_slot = [&] {
+        ++slot;
+        if (++stage == kStages) stage = 0, turn ^= 1;
+    };
+    const auto pass = [&] {   // a unit of the other stream
+        foreign |= 1u << stage;
+        next_slot();
+        foreign |= 1u << stage;
+        next_slot();
+    };
+    const auto full = [&](bool two) {
         if (foreign >> stage & 1) {
-            if (!__all_sync(0xffffffffu, sh.wait_landed(1 - g, slot - kStages, p.status, 4))) return false;
+            if (!sh.wait_landed(1 - g, slot - kStages, p.status, 4)) return false;
             foreign &= ~(1u << stage);
         }
-        if (!sh.warp_wait(kFull + stage, (slot / kStages) & 1, p.status, 4)) return false;
-        if ((threadIdx.x & 31) == 0) Shared::store(sh.at + Shared::kLanded + g * 4, slot);
+        if (!wait(kFull + stage, turn, 4)) return false;
+        if (!two) Shared::store(sh.at + Shared::kLanded + g * 4, slot);   // (of two tiles both streams see every slot)
         return true;
     };
-    const auto pass = [&](int unit) { foreign |= 1u << (2 * unit) % kStages | 1u << (2 * unit + 1) % kStages; };
-    for (int n = 0; !dead && take(sh, n, p.status); ++n) {
+    bool dead = false;
+#pragma unroll 1
+    for (int n = 0; !dead && wait(kItem + (n & 1), (n >> 1) & 1, 64) && sh.item(n, kUnits) >= 0; ++n) {
         const int n_units = sh.item(n, kU1) - sh.item(n, kU0);
         const bool two = sh.item(n, kTokens) > p.TT, none = sh.item(n, kUnits) == 0;
-        taken(sh, n);
+        mbar_arrive(sh.bar(kItemTaken + (n & 1)));
         if (none) continue;
         const int step = two ? 1 : 2, begin = two ? 0 : g;
-        if (!sh.warp_wait(kQFull, items & 1, p.status, 4)) break;
+        if (!wait(kQFull, items & 1, 4)) break;
         ++items;
-        if (begin >= n_units && elect_one()) mbar_arrive(sh.bar(kQFree));
-        __syncwarp();
-        if (begin) pass(unit0);
-        for (int j = begin; j < n_units && !dead; j += step, ++mine) {
-            const int slot = 2 * (unit0 + j), sk = slot % kStages, sv = (slot + 1) % kStages;
+        if (begin >= n_units) mbar_arrive(sh.bar(kQFree));
+        if (begin) pass();
+        const uint64_t dq_g = dq + (uint64_t)(two ? g * (kTileBytes >> 4) : 0);
+#pragma unroll 1
+        for (int j = begin; j < n_units; j += step) {
             const bool last = j + step >= n_units;
-            if (!full(slot)) {
-                dead = true;
-                break;
-            }
+            dead = !full(two);
+            if (dead) break;
             tc_fence_after_sync();
-            if (elect_one()) {
+            {
+                const uint64_t dk_u = dk + (uint64_t)(stage * (kTileBytes >> 4));
 #pragma unroll
                 for (int ks = 0; ks < 8; ++ks) {
-                    const uint32_t o = (uint32_t)(((ks >> 2) * kHalf + (ks & 3) * 32) >> 4);
-                    tc_mma_bf16(t_s, d_hi | (dq_lo + (uint32_t)((two ? g * kTileBytes : 0) >> 4) + o), d_hi | (dk_lo + (uint32_t)((sk * kTileBytes) >> 4) + o),
-                                idesc_s, ks > 0);
+                    constexpr int kStep[8] = {0, 2, 4, 6, kHalf >> 4, (kHalf >> 4) + 2, (kHalf >> 4) + 4, (kHalf >> 4) + 6};
+                    tc_mma_bf16(t_s, dq_g + kStep[ks], dk_u + kStep[ks], idesc_s, ks > 0);
                 }
                 tc_commit(sh.bar(kS + g));
-                tc_commit(sh.bar(kEmpty + sk));
-                if (!two) tc_commit(sh.bar(kEmpty + sk));   // (a stage has two readers)
+                tc_commit(sh.bar(kEmpty + stage));
+                if (!two) tc_commit(sh.bar(kEmpty + stage));   // (a stage has two readers)
                 if (last) tc_commit(sh.bar(kQFree));
             }
-            __syncwarp();
-            if (!full(slot + 1)) {
-                dead = true;
-                break;
-            }
+            next_slot();
+            dead = !full(two) || !wait(kP0 + g, of_p, 8);
+            if (dead) break;
+            const uint64_t dv_u = dv + (uint64_t)(stage * (kTileBytes >> 4));
+            const uint32_t bar_empty = sh.bar(kEmpty + stage);
+            tc_fence_after_sync();
+            {
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                if (!sh.warp_wait((half ? kP1 : kP0) + g, mine & 1, p.status, 8)) {
-                    dead = true;
-                    break;
-                }
-                tc_fence_after_sync();
-                if (elect_one()) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        tc_mma_bf16_ta(t_o, t_s + (half * 4 + i) * 8, dv_hi | (dv_lo + (uint32_t)((sv * kTileBytes + half * kHalf + i * 2048) >> 4)), idesc_pv,
-                                       j > begin || half > 0 || i > 0);
-                    if (half) {
-                        tc_commit(sh.bar(kEmpty + sv));
-                        if (!two) tc_commit(sh.bar(kEmpty + sv));
-                        if (last) tc_commit(sh.bar(kO + g));
-                    }
-                }
-                __syncwarp();
+                for (int i = 0; i < 4; ++i) tc_mma_bf16_ta(t_o, t_s + i * 8, dv_u + (uint64_t)(i * 2048 >> 4), idesc_pv, j > begin || i > 0);
             }
-            if (!two && j + 1 < n_units) pass(unit0 + j + 1);
+            dead = !wait(kP1 + g, of_p, 8);
+            if (dead) break;
+            tc_fence_after_sync();
+            {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) tc_mma_bf16_ta(t_o, t_s + (4 + i) * 8, dv_u + (uint64_t)((kHalf + i * 2048) >> 4), idesc_pv, 1);
+                tc_commit(bar_empty);
+                if (!two) tc_commit(bar_empty);
+                if (last) tc_commit(sh.bar(kO + g));
+            }
+            of_p ^= 1;
+            next_slot();
+            if (!two && j + 1 < n_units) pass();
         }
-        unit0 += n_units;
     }
-    if (elect_one()) tc_commit(sh.bar(kDone));
-    __syncwarp();
+    tc_commit(sh.bar(kDone));
 }
 
 // ---------------------------------------------------------------------- warps 0-7 and 8-15: the softmax of stream g
@@ -737,8 +759,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (warp >= kSoftmax) {
             reg_dealloc<kRegsFew>();
             if (warp == kSoftmax) produce(p, sh, smem0, tm_q, tm_k, tm_v);
-            else if (warp < kSoftmax + 3) issue(p, sh, smem0, tmem, warp - kSoftmax - 1);
-            else hand_out(walk, sh, reinterpret_cast<ChunkItem *>(misc + Shared::kItems), p.status);
+            else if (warp < kSoftmax + 3 && elect_one()) issue(p, sh, smem0, tmem, warp - kSoftmax - 1);
+            else if (warp == kSoftmax + 3) hand_out(walk, sh, reinterpret_cast<ChunkItem *>(misc + Shared::kItems), p.status);
         } else {
             reg_alloc<kRegsMany>();
             softmax(p, sh, smem0, tmem, warp >> 3);
