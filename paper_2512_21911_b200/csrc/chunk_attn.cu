@@ -7,7 +7,7 @@
 //
 // A row tile is 128 of the G * n rows (token-major: token r / G, head r % G) of a (sequence, KV head); an item is two neighbouring row tiles
 // of TT = 128 / G tokens each, or the one that is left (always the case for single tokens).  A CTA runs two streams, each with eight
-// softmax warps, an issuing warp and S and O of its own in TMEM (4 x 128 columns), over units of 128 keys:
+// softmax warps and S and O of its own in TMEM (4 x 128 columns), over units of 128 keys:
 //   two tiles   stream g has tile g and takes every unit; K and V of a unit are fetched once for both
 //   one tile    the streams take the units in turn and add their sums at the end
 //   S[128 x 128] = Q . K^T      8 x tcgen05.mma (M128 N128 K16), both operands from shared memory (TMA, 128-byte swizzle)
@@ -53,7 +53,7 @@ constexpr float kLag = 8.f;                  // what the maximum may exceed the 
 
 enum Bar {
     kFull = 0,                   // [kStages] a K or V tile has landed
-    kEmpty = kFull + kStages,    // [kStages] both streams are through with it
+    kEmpty = kFull + kStages,    // [kStages] the MMAs are through with it
     kQFull = kEmpty + kStages,   // the item's Q has landed
     kQFree,                      // all S of the item are through
     kS,                          // [2] S of the stream's unit is in TMEM
@@ -65,18 +65,14 @@ enum Bar {
     kDone,                       // all MMAs are through
     kItem,                       // [2] the next item is in shared memory (items take the two places in turn)
     kItemTaken = kItem + 2,      // [2] ... and has been read by all roles
-    kTurn = kItemTaken + 2,      // [2][4] the stream's two warps of a lane quarter have their turn at the exponentials
-    kNumBars = kTurn + 8
+    kNumBars = kItemTaken + 2
 };
-constexpr int kReaders = kSoftmax + 3;   // warps that read the items
+constexpr int kReaders = kSoftmax + 2;   // warps that read the items
 enum ItemWord { kSeq, kHead, kRow0, kTokens, kPos0, kKvEnd, kU0, kU1, kUnits, kParts };   // of a ChunkItem
 static_assert(sizeof(ChunkItem) == 10 * 4 && offsetof(ChunkItem, units) == kUnits * 4 && offsetof(ChunkItem, kv_end) == kKvEnd * 4, "");
 __device__ __forceinline__ int arrivals(int bar)
 {
-    if (bar >= kEmpty && bar < kEmpty + kStages) return 2;
-    if (bar == kQFree || bar == kDone) return 2;
-    if (bar >= kItemTaken && bar < kTurn) return kReaders;
-    if (bar >= kTurn) return 2;
+    if (bar >= kItemTaken) return kReaders;
     return (bar >= kP0 && bar < kO) || bar == kX || bar == kXFree ? kSoftmax / 2 : 1;   // (one lane of each warp of a stream)
 }
 
@@ -170,7 +166,7 @@ __device__ __forceinline__ float2 load_pair(uint32_t at)
 // What the warps of a CTA share, by its address in shared memory: barriers, and whether one of their waits gave up.
 struct Shared {
     uint32_t at;
-    static constexpr uint32_t kAbort = 384, kTmem = 388, kLanded = 392, kScratch = 400, kExchange = 576, kItems = 1600;
+    static constexpr uint32_t kAbort = 384, kTmem = 388, kScratch = 400, kExchange = 576, kItems = 1600;
     __device__ uint32_t bar(int i) const { return at + i * 8; }
     __device__ static int load(uint32_t a)
     {
@@ -216,17 +212,6 @@ struct Shared {
         give_up(status, bit);
         return false;
     }
-    // until the stream's issuing warp has seen this slot full
-    __device__ bool wait_landed(int stream, int slot, int32_t *status, int bit) const
-    {
-#pragma unroll 1
-        for (int i = 0; i < 1 << 22; ++i) {
-            if (load(at + kLanded + stream * 4) >= slot) return true;
-            if (load(at + kAbort)) return false;
-        }
-        give_up(status, bit);
-        return false;
-    }
     // the same for a converged warp: true if every lane has seen the phase
     __device__ bool warp_wait(int i, uint32_t parity, int32_t *status, int bit) const { return __all_sync(0xffffffffu, wait(i, parity, status, bit)); }
     // words of an item (ChunkItem)
@@ -236,7 +221,7 @@ static_assert(kNumBars * 8 <= Shared::kAbort && Shared::kScratch + (kFound + 2) 
                   Shared::kItems + 2 * sizeof(ChunkItem) <= 2048,
               "");
 
-// ---------------------------------------------------------------------- warp 19: the items, two ahead of the roles that read them
+// ---------------------------------------------------------------------- warp 18: the items, two ahead of the roles that read them
 // (A walk of their own in every role cost the softmax its registers: spills of 17 loads a unit, two thirds of them from L2, were most of
 // the time of a prompt of 8K.)
 __device__ __forceinline__ void hand_out(ChunkWalk &walk, const Shared &sh, ChunkItem *items, int32_t *status)
@@ -341,95 +326,89 @@ __device__ __forceinline__ void produce(const Params &p, const Shared &sh, uint3
     if (items > 0 && !__all_sync(0xffffffffu, mbar_wait_bounded(sh.bar(kQFull), (items - 1) & 1)) && p.status) atomicOr(p.status, 1);
 }
 
-// ---------------------------------------------------------------------- warps 17 and 18: the MMAs of stream g
-// A wait on a parity cannot tell a phase from the one two before it, so a stage's phase may only be waited for when the one before is known
-// to be complete.  Of a stage that the other stream had last, this one knows that from the other's word (Shared::kLanded).
-__device__ __forceinline__ void issue(const Params &p, const Shared &sh, uint32_t smem0, uint32_t tmem, int g)
+// ---------------------------------------------------------------------- warp 17: all MMAs, of the two streams in turn
+// The turns keep the streams half a unit apart, one in its softmax while the tensor cores work for the other; issued by a warp each, the streams
+// fall into step and wait for the tensor cores together (4750 cycles a unit of a prompt).  What a step waits for is waited for ahead of the
+// P that it needs, so that PV and the next S go out together: a wait takes 120 cycles even when there is nothing to wait for.
+__device__ __forceinline__ void issue(const Params &p, const Shared &sh, uint32_t smem0, uint32_t tmem)
 {
     constexpr uint32_t idesc_s = umma_idesc_bf16(128, kUnit, false), idesc_pv = umma_idesc_bf16(128, 128, true);
     const uint64_t dq = umma_desc_sw128(smem0 + kOffQ, 16, 1024), dk = umma_desc_sw128(smem0, 16, 1024);
     const uint64_t dv = umma_desc_sw128(smem0, kHalf / 2, 1024);
-    const uint32_t t_s = tmem + g * 128, t_o = tmem + 256 + g * 128;
-    const auto wait = [&](int bar, uint32_t parity, int bit) { return sh.wait(bar, parity, p.status, bit); };
-    int slot = 0, stage = 0, items = 0;   // ring slots and items so far, slot % kStages
-    uint32_t turn = 0, of_p = 0;          // parity of slot / kStages and of the units of this stream
-    uint32_t foreign = 0;                 // the stages that the other stream alone had last
-    const auto next_slot = [&] {
-        ++slot;
-        if (++stage == kStages) stage = 0, turn ^= 1;
-    };
-    const auto pass = [&] {   // a unit of the other stream
-        foreign |= 1u << stage;
-        next_slot();
-        foreign |= 1u << stage;
-        next_slot();
-    };
-    const auto full = [&](bool two) {
-        if (foreign >> stage & 1) {
-            if (!sh.wait_landed(1 - g, slot - kStages, p.status, 4)) return false;
-            foreign &= ~(1u << stage);
+    const auto wait = [&](int bar, uint32_t parity, int bit) { return sh.warp_wait(bar, parity, p.status, bit); };
+    const auto full = [&](int slot) { return wait(kFull + slot % kStages, (slot / kStages) & 1, 4); };
+    const auto issue_s = [&](int g, uint64_t dq_g, int slot) {
+        const uint64_t dk_u = dk + (uint64_t)(slot % kStages * (kTileBytes >> 4));
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) {
+            constexpr int kStep[8] = {0, 2, 4, 6, kHalf >> 4, (kHalf >> 4) + 2, (kHalf >> 4) + 4, (kHalf >> 4) + 6};
+            tc_mma_bf16(tmem + g * 128, dq_g + kStep[ks], dk_u + kStep[ks], idesc_s, ks > 0);
         }
-        if (!wait(kFull + stage, turn, 4)) return false;
-        if (!two) Shared::store(sh.at + Shared::kLanded + g * 4, slot);   // (of two tiles both streams see every slot)
-        return true;
+        tc_commit(sh.bar(kS + g));
     };
+    int unit0 = 0;               // units of the CTA before this item
+    uint32_t of_p = 0, of_q = 0; // parities: of the streams' next P, of the next Q
     bool dead = false;
 #pragma unroll 1
-    for (int n = 0; !dead && wait(kItem + (n & 1), (n >> 1) & 1, 64) && sh.item(n, kUnits) >= 0; ++n) {
+    for (int n = 0; !dead && take(sh, n, p.status); ++n) {
         const int n_units = sh.item(n, kU1) - sh.item(n, kU0);
         const bool two = sh.item(n, kTokens) > p.TT, none = sh.item(n, kUnits) == 0;
-        mbar_arrive(sh.bar(kItemTaken + (n & 1)));
+        taken(sh, n);
         if (none) continue;
-        const int step = two ? 1 : 2, begin = two ? 0 : g;
-        if (!wait(kQFull, items & 1, 4)) break;
-        ++items;
-        if (begin >= n_units) mbar_arrive(sh.bar(kQFree));
-        if (begin) pass();
-        const uint64_t dq_g = dq + (uint64_t)(two ? g * (kTileBytes >> 4) : 0);
-#pragma unroll 1
-        for (int j = begin; j < n_units; j += step) {
-            const bool last = j + step >= n_units;
-            dead = !full(two);
-            if (dead) break;
-            tc_fence_after_sync();
-            {
-                const uint64_t dk_u = dk + (uint64_t)(stage * (kTileBytes >> 4));
-#pragma unroll
-                for (int ks = 0; ks < 8; ++ks) {
-                    constexpr int kStep[8] = {0, 2, 4, 6, kHalf >> 4, (kHalf >> 4) + 2, (kHalf >> 4) + 4, (kHalf >> 4) + 6};
-                    tc_mma_bf16(t_s, dq_g + kStep[ks], dk_u + kStep[ks], idesc_s, ks > 0);
-                }
-                tc_commit(sh.bar(kS + g));
-                tc_commit(sh.bar(kEmpty + stage));
-                if (!two) tc_commit(sh.bar(kEmpty + stage));   // (a stage has two readers)
-                if (last) tc_commit(sh.bar(kQFree));
+        const uint64_t dq_1 = dq + (uint64_t)(two ? kTileBytes >> 4 : 0);
+        const int ahead = two ? 1 : 2;   // units from a stream's unit to its next one
+        dead = !wait(kQFull, of_q, 4) || !full(2 * unit0) || (!two && n_units > 1 && !full(2 * unit0 + 2));
+        if (dead) break;
+        of_q ^= 1;
+        tc_fence_after_sync();
+        if (elect_one()) {   // S of the streams' first units
+            issue_s(0, dq, 2 * unit0);
+            if (!two) tc_commit(sh.bar(kEmpty + 2 * unit0 % kStages));
+            if (two || n_units > 1) {
+                const int slot = 2 * unit0 + (two ? 0 : 2);
+                issue_s(1, dq_1, slot);
+                tc_commit(sh.bar(kEmpty + slot % kStages));
             }
-            next_slot();
-            dead = !full(two) || !wait(kP0 + g, of_p, 8);
-            if (dead) break;
-            const uint64_t dv_u = dv + (uint64_t)(stage * (kTileBytes >> 4));
-            const uint32_t bar_empty = sh.bar(kEmpty + stage);
-            tc_fence_after_sync();
-            {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) tc_mma_bf16_ta(t_o, t_s + i * 8, dv_u + (uint64_t)(i * 2048 >> 4), idesc_pv, j > begin || i > 0);
-            }
-            dead = !wait(kP1 + g, of_p, 8);
-            if (dead) break;
-            tc_fence_after_sync();
-            {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) tc_mma_bf16_ta(t_o, t_s + (4 + i) * 8, dv_u + (uint64_t)((kHalf + i * 2048) >> 4), idesc_pv, 1);
-                tc_commit(bar_empty);
-                if (!two) tc_commit(bar_empty);
-                if (last) tc_commit(sh.bar(kO + g));
-            }
-            of_p ^= 1;
-            next_slot();
-            if (!two && j + 1 < n_units) pass();
+            if (n_units <= ahead) tc_commit(sh.bar(kQFree));
         }
+        __syncwarp();
+        const int steps = two ? 2 * n_units : n_units;
+#pragma unroll 1
+        for (int i = 0; i < steps; ++i) {   // PV of a stream's unit and S of its next
+            const int g = i & 1, j = two ? i >> 1 : i, slot_v = 2 * (unit0 + j) + 1, slot_k = 2 * (unit0 + j + ahead);
+            const bool more = j + ahead < n_units, first_reader = two && g == 0;   // (of two tiles the second stream's is the last)
+            dead = !(two && g) && (!full(slot_v) || (more && !full(slot_k)));
+            dead = dead || !wait(kP0 + g, of_p >> g & 1, 8);
+            if (dead) break;
+            const uint64_t dv_u = dv + (uint64_t)(slot_v % kStages * (kTileBytes >> 4));
+            const uint32_t t_o = tmem + 256 + g * 128, t_p = tmem + g * 128;
+            tc_fence_after_sync();
+            if (elect_one()) {
+#pragma unroll
+                for (int m = 0; m < 4; ++m) tc_mma_bf16_ta(t_o, t_p + m * 8, dv_u + (uint64_t)(m * 2048 >> 4), idesc_pv, j >= ahead || m > 0);
+            }
+            __syncwarp();
+            dead = !wait(kP1 + g, of_p >> g & 1, 8);
+            if (dead) break;
+            of_p ^= 1u << g;
+            tc_fence_after_sync();
+            if (elect_one()) {
+#pragma unroll
+                for (int m = 0; m < 4; ++m) tc_mma_bf16_ta(t_o, t_p + (4 + m) * 8, dv_u + (uint64_t)((kHalf + m * 2048) >> 4), idesc_pv, 1);
+                if (more) issue_s(g, g ? dq_1 : dq, slot_k);
+                else tc_commit(sh.bar(kO + g));
+                if (!first_reader) {
+                    tc_commit(sh.bar(kEmpty + slot_v % kStages));
+                    if (more) tc_commit(sh.bar(kEmpty + slot_k % kStages));
+                    if (j + ahead == n_units - 1) tc_commit(sh.bar(kQFree));
+                }
+            }
+            __syncwarp();
+        }
+        unit0 += n_units;
     }
-    tc_commit(sh.bar(kDone));
+    if (elect_one()) tc_commit(sh.bar(kDone));
+    __syncwarp();
 }
 
 // ---------------------------------------------------------------------- warps 0-7 and 8-15: the softmax of stream g
@@ -502,25 +481,11 @@ __device__ __forceinline__ void softmax(const Params &p, const Shared sh, uint32
     const int r0 = (warp & 3) * 32 + (warp >> 2 & 1) * 16 + (lane >> 2);   // first of the thread's rows of the tile
     const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32 + (warp >> 2 & 1) * 16) << 16), t_s = t_lane + g * 128, t_o = t_lane + 256 + g * 128;
     uint32_t phases = 0;   // parities of what this warp has waited for
-    constexpr uint32_t kOfS = 1, kOfTurn = 2, kOfO = 4, kOfX = 8;
+    constexpr uint32_t kOfS = 1, kOfO = 2, kOfX = 4;
     const auto wait = [&](int bar, uint32_t of, int bit) {
         const bool ok = sh.warp_wait(bar, (phases & of) != 0, p.status, bit);
         phases ^= of;
         return ok;
-    };
-    // The warps of both streams that share a scheduler take their exponentials in turns, the first stream first.  Left alone, the streams fall
-    // into step: both wait for the tensor cores, then both share the special-function unit (4750 cycles a unit of a prompt).
-    const uint32_t turn_bar = kTurn + (warp & 3);
-    bool first_turn = g == 0;
-    const auto my_turn = [&] {
-        if (first_turn) {
-            first_turn = false;
-            return true;
-        }
-        return wait(turn_bar + g * 4, kOfTurn, 32);
-    };
-    const auto next_turn = [&] {
-        if (lane == 0) mbar_arrive(sh.bar(turn_bar + (1 - g) * 4));
     };
     const auto arrive = [&](int bar) {
         tc_fence_before_sync();
@@ -609,7 +574,6 @@ __device__ __forceinline__ void softmax(const Params &p, const Shared sh, uint32
                 const float use = m[h] == -INFINITY ? 0.f : -m[h];
                 ref2[h] = f2_pack(use, use);
             }
-            if (!my_turn()) return;
             const auto quarter = [&](int c) {
                 uint32_t w[8];
 #pragma unroll
@@ -622,7 +586,6 @@ __device__ __forceinline__ void softmax(const Params &p, const Shared sh, uint32
             arrive(kP0 + g);
             quarter(2);
             quarter(3);
-            next_turn();
             tmem_st_wait();
             arrive(kP1 + g);
 #pragma unroll
@@ -633,10 +596,6 @@ __device__ __forceinline__ void softmax(const Params &p, const Shared sh, uint32
             }
         }
         v_slot += 2 * n_units;
-        if (!two && g && (n_units & 1)) {   // (the first stream had one unit more)
-            if (!my_turn()) return;
-            next_turn();
-        }
         const bool had = begin < n_units, both = !two && n_units > 1;
         if (had) {
             if (!wait(kO + g, kOfO, 16)) return;
@@ -743,7 +702,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int i = 0; i < kNumBars; ++i) mbar_init(sh.bar(i), arrivals(i));
         mbar_fence_init();
         Shared::store(sh.at + Shared::kAbort, 0);
-        Shared::store(sh.at + Shared::kLanded, -1), Shared::store(sh.at + Shared::kLanded + 4, -1);
     }
     if (warp == kSoftmax && (tid & 31) == 0) tma_prefetch_desc(&tm_q), tma_prefetch_desc(&tm_k), tma_prefetch_desc(&tm_v);
     if (warp == kSoftmax + 1) tmem_alloc(sh.at + Shared::kTmem, 512);
@@ -759,8 +717,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (warp >= kSoftmax) {
             reg_dealloc<kRegsFew>();
             if (warp == kSoftmax) produce(p, sh, smem0, tm_q, tm_k, tm_v);
-            else if (warp < kSoftmax + 3 && elect_one()) issue(p, sh, smem0, tmem, warp - kSoftmax - 1);
-            else if (warp == kSoftmax + 3) hand_out(walk, sh, reinterpret_cast<ChunkItem *>(misc + Shared::kItems), p.status);
+            else if (warp == kSoftmax + 1) issue(p, sh, smem0, tmem);
+            else if (warp == kSoftmax + 2) hand_out(walk, sh, reinterpret_cast<ChunkItem *>(misc + Shared::kItems), p.status);
         } else {
             reg_alloc<kRegsMany>();
             softmax(p, sh, smem0, tmem, warp >> 3);
