@@ -328,15 +328,21 @@ __device__ __forceinline__ void produce(const Params &p, const Shared &sh, uint3
 
 // ---------------------------------------------------------------------- warp 17: all MMAs, of the two streams in turn
 // The turns keep the streams half a unit apart, one in its softmax while the tensor cores work for the other; issued by a warp each, the streams
-// fall into step and wait for the tensor cores together (4750 cycles a unit of a prompt).  What a step waits for is waited for ahead of the
-// P that it needs, so that PV and the next S go out together: a wait takes 120 cycles even when there is nothing to wait for.
+// fall into step and wait for the tensor cores together (4750 cycles a unit of a prompt).  A wait takes 250 to 300 cycles here even when there is nothing to
+// wait for, so the lanes wait for different barriers at once: the stage of V, that of the next unit's K and the first half of P, then the rest of
+// P, behind which PV and the next S go out together (a wait after the other, the warp itself was what a unit took: 4200 cycles).
 __device__ __forceinline__ void issue(const Params &p, const Shared &sh, uint32_t smem0, uint32_t tmem)
 {
     constexpr uint32_t idesc_s = umma_idesc_bf16(128, kUnit, false), idesc_pv = umma_idesc_bf16(128, 128, true);
     const uint64_t dq = umma_desc_sw128(smem0 + kOffQ, 16, 1024), dk = umma_desc_sw128(smem0, 16, 1024);
     const uint64_t dv = umma_desc_sw128(smem0, kHalf / 2, 1024);
     const auto wait = [&](int bar, uint32_t parity, int bit) { return sh.warp_wait(bar, parity, p.status, bit); };
-    const auto full = [&](int slot) { return wait(kFull + slot % kStages, (slot / kStages) & 1, 4); };
+    const int lane = threadIdx.x & 31;
+    // lanes 0, 3, 6, ..: this barrier; 1, 4, ..: the stage of slot a; 2, 5, ..: that of slot b (less than 0: the barrier as well)
+    const auto wait_all = [&](int bar, uint32_t parity, int a, int b, int bit) {
+        const int slot = lane % 3 == 1 ? a : lane % 3 == 2 ? b : -1;
+        return wait(slot < 0 ? bar : kFull + slot % kStages, slot < 0 ? parity : (slot / kStages) & 1, bit);
+    };
     const auto issue_s = [&](int g, uint64_t dq_g, int slot) {
         const uint64_t dk_u = dk + (uint64_t)(slot % kStages * (kTileBytes >> 4));
 #pragma unroll
@@ -357,7 +363,7 @@ __device__ __forceinline__ void issue(const Params &p, const Shared &sh, uint32_
         if (none) continue;
         const uint64_t dq_1 = dq + (uint64_t)(two ? kTileBytes >> 4 : 0);
         const int ahead = two ? 1 : 2;   // units from a stream's unit to its next one
-        dead = !wait(kQFull, of_q, 4) || !full(2 * unit0) || (!two && n_units > 1 && !full(2 * unit0 + 2));
+        dead = !wait_all(kQFull, of_q, 2 * unit0, !two && n_units > 1 ? 2 * unit0 + 2 : -1, 4);
         if (dead) break;
         of_q ^= 1;
         tc_fence_after_sync();
@@ -377,8 +383,8 @@ __device__ __forceinline__ void issue(const Params &p, const Shared &sh, uint32_
         for (int i = 0; i < steps; ++i) {   // PV of a stream's unit and S of its next
             const int g = i & 1, j = two ? i >> 1 : i, slot_v = 2 * (unit0 + j) + 1, slot_k = 2 * (unit0 + j + ahead);
             const bool more = j + ahead < n_units, first_reader = two && g == 0;   // (of two tiles the second stream's is the last)
-            dead = !(two && g) && (!full(slot_v) || (more && !full(slot_k)));
-            dead = dead || !wait(kP0 + g, of_p >> g & 1, 8);
+            const bool seen = two && g;   // ... and the first has seen the stages
+            dead = !wait_all(kP0 + g, of_p >> g & 1, seen ? -1 : slot_v, seen || !more ? -1 : slot_k, 8);
             if (dead) break;
             const uint64_t dv_u = dv + (uint64_t)(slot_v % kStages * (kTileBytes >> 4));
             const uint32_t t_o = tmem + 256 + g * 128, t_p = tmem + g * 128;
