@@ -336,15 +336,22 @@ __device__ __forceinline__ void issue(const Params &p, const Shared &sh, uint32_
     constexpr uint32_t idesc_s = umma_idesc_bf16(128, kUnit, false), idesc_pv = umma_idesc_bf16(128, 128, true);
     const uint64_t dq = umma_desc_sw128(smem0 + kOffQ, 16, 1024), dk = umma_desc_sw128(smem0, 16, 1024);
     const uint64_t dv = umma_desc_sw128(smem0, kHalf / 2, 1024);
-    const auto wait = [&](int bar, uint32_t parity, int bit) { return sh.warp_wait(bar, parity, p.status, bit); };
-    const int lane = threadIdx.x & 31;
-    // lanes 0, 3, 6, ..: this barrier; 1, 4, ..: the stage of slot a; 2, 5, ..: that of slot b (less than 0: the barrier as well)
-    const auto wait_all = [&](int bar, uint32_t parity, int a, int b, int bit) {
-        const int slot = lane % 3 == 1 ? a : lane % 3 == 2 ? b : -1;
-        return wait(slot < 0 ? bar : kFull + slot % kStages, slot < 0 ? parity : (slot / kStages) & 1, bit);
+    // Of every three lanes the second waits for stages of V and the third for stages of K: the ring stage and its parity of what a lane waits for next.
+    const int lane = threadIdx.x & 31, part = lane % 3;
+    int stage = 0;
+    uint32_t turn = 0;
+    const auto wait = [&](int bar, uint32_t parity, bool for_stage, int bit) {
+        return sh.warp_wait(for_stage ? kFull + stage : bar, for_stage ? turn : parity, p.status, bit);
     };
-    const auto issue_s = [&](int g, uint64_t dq_g, int slot) {
-        const uint64_t dk_u = dk + (uint64_t)(slot % kStages * (kTileBytes >> 4));
+    const auto skip = [&](int slots) {   // (fewer than kStages)
+        stage += slots;
+        if (stage >= kStages) stage -= kStages, turn ^= 1;
+    };
+    // (the warp's own stages of V and K, as descriptors and barriers)
+    int stage_v = 1, stage_k = 0;
+    const auto next = [](int &at) { at += at >= kStages - 2 ? 2 - kStages : 2; };
+    const auto issue_s = [&](int g, uint64_t dq_g) {
+        const uint64_t dk_u = dk + (uint64_t)(stage_k * (kTileBytes >> 4));
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) {
             constexpr int kStep[8] = {0, 2, 4, 6, kHalf >> 4, (kHalf >> 4) + 2, (kHalf >> 4) + 4, (kHalf >> 4) + 6};
@@ -352,7 +359,7 @@ __device__ __forceinline__ void issue(const Params &p, const Shared &sh, uint32_
         }
         tc_commit(sh.bar(kS + g));
     };
-    int unit0 = 0;               // units of the CTA before this item
+    if (part == 1) skip(1);
     uint32_t of_p = 0, of_q = 0; // parities: of the streams' next P, of the next Q
     bool dead = false;
 #pragma unroll 1
@@ -363,55 +370,65 @@ __device__ __forceinline__ void issue(const Params &p, const Shared &sh, uint32_
         if (none) continue;
         const uint64_t dq_1 = dq + (uint64_t)(two ? kTileBytes >> 4 : 0);
         const int ahead = two ? 1 : 2;   // units from a stream's unit to its next one
-        dead = !wait_all(kQFull, of_q, 2 * unit0, !two && n_units > 1 ? 2 * unit0 + 2 : -1, 4);
+        // S of the streams' first units
+        dead = !wait(kQFull, of_q, part == 2, 4);
+        if (part == 2) skip(2);
+        if (!dead && !two && n_units > 1) {
+            dead = !wait(kQFull, of_q, part == 2, 4);
+            if (part == 2) skip(2);
+        }
         if (dead) break;
         of_q ^= 1;
         tc_fence_after_sync();
-        if (elect_one()) {   // S of the streams' first units
-            issue_s(0, dq, 2 * unit0);
-            if (!two) tc_commit(sh.bar(kEmpty + 2 * unit0 % kStages));
-            if (two || n_units > 1) {
-                const int slot = 2 * unit0 + (two ? 0 : 2);
-                issue_s(1, dq_1, slot);
-                tc_commit(sh.bar(kEmpty + slot % kStages));
-            }
-            if (n_units <= ahead) tc_commit(sh.bar(kQFree));
+        if (elect_one()) issue_s(0, dq);
+        if (!two) {
+            if (elect_one()) tc_commit(sh.bar(kEmpty + stage_k));
+            next(stage_k);
         }
+        if (two || n_units > 1) {
+            if (elect_one()) issue_s(1, dq_1), tc_commit(sh.bar(kEmpty + stage_k));
+            next(stage_k);
+        }
+        if (n_units <= ahead && elect_one()) tc_commit(sh.bar(kQFree));
         __syncwarp();
-        const int steps = two ? 2 * n_units : n_units;
+        int left = n_units;   // units whose PV is to come
 #pragma unroll 1
-        for (int i = 0; i < steps; ++i) {   // PV of a stream's unit and S of its next
-            const int g = i & 1, j = two ? i >> 1 : i, slot_v = 2 * (unit0 + j) + 1, slot_k = 2 * (unit0 + j + ahead);
-            const bool more = j + ahead < n_units, first_reader = two && g == 0;   // (of two tiles the second stream's is the last)
-            const bool seen = two && g;   // ... and the first has seen the stages
-            dead = !wait_all(kP0 + g, of_p >> g & 1, seen ? -1 : slot_v, seen || !more ? -1 : slot_k, 8);
+        for (int g = 0; left > 0; g ^= 1) {   // PV of a stream's unit and S of its next
+            const bool more = left > ahead, second = two && g, first_reader = two && !g;   // (of two tiles the second stream is the last reader, and the
+                                                                                          // first one has seen the stages)
+            const uint64_t dv_u = dv + (uint64_t)(stage_v * (kTileBytes >> 4));
+            const uint32_t t_o = tmem + 256 + g * 128, t_p = tmem + g * 128, starts = n_units - left >= ahead;
+            dead = !wait(kP0 + g, of_p >> g & 1, !second && (part == 1 || (part == 2 && more)), 8);
             if (dead) break;
-            const uint64_t dv_u = dv + (uint64_t)(slot_v % kStages * (kTileBytes >> 4));
-            const uint32_t t_o = tmem + 256 + g * 128, t_p = tmem + g * 128;
             tc_fence_after_sync();
             if (elect_one()) {
 #pragma unroll
-                for (int m = 0; m < 4; ++m) tc_mma_bf16_ta(t_o, t_p + m * 8, dv_u + (uint64_t)(m * 2048 >> 4), idesc_pv, j >= ahead || m > 0);
+                for (int m = 0; m < 4; ++m) tc_mma_bf16_ta(t_o, t_p + m * 8, dv_u + (uint64_t)(m * 2048 >> 4), idesc_pv, m ? 1u : starts);
             }
             __syncwarp();
-            dead = !wait(kP1 + g, of_p >> g & 1, 8);
+            dead = !sh.warp_wait(kP1 + g, of_p >> g & 1, p.status, 8);
             if (dead) break;
-            of_p ^= 1u << g;
             tc_fence_after_sync();
             if (elect_one()) {
 #pragma unroll
                 for (int m = 0; m < 4; ++m) tc_mma_bf16_ta(t_o, t_p + (4 + m) * 8, dv_u + (uint64_t)((kHalf + m * 2048) >> 4), idesc_pv, 1);
-                if (more) issue_s(g, g ? dq_1 : dq, slot_k);
+                if (more) issue_s(g, g ? dq_1 : dq);
                 else tc_commit(sh.bar(kO + g));
                 if (!first_reader) {
-                    tc_commit(sh.bar(kEmpty + slot_v % kStages));
-                    if (more) tc_commit(sh.bar(kEmpty + slot_k % kStages));
-                    if (j + ahead == n_units - 1) tc_commit(sh.bar(kQFree));
+                    tc_commit(sh.bar(kEmpty + stage_v));
+                    if (more) tc_commit(sh.bar(kEmpty + stage_k));
+                    if (left == ahead + 1) tc_commit(sh.bar(kQFree));
                 }
             }
             __syncwarp();
+            of_p ^= 1u << g;
+            if (!second && (part == 1 || (part == 2 && more))) skip(2);
+            if (!first_reader) {
+                next(stage_v);
+                if (more) next(stage_k);
+                --left;
+            }
         }
-        unit0 += n_units;
     }
     if (elect_one()) tc_commit(sh.bar(kDone));
     __syncwarp();
