@@ -214,6 +214,18 @@ struct Shared {
     }
     // the same for a converged warp: true if every lane has seen the phase
     __device__ bool warp_wait(int i, uint32_t parity, int32_t *status, int bit) const { return __all_sync(0xffffffffu, wait(i, parity, status, bit)); }
+    // The same without the suspension that try_wait may take, for the issuing warp alone (for all warps, their polls get into one another's way).
+    __device__ bool spin_wait(int i, uint32_t parity, int32_t *status, int bit) const
+    {
+        const uint32_t b = bar(i);
+#pragma unroll 1
+        for (int n = 1; n < 1 << 22; ++n) {
+            if (__all_sync(0xffffffffu, mbar_test(b, parity))) return true;
+            if ((n & 8191) == 0 && __any_sync(0xffffffffu, load(at + kAbort))) return false;
+        }
+        give_up(status, bit);
+        return false;
+    }
     // words of an item (ChunkItem)
     __device__ int item(int n, int word) const { return load(at + kItems + (n & 1) * (uint32_t)sizeof(ChunkItem) + word * 4); }
 };
@@ -341,7 +353,7 @@ __device__ __forceinline__ void issue(const Params &p, const Shared &sh, uint32_
     int stage = 0;
     uint32_t turn = 0;
     const auto wait = [&](int bar, uint32_t parity, bool for_stage, int bit) {
-        return sh.warp_wait(for_stage ? kFull + stage : bar, for_stage ? turn : parity, p.status, bit);
+        return sh.spin_wait(for_stage ? kFull + stage : bar, for_stage ? turn : parity, p.status, bit);
     };
     const auto skip = [&](int slots) {   // (fewer than kStages)
         stage += slots;
@@ -398,7 +410,7 @@ __device__ __forceinline__ void issue(const Params &p, const Shared &sh, uint32_
                                                                                           // first one has seen the stages)
             const uint64_t dv_u = dv + (uint64_t)(stage_v * (kTileBytes >> 4));
             const uint32_t t_o = tmem + 256 + g * 128, t_p = tmem + g * 128, starts = n_units - left >= ahead;
-            dead = !wait(kP0 + g, of_p >> g & 1, !second && (part == 1 || (part == 2 && more)), 8);
+            dead = !wait(kP0 + g, of_p >> g & 1, !second && (part == 1 || (part == 2 && more && two)), 8);
             if (dead) break;
             tc_fence_after_sync();
             if (elect_one()) {
@@ -406,19 +418,27 @@ __device__ __forceinline__ void issue(const Params &p, const Shared &sh, uint32_
                 for (int m = 0; m < 4; ++m) tc_mma_bf16_ta(t_o, t_p + m * 8, dv_u + (uint64_t)(m * 2048 >> 4), idesc_pv, m ? 1u : starts);
             }
             __syncwarp();
-            dead = !sh.warp_wait(kP1 + g, of_p >> g & 1, p.status, 8);
+            dead = !sh.spin_wait(kP1 + g, of_p >> g & 1, p.status, 8);
             if (dead) break;
             tc_fence_after_sync();
             if (elect_one()) {
 #pragma unroll
                 for (int m = 0; m < 4; ++m) tc_mma_bf16_ta(t_o, t_p + (4 + m) * 8, dv_u + (uint64_t)((kHalf + m * 2048) >> 4), idesc_pv, 1);
-                if (more) issue_s(g, g ? dq_1 : dq);
-                else tc_commit(sh.bar(kO + g));
-                if (!first_reader) {
-                    tc_commit(sh.bar(kEmpty + stage_v));
-                    if (more) tc_commit(sh.bar(kEmpty + stage_k));
-                    if (left == ahead + 1) tc_commit(sh.bar(kQFree));
-                }
+                if (two && more) issue_s(g, g ? dq_1 : dq);
+                if (!more) tc_commit(sh.bar(kO + g));
+                if (!first_reader) tc_commit(sh.bar(kEmpty + stage_v));
+            }
+            __syncwarp();
+            if (!two && more) {   // (one tile: bound by the loads, V goes back before the next K is waited for)
+                dead = !wait(kP1 + g, of_p >> g & 1, part == 2, 8);
+                if (dead) break;
+                tc_fence_after_sync();
+                if (elect_one()) issue_s(g, dq);
+                __syncwarp();
+            }
+            if (more && !first_reader && elect_one()) {
+                tc_commit(sh.bar(kEmpty + stage_k));
+                if (left == ahead + 1) tc_commit(sh.bar(kQFree));
             }
             __syncwarp();
             of_p ^= 1u << g;
