@@ -1,7 +1,8 @@
 // How sv_chunk_attn divides a ragged batch among its CTAs (plain C++: the same arithmetic runs in the kernel and in its test).
 //
-// An item is up to 2 * TT tokens of a (sequence, KV head) and costs the keys it sees plus kItemCost.  The items of the batch, by sequence,
-// KV head and place, lie one behind the other on a line, which is cut into equal shares.  Where an item is cut follows from the share's
+// An item is up to 2 * TT tokens of a (sequence, KV head) and costs the keys it sees -- twice where it is two row tiles, whose streams both
+// take every unit -- plus kItemCost.  The items of the batch, by sequence, KV head and place, lie one behind the other on a line, which
+// is cut into equal shares.  Where an item is cut follows from the share's
 // bounds alone, so neighbours agree without talking to one another.  Costs are whole numbers with closed sums: no table is needed.
 #pragma once
 #include <stdint.h>
@@ -15,8 +16,10 @@
 namespace svk {
 
 constexpr int kChunkUnit = 128;   // keys of a unit, the grain of a cut
-constexpr int kItemCost = 192;    // keys that the beginning and the end of an item cost as much as
-constexpr int kLeastShare = 256;  // keys of the shortest share worth a CTA; two units, so that no share inside an item is empty
+// A unit of two tiles takes 3900 cycles, of one tile 1900 (a prompt of 8K; single tokens whose keys are in L2), an item's beginning and end 5000, and more
+// where they wait for nothing else (512 against 320: a ragged batch 104.7 -> 100.6 us, the prompt 515 -> 512).
+constexpr int kItemCost = 512;    // keys (of one tile) that the beginning and the end of an item cost as much as
+constexpr int kLeastShare = 256;  // ... of the shortest share worth a CTA; a unit of two tiles, so that no share inside an item is empty
 
 struct ChunkBatch {
     const int32_t *q_start, *seq_lens;
@@ -36,7 +39,7 @@ struct ChunkItem {
 // The items of a share, in order.
 struct ChunkWalk {
     const ChunkBatch &b;
-    long long total, lo, hi, at;   // in keys; `at`: where the next item begins
+    long long total, lo, hi, at;   // on the line; `at`: where the next item begins
     int shares, mine;
     int s, h, t, n, row, prefix, tiles;   // next item: sequence (its tokens, first row, tokens cached before, items per head), KV head, number
 
@@ -54,13 +57,14 @@ struct ChunkWalk {
         prefix = b.seq_lens[i] - n, tiles = (n + 2 * b.TT - 1) / (2 * b.TT);
     }
     SV_HD long long seen_before() const { return prefix < 0 ? 0 : least(prefix, b.cap); }
-    // cost of the items before number i of a KV head, of all of them, of one
-    SV_HD long long before(long long i) const { return i * (seen_before() + kItemCost) + b.TT * i * (i + 1); }
-    SV_HD long long per_head() const { return n ? before(tiles - 1) + seen_before() + n + kItemCost : 0; }
-    SV_HD long long cost(int i) const { return seen_before() + kItemCost + least(n, (i + 1) * 2ll * b.TT); }
+    // cost of a key of item i of a KV head, of the items before it (two tiles each), of itself, of all of them
+    SV_HD int weight(int i) const { return n - i * 2 * b.TT > b.TT ? 2 : 1; }
+    SV_HD long long before(long long i) const { return i * (2 * seen_before() + kItemCost) + 2 * b.TT * i * (i + 1); }
+    SV_HD long long cost(int i) const { return weight(i) * (seen_before() + least(n, (i + 1) * 2ll * b.TT)) + kItemCost; }
+    SV_HD long long per_head() const { return n ? before(tiles - 1) + cost(tiles - 1) : 0; }
     SV_HD long long bound(int share) const { return total * share / shares; }
 
-    // Of `all` keys among `ctas`: the share of number `cta`, if it has one.
+    // Of a line of this length among `ctas`: the share of number `cta`, if it has one.
     SV_HD bool divide(long long all, int ctas, int cta)
     {
         total = all, mine = cta;
@@ -85,25 +89,25 @@ struct ChunkWalk {
         }
         t = a, at += before(a);
     }
-    // the unit at x keys behind the beginning of an item of this cost
-    SV_HD static int unit_at(long long x, long long cost, int units)
+    // the unit at x behind the beginning of an item of this cost
+    SV_HD static int unit_at(long long x, long long cost, int weight, int units)
     {
-        return x >= cost ? units : x <= kItemCost ? 0 : (int)least(units, (x - kItemCost) / kChunkUnit);
+        return x >= cost ? units : x <= kItemCost ? 0 : (int)least(units, (x - kItemCost) / (weight * kChunkUnit));
     }
     SV_HD bool next(ChunkItem &it)
     {
         while (s < b.S && at < hi) {
             const long long c = cost(t), x0 = lo - at, x1 = hi - at;
-            const int t0 = t * 2 * b.TT;
+            const int t0 = t * 2 * b.TT, w = weight(t);
             it.s = s, it.h = h, it.row0 = row + t0, it.tokens = (int)least(2 * b.TT, n - t0), it.pos0 = prefix + t0;
             const long long end = least((long long)it.pos0 + it.tokens, b.cap);
             it.kv_end = end < 0 ? 0 : (int)end;
             it.units = (it.kv_end + kChunkUnit - 1) / kChunkUnit;
-            it.u0 = unit_at(x0, c, it.units), it.u1 = unit_at(x1, c, it.units);
+            it.u0 = unit_at(x0, c, w, it.units), it.u1 = unit_at(x1, c, w, it.units);
             it.parts = 0;
             if (it.u0 == 0 && it.u1 > 0 && it.u1 < it.units) {
                 it.parts = 1;
-                for (int share = mine + 1, u = it.u1; u < it.units; ++share, ++it.parts) u = unit_at(bound(share + 1) - at, c, it.units);
+                for (int share = mine + 1, u = it.u1; u < it.units; ++share, ++it.parts) u = unit_at(bound(share + 1) - at, c, w, it.units);
             }
             const bool take = it.u1 > it.u0 || (it.units == 0 && x0 <= 0);
             at += c;

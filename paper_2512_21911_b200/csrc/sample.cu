@@ -9,7 +9,8 @@
 //
 // Sums of masses are sums of whole numbers, exact in any order.  Of the nucleus: multiples of 2^-32 of the largest entry's mass, so that a bin is
 // two 32-bit words that shared-memory atomics add to (2^-32 is less than fp32 sums keep; what is lost are entries below 2^-33 of
-// the largest, 2^-16 of its mass if there were 2^17 of them).  Of the draw: multiples of 2^-40, added in registers.
+// the largest, 2^-16 of its mass if there were 2^17 of them); they also do for the draw from a nucleus, whose histogram has them by CTA.  Of
+// other draws: multiples of 2^-40, added in registers.
 //
 // A cluster of 1 to 8 CTAs per row; a CTA keeps its part of the row in shared memory, so the logits are read once from HBM.  Warps
 // own contiguous parts: a token is found by sums per CTA, warp and lane.
@@ -30,8 +31,9 @@ constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
 constexpr int kBins = 2048;
+constexpr int kGroups = 64;                    // of 32 bins each
 constexpr float kBinsPerBit = 2048.f / 36.f;   // bins of the first histogram: 36 powers of two below the maximum, beyond what has a mass
-constexpr int kList = 1024;                    // entries that are ranked one against another
+constexpr int kList = 768;                     // entries that are ranked one against another
 constexpr int kGrain = kWarps * 128;           // a CTA's part of a row is a multiple of this: 32 lanes x 4 entries for each warp
 constexpr int kMostPart = 24 * kGrain;         // entries that fit in shared memory
 constexpr int kPart = 8 * kGrain;              // ... and leave room for a second CTA on the SM
@@ -83,6 +85,7 @@ __device__ __forceinline__ Mass mass_of(float e)
     return whole<N>(p.high, p.low);
 }
 constexpr int kNucleus = 16, kDraw = 20;   // halves of the bits of a mass
+constexpr int kEach = (kList + kThreads - 1) / kThreads;   // entries of a list for each thread
 
 struct Boundary {
     float x;
@@ -90,23 +93,24 @@ struct Boundary {
     __device__ bool keeps(float y, uint32_t i) const { return y > x || (y == x && i <= index); }
 };
 
-struct Smem {
-    uint32_t high[kBins];     // histogram: sums of masses in two words, or counts in the first;
-    int low[kBins];           // the first CTA also sorts its list into the one and keeps masses in the other
-    uint64_t list[kList];     // key << 32 | ~index: descending is the order of the rule
+struct alignas(16) Smem {
+    uint32_t high[kBins];     // histogram: sums of masses in two words, or counts in the second;
+    int low[kBins];           // the first CTA keeps masses of its list in the first
+    Mass list[kList], sorted[kList];   // key << 32 | ~index: descending is the order of the rule
     Mass sums[kWarps], scan[kWarps];
     Mass of_cta[2][kMaxCluster];   // written by all CTAs of the cluster; two in turn, so that no CTA writes what another still reads
     float top_of_cta[kMaxCluster], of_warp[kWarps];
     uint32_t count_of_cta[kMaxCluster];
     uint32_t range[kMaxCluster][2];
-    Mass found_ahead;              // written by the CTA that finds it
+    Mass found_ahead, found_goal;
     int found_bin, token;
     Boundary boundary;
     uint32_t n_list;
-    __device__ uint64_t *sorted() { return reinterpret_cast<uint64_t *>(low); }
+    // The sums of every CTA's groups of bins, written by it, where the sorted list is later.  (Between two uses there is a barrier of the cluster.)
+    __device__ Mass *groups(int cta) { return sorted + cta * kGroups; }
     __device__ Mass *masses() { return reinterpret_cast<Mass *>(high); }
 };
-static_assert(kBins * 4 >= kList * 8 && sizeof(Smem) % 16 == 0, "");
+static_assert(kBins * 4 >= kList * 8 && kList >= kMaxCluster * kGroups, "");
 
 template <class T, class Op>
 __device__ __forceinline__ T over_warp(T v, Op op)
@@ -127,6 +131,145 @@ __device__ __forceinline__ T scan_warp(T v)   // inclusive
     return v;
 }
 
+// The cluster's CTAs, and a word of this CTA's shared memory in each of them (one warp).
+__device__ __forceinline__ int cluster_size() { return (int)cg::this_cluster().num_blocks(); }
+__device__ __forceinline__ int cluster_rank() { return (int)cg::this_cluster().block_rank(); }
+template <class T>
+__device__ __forceinline__ void everywhere(T *at, T v)
+{
+    const int lane = threadIdx.x & 31;
+    if (lane < cluster_size()) *cg::this_cluster().map_shared_rank(at, lane) = v;
+}
+
+// The steps between the passes are functions of their own: inlined where they are used, the kernel had 230 KB of code that is run through
+// once, and the time was that of fetching it.
+
+// Exclusive prefix and total over the CTA, in thread order.
+struct Scan {
+    Mass before, total;
+};
+__device__ __noinline__ Scan scan_block(Smem &sm, Mass v)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const Mass upto = scan_warp(v);
+    __syncthreads();
+    if (lane == 31) sm.scan[warp] = upto;
+    __syncthreads();
+    Scan s = {upto - v, 0};
+#pragma unroll 1
+    for (int w = 0; w < kWarps; ++w) {
+        if (w < warp) s.before += sm.scan[w];
+        s.total += sm.scan[w];
+    }
+    return s;
+}
+// Total over the cluster of a value of each thread; sums keeps the warps' totals, of_cta[turn] the CTAs'.
+__device__ __noinline__ Mass sum_over_cluster(Smem &sm, int turn, Mass v)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    v = sum_over_warp(v);
+    __syncthreads();
+    if (lane == 0) sm.sums[warp] = v;
+    __syncthreads();
+    if (warp == 0) everywhere(&sm.of_cta[turn][cluster_rank()], sum_over_warp(lane < kWarps ? sm.sums[lane] : 0));
+    cg::this_cluster().sync();
+    return sum_over_warp(lane < cluster_size() ? sm.of_cta[turn][lane] : 0);
+}
+// The bin in which the sums over the cluster's histograms reach the goal (0: `of_all` of the sum of all), and what is in the bins ahead of
+// it.  Every CTA tells all others the sums of its groups of bins, finds the group of the goal by itself and reads the bins of that group from
+// all CTAs: one barrier of the cluster (1.8 us each, with what goes before it), where shares of the bins added up by different CTAs take
+// three.  -1: there is not as much.  The bins have to stay until the cluster's next barrier.
+struct Found {
+    int bin;
+    Mass goal, ahead;
+};
+__device__ __noinline__ Found find_in_bins(Smem &sm, Mass goal, float of_all)
+{
+    const cg::cluster_group cluster = cg::this_cluster();
+    const int CL = cluster_size(), rank = cluster_rank(), tid = threadIdx.x, lane = tid & 31;
+    static_assert(kBins == 4 * kThreads && kBins == 32 * kGroups, "");
+    __syncthreads();
+    Mass mine = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mine += whole<kNucleus>(sm.high[4 * tid + i], sm.low[4 * tid + i]);
+#pragma unroll
+    for (int d = 4; d > 0; d >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, d);
+    if ((lane & 7) < CL) *cluster.map_shared_rank(sm.groups(rank) + (tid >> 3), lane & 7) = mine;   // (lanes of a group: the CTA to tell)
+    cluster.sync();
+    if (tid < 32) {
+        Mass g[2] = {0, 0};
+#pragma unroll 1
+        for (int c = 0; c < CL; ++c) g[0] += sm.groups(c)[2 * lane], g[1] += sm.groups(c)[2 * lane + 1];
+        const Mass upto = scan_warp(g[0] + g[1]), total = __shfl_sync(0xffffffffu, upto, 31);
+        if (goal == 0) goal = max((Mass)1, (Mass)ceil((double)fmaxf(of_all, 0.f) * (double)total));
+        int bin = -1;
+        Mass ahead = 0;
+        if (goal <= total) {
+            const Mass before = upto - g[0] - g[1];
+            const bool here = before < goal && upto >= goal, second = before + g[0] < goal;
+            const int at = __ffs(__ballot_sync(0xffffffffu, here)) - 1;
+            const int group = 2 * at + __shfl_sync(0xffffffffu, (int)second, at);
+            ahead = __shfl_sync(0xffffffffu, second ? before + g[0] : before, at);
+            Mass v = 0;
+#pragma unroll 1
+            for (int c = 0; c < CL; c += 4) {
+                uint32_t high[4];
+                int low[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int from = min(c + k, CL - 1);
+                    high[k] = *cluster.map_shared_rank(&sm.high[group * 32 + lane], from), low[k] = *cluster.map_shared_rank(&sm.low[group * 32 + lane], from);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v += c + k < CL ? whole<kNucleus>(high[k], low[k]) : 0;
+            }
+            const Mass sum = ahead + scan_warp(v);
+            const int in = __ffs(__ballot_sync(0xffffffffu, sum >= goal)) - 1;   // (the group reaches the goal)
+            bin = group * 32 + in;
+            ahead = __shfl_sync(0xffffffffu, sum - v, in);
+        }
+        if (lane == 0) sm.found_bin = bin, sm.found_ahead = ahead, sm.found_goal = goal;
+    }
+    __syncthreads();
+    return {sm.found_bin, sm.found_goal, sm.found_ahead};
+}
+// All CTAs' lists behind this one's own, and sorted; their length (over kList: there is no list).  mine: what the CTA tells the others,
+// into of_cta[turn].  The lists have to stay until the cluster's next barrier.
+__device__ __noinline__ uint32_t collect(Smem &sm, int turn, Mass mine)
+{
+    const cg::cluster_group cluster = cg::this_cluster();
+    const int CL = cluster_size(), rank = cluster_rank(), tid = threadIdx.x;
+    mine = scan_block(sm, mine).total;
+    if (tid < 32) everywhere(&sm.count_of_cta[rank], sm.n_list), everywhere(&sm.of_cta[turn][rank], mine);
+    cluster.sync();
+    uint32_t n = 0;
+#pragma unroll 1
+    for (int c = 0; c < CL; ++c) n += sm.count_of_cta[c];
+    if (n > kList) {
+        cluster.sync();   // (the counts and the bins may be written again)
+        return n;
+    }
+    uint32_t at = sm.count_of_cta[rank];
+#pragma unroll 1
+    for (int k = 1; k < CL; ++k) {
+        const int c = rank + k < CL ? rank + k : rank + k - CL;
+#pragma unroll 1
+        for (uint32_t i = tid; i < sm.count_of_cta[c]; i += kThreads) sm.list[at + i] = *cluster.map_shared_rank(&sm.list[i], c);
+        at += sm.count_of_cta[c];
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (uint32_t i = tid; i < n; i += kThreads) {
+        const uint64_t me = sm.list[i];
+        int place = 0;
+#pragma unroll 4
+        for (uint32_t o = 0; o < n; ++o) place += sm.list[o] > me;
+        sm.sorted[place] = me;
+    }
+    __syncthreads();
+    return n;
+}
+
 template <bool kHalf>
 __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_constant__ Params p)
 {
@@ -138,9 +281,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int first = rank * p.part, n_here = min(p.part, p.V - first);   // entries of this CTA (possibly none), from `first` on
     const int words = p.part / kGrain, w0 = warp * (p.part / kWarps) + lane * 4;   // a lane's words of four entries: w0, w0 + 128, ...
-    const auto everywhere = [&](auto *at, auto v) {   // (one warp) the same word of every CTA's shared memory
-        if (lane < CL) *cluster.map_shared_rank(at, lane) = v;
-    };
     svk::grid_dependency_wait();
     svk::grid_launch_dependents();
 
@@ -163,6 +303,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         };
         const int n_wide = (reinterpret_cast<uintptr_t>(row) & 15) == 0 ? max(0, n_here) / 8 * 8 : 0;   // read 16 bytes at a time
         constexpr int kAhead = 4;
+#pragma unroll 1
         for (int base = 0; base < n_wide; base += kAhead * kThreads * (kHalf ? 8 : 4)) {
             uint4 v[kAhead];
 #pragma unroll
@@ -186,6 +327,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         }
         // what is left, an entry at a time; entries behind the end are not there
         constexpr int kSingles = 8;
+#pragma unroll 1
         for (int base = n_wide; base < p.part; base += kSingles * kThreads) {
             float v[kSingles];
 #pragma unroll
@@ -205,6 +347,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     }
     const float top_here = over_warp(most, [](float a, float b) { return fmaxf(a, b); });
     if (lane == 0) sm.of_warp[warp] = top_here;
+#pragma unroll 1
     for (int i = tid; i < kBins; i += kThreads) sm.high[i] = 0, sm.low[i] = 0;
     if (tid == 0) sm.n_list = 0;
     __syncthreads();
@@ -216,6 +359,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     const float peak = over_warp(sm.top_of_cta[lane < CL ? lane : 0], [](float a, float b) { return fmaxf(a, b); });
     if (peak == -INFINITY) {   // no entry
         if (p.probs)
+#pragma unroll 1
             for (int i = tid; i < n_here; i += kThreads) p.probs[(size_t)r * p.V + first + i] = 0.f;
         if (p.tokens && rank == 0 && tid == 0) p.tokens[r] = -1;
         return;
@@ -227,6 +371,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     const auto place_of = [&](float bits) { return __fadd_rn(fminf(__fmul_rn(bits, kBinsPerBit), (float)(kBins - 1)), kPlace); };
     const auto bin_at = [](float place) { return __float_as_uint(place) & (kBins - 1); };
     const auto each = [&](auto f) {   // f(index, logit), all entries of this lane in ascending order
+#pragma unroll 1
         for (int j = 0; j < words; ++j) {
             const int at = w0 + j * 128;
             const float4 v = *reinterpret_cast<const float4 *>(held + at);
@@ -234,78 +379,21 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         }
     };
 
-    // exclusive prefix and total over the CTA, in thread order
-    const auto scan_block = [&](Mass v, Mass &total) {
-        const Mass upto = scan_warp(v);
-        __syncthreads();
-        if (lane == 31) sm.scan[warp] = upto;
-        __syncthreads();
-        Mass before = upto - v;
-        total = 0;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            if (w < warp) before += sm.scan[w];
-            total += sm.scan[w];
-        }
-        return before;
-    };
-    int turn = 0;
-    // total over the cluster of a value of each thread; sums keeps the warps' totals, of_cta[turn] the CTAs'
-    const auto sum_cluster = [&](Mass v) {
-        turn ^= 1;
-        v = sum_over_warp(v);
-        __syncthreads();
-        if (lane == 0) sm.sums[warp] = v;
-        __syncthreads();
-        if (warp == 0) everywhere(&sm.of_cta[turn][rank], sum_over_warp(lane < kWarps ? sm.sums[lane] : 0));
-        cluster.sync();
-        return sum_over_warp(lane < CL ? sm.of_cta[turn][lane] : 0);
-    };
+    int turn = 0;   // of of_cta
+    Mass mine = 0;
+    const auto sum_cluster = [&](Mass v) { return sum_over_cluster(sm, turn ^= 1, v); };
     const auto before_warp = [&] {   // ... of the CTAs and warps before this one
         Mass before = 0;
+#pragma unroll 1
         for (int c = 0; c < rank; ++c) before += sm.of_cta[turn][c];
+#pragma unroll 1
         for (int w = 0; w < warp; ++w) before += sm.sums[w];
         return before;
     };
-    // The bin in which the sums over the cluster's histograms reach the goal, and what is in the bins ahead of it.  A CTA adds up its share of the
-    // bins of all CTAs; the CTA in whose share the goal lies finds the bin.  goal <= the sum of all.
-    const auto find_bin = [&](Mass goal, Mass &ahead) {
-        const int share = kBins / CL, per = (share + kThreads - 1) / kThreads;
-        cluster.sync();
-        Mass v[kBins / kThreads], mine = 0;
-#pragma unroll
-        for (int i = 0; i < kBins / kThreads; ++i) {
-            v[i] = 0;
-            const int b = tid * per + i;
-            if (i < per && b < share)
-                for (int c = 0; c < CL; ++c)
-                    v[i] += whole<kNucleus>(*cluster.map_shared_rank(&sm.high[rank * share + b], c), *cluster.map_shared_rank(&sm.low[rank * share + b], c));
-            mine += v[i];
-        }
-        Mass total;
-        Mass before = scan_block(mine, total);
-        turn ^= 1;
-        if (warp == 0) everywhere(&sm.of_cta[turn][rank], total);
-        cluster.sync();
-        for (int c = 0; c < rank; ++c) before += sm.of_cta[turn][c];
-        if (before < goal && before + mine >= goal) {
-            int b = 0;
-#pragma unroll
-            for (int i = 0; i < kBins / kThreads; ++i) {
-                if (before + v[i] >= goal) break;
-                before += v[i], ++b;
-            }
-            for (int c = 0; c < CL; ++c) {
-                *cluster.map_shared_rank(&sm.found_bin, c) = rank * share + tid * per + b;
-                *cluster.map_shared_rank(&sm.found_ahead, c) = before;
-            }
-        }
-        cluster.sync();
-        ahead = sm.found_ahead;
-        return sm.found_bin;
-    };
+    const auto find_bin = [&](Mass goal, float of_all) { return find_in_bins(sm, goal, of_all); };
     const auto clear = [&] {
         __syncthreads();
+#pragma unroll 1
         for (int i = tid; i < kBins; i += kThreads) sm.high[i] = 0, sm.low[i] = 0;
         if (tid == 0) sm.n_list = 0;
         __syncthreads();
@@ -320,44 +408,23 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
                 if (at < kList) sm.list[at] = (uint64_t)key_of(x) << 32 | (uint32_t)~i;
             }
         });
-        __syncthreads();
-        if (warp == 0) everywhere(&sm.count_of_cta[rank], sm.n_list);
-        cluster.sync();
-        uint32_t n = 0;
-        for (int c = 0; c < CL; ++c) n += sm.count_of_cta[c];
-        if (n > kList) {
-            cluster.sync();   // (the counts may be written again)
-        } else if (rank == 0) {
-            uint32_t at = sm.count_of_cta[0];
-            for (int c = 1; c < CL; ++c) {
-                for (uint32_t i = tid; i < sm.count_of_cta[c]; i += kThreads) sm.list[at + i] = *cluster.map_shared_rank(&sm.list[i], c);
-                at += sm.count_of_cta[c];
-            }
-            __syncthreads();
-            for (uint32_t i = tid; i < n; i += kThreads) {
-                const uint64_t me = sm.list[i];
-                int place = 0;
-                for (uint32_t o = 0; o < n; ++o) place += sm.list[o] > me;
-                sm.sorted()[place] = me;
-            }
-            __syncthreads();
-        }
-        return n;
+        return collect(sm, turn ^= 1, mine);
     };
 
     Boundary last{-FLT_MAX, 0xffffffffu};   // all of them
     const bool by_count = k > 0 && k < p.V, by_mass = top_p < 1.f;
     bool listed = false;   // the first CTA's sorted list begins with all entries that stay
     uint32_t n_listed = 0;
+    bool drawn = false;    // of_cta[turn] is what stays of the CTAs but for the list, and `sorted` up to `last` the rest, in masses of the nucleus
     for (int step = 0; step < 2 && !listed; ++step) {
         if (!(step ? by_mass : by_count)) continue;
-        Mass ahead;
+        Found found;
         if (step == 0) {
             // the k-th largest of the threads' maxima
             if (most > -INFINITY) add_one(bin_at(place_of(bits_of(most))));
-            const Mass maxima = sum_cluster(most > -INFINITY ? 1 : 0);
-            if (maxima >= (Mass)k) {
-                const float place = kPlace + find_bin((Mass)k, ahead);
+            found = find_bin((Mass)k, 0.f);
+            if (found.bin >= 0) {
+                const float place = kPlace + found.bin;
                 const uint32_t n = gather([&](float x, uint32_t) { return x > -INFINITY && place_of(bits_of(x)) <= place; });
                 if (n <= kList) {
                     listed = true, n_listed = n;
@@ -377,34 +444,39 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
             if (q.low) atomicAdd(&sm.low[bin], q.low);
         };
         // first histogram: by the distance from the maximum
-        clear();
-        Mass all = 0;
+        if (by_count) {   // (else it still is clear)
+            if (step || found.bin < 0) cluster.sync();   // the list of the first step, and the sums of its groups, have been read
+            clear();
+        }
         if (step == 0) {
             each([&](int, float x) {
-                if (x > -INFINITY) add_one(bin_at(place_of(bits_of(x)))), ++all;
+                if (x > -INFINITY) add_one(bin_at(place_of(bits_of(x))));
             });
         } else {
-            uint32_t high = 0;   // (a lane has at most 96 entries)
-            int low = 0;
-            each([&](int i, float x) {
-                if (!within.keeps(x, i)) return;
+            each([&](int i, float x) {   // (an entry that is not there has no mass)
+                if (by_count && !within.keeps(x, i)) return;
                 const float bits = bits_of(x);
-                const Parts q = parts_of<kNucleus>(svk::fast_exp2(-bits));
-                const uint32_t bin = bin_at(place_of(bits));
-                high += q.high, low += q.low;
-                if (q.high) atomicAdd(&sm.high[bin], q.high);
-                if (q.low) atomicAdd(&sm.low[bin], q.low);
+                add(bin_at(place_of(bits)), bits);
             });
-            all = whole<kNucleus>(high, low);
         }
-        all = sum_cluster(all);
-        const Mass goal = step ? max((Mass)1, (Mass)ceil((double)fmaxf(top_p, 0.f) * (double)all)) : (Mass)k;
-        if (goal > all) continue;   // (fewer entries than k)
-        const float place = kPlace + find_bin(goal, ahead);
+        found = find_bin(step ? 0 : (Mass)k, top_p);
+        if (found.bin < 0) continue;   // (fewer entries than k)
+        const Mass goal = found.goal;
+        Mass ahead = found.ahead;
+        const float place = kPlace + found.bin;
+        drawn = !by_count && min_e == 0.f;
+        if (drawn) {
+#pragma unroll
+            for (int i = 0; i < kBins / kThreads; ++i) {
+                const int b = i * kThreads + tid;
+                mine += b < found.bin ? whole<kNucleus>(sm.high[b], sm.low[b]) : 0;
+            }
+        }
         __syncthreads();
         if (tid == 0) sm.n_list = 0;
         __syncthreads();
         uint32_t n = gather([&](float x, uint32_t i) { return place_of(bits_of(x)) == place && within.keeps(x, i); });
+        drawn = drawn && n <= kList;
         // too many: the keys of the bin, then of a part of them, divided evenly
         uint32_t lo = 0, hi = 0;
         if (n > kList) {
@@ -432,8 +504,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
             each([&](int i, float x) {
                 if (in(x, i)) add((hi - key_of(x)) >> shift, bits_of(x));
             });
-            const int b = find_bin(goal - ahead, all);
-            ahead += all;
+            found = find_bin(goal - ahead, 0.f);
+            const int b = found.bin;
+            ahead += found.ahead;
             const uint32_t below = (uint32_t)(((Mass)(b + 1) << shift) - 1);
             lo = hi - lo < below ? lo : hi - below, hi -= (uint32_t)b << shift;
             __syncthreads();
@@ -441,22 +514,24 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
             __syncthreads();
             n = gather(in);
         }
-        const auto found = [&](float x, uint32_t i) {
+        const auto is_last = [&](float x, uint32_t i) {
+#pragma unroll 1
             for (int c = 0; c < CL; ++c) *cluster.map_shared_rank(&sm.boundary, c) = Boundary{x, i};
         };
-        if (n <= kList) {   // ranked by the first CTA
-            if (rank == 0) {
-                Mass sum = ahead;
-                for (uint32_t base = 0; base < n; base += kThreads) {
-                    const bool in = base + tid < n;
-                    const uint64_t me = in ? sm.sorted()[base + tid] : 0;
-                    const Mass w = in ? weight(logit_of((uint32_t)(me >> 32))) : 0;
-                    Mass total;
-                    const Mass before = sum + scan_block(w, total);
-                    if (in && before < goal && before + w >= goal) found(logit_of((uint32_t)(me >> 32)), ~(uint32_t)me);
-                    sum += total;
-                }
+        if (n <= kList) {   // by the sorted list, which every CTA has
+            Mass sum = ahead;
+#pragma unroll 1
+            for (uint32_t base = 0; base < n; base += kThreads) {
+                const bool in = base + tid < n;
+                const uint64_t me = in ? sm.sorted[base + tid] : 0;
+                const Mass w = in ? weight(logit_of((uint32_t)(me >> 32))) : 0;
+                const Scan scan = scan_block(sm, w);
+                const Mass before = sum + scan.before;
+                if (in && before < goal && before + w >= goal) sm.boundary = Boundary{logit_of((uint32_t)(me >> 32)), ~(uint32_t)me};
+                sum += scan.total;
             }
+            n_listed = n;
+            __syncthreads();
         } else {   // all equal: counted off in the order of the vocabulary
             const float x_all = logit_of(hi);
             const Mass one = weight(x_all), nth = (goal - ahead + one - 1) / one;   // the nth of them (from 1) is the last
@@ -464,6 +539,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
             each([&](int i, float x) { mine += x == x_all && within.keeps(x, i); });
             (void)sum_cluster(mine);
             Mass before = before_warp();
+#pragma unroll 1
             for (int j = 0; j < words && before < nth; ++j) {   // (uniform over a warp)
                 const int at = w0 + j * 128;
                 const float4 v = *reinterpret_cast<const float4 *>(held + at);
@@ -475,114 +551,151 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
                 Mass place_in = before + upto - m;
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (x[e] == x_all && within.keeps(x[e], first + at + e) && ++place_in == nth) found(x_all, first + at + e);
+                    if (x[e] == x_all && within.keeps(x[e], first + at + e) && ++place_in == nth) is_last(x_all, first + at + e);
                 before += __shfl_sync(0xffffffffu, upto, 31);
             }
+            cluster.sync();
         }
-        cluster.sync();
         last = sm.boundary;
     }
+    if (listed || drawn) svk::cluster_arrive();   // nobody leaves while another CTA reads its list
 
     Mass total;   // of the draw
+    float scale = 1099511627776.f;   // ... and what the largest entry counts
     if (listed) {
-        if (rank == 0) {
-            // of the sorted list: the first k, their nucleus, those that are likely enough; at most two entries a thread
-            uint64_t *const sorted = sm.sorted();
-            const uint32_t n_k = min(n_listed, (uint32_t)k);
-            float e[kList / kThreads];
-            Mass ahead[kList / kThreads], all = 0;
+        // of the sorted list: the first k, their nucleus, those that are likely enough; at most two entries a thread
+        const uint32_t n_k = min(n_listed, (uint32_t)k);
+        float e[kEach];
+        Mass ahead[kEach], all = 0;
 #pragma unroll
-            for (int i = 0; i < kList / kThreads; ++i) {
-                const uint32_t at = i * kThreads + tid;
-                e[i] = at < n_k ? e_of(logit_of((uint32_t)(sorted[at] >> 32))) : 0.f;
-                Mass sum;
-                ahead[i] = all + scan_block(mass_of<kNucleus>(e[i]), sum);
-                all += sum;
-            }
-            const Mass goal = by_mass ? max((Mass)1, (Mass)ceil((double)fmaxf(top_p, 0.f) * (double)all)) : all + 1;
-            uint32_t n_keep = 0;
+        for (int i = 0; i < kEach; ++i) {
+            const uint32_t at = i * kThreads + tid;
+            e[i] = at < n_k ? e_of(logit_of((uint32_t)(sm.sorted[at] >> 32))) : 0.f;
+            const Scan scan = scan_block(sm, mass_of<kNucleus>(e[i]));
+            ahead[i] = all + scan.before;
+            all += scan.total;
+        }
+        const Mass goal = by_mass ? max((Mass)1, (Mass)ceil((double)fmaxf(top_p, 0.f) * (double)all)) : all + 1;
+        uint32_t n_keep = 0;
+        Mass kept = 0;
 #pragma unroll
-            for (int i = 0; i < kList / kThreads; ++i) {
-                const uint32_t at = i * kThreads + tid;
-                n_keep += __syncthreads_count(at < n_k && (at == 0 || (ahead[i] < goal && (e[i] >= min_e || logit_of((uint32_t)(sorted[at] >> 32)) == peak))));
-            }
-            Mass kept = 0;
+        for (int i = 0; i < kEach; ++i) {
+            const uint32_t at = i * kThreads + tid;
+            const bool keep = at < n_k && (at == 0 || (ahead[i] < goal && (e[i] >= min_e || logit_of((uint32_t)(sm.sorted[at] >> 32)) == peak)));
+            n_keep += __syncthreads_count(keep);
+            kept += keep ? mass_of<kDraw>(e[i]) : 0;
+        }
+        total = scan_block(sm, kept).total;
+        const uint64_t final_entry = sm.sorted[n_keep - 1];
+        last = {logit_of((uint32_t)(final_entry >> 32)), ~(uint32_t)final_entry}, min_e = 0.f;
+        if (p.tokens && rank == 0) {   // the first entry in the order of the vocabulary up to which the masses reach the target
+            const Mass target = max((Mass)1, min(total, (Mass)ceil((double)u * (double)total)));
+            Mass *const of = sm.masses();
+            if (tid == 0) sm.token = 0x7fffffff;
 #pragma unroll
-            for (int i = 0; i < kList / kThreads; ++i) kept += i * kThreads + tid < n_keep ? mass_of<kDraw>(e[i]) : 0;
-            (void)scan_block(kept, total);
-            if (tid == 0) {
-                const uint64_t at = sorted[n_keep - 1];
-                for (int c = 0; c < CL; ++c) {
-                    *cluster.map_shared_rank(&sm.boundary, c) = Boundary{logit_of((uint32_t)(at >> 32)), ~(uint32_t)at};
-                    *cluster.map_shared_rank(&sm.found_ahead, c) = total;
-                }
-                sm.token = 0x7fffffff;
+            for (int i = 0; i < kEach; ++i)
+                if (i * kThreads + tid < n_keep) of[i * kThreads + tid] = mass_of<kDraw>(e[i]);
+            __syncthreads();
+#pragma unroll 1
+            for (uint32_t i = tid; i < n_keep; i += kThreads) {
+                const uint32_t me = (uint32_t)sm.sorted[i];   // (complement of the index)
+                Mass upto = 0;
+#pragma unroll 2
+                for (uint32_t o = 0; o < n_keep; ++o) upto += (uint32_t)sm.sorted[o] >= me ? of[o] : 0;
+                if (of[i] && upto >= target) atomicMin(&sm.token, (int)~me);
             }
             __syncthreads();
-            if (p.tokens) {   // the first entry in the order of the vocabulary up to which the masses reach the target
-                const Mass target = max((Mass)1, min(total, (Mass)ceil((double)u * (double)total)));
-                Mass *const of = sm.masses();
-#pragma unroll
-                for (int i = 0; i < kList / kThreads; ++i)
-                    if (i * kThreads + tid < n_keep) of[i * kThreads + tid] = mass_of<kDraw>(e[i]);
-                __syncthreads();
-                for (uint32_t i = tid; i < n_keep; i += kThreads) {
-                    const uint32_t me = (uint32_t)sorted[i];   // (complement of the index)
-                    Mass upto = 0;
-                    for (uint32_t o = 0; o < n_keep; ++o) upto += (uint32_t)sorted[o] >= me ? of[o] : 0;
-                    if (of[i] && upto >= target) atomicMin(&sm.token, (int)~me);
-                }
-                __syncthreads();
-                if (tid == 0) p.tokens[r] = sm.token;
-            }
+            if (tid == 0) p.tokens[r] = sm.token;
         }
-        cluster.sync();   // (nobody leaves while the first CTA reads its list)
-        if (!p.probs) return;
-        last = sm.boundary, total = sm.found_ahead, min_e = 0.f;
     } else {
-        // the mass that stays, by CTA and warp
-        const auto mass = [&](float x, uint32_t i) {
-            if (!last.keeps(x, i)) return Parts{0u, 0};
+        // the mass that stays, by CTA; of the CTA in which the target lies by warp, word and entry
+        const auto mass = [&](float x, uint32_t i) -> Mass {
+            if (!last.keeps(x, i)) return 0;
             const float e = e_of(x);
-            return e >= min_e || x == peak ? parts_of<kDraw>(e) : Parts{0u, 0};
+            if (!(e >= min_e || x == peak)) return 0;
+            return drawn ? mass_of<kNucleus>(e) : mass_of<kDraw>(e);
         };
-        uint32_t high = 0;   // (a lane has at most 96 entries)
-        int low = 0;
-        each([&](int i, float x) {
-            const Parts q = mass(x, i);
-            high += q.high, low += q.low;
-        });
-        total = sum_cluster(whole<kDraw>(high, low));
+        if (!drawn) {
+            uint32_t high = 0;   // (a lane has at most 96 entries)
+            int low = 0;
+            each([&](int i, float x) {
+                if (!last.keeps(x, i)) return;
+                const float e = e_of(x);
+                if (!(e >= min_e || x == peak)) return;
+                const Parts q = parts_of<kDraw>(e);
+                high += q.high, low += q.low;
+            });
+            mine = whole<kDraw>(high, low);
+        }
+        scale = drawn ? 4294967296.f : 1099511627776.f;
+        Mass before = 0, here;
+        if (drawn) {   // a warp for each CTA adds up what the list has of it
+            if (warp < CL) {
+                Mass m = 0;
+#pragma unroll 1
+                for (uint32_t i = lane; i < n_listed; i += 32) {
+                    const uint64_t entry = sm.sorted[i];
+                    const uint32_t index = ~(uint32_t)entry;
+                    if ((int)(index / (uint32_t)p.part) == warp) m += mass(logit_of((uint32_t)(entry >> 32)), index);
+                }
+                m = sum_over_warp(m);
+                if (lane == 0) sm.sums[warp] = sm.of_cta[turn][warp] + m;
+            }
+            __syncthreads();
+            total = 0;
+#pragma unroll 1
+            for (int c = 0; c < CL; ++c) {
+                if (c < rank) before += sm.sums[c];
+                total += sm.sums[c];
+            }
+            here = sm.sums[rank];
+            __syncthreads();
+        } else {
+            total = sum_cluster(mine);
+#pragma unroll 1
+            for (int c = 0; c < rank; ++c) before += sm.of_cta[turn][c];
+            here = sm.of_cta[turn][rank];
+        }
         if (p.tokens) {
             const Mass target = max((Mass)1, min(total, (Mass)ceil((double)u * (double)total)));
-            Mass before = before_warp();
-            if (before < target && before + sm.sums[warp] >= target) {   // this warp has it
-                for (int j = 0; j < words && before < target; ++j) {
-                    const int at = w0 + j * 128;
-                    const float4 v = *reinterpret_cast<const float4 *>(held + at);
-                    const float x[4] = {v.x, v.y, v.z, v.w};
-                    Mass w[4], m = 0;
+            if (before < target && before + here >= target) {
+                if (drawn) {
+                    mine = 0;
+                    each([&](int i, float x) { mine += mass(x, i); });
+                    mine = sum_over_warp(mine);
+                    if (lane == 0) sm.sums[warp] = mine;
+                    __syncthreads();
+                }
+#pragma unroll 1
+                for (int w = 0; w < warp; ++w) before += sm.sums[w];
+                if (before < target && before + sm.sums[warp] >= target) {   // this warp has it
+#pragma unroll 1
+                    for (int j = 0; j < words && before < target; ++j) {
+                        const int at = w0 + j * 128;
+                        const float4 v = *reinterpret_cast<const float4 *>(held + at);
+                        const float x[4] = {v.x, v.y, v.z, v.w};
+                        Mass w[4], m = 0;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const Parts q = mass(x[e], first + at + e);
-                        w[e] = whole<kDraw>(q.high, q.low);
-                        m += w[e];
-                    }
-                    const Mass upto = scan_warp(m);
-                    Mass sum = before + upto - m;
+                        for (int e = 0; e < 4; ++e) w[e] = mass(x[e], first + at + e), m += w[e];
+                        const Mass upto = scan_warp(m);
+                        Mass sum = before + upto - m;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (sum < target && sum + w[e] >= target) p.tokens[r] = first + at + e;
-                        sum += w[e];
+                        for (int e = 0; e < 4; ++e) {
+                            if (sum < target && sum + w[e] >= target) p.tokens[r] = first + at + e;
+                            sum += w[e];
+                        }
+                        before += __shfl_sync(0xffffffffu, upto, 31);
                     }
-                    before += __shfl_sync(0xffffffffu, upto, 31);
                 }
             }
         }
-        if (!p.probs) return;
     }
 
-    const float inv = 1099511627776.f / (float)total;
+    if (!p.probs) {
+        if (listed || drawn) svk::cluster_wait();
+        return;
+    }
+    const float inv = scale / (float)total;
     const auto prob = [&](float x, uint32_t i) {
         if (!last.keeps(x, i)) return 0.f;
         const float e = e_of(x);
@@ -597,6 +710,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     }
 #pragma unroll 4
     for (int at = n_wide + tid; at < n_here; at += kThreads) to[at] = prob(held[at], first + at);
+    if (listed || drawn) svk::cluster_wait();
 }
 
 int part_for(int vocab, int cluster) { return ((vocab + cluster - 1) / cluster + kGrain - 1) / kGrain * kGrain; }

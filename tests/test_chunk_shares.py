@@ -13,6 +13,7 @@ CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
 SOURCE = r'''
 #include "chunk_shares.h"
 using namespace svk;
+extern "C" int item_cost() { return kItemCost; }
 extern "C" int shares_of(const int32_t *q_start, const int32_t *lens, int S, int N, int Hkv, int TT, long long cap, int ctas, int cta, int32_t *out, int room)
 {
     const ChunkBatch b{q_start, lens, S, N, Hkv, TT, cap};
@@ -70,7 +71,7 @@ def _check(lib, lens, new, Hkv, G, cap, ctas):
             begun += u0 > 0
             going += u0 == 0 and u1 < units
             # on the line a whole item is up to 128 keys shorter than its units, and what is ahead of a cut has paid the item's cost
-            work[-1] += max(0, (u1 - u0) * 128 - 128)
+            work[-1] += (2 if tokens > TT else 1) * max(0, (u1 - u0) * 128 - 128)
         assert begun <= 1 and going <= 1
     # every token of every head, every unit once
     for s in range(S):
@@ -108,7 +109,8 @@ def test_drawn_batches(lib):
 
 def test_shares_are_even(lib):
     """No CTA has more than the line's length / CTAs, but for the rounding to units that _check has taken off."""
+    item_cost = lib.item_cost()
     for lens, new, Hkv, G in (([8192], [8192], 8, 4), ([9000, 300, 16000, 5], [1, 1, 1, 1], 8, 4), ([3000, 5000, 100], [700, 1, 100], 4, 7)):
         TT = 128 // G
-        line = Hkv * sum(L - n + min(n, t + 2 * TT) + 192 for L, n in zip(lens, new) for t in range(0, n, 2 * TT))
+        line = Hkv * sum((2 if n - t > TT else 1) * (L - n + min(n, t + 2 * TT)) + item_cost for L, n in zip(lens, new) for t in range(0, n, 2 * TT))
         assert max(_check(lib, lens, new, Hkv, G, 1 << 20, 148)) <= line / 148 + 1
