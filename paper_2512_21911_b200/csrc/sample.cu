@@ -242,20 +242,24 @@ __device__ __noinline__ uint32_t collect(Smem &sm, int turn, Mass mine)
     mine = scan_block(sm, mine).total;
     if (tid < 32) everywhere(&sm.count_of_cta[rank], sm.n_list), everywhere(&sm.of_cta[turn][rank], mine);
     cluster.sync();
-    uint32_t n = 0;
+    // 64 threads for every CTA's list, all of them at once: behind this CTA's own, in the order of the CTAs
+    constexpr int kPull = kThreads / kMaxCluster;
+    const int from = tid / kPull;
+    uint32_t n = 0, at = 0;
 #pragma unroll 1
-    for (int c = 0; c < CL; ++c) n += sm.count_of_cta[c];
+    for (int c = 0; c < CL; ++c) {
+        if (c == from) at = n;
+        n += sm.count_of_cta[c];
+    }
     if (n > kList) {
         cluster.sync();   // (the counts and the bins may be written again)
         return n;
     }
-    uint32_t at = sm.count_of_cta[rank];
+    if (from < CL && from != rank) {
+        const uint32_t count = sm.count_of_cta[from];
+        if (from < rank) at += sm.count_of_cta[rank];
 #pragma unroll 1
-    for (int k = 1; k < CL; ++k) {
-        const int c = rank + k < CL ? rank + k : rank + k - CL;
-#pragma unroll 1
-        for (uint32_t i = tid; i < sm.count_of_cta[c]; i += kThreads) sm.list[at + i] = *cluster.map_shared_rank(&sm.list[i], c);
-        at += sm.count_of_cta[c];
+        for (uint32_t i = tid % kPull; i < count; i += kPull) sm.list[at + i] = *cluster.map_shared_rank(&sm.list[i], from);
     }
     __syncthreads();
 #pragma unroll 1
@@ -660,9 +664,13 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
             const Mass target = max((Mass)1, min(total, (Mass)ceil((double)u * (double)total)));
             if (before < target && before + here >= target) {
                 if (drawn) {
-                    mine = 0;
-                    each([&](int i, float x) { mine += mass(x, i); });
-                    mine = sum_over_warp(mine);
+                    uint32_t high = 0;
+                    int low = 0;
+                    each([&](int i, float x) {
+                        const Parts q = last.keeps(x, i) ? parts_of<kNucleus>(e_of(x)) : Parts{0u, 0};
+                        high += q.high, low += q.low;
+                    });
+                    mine = sum_over_warp(whole<kNucleus>(high, low));
                     if (lane == 0) sm.sums[warp] = mine;
                     __syncthreads();
                 }
