@@ -1,5 +1,8 @@
 """SparseVerifier: runs block selection and sparse verification attention for a stack of layers.
 
+Around the verification steps of a sequence, ``prefill_layer`` / ``end_prefill`` bring its prompt into the cache and
+``draw`` makes distributions and tokens of logits.
+
 A thin driver over the C-ABI calls: it owns the per-layer representatives, the block lists,
 the split-KV workspace and the outputs.  ``verify_layer`` enqueues one layer: ``sv_select_blocks`` (anchor
 layers) or the reuse of the previous layer's list (Eq. 9), then ``sv_verify_attn``.  ``verify_step`` is handed the inputs
@@ -107,6 +110,10 @@ class SparseVerifier:
         self._stack_bytes = [sv._native.workspace_bytes_host_step(self.geom, n_layers, max_sel) if stackable else 0, need[1]]
         self._stack_workspace = [torch.zeros(n, dtype=torch.uint8, device=dev) if k else None for n, k in zip(self._stack_bytes, keeps)]
 
+        self._grown = torch.zeros(n_seq, dtype=torch.int32, device=dev)   # lengths with the new tokens, between prefill_layer and end_prefill
+        self._grown_kv: List[Optional[sv.sv_kv]] = [None] * n_layers
+        self._turned = self._chunk_workspace = None
+
     def _make_lists(self, flags: bytes, dev) -> None:
         """One block list per anchor layer; sel_idx / sel_cnt is the last one, which is also what verify_layer keeps its
         current list in."""
@@ -120,6 +127,7 @@ class SparseVerifier:
         new = self.kv[layer] is None
         self._pools[layer] = (k_pool, v_pool)
         self.kv[layer] = sv.make_kv(k_pool, v_pool, self.block_table, self.seq_lens)
+        self._grown_kv[layer] = sv.make_kv(k_pool, v_pool, self.block_table, self._grown)
         if self._table is not None:
             row = sv._native.layer_row(self.geom, self.kv[layer])
             if isinstance(row, int):
@@ -313,6 +321,37 @@ class SparseVerifier:
             return False
         sv._check(st, "sv_verify_step_from_host")
         return True
+
+    def prefill_layer(self, layer: int, q, k, v, q_start, out, rope=None, interleaved: bool = False, lse=None) -> None:
+        """New tokens of the sequences (prompts, chunks of them, single tokens; rows q_start[s] .. q_start[s + 1] - 1 are sequence
+        s's) in one layer: rotary positions on q and k, k and v into the cache behind its seq_lens tokens, the representatives of
+        the grown blocks, and causal attention of the new tokens over everything up to them.  q, out [N][Hq][D], k, v [N][Hkv][D],
+        tokens of q, k and v any distance apart (sv_rope_append, sv_chunk_attn).  The block table must hold pages for the blocks that
+        are entered.  Every layer sees the old lengths; end_prefill advances them when all layers are through."""
+        n = int(k.shape[0])
+        if self._turned is None or self._turned.shape[0] < n:
+            self._turned = torch.empty((n, self.geom.n_q_heads, self.geom.head_dim), dtype=torch.bfloat16, device=k.device)
+        need = max(16, sv.sv_chunk_workspace_bytes(self.geom, n))
+        if self._chunk_workspace is None or self._chunk_workspace.numel() < need:
+            self._chunk_workspace = torch.empty(need, dtype=torch.uint8, device=k.device)
+        k_pool, v_pool = self._pools[layer]
+        turned = self._turned[:n]
+        sv.sv_rope_append(self.geom, k_pool, v_pool, self.block_table, self.seq_lens, q, k, v, q_start, turned, self._grown, rope=rope,
+                          interleaved=interleaved, reps=self.reps[layer], status_word=self.status)
+        sv.sv_chunk_attn(self.geom, turned, self._grown_kv[layer], q_start, out, lse=lse, workspace=self._chunk_workspace,
+                         status_word=self.status)
+
+    def end_prefill(self) -> None:
+        """The lengths with the tokens that prefill_layer has written become the cache's."""
+        self.seq_lens.copy_(self._grown)
+
+    def draw(self, logits, u, distributions: bool = True, **parameters):
+        """Distributions (what accept takes) and tokens of rows of logits [S][T][V] or [R][V]: (probs, tokens), probs None unless they
+        are wanted.  u [R]: uniform numbers; parameters: temperature, top_k, top_p, min_p of sv_sample, one entry a sequence."""
+        probs = torch.empty(logits.shape, dtype=torch.float32, device=logits.device) if distributions else None
+        tokens = torch.empty(logits.shape[:-1], dtype=torch.int32, device=logits.device)
+        sv.sv_sample(logits, u, tokens, probs=probs, **parameters)
+        return probs, tokens
 
     def accept(self, p_target, p_draft, tokens, u_accept, u_next):
         """Acceptance of the step's draft tokens (Eq. 2-3).  Returns (path [S][T], n_path [S], next_token [S]):
