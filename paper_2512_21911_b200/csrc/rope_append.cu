@@ -2,15 +2,19 @@
 // the blocks that grew (the mean key of a block, Eq. 5) -- what happens to a projection's output before anything attends over it.
 //
 // Mathematics: a pair (a, b) of a head's dims at position p becomes (a cos - b sin, b cos + a sin), cos and sin from a table.  Bound by
-// HBM: (Hq + 2 Hkv) * 256 bytes read and written per token, a table row of 512 bytes shared by all heads, no reuse.
+// HBM: (Hq + 2 Hkv) * 256 bytes read and written per token, a table row of 512 bytes shared by all heads, no reuse.  A prompt of 32,768
+// tokens with 32 query and 8 KV heads moves 826 MB in 158 us, 5.2 TB/s, 80 % of a plain copy's rate; a token for each of 64 sequences
+// takes 7.1 us, three dependent loads (starts, length and table, rows) behind a launch.
 //
 // One launch of two kinds of CTAs.  The first take a block of a sequence and a KV head: 16 threads hold a 256-byte row, so that the
 // partner of a dim is in the same thread (neighbours) or 2 to 8 lanes away (halves), the rows of the block go to its page, and the mean
-// of the keys, rounded as they are stored, is summed in the order of sv_block_reps.  The others take kQTokens tokens and all their query heads;
-// a thread keeps its part of a token's table row for all its heads.  The batch is ragged and its lengths are only on the device: the
-// blocks that sequence s enters are at most n / B + 2, so that numbering them from q_start[s] / B + 2 s gives every sequence room of its
-// own, and a CTA finds its sequence by counting the starts up to its number instead of by a prefix sum.
+// of the keys, rounded as they are stored, is summed in the order of sv_block_reps.  The others take a few tokens and all their query
+// heads.  The batch is ragged and its lengths are only on the device: the blocks that sequence s enters are at most n / B + 2, so that
+// numbering them from q_start[s] / B + 2 s gives every sequence room of its own, and a CTA finds its sequence by counting the starts up to
+// its number instead of by a prefix sum.
 #include <cuda_bf16.h>
+
+#include <type_traits>
 
 #include "attn_common.cuh"
 #include "sv_host.h"
@@ -20,7 +24,11 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kRowGroups = kThreads / 16;
-constexpr int kQTokens = 4;   // tokens of a CTA that rotates queries
+// Tokens of a CTA that rotates queries: two in calls of up to kFew tokens, where the query CTAs of many would not fill the machine and a
+// CTA's own chain of loads is what counts; many beyond, where reading the batch's starts and lengths is shared by more rows.  32 (28)
+// query heads: 64 tokens take 7.1 us with two and 8.1 us with four; 3,512 take 12.8 us with two and 12.0 us with eight; 32,768 take
+// 193 us with two, 167 us with four and 158 us with eight (156 us with sixteen, which cost the 3,512 0.6 us).
+constexpr int kFew = 1024, kTokensOfFew = 2, kTokensOfMany = 8;
 
 struct Params {
     uint4 *k_pool, *v_pool;
@@ -196,8 +204,9 @@ __device__ __forceinline__ void append_block(const Params &p, int slot, int h)
     }
 }
 
-// Query heads of kQTokens tokens: four groups of 16 threads per token, each with every fourth head.
-template <bool kNeighbours>
+// Query heads of kQTokens tokens: a token's heads are dealt to kStep groups of 16 threads; a thread has kAhead of them on their way at
+// once and keeps its part of the token's table row for all of them.
+template <bool kNeighbours, int kQTokens>
 __device__ __forceinline__ void turn_queries(const Params &p, int tile)
 {
     const int c = threadIdx.x & 15, rg = threadIdx.x >> 4;
@@ -212,28 +221,30 @@ __device__ __forceinline__ void turn_queries(const Params &p, int tile)
         if (at != pos && p.status) atomicOr(p.status, svk::kStatusIndex);
         if (8 * c < p.rot) turn = load_turn<kNeighbours>(p.rope + (size_t)at * p.rot, c, p.rot);
     }
-    constexpr int kAhead = 4;
-    for (int h0 = rg / kQTokens; h0 < p.Hq; h0 += 4 * kAhead) {   // (uniform over a warp: rotate exchanges between lanes)
+    constexpr int kStep = kRowGroups / kQTokens, kAhead = kQTokens == kTokensOfFew ? 4 : 8;
+    for (int h0 = rg / kQTokens; h0 < p.Hq; h0 += kStep * kAhead) {   // (uniform over a warp: rotate exchanges between lanes)
         uint4 x[kAhead];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i)
-            x[i] = mine && h0 + 4 * i < p.Hq ? p.q[token * p.q_stride + (h0 + 4 * i) * 16 + c] : make_uint4(0u, 0u, 0u, 0u);
+            x[i] = mine && h0 + kStep * i < p.Hq ? p.q[token * p.q_stride + (h0 + kStep * i) * 16 + c] : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             if (p.rope) x[i] = rotate<kNeighbours>(x[i], turn, c, p.rot);
-            if (mine && h0 + 4 * i < p.Hq) p.q_out[((size_t)token * p.Hq + h0 + 4 * i) * 16 + c] = x[i];
+            if (mine && h0 + kStep * i < p.Hq) p.q_out[((size_t)token * p.Hq + h0 + kStep * i) * 16 + c] = x[i];
         }
     }
 }
 
-template <int B, bool kNeighbours>
-__global__ void __launch_bounds__(kThreads) rope_append_kernel(const Params p)
+// Three CTAs an SM (80 registers): without the bound it takes 128, two CTAs an SM, and the 3,512 tokens 12.8 us; four CTAs (64 registers)
+// take 17 us for them, since the rows of a cache block then no longer all start to load at once.
+template <int B, bool kNeighbours, int kQTokens>
+__global__ void __launch_bounds__(kThreads, 3) rope_append_kernel(const Params p)
 {
     svk::grid_dependency_wait();
     svk::grid_launch_dependents();
     const int i = blockIdx.x, cache = p.slots * p.Hkv;
     if (i < cache) append_block<B, kNeighbours>(p, i / p.Hkv, i % p.Hkv);
-    else turn_queries<kNeighbours>(p, i - cache);
+    else turn_queries<kNeighbours, kQTokens>(p, i - cache);
 }
 
 }  // namespace
@@ -270,7 +281,8 @@ extern "C" sv_status sv_rope_append(const sv_geom *geom, void *k_pool, void *v_p
     p.S = geom->n_seq, p.N = n_tokens, p.Hq = Hq, p.Hkv = Hkv, p.NBmax = geom->max_blocks, p.n_pages = n_pages;
     p.rope_rows = rope_rows, p.rot = rot_dim;
     const long long slots = (long long)n_tokens / B + 2ll * geom->n_seq;
-    const long long ctas = slots * Hkv + (q ? ((long long)n_tokens + kQTokens - 1) / kQTokens : 0);
+    const int tokens = n_tokens <= kFew ? kTokensOfFew : kTokensOfMany;
+    const long long ctas = slots * Hkv + (q ? ((long long)n_tokens + tokens - 1) / tokens : 0);
     if (ctas > 0x7fffffff) return SV_ERR_SHAPE;
     p.slots = (int)slots;
     cudaLaunchConfig_t cfg = {};
@@ -281,7 +293,11 @@ extern "C" sv_status sv_rope_append(const sv_geom *geom, void *k_pool, void *v_p
     svh::pdl_attribute(attr);
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    const auto kernel = B == 64 ? interleaved ? rope_append_kernel<64, true> : rope_append_kernel<64, false>
-                                : interleaved ? rope_append_kernel<128, true> : rope_append_kernel<128, false>;
+    const auto pick = [&](auto block, auto turned) {
+        return tokens == kTokensOfFew ? rope_append_kernel<decltype(block)::value, decltype(turned)::value, kTokensOfFew>
+                             : rope_append_kernel<decltype(block)::value, decltype(turned)::value, kTokensOfMany>;
+    };
+    const auto by_order = [&](auto block) { return interleaved ? pick(block, std::true_type{}) : pick(block, std::false_type{}); };
+    const auto kernel = B == 64 ? by_order(std::integral_constant<int, 64>{}) : by_order(std::integral_constant<int, 128>{});
     return cudaLaunchKernelEx(&cfg, kernel, p) == cudaSuccess ? svh::launch_status() : SV_ERR_CUDA;
 }
