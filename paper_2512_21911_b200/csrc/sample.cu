@@ -19,6 +19,7 @@
 #include <float.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "sv_host.h"
 #include "sv_ptx.cuh"
@@ -36,7 +37,7 @@ constexpr float kBinsPerBit = 2048.f / 36.f;   // bins of the first histogram: 3
 constexpr int kList = 768;                     // entries that are ranked one against another
 constexpr int kGrain = kWarps * 128;           // a CTA's part of a row is a multiple of this: 32 lanes x 4 entries for each warp
 constexpr int kMostPart = 24 * kGrain;         // entries that fit in shared memory
-constexpr int kPart = 8 * kGrain;              // ... and leave room for a second CTA on the SM
+constexpr int kTwo = 80 * 1024;                // bytes of a part that leave room for a second CTA on the SM
 constexpr int kMaxVocab = kMaxCluster * kMostPart;
 static_assert((1ll << 16) * kMostPart < 1ll << 32 && (1ll << 15) * kMostPart < 1ll << 31, "words of a bin");
 
@@ -279,7 +280,19 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
 {
     extern __shared__ __align__(16) uint8_t raw[];
     Smem &sm = *reinterpret_cast<Smem *>(raw);
-    float *const held = reinterpret_cast<float *>(raw + sizeof(Smem));
+    // the CTA's part of the row as it is read, but for NaNs
+    using Held = std::conditional_t<kHalf, __nv_bfloat16, float>;
+    Held *const held = reinterpret_cast<Held *>(raw + sizeof(Smem));
+    const auto held1 = [&](int at) { return taken((float)held[at]); };
+    const auto held4 = [&](int at) {
+        if constexpr (kHalf) {
+            const uint2 w = *reinterpret_cast<const uint2 *>(held + at);
+            return make_float4(fminf(__uint_as_float(w.x << 16), FLT_MAX), fminf(__uint_as_float(w.x & 0xffff0000u), FLT_MAX),
+                               fminf(__uint_as_float(w.y << 16), FLT_MAX), fminf(__uint_as_float(w.y & 0xffff0000u), FLT_MAX));
+        } else {
+            return *reinterpret_cast<const float4 *>(held + at);
+        }
+    };
     const cg::cluster_group cluster = cg::this_cluster();
     const int CL = (int)cluster.num_blocks(), rank = (int)cluster.block_rank(), r = blockIdx.x / CL, g = r / p.rows_per_param;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -299,55 +312,58 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     // the row, its maximum, and the maximum of the entries that this thread has read
     float most = -INFINITY;
     {
-        const char *row = static_cast<const char *>(p.logits) + (r * p.stride + first) * (kHalf ? 2 : 4);
-        const auto keep4 = [&](int at, float4 v) {
-            v = make_float4(taken(v.x), taken(v.y), taken(v.z), taken(v.w));
-            *reinterpret_cast<float4 *>(held + at) = v;
-            most = fmaxf(most, fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)));
-        };
-        const int n_wide = (reinterpret_cast<uintptr_t>(row) & 15) == 0 ? max(0, n_here) / 8 * 8 : 0;   // read 16 bytes at a time
-        constexpr int kAhead = 4;
+        const Held *const row = static_cast<const Held *>(p.logits) + r * p.stride + first;
+        constexpr int kWide = 16 / sizeof(Held), kAhead = 4;
+        const int n_wide = (reinterpret_cast<uintptr_t>(row) & 15) == 0 ? max(0, n_here) / kWide * kWide : 0;   // read 16 bytes at a time
 #pragma unroll 1
-        for (int base = 0; base < n_wide; base += kAhead * kThreads * (kHalf ? 8 : 4)) {
+        for (int base = 0; base < n_wide; base += kAhead * kThreads * kWide) {
             uint4 v[kAhead];
 #pragma unroll
             for (int a = 0; a < kAhead; ++a) {
-                const int at = base + (a * kThreads + tid) * (kHalf ? 8 : 4);
-                if (at < n_wide) v[a] = __ldg(reinterpret_cast<const uint4 *>(row + at * (kHalf ? 2 : 4)));
+                const int at = base + (a * kThreads + tid) * kWide;
+                if (at < n_wide) v[a] = __ldg(reinterpret_cast<const uint4 *>(row + at));
             }
 #pragma unroll
             for (int a = 0; a < kAhead; ++a) {
-                const int at = base + (a * kThreads + tid) * (kHalf ? 8 : 4);
+                const int at = base + (a * kThreads + tid) * kWide;
                 if (at >= n_wide) continue;
-                const auto lo = [](uint32_t w) { return __uint_as_float(w << 16); };
-                const auto hi = [](uint32_t w) { return __uint_as_float(w & 0xffff0000u); };
-                if constexpr (kHalf) {
-                    keep4(at, make_float4(lo(v[a].x), hi(v[a].x), lo(v[a].y), hi(v[a].y)));
-                    keep4(at + 4, make_float4(lo(v[a].z), hi(v[a].z), lo(v[a].w), hi(v[a].w)));
-                } else {
-                    keep4(at, make_float4(__uint_as_float(v[a].x), __uint_as_float(v[a].y), __uint_as_float(v[a].z), __uint_as_float(v[a].w)));
+                uint32_t w[4] = {v[a].x, v[a].y, v[a].z, v[a].w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (kHalf) {
+                        const __nv_bfloat162 least = __float2bfloat162_rn(-INFINITY);
+                        const __nv_bfloat162 kept = __hmax2(*reinterpret_cast<const __nv_bfloat162 *>(&w[i]), least);   // (a NaN: the other)
+                        w[i] = *reinterpret_cast<const uint32_t *>(&kept);
+                        most = fmaxf(most, fmaxf(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u)));
+                    } else {
+                        const float x = taken(__uint_as_float(w[i]));
+                        w[i] = __float_as_uint(x);
+                        most = fmaxf(most, x);
+                    }
                 }
+                *reinterpret_cast<uint4 *>(held + at) = make_uint4(w[0], w[1], w[2], w[3]);
             }
         }
         // what is left, an entry at a time; entries behind the end are not there
         constexpr int kSingles = 8;
 #pragma unroll 1
         for (int base = n_wide; base < p.part; base += kSingles * kThreads) {
-            float v[kSingles];
+            Held v[kSingles];
 #pragma unroll
             for (int a = 0; a < kSingles; ++a) {
                 const int at = base + a * kThreads + tid;
-                v[a] = at >= n_here ? -INFINITY
-                     : kHalf ? __bfloat162float(__ldg(reinterpret_cast<const __nv_bfloat16 *>(row) + at)) : __ldg(reinterpret_cast<const float *>(row) + at);
+                v[a] = at < n_here ? row[at] : (Held)-INFINITY;
             }
 #pragma unroll
             for (int a = 0; a < kSingles; ++a) {
                 const int at = base + a * kThreads + tid;
                 if (at >= p.part) continue;
-                held[at] = taken(v[a]);
-                most = fmaxf(most, held[at]);
+                const float x = fmaxf((float)v[a], -INFINITY);
+                held[at] = (Held)(kHalf ? x : taken(x));
+                most = fmaxf(most, x);
             }
         }
+        most = taken(most);
     }
     const float top_here = over_warp(most, [](float a, float b) { return fmaxf(a, b); });
     if (lane == 0) sm.of_warp[warp] = top_here;
@@ -378,7 +394,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
 #pragma unroll 1
         for (int j = 0; j < words; ++j) {
             const int at = w0 + j * 128;
-            const float4 v = *reinterpret_cast<const float4 *>(held + at);
+            const float4 v = held4(at);
             f(first + at, v.x), f(first + at + 1, v.y), f(first + at + 2, v.z), f(first + at + 3, v.w);
         }
     };
@@ -404,7 +420,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     };
     // Counts are kept in units that make them masses of the nucleus' kind.
     const auto add_one = [&](uint32_t bin) { atomicAdd(&sm.low[bin], 1); };
-    // Entries for which `in` holds, sorted by the first CTA; their number (over kList: there is no list).
+    // Entries for which `in` holds, sorted, in every CTA; their number (over kList: there is no list).
     const auto gather = [&](auto in) {
         each([&](int i, float x) {
             if (in(x, (uint32_t)i)) {
@@ -417,7 +433,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
 
     Boundary last{-FLT_MAX, 0xffffffffu};   // all of them
     const bool by_count = k > 0 && k < p.V, by_mass = top_p < 1.f;
-    bool listed = false;   // the first CTA's sorted list begins with all entries that stay
+    bool listed = false;   // the sorted list begins with all entries that stay
     uint32_t n_listed = 0;
     bool drawn = false;    // of_cta[turn] is what stays of the CTAs but for the list, and `sorted` up to `last` the rest, in masses of the nucleus
     for (int step = 0; step < 2 && !listed; ++step) {
@@ -546,7 +562,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
 #pragma unroll 1
             for (int j = 0; j < words && before < nth; ++j) {   // (uniform over a warp)
                 const int at = w0 + j * 128;
-                const float4 v = *reinterpret_cast<const float4 *>(held + at);
+                const float4 v = held4(at);
                 const float x[4] = {v.x, v.y, v.z, v.w};
                 uint32_t m = 0;
 #pragma unroll
@@ -680,7 +696,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
 #pragma unroll 1
                     for (int j = 0; j < words && before < target; ++j) {
                         const int at = w0 + j * 128;
-                        const float4 v = *reinterpret_cast<const float4 *>(held + at);
+                        const float4 v = held4(at);
                         const float x[4] = {v.x, v.y, v.z, v.w};
                         Mass w[4], m = 0;
 #pragma unroll
@@ -713,11 +729,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     const int n_wide = (reinterpret_cast<uintptr_t>(to) & 15) == 0 ? max(0, n_here) / 4 * 4 : 0;
 #pragma unroll 2
     for (int at = tid * 4; at < n_wide; at += kThreads * 4) {
-        const float4 v = *reinterpret_cast<const float4 *>(held + at);
+        const float4 v = held4(at);
         *reinterpret_cast<float4 *>(to + at) = make_float4(prob(v.x, first + at), prob(v.y, first + at + 1), prob(v.z, first + at + 2), prob(v.w, first + at + 3));
     }
 #pragma unroll 4
-    for (int at = n_wide + tid; at < n_here; at += kThreads) to[at] = prob(held[at], first + at);
+    for (int at = n_wide + tid; at < n_here; at += kThreads) to[at] = prob(held1(at), first + at);
     if (listed || drawn) svk::cluster_wait();
 }
 
@@ -736,16 +752,17 @@ extern "C" sv_status sv_sample(int32_t n_rows, int32_t vocab, const void *logits
     if (n_rows == 0) return SV_OK;
     if ((int64_t)n_rows * kMaxCluster > INT32_MAX) return SV_ERR_SHAPE;
     // the smallest cluster whose CTAs share an SM by two, and larger ones while they find SMs
+    const int bytes = logits_bf16 ? 2 : 4;
     int cluster = 1;
     while (cluster < kMaxCluster && part_for(vocab, cluster) > kGrain &&
-           (part_for(vocab, cluster) > kPart || 2ll * cluster * n_rows <= svh::sm_count()))
+           (part_for(vocab, cluster) * bytes > kTwo || 2ll * cluster * n_rows <= svh::sm_count()))
         cluster *= 2;
     const int part = part_for(vocab, cluster);
     const Params p = {logits, row_stride, temperature, top_p, min_p, u, top_k, tokens, probs, vocab, rows_per_param, part};
     const auto kernel = logits_bf16 ? sample_kernel<true> : sample_kernel<false>;
     static svh::OncePerDevice once[2];
     if (once[logits_bf16 != 0].run([&] {
-            return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(sizeof(Smem) + kMostPart * sizeof(float)));
+            return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(sizeof(Smem) + kMostPart * bytes));
         }) != cudaSuccess) {
         (void)cudaGetLastError();
         return SV_ERR_CUDA;
@@ -753,7 +770,7 @@ extern "C" sv_status sv_sample(int32_t n_rows, int32_t vocab, const void *logits
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(n_rows * cluster));
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = sizeof(Smem) + part * sizeof(float);
+    cfg.dynamicSmemBytes = sizeof(Smem) + part * bytes;
     cfg.stream = static_cast<cudaStream_t>(stream);
     cudaLaunchAttribute attr[2];
     svh::pdl_attribute(attr);
