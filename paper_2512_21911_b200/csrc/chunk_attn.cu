@@ -48,7 +48,6 @@ constexpr int kSmemBytes = 1024 + kOffMisc + 2048;
 static_assert(kSmemBytes <= 232448, "shared memory budget");
 constexpr int kRegsMany = 104, kRegsFew = 64;
 static_assert((4 * kRegsMany + kRegsFew) * 128 <= 96 * kThreads, "registers of the launch");
-constexpr int kPoly = 0;                      // of every four pairs of exponentials, those computed without the special-function unit
 constexpr float kLag = 8.f;                  // what the maximum may exceed the reference by (log2)
 
 enum Bar {
@@ -455,45 +454,18 @@ __device__ __forceinline__ void issue(const Params &p, const Shared &sh, uint32_
 }
 
 // ---------------------------------------------------------------------- warps 0-7 and 8-15: the softmax of stream g
-// 2^x of two numbers, none above 2^7, without the special-function unit: x = n + f with n whole and |f| <= 1/2, 2^f as a polynomial, n added to
-// the exponent.  The polynomial is 1 at 0 (minimax under that condition, off by 2.8e-6 of itself at most), so that -127, which stands for
-// everything below, -infinity included, gives 0.
-__device__ __forceinline__ unsigned long long exp2_pair(unsigned long long x2)
-{
-    const auto both = [](float v) { return f2_pack(v, v); };
-    float a, b;
-    f2_unpack(x2, a, b);
-    x2 = f2_pack(fmaxf(a, -127.f), fmaxf(b, -127.f));
-    const unsigned long long z = f2_add(x2, both(12582912.f));   // n in the last places
-    const unsigned long long f = f2_fma(f2_add(z, both(-12582912.f)), both(-1.f), x2);
-    unsigned long long y = f2_fma(both(0.009582553f), f, both(0.055906326f));
-    y = f2_fma(y, f, both(0.24024104f));
-    y = f2_fma(y, f, both(0.69312423f));
-    y = f2_fma(y, f, both(1.f));
-    float ya, yb, za, zb;
-    f2_unpack(y, ya, yb);
-    f2_unpack(z, za, zb);
-    return f2_pack(__uint_as_float(__float_as_uint(ya) + (__float_as_uint(za) << 23)), __uint_as_float(__float_as_uint(yb) + (__float_as_uint(zb) << 23)));
-}
 // P of two rows of 8 scores each, from x (four words of the fragment of tcgen05.ld 16x256b for either eight keys): rounded to one word a row and
-// eight keys, the unrounded ones added to the sums.  Of every four such steps kPoly go by exp2_pair: the special-function unit has a quarter
-// of the rate of the other pipes.
+// eight keys, the unrounded ones added to the sums.  (P is bf16 because the matrix instruction takes A of V's type; l is the sum of what P was
+// before, so that a row's weights are off by the rounding of each, 2^-9 at most, and not by that of the sum.)
 __device__ __forceinline__ void exponentials(const uint32_t *x, uint32_t *w, unsigned long long scale2, const unsigned long long (&ref2)[2],
-                                             unsigned long long (&sum2)[2], bool poly)
+                                             unsigned long long (&sum2)[2])
 {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        unsigned long long v = f2_fma(f2_pack(__uint_as_float(x[2 * h]), __uint_as_float(x[2 * h + 1])), scale2, ref2[h]);
         float a, b;
-        if (poly) {
-            v = exp2_pair(v);
-            f2_unpack(v, a, b);
-        } else {
-            f2_unpack(v, a, b);
-            a = fast_exp2(a), b = fast_exp2(b);
-            v = f2_pack(a, b);
-        }
-        sum2[h] = f2_add(sum2[h], v);
+        f2_unpack(f2_fma(f2_pack(__uint_as_float(x[2 * h]), __uint_as_float(x[2 * h + 1])), scale2, ref2[h]), a, b);
+        a = fast_exp2(a), b = fast_exp2(b);
+        sum2[h] = f2_add(sum2[h], f2_pack(a, b));
         w[h] = pack_bf16(a, b);
     }
 }
@@ -620,7 +592,7 @@ __device__ __forceinline__ void softmax(const Params &p, const Shared sh, uint32
             const auto quarter = [&](int c) {
                 uint32_t w[8];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) exponentials(x + 16 * c + 4 * i, w + 2 * i, scale2, ref2, sum2, i >= 4 - kPoly);
+                for (int i = 0; i < 4; ++i) exponentials(x + 16 * c + 4 * i, w + 2 * i, scale2, ref2, sum2);
                 tmem_st_16x128b_x4(t_s + c * 16, w);
             };
             quarter(0);
@@ -779,38 +751,39 @@ __global__ void __launch_bounds__(kThreads, 1)
     grid_launch_dependents();
 }
 
-// A cut item: the partial sums of its shares, which are numbered from the CTA that it begins in.  A warp per row, four dims a lane.
-constexpr int kMergeRows = 32;   // rows of a CTA
-__global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant__ Params p)
+// A cut item: the partial sums of its shares, which are numbered from the CTA that it begins in.  A warp per row, four dims a lane, four shares
+// on their way at once.  Bound by latency: the 148 places where an item may begin, each with all the rows that a partial has room for, are
+// more CTAs than there is work for, and most leave after a look at their cut (with four rows a warp one behind the other 1.4 us more for a batch
+// of 1,500 rows in three chunks).  Launched when the attention's CTAs are through: with the trigger at their beginning the calls take 0.5 to 1 us
+// longer, since the merging CTAs then wait beside them.
+constexpr int kMergeRows = 8;   // rows of a CTA
+__global__ void __launch_bounds__(kMergeRows * 32) chunk_merge_kernel(const __grid_constant__ Params p)
 {
     grid_dependency_wait();
     const int cta = blockIdx.x, lane = threadIdx.x & 31;
     const int4 cut = p.cuts[cta];
     if (cut.w == 0) return;
     const bool two = cut.y > p.TT;
-    for (int i = threadIdx.x >> 5; i < kMergeRows; i += 8) {
-        const int at = blockIdx.y * kMergeRows + i;
-        if (at >= p.slot_rows) return;
-        const int r = at & 127, token = (two ? (at >> 7) * p.TT : 0) + r / p.G;
-        if (r >= p.G * p.TT || token >= cut.y || (!two && at >= 128)) continue;
-        SplitSum sum;
-        constexpr int U = 4;
-        for (int base = 0; base < cut.w; base += U) {
-            float2 ml[U];
-            float4 o[U];
+    const int at = blockIdx.y * kMergeRows + (int)(threadIdx.x >> 5);
+    const int r = at & 127, token = (two ? (at >> 7) * p.TT : 0) + r / p.G;
+    if (at >= p.slot_rows || r >= p.G * p.TT || token >= cut.y || (!two && at >= 128)) return;
+    SplitSum sum;
+    constexpr int U = 4;
+    for (int base = 0; base < cut.w; base += U) {
+        float2 ml[U];
+        float4 o[U];
 #pragma unroll
-            for (int k = 0; k < U; ++k) {
-                const size_t part = ((size_t)(cta + base + k) * 2 + (base + k == 0)) * p.slot_rows + at;
-                const bool in = base + k < cut.w;
-                ml[k] = in ? __ldcg(p.ws_ml + part) : make_float2(-INFINITY, 0.f);
-                o[k] = in ? __ldcg(reinterpret_cast<const float4 *>(p.ws_o + part * 128) + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
-            }
-            sum.add(ml, o);
+        for (int k = 0; k < U; ++k) {
+            const size_t part = ((size_t)(cta + base + k) * 2 + (base + k == 0)) * p.slot_rows + at;
+            const bool in = base + k < cut.w;
+            ml[k] = in ? __ldcg(p.ws_ml + part) : make_float2(-INFINITY, 0.f);
+            o[k] = in ? __ldcg(reinterpret_cast<const float4 *>(p.ws_o + part * 128) + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
-        const size_t row = (size_t)(cut.x + token) * p.Hq + cut.z * p.G + r % p.G;
-        reinterpret_cast<uint2 *>(p.out + row * 128)[lane] = sum.l > 0.f ? sum.out() : make_uint2(0u, 0u);
-        if (p.lse && lane == 0) p.lse[row] = sum.l > 0.f ? sum.lse() : -INFINITY;
+        sum.add(ml, o);
     }
+    const size_t row = (size_t)(cut.x + token) * p.Hq + cut.z * p.G + r % p.G;
+    reinterpret_cast<uint2 *>(p.out + row * 128)[lane] = sum.l > 0.f ? sum.out() : make_uint2(0u, 0u);
+    if (p.lse && lane == 0) p.lse[row] = sum.l > 0.f ? sum.lse() : -INFINITY;
 }
 
 // Rows of a partial: the rows of the batch where these are one tile at most.
@@ -875,7 +848,7 @@ extern "C" sv_status sv_chunk_attn(const sv_geom *geom, const void *q, const sv_
     cfg.numAttrs = 1;
     if (cudaLaunchKernelEx(&cfg, chunk_attn_kernel, tm_q, tm_k, tm_v, p) != cudaSuccess) return SV_ERR_CUDA;
     cfg.gridDim = dim3(ctas, (p.slot_rows + kMergeRows - 1) / kMergeRows);
-    cfg.blockDim = dim3(256);
+    cfg.blockDim = dim3(kMergeRows * 32);
     cfg.dynamicSmemBytes = 0;
     return cudaLaunchKernelEx(&cfg, chunk_merge_kernel, p) == cudaSuccess ? svh::launch_status() : SV_ERR_CUDA;
 }
