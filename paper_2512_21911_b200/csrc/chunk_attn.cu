@@ -5,9 +5,9 @@
 // maximum, l = sum 2^(s_t - m), o = sum 2^(s_t - m) v_t; the output is o / l.  When the maximum outgrows the reference by more than 8,
 // m moves and l and o are multiplied by 2^(old - new); o / l does not depend on m, and bf16 and fp32 have the same exponents.
 //
-// A row tile is 128 of the G * n rows (token-major: token r / G, head r % G) of a (sequence, KV head); an item is two neighbouring row tiles
-// of TT = 128 / G tokens each, or the one that is left (always the case for single tokens).  A CTA runs two streams, each with eight
-// softmax warps and S and O of its own in TMEM (4 x 128 columns), over units of 128 keys:
+// A row tile is 128 of the G * n rows (token-major: token r / G, head r % G) of a (sequence, KV head); an item is two neighbouring row
+// tiles of TT = 128 / G tokens each, or the one that is left (always the case for single tokens).  A CTA runs two streams, each with
+// eight softmax warps and S and O of its own in TMEM (4 x 128 columns), over units of 128 keys:
 //   two tiles   stream g has tile g and takes every unit; K and V of a unit are fetched once for both
 //   one tile    the streams take the units in turn and add their sums at the end
 //   S[128 x 128] = Q . K^T      8 x tcgen05.mma (M128 N128 K16), both operands from shared memory (TMA, 128-byte swizzle)
@@ -15,11 +15,20 @@
 //   O[128 x 128] += P . V       8 x tcgen05.mma, P from TMEM, V MN-major as TMA stored it
 // A stream's chain is S, softmax, PV, S, ...; while one stream is in its softmax the tensor cores work for the other.
 //
-// The batch is ragged and its lengths are on the device, so the work is divided there: all items of the batch in a row, an item as long as
-// the keys it sees plus kItemCost, are cut into equal shares, a CTA each (chunk_shares.h).  An item that is cut is written as partial sums to the workspace
-// and merged by a second kernel; a CTA has at most two cuts.  That balances a prompt's triangle of items, single tokens over long
-// caches and any mixture of the two without a case of its own.
-// All waits are on mbarriers and bounded; one that gives up sets the status word, the CTA drains its copies and MMAs, frees TMEM and returns.
+// The batch is ragged and its lengths are on the device, so the work is divided there: all items of the batch in a row, an item as long
+// as the keys it sees plus kItemCost, are cut into equal shares, a CTA each (chunk_shares.h).  An item that is cut is written as partial
+// sums to the workspace and merged by a second kernel; a CTA has at most two cuts.  That balances a prompt's triangle of items, single
+// tokens over long caches and any mixture of the two without a case of its own.
+//
+// Bound by, and measured (32 query and 8 KV heads; the faster and the slower of the machines it was timed on): a prompt of 8,192 tokens
+// takes 495 to 575 us for 0.55 TFLOP, 0.96 to 1.1 PFLOP/s or 58 to 68 % of a large library product, the tensor pipe active for 52 % of
+// the time: a unit of two tiles takes 3900 cycles where its MMAs take 2048, the rest being what passes a unit from S to the softmax, to
+// PV and on (issue()).  2,048 tokens behind 30,001 (64 heads): 2.0 to 2.1 ms for 2.08 TFLOP, 0.98 to 1.0 PFLOP/s.  16 single tokens over
+// 4K to 16K keys: 727 MB in 126 to 141 us, 79 to 88 % of a copy's rate.  One token over 4K keys of 2 heads: 19 us, of which 5 are the
+// merging launch and the rest a chain of cold steps (batch, division, tensor maps, page, tile, softmax).
+//
+// All waits are on mbarriers and bounded; one that gives up sets the status word, the CTA drains its copies and MMAs, frees TMEM and
+// returns.
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -179,9 +188,9 @@ struct Shared {
         store(at + kAbort, 1);
         if (status) atomicOr(status, bit);
     }
-    // As few instructions as it takes: the code of a hand-over is cold when it is reached (the softmax has run through the instruction caches
-    // meanwhile), and is fetched line by line.  With the waits unrolled four by four the kernel had 158 KB of code, and every step of a
-    // hand-over took 400 cycles.
+    // As few instructions as it takes: the code of a hand-over is cold when it is reached (the softmax has run through the instruction
+    // caches meanwhile), and is fetched line by line.  With the waits unrolled four by four the kernel had 158 KB of code, and every step
+    // of a hand-over took 400 cycles.
     __device__ static bool poll(uint32_t bar, uint32_t parity)   // 2^13 times
     {
         uint32_t ok;
@@ -213,7 +222,8 @@ struct Shared {
     }
     // the same for a converged warp: true if every lane has seen the phase
     __device__ bool warp_wait(int i, uint32_t parity, int32_t *status, int bit) const { return __all_sync(0xffffffffu, wait(i, parity, status, bit)); }
-    // The same without the suspension that try_wait may take, for the issuing warp alone (for all warps, their polls get into one another's way).
+    // The same without the suspension that try_wait may take, for the issuing warp alone (for all warps, their polls get into one
+    // another's way).
     __device__ bool spin_wait(int i, uint32_t parity, int32_t *status, int bit) const
     {
         const uint32_t b = bar(i);
@@ -251,7 +261,8 @@ __device__ __forceinline__ void hand_out(ChunkWalk &walk, const Shared &sh, Chun
         if (!more) return;
     }
 }
-// The item of this number is there, for a whole warp, until it says that it is through with it; false: there are no more, or a wait gave up.
+// The item of this number is there, for a whole warp, until it says that it is through with it; false: there are no more, or a wait gave
+// up.
 __device__ __forceinline__ bool take(const Shared &sh, int n, int32_t *status)
 {
     return sh.warp_wait(kItem + (n & 1), (n >> 1) & 1, status, 64) && sh.item(n, kUnits) >= 0;
@@ -338,16 +349,18 @@ __device__ __forceinline__ void produce(const Params &p, const Shared &sh, uint3
 }
 
 // ---------------------------------------------------------------------- warp 17: all MMAs, of the two streams in turn
-// The turns keep the streams half a unit apart, one in its softmax while the tensor cores work for the other; issued by a warp each, the streams
-// fall into step and wait for the tensor cores together (4750 cycles a unit of a prompt).  A wait takes 250 to 300 cycles here even when there is nothing to
-// wait for, so the lanes wait for different barriers at once: the stage of V, that of the next unit's K and the first half of P, then the rest of
-// P, behind which PV and the next S go out together (a wait after the other, the warp itself was what a unit took: 4200 cycles).
+// The turns keep the streams half a unit apart, one in its softmax while the tensor cores work for the other; issued by a warp each, the
+// streams fall into step and wait for the tensor cores together (4750 cycles a unit of a prompt).  A wait takes 250 to 300 cycles here even
+// when there is nothing to wait for, so the lanes wait for different barriers at once: the stage of V, that of the next unit's K and the
+// first half of P, then the rest of P, behind which PV and the next S go out together (a wait after the other, the warp itself was what a
+// unit took: 4200 cycles).
 __device__ __forceinline__ void issue(const Params &p, const Shared &sh, uint32_t smem0, uint32_t tmem)
 {
     constexpr uint32_t idesc_s = umma_idesc_bf16(128, kUnit, false), idesc_pv = umma_idesc_bf16(128, 128, true);
     const uint64_t dq = umma_desc_sw128(smem0 + kOffQ, 16, 1024), dk = umma_desc_sw128(smem0, 16, 1024);
     const uint64_t dv = umma_desc_sw128(smem0, kHalf / 2, 1024);
-    // Of every three lanes the second waits for stages of V and the third for stages of K: the ring stage and its parity of what a lane waits for next.
+    // Of every three lanes the second waits for stages of V and the third for stages of K: the ring stage and its parity of what a lane
+    // waits for next.
     const int lane = threadIdx.x & 31, part = lane % 3;
     int stage = 0;
     uint32_t turn = 0;
@@ -454,9 +467,9 @@ __device__ __forceinline__ void issue(const Params &p, const Shared &sh, uint32_
 }
 
 // ---------------------------------------------------------------------- warps 0-7 and 8-15: the softmax of stream g
-// P of two rows of 8 scores each, from x (four words of the fragment of tcgen05.ld 16x256b for either eight keys): rounded to one word a row and
-// eight keys, the unrounded ones added to the sums.  (P is bf16 because the matrix instruction takes A of V's type; l is the sum of what P was
-// before, so that a row's weights are off by the rounding of each, 2^-9 at most, and not by that of the sum.)
+// P of two rows of 8 scores each, from x (four words of the fragment of tcgen05.ld 16x256b for either eight keys): rounded to one word a
+// row and eight keys, the unrounded ones added to the sums.  (P is bf16 because the matrix instruction takes A of V's type; l is the sum
+// of what P was before, so that a row's weights are off by the rounding of each, 2^-8 at most, and not by that of the sum.)
 __device__ __forceinline__ void exponentials(const uint32_t *x, uint32_t *w, unsigned long long scale2, const unsigned long long (&ref2)[2],
                                              unsigned long long (&sum2)[2])
 {
@@ -489,7 +502,8 @@ __device__ __forceinline__ void transpose_4(uint32_t (&w)[4], int q)
     else w[2] = a, w[3] = b;
 }
 
-// The eight warps of a stream: a lane quarter has two, for 16 rows each; a thread has rows i and i + 8 of these and every fourth pair of keys.
+// The eight warps of a stream: a lane quarter has two, for 16 rows each; a thread has rows i and i + 8 of these and every fourth pair of
+// keys.
 __device__ __forceinline__ void softmax(const Params &p, const Shared sh, uint32_t smem0, uint32_t tmem, int g)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, q = lane & 3;
@@ -751,11 +765,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     grid_launch_dependents();
 }
 
-// A cut item: the partial sums of its shares, which are numbered from the CTA that it begins in.  A warp per row, four dims a lane, four shares
-// on their way at once.  Bound by latency: the 148 places where an item may begin, each with all the rows that a partial has room for, are
-// more CTAs than there is work for, and most leave after a look at their cut (with four rows a warp one behind the other 1.4 us more for a batch
-// of 1,500 rows in three chunks).  Launched when the attention's CTAs are through: with the trigger at their beginning the calls take 0.5 to 1 us
-// longer, since the merging CTAs then wait beside them.
+// A cut item: the partial sums of its shares, which are numbered from the CTA that it begins in.  A warp per row, four dims a lane, four
+// shares on their way at once.  Bound by latency: the 148 places where an item may begin, each with all the rows that a partial has room
+// for, are more CTAs than there is work for, and most leave after a look at their cut (with four rows a warp one behind the other 1.4 us
+// more for a batch of 1,582 tokens, most of them in three chunks).  Launched when the attention's CTAs are through: with the trigger at
+// their beginning the calls take 0.5 to 1 us longer, since the merging CTAs then wait beside them.
 constexpr int kMergeRows = 8;   // rows of a CTA
 __global__ void __launch_bounds__(kMergeRows * 32) chunk_merge_kernel(const __grid_constant__ Params p)
 {

@@ -1,9 +1,9 @@
 // How sv_chunk_attn divides a ragged batch among its CTAs (plain C++: the same arithmetic runs in the kernel and in its test).
 //
-// An item is up to 2 * TT tokens of a (sequence, KV head) and costs the keys it sees -- twice where it is two row tiles, whose streams both
-// take every unit -- plus kItemCost.  The items of the batch, by sequence, KV head and place, lie one behind the other on a line, which
-// is cut into equal shares.  Where an item is cut follows from the share's
-// bounds alone, so neighbours agree without talking to one another.  Costs are whole numbers with closed sums: no table is needed.
+// An item is up to 2 * TT tokens of a (sequence, KV head) and costs the keys it sees -- twice where it is two row tiles, whose streams
+// both take every unit -- plus kItemCost.  The items of the batch, by sequence, KV head and place, lie one behind the other on a line,
+// which is cut into equal shares.  Where an item is cut follows from the share's bounds alone, so neighbours agree without talking to one
+// another.  Costs are whole numbers with closed sums: no table is needed.
 #pragma once
 #include <stdint.h>
 
@@ -16,8 +16,8 @@
 namespace svk {
 
 constexpr int kChunkUnit = 128;   // keys of a unit, the grain of a cut
-// A unit of two tiles takes 3900 cycles, of one tile 1900 (a prompt of 8K; single tokens whose keys are in L2), an item's beginning and end 5000, and more
-// where they wait for nothing else (512 against 320: a ragged batch 104.7 -> 100.6 us, the prompt 515 -> 512).
+// A unit of two tiles takes 3900 cycles, of one tile 1900 (a prompt of 8K; single tokens whose keys are in L2), an item's beginning and end
+// 5000, and more where they wait for nothing else (512 against 320: a ragged batch 104.7 -> 100.6 us, the prompt 515 -> 512).
 constexpr int kItemCost = 512;    // keys (of one tile) that the beginning and the end of an item cost as much as
 constexpr int kLeastShare = 256;  // ... of the shortest share worth a CTA; a unit of two tiles, so that no share inside an item is empty
 

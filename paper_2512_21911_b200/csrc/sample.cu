@@ -1,19 +1,26 @@
 // sv_sample: temperature, top-k, top-p and min-p on rows of logits, the kept entries' distribution and a token drawn from it.
 //
 // Mathematics: e(x) = 2^((x - max) log2 e / temperature).  The entries are never sorted: what stays is everything up to one entry, the
-// boundary (logit, index), in the order "larger logit first, then smaller index".  Search for the boundary by count (top-k) or mass (top-p):
-// a histogram of the entries by their distance from the maximum, the bin in which the goal is reached, and the few entries of that bin,
-// ranked exactly.  A bin with too many of them is divided again by the bits of its keys; entries that are all equal are counted off by
-// index.  For a short top-k the histogram holds the threads' maxima only: the k-th largest of these bounds the k-th entry
-// from below, all entries up to its bin are ranked at once, and top-p, min-p and the token follow from that list.
+// boundary (logit, index), in the order "larger logit first, then smaller index".  Search for the boundary by count (top-k) or mass
+// (top-p): a histogram of the entries by their distance from the maximum, the bin in which the goal is reached, and the few entries of
+// that bin, ranked exactly.  A bin with too many of them is divided again by the bits of its keys; entries that are all equal are counted
+// off by index.  For a short top-k the histogram holds the threads' maxima only: the k-th largest of these bounds the k-th entry from
+// below, all entries up to its bin are ranked at once, and top-p, min-p and the token follow from that list.
 //
-// Sums of masses are sums of whole numbers, exact in any order.  Of the nucleus: multiples of 2^-32 of the largest entry's mass, so that a bin is
-// two 32-bit words that shared-memory atomics add to (2^-32 is less than fp32 sums keep; what is lost are entries below 2^-33 of
-// the largest, 2^-16 of its mass if there were 2^17 of them); they also do for the draw from a nucleus, whose histogram has them by CTA.  Of
-// other draws: multiples of 2^-40, added in registers.
+// Sums of masses are sums of whole numbers, exact in any order.  Of the nucleus: multiples of 2^-32 of the largest entry's mass, so that a
+// bin is two 32-bit words that shared-memory atomics add to (2^-32 is less than fp32 sums keep; what is lost are entries below 2^-33 of
+// the largest, 2^-16 of its mass if there were 2^17 of them); they also do for the draw from a nucleus, whose histogram has them by CTA.
+// Of other draws: multiples of 2^-40, added in registers.
 //
-// A cluster of 1 to 8 CTAs per row; a CTA keeps its part of the row in shared memory, so the logits are read once from HBM.  Warps
-// own contiguous parts: a token is found by sums per CTA, warp and lane.
+// A cluster of 1 to 8 CTAs per row; a CTA keeps its part of the row in shared memory, so the logits are read once from HBM (19.5 MB of 19.4
+// for 64 bfloat16 rows of 151,936).  Warps own contiguous parts: a token is found by sums per CTA, warp and lane.
+//
+// Bound by the steps between the passes (a barrier of the cluster is 1.8 us, the ranking of a list as much) and by the instructions of the
+// passes, two CTAs an SM overlapping one's steps with the other's passes: warps issue in 52 to 58 % of the cycles, and HBM, whose floor for
+// these cases is 3 to 12 us, idles.  Measured: one row of 128,256 with a top-k of 50 14 us, 10 of them the chain of steps; 64 bfloat16 rows
+// of 151,936 with a nucleus 57 to 60 us, one round of clusters of four; 80 rows of 128,256 with a nucleus and their distributions 83 us,
+// three rounds of clusters of eight (load and store 27, histogram 11, its search 8, the boundary's bin gathered and ranked 14, draw and
+// probabilities 24); 256 rows of 32,003 with top-k, min-p and distributions 39 to 45 us.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <float.h>
@@ -95,8 +102,8 @@ struct Boundary {
 };
 
 struct alignas(16) Smem {
-    uint32_t high[kBins];     // histogram: sums of masses in two words, or counts in the second;
-    int low[kBins];           // the first CTA keeps masses of its list in the first
+    uint32_t high[kBins];     // histogram: sums of masses in two words, or counts in the second; later the list's masses
+    int low[kBins];
     Mass list[kList], sorted[kList];   // key << 32 | ~index: descending is the order of the rule
     Mass sums[kWarps], scan[kWarps];
     Mass of_cta[2][kMaxCluster];   // written by all CTAs of the cluster; two in turn, so that no CTA writes what another still reads
@@ -107,7 +114,7 @@ struct alignas(16) Smem {
     int found_bin, token;
     Boundary boundary;
     uint32_t n_list;
-    // The sums of every CTA's groups of bins, written by it, where the sorted list is later.  (Between two uses there is a barrier of the cluster.)
+    // The sums of every CTA's groups of bins, written by it, where the sorted list is later.  (Between two uses the cluster has a barrier.)
     __device__ Mass *groups(int cta) { return sorted + cta * kGroups; }
     __device__ Mass *masses() { return reinterpret_cast<Mass *>(high); }
 };
@@ -176,10 +183,10 @@ __device__ __noinline__ Mass sum_over_cluster(Smem &sm, int turn, Mass v)
     cg::this_cluster().sync();
     return sum_over_warp(lane < cluster_size() ? sm.of_cta[turn][lane] : 0);
 }
-// The bin in which the sums over the cluster's histograms reach the goal (0: `of_all` of the sum of all), and what is in the bins ahead of
-// it.  Every CTA tells all others the sums of its groups of bins, finds the group of the goal by itself and reads the bins of that group from
-// all CTAs: one barrier of the cluster (1.8 us each, with what goes before it), where shares of the bins added up by different CTAs take
-// three.  -1: there is not as much.  The bins have to stay until the cluster's next barrier.
+// The bin in which the sums over the cluster's histograms reach the goal (0: `of_all` of the sum of all), and what is in the bins ahead
+// of it.  Every CTA tells all others the sums of its groups of bins, finds the group of the goal by itself and reads the bins of that
+// group from all CTAs: one barrier of the cluster (1.8 us each, with what goes before it), where shares of the bins added up by different
+// CTAs take three.  -1: there is not as much.  The bins have to stay until the cluster's next barrier.
 struct Found {
     int bin;
     Mass goal, ahead;
