@@ -70,8 +70,9 @@ def _check(lib, lens, new, Hkv, G, cap, ctas):
             assert 0 <= u0 <= u1 <= units and (u0 < u1 or units == 0)
             begun += u0 > 0
             going += u0 == 0 and u1 < units
-            # on the line a whole item is up to 128 keys shorter than its units, and what is ahead of a cut has paid the item's cost
-            work[-1] += (2 if tokens > TT else 1) * max(0, (u1 - u0) * 128 - 128)
+            # on the line a whole item is less than 128 keys shorter than its units; a cut lies less than a unit behind its place on the line,
+            # so that a share that begins at a cut has that unit too (and, where it ends with the item, both)
+            work[-1] += (2 if tokens > TT else 1) * max(0, (u1 - u0) * 128 - (256 if u0 > 0 and u1 == units else 128))
         assert begun <= 1 and going <= 1
     # every token of every head, every unit once
     for s in range(S):
