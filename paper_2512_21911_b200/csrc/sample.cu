@@ -3,7 +3,7 @@
 // Mathematics: e(x) = 2^((x - max) log2 e / temperature).  The entries are never sorted: what stays is everything up to one entry, the
 // boundary (logit, index), in the order "larger logit first, then smaller index".  Search for the boundary by count (top-k) or mass
 // (top-p): a histogram of the entries by their distance from the maximum, the bin in which the goal is reached, and the few entries of
-// that bin, ranked exactly.  A bin with too many of them is divided again by the bits of its keys; entries that are all equal are counted
+// that bin, divided again in the same way until a warp has them.  A bin with too many of them is divided again by the bits of its keys; entries that are all equal are counted
 // off by index.  For a short top-k the histogram holds the threads' maxima only: the k-th largest of these bounds the k-th entry from
 // below, all entries up to its bin are ranked at once, and top-p, min-p and the token follow from that list.
 //
@@ -15,12 +15,13 @@
 // A cluster of 1 to 8 CTAs per row; a CTA keeps its part of the row in shared memory, so the logits are read once from HBM (19.5 MB of 19.4
 // for 64 bfloat16 rows of 151,936).  Warps own contiguous parts: a token is found by sums per CTA, warp and lane.
 //
-// Bound by the steps between the passes (a barrier of the cluster is 1.8 us, the ranking of a list as much) and by the instructions of the
-// passes, two CTAs an SM overlapping one's steps with the other's passes: warps issue in 52 to 58 % of the cycles, and HBM, whose floor for
-// these cases is 3 to 12 us, idles.  Measured: one row of 128,256 with a top-k of 50 14 us, 10 of them the chain of steps; 64 bfloat16 rows
-// of 151,936 with a nucleus 57 to 60 us, one round of clusters of four; 80 rows of 128,256 with a nucleus and their distributions 83 us,
-// three rounds of clusters of eight (load and store 27, histogram 11, its search 8, the boundary's bin gathered and ranked 14, draw and
-// probabilities 24); 256 rows of 32,003 with top-k, min-p and distributions 39 to 45 us.
+// Bound by the instructions of the passes (some 30 an entry for the histogram, 14 to gather a bin, 18 for the probabilities) and by the
+// steps between them (a barrier of the cluster is 1.8 us), two CTAs an SM overlapping one's steps with the other's passes: warps issue in
+// half of the cycles, and HBM, whose floor for these cases is 3 to 12 us, idles.  Measured: one row of 128,256 with a top-k of 50 12.8 us;
+// 64 bfloat16 rows of 151,936 with a nucleus 50 us, one round of clusters of four; 80 rows of 128,256 with a nucleus and their
+// distributions 77 us, three rounds of clusters of eight (12 of them the load, 10 the probabilities); 256 rows of 32,003 with top-k, min-p
+// and distributions 38 us.  Tests of an entry are written without branches, of which a pass had 20 an entry before (one row 13.7, then
+// 57, 84 and 40 us, with lists ranked entry against entry by every CTA).
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <float.h>
@@ -41,7 +42,7 @@ constexpr int kMaxCluster = 8;
 constexpr int kBins = 2048;
 constexpr int kGroups = 64;                    // of 32 bins each
 constexpr float kBinsPerBit = 2048.f / 36.f;   // bins of the first histogram: 36 powers of two below the maximum, beyond what has a mass
-constexpr int kList = 768;                     // entries that are ranked one against another
+constexpr int kList = 768;                     // entries that are looked at one by one
 constexpr int kGrain = kWarps * 128;           // a CTA's part of a row is a multiple of this: 32 lanes x 4 entries for each warp
 constexpr int kMostPart = 24 * kGrain;         // entries that fit in shared memory
 constexpr int kTwo = 80 * 1024;                // bytes of a part that leave room for a second CTA on the SM
@@ -80,8 +81,7 @@ template <int N>
 __device__ __forceinline__ Parts parts_of(float e)
 {
     constexpr float kOne = (float)(1 << N);
-    const float f = __fmul_rn(e, kOne), t = __fadd_rn(f, 8388608.f);
-    const float rest = __fsub_rn(f, __fsub_rn(t, 8388608.f));
+    const float t = __fmaf_rn(e, kOne, 8388608.f), rest = __fmaf_rn(e, kOne, -__fsub_rn(t, 8388608.f));
     return {__float_as_uint(t) - 0x4b000000u, (int)(__float_as_uint(__fmaf_rn(rest, kOne, 12582912.f)) - 0x4b400000u)};
 }
 template <int N>
@@ -98,7 +98,7 @@ constexpr int kEach = (kList + kThreads - 1) / kThreads;   // entries of a list 
 struct Boundary {
     float x;
     uint32_t index;   // the last entry that stays
-    __device__ bool keeps(float y, uint32_t i) const { return y > x || (y == x && i <= index); }
+    __device__ bool keeps(float y, uint32_t i) const { return (y > x) | ((y == x) & (i <= index)); }
 };
 
 struct alignas(16) Smem {
@@ -137,6 +137,13 @@ __device__ __forceinline__ T scan_warp(T v)   // inclusive
         if ((threadIdx.x & 31) >= d) v += o;
     }
     return v;
+}
+
+// (one instruction with a predicate: as a branch it was a quarter of a pass)
+__device__ __forceinline__ void add_shared(int *at, int v, bool really)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p red.shared.add.u32 [%0], %1;\n\t}" ::"r"(svk::smem_u32(at)), "r"(v), "r"((int)really)
+                 : "memory");
 }
 
 // The cluster's CTAs, and a word of this CTA's shared memory in each of them (one warp).
@@ -241,14 +248,17 @@ __device__ __noinline__ Found find_in_bins(Smem &sm, Mass goal, float of_all)
     __syncthreads();
     return {sm.found_bin, sm.found_goal, sm.found_ahead};
 }
-// All CTAs' lists behind this one's own, and sorted; their length (over kList: there is no list).  mine: what the CTA tells the others,
+// All CTAs' lists behind this one's own, and sorted where that is asked for; their length (over kList: there is no list).  mine: what the CTA tells the others,
 // into of_cta[turn].  The lists have to stay until the cluster's next barrier.
-__device__ __noinline__ uint32_t collect(Smem &sm, int turn, Mass mine)
+__device__ __noinline__ uint32_t collect(Smem &sm, int turn, Mass mine, bool sort)
 {
     const cg::cluster_group cluster = cg::this_cluster();
     const int CL = cluster_size(), rank = cluster_rank(), tid = threadIdx.x;
-    mine = scan_block(sm, mine).total;
-    if (tid < 32) everywhere(&sm.count_of_cta[rank], sm.n_list), everywhere(&sm.of_cta[turn][rank], mine);
+    mine = sum_over_warp(mine);
+    __syncthreads();
+    if ((tid & 31) == 0) sm.sums[tid >> 5] = mine;
+    __syncthreads();
+    if (tid < 32) everywhere(&sm.count_of_cta[rank], sm.n_list), everywhere(&sm.of_cta[turn][rank], sum_over_warp(tid < kWarps ? sm.sums[tid] : 0));
     cluster.sync();
     // 64 threads for every CTA's list, all of them at once: behind this CTA's own, in the order of the CTAs
     constexpr int kPull = kThreads / kMaxCluster;
@@ -270,6 +280,7 @@ __device__ __noinline__ uint32_t collect(Smem &sm, int turn, Mass mine)
         for (uint32_t i = tid % kPull; i < count; i += kPull) sm.list[at + i] = *cluster.map_shared_rank(&sm.list[i], from);
     }
     __syncthreads();
+    if (!sort) return n;
 #pragma unroll 1
     for (uint32_t i = tid; i < n; i += kThreads) {
         const uint64_t me = sm.list[i];
@@ -282,6 +293,89 @@ __device__ __noinline__ uint32_t collect(Smem &sm, int turn, Mass mine)
     return n;
 }
 
+// Of the list's n entries, in their order, the one that brings the sum of their weights to the goal (it exists): divided into 256 parts of
+// their range by sums as in the large histogram, the part of the goal divided again until a warp has what is left of it.  (Ranked one against
+// another by all CTAs, 300 to 700 entries were most of a row's instructions.)
+__device__ __noinline__ Boundary pick(Smem &sm, uint32_t n, Mass goal, bool by_mass, float peak, float rate)
+{
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    constexpr int kParts = 256, kWarpHas = 32;
+    Mass me[kEach];   // 0: none, or not in question any more
+    Parts w[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const uint32_t at = i * kThreads + tid;
+        me[i] = at < n ? sm.list[at] : 0;
+        const float x = logit_of((uint32_t)(me[i] >> 32));
+        w[i] = by_mass && me[i] ? parts_of<kNucleus>(svk::fast_exp2(-__fmul_rn(__fsub_rn(peak, x), rate))) : Parts{0u, me[i] ? 1 : 0};
+    }
+    uint32_t left = n;
+#pragma unroll 1
+    while (left > kWarpHas) {   // (the entries are different numbers: a part of two or more has a smaller range)
+        Mass most = 0, least = ~0ull;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (me[i]) most = max(most, me[i]), least = min(least, me[i]);
+        most = over_warp(most, [](Mass a, Mass b) { return max(a, b); }), least = over_warp(least, [](Mass a, Mass b) { return min(a, b); });
+        __syncthreads();   // (what the round before has found is read)
+        if (lane == 0) sm.sums[warp] = most, sm.scan[warp] = least;
+        if (tid < kParts) sm.high[tid] = 0, sm.low[tid] = 0;
+        __syncthreads();
+        most = over_warp(sm.sums[lane & (kWarps - 1)], [](Mass a, Mass b) { return max(a, b); });
+        least = over_warp(sm.scan[lane & (kWarps - 1)], [](Mass a, Mass b) { return min(a, b); });
+        const int shift = max(0, 64 - 8 - __clzll((long long)(most - least)));   // (most - least) >> shift < kParts
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const uint32_t part = me[i] ? (uint32_t)((most - me[i]) >> shift) : 0u;
+            add_shared(reinterpret_cast<int *>(&sm.high[part]), (int)w[i].high, me[i] && w[i].high);
+            add_shared(&sm.low[part], w[i].low, me[i] && w[i].low);
+        }
+        __syncthreads();
+        if (warp == 0) {
+            Mass v[kParts / 32], mine = 0;
+#pragma unroll
+            for (int i = 0; i < kParts / 32; ++i) mine += v[i] = whole<kNucleus>(sm.high[lane * (kParts / 32) + i], sm.low[lane * (kParts / 32) + i]);
+            const Mass upto = scan_warp(mine);
+            Mass before = upto - mine;
+            if (before < goal && upto >= goal) {
+                int part = lane * (kParts / 32);
+#pragma unroll
+                for (int i = 0; i < kParts / 32 - 1; ++i)
+                    if (before + v[i] < goal && part == lane * (kParts / 32) + i) before += v[i], ++part;
+                sm.found_bin = part, sm.found_ahead = before;
+            }
+        }
+        __syncthreads();
+        const uint32_t found = (uint32_t)sm.found_bin;
+        goal -= sm.found_ahead;
+        left = 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            if (me[i] && (uint32_t)((most - me[i]) >> shift) != found) me[i] = 0;
+            left += __syncthreads_count(me[i] != 0);
+        }
+    }
+    __syncthreads();
+    if (tid == 0) sm.n_list = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        if (!me[i]) continue;
+        const uint32_t at = atomicAdd(&sm.n_list, 1u);
+        sm.sorted[at] = me[i], sm.masses()[at] = whole<kNucleus>(w[i].high, w[i].low);
+    }
+    __syncthreads();
+    if (warp == 0) {
+        const Mass mine = lane < left ? sm.sorted[lane] : 0, weight = lane < left ? sm.masses()[lane] : 0;
+        Mass before = 0;
+#pragma unroll 1
+        for (uint32_t o = 0; o < left; ++o) before += sm.sorted[o] > mine ? sm.masses()[o] : 0;
+        if (lane < left && before < goal && before + weight >= goal) sm.boundary = Boundary{logit_of((uint32_t)(mine >> 32)), ~(uint32_t)mine};
+    }
+    __syncthreads();
+    return sm.boundary;
+}
+
 template <bool kHalf>
 __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_constant__ Params p)
 {
@@ -290,7 +384,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     // the CTA's part of the row as it is read, but for NaNs
     using Held = std::conditional_t<kHalf, __nv_bfloat16, float>;
     Held *const held = reinterpret_cast<Held *>(raw + sizeof(Smem));
-    const auto held1 = [&](int at) { return taken((float)held[at]); };
+    const auto held1 = [&](int at) { return kHalf ? fminf((float)held[at], FLT_MAX) : (float)held[at]; };
     const auto held4 = [&](int at) {
         if constexpr (kHalf) {
             const uint2 w = *reinterpret_cast<const uint2 *>(held + at);
@@ -395,7 +489,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     const auto bits_of = [&](float x) { return __fmul_rn(__fsub_rn(peak, x), rate); };   // -log2 e
     const auto e_of = [&](float x) { return svk::fast_exp2(-bits_of(x)); };
     constexpr float kPlace = 8388608.f;   // (the last place of a sum with it is 1)
-    const auto place_of = [&](float bits) { return __fadd_rn(fminf(__fmul_rn(bits, kBinsPerBit), (float)(kBins - 1)), kPlace); };
+    const auto place_of = [&](float bits) { return fminf(__fmaf_rn(bits, kBinsPerBit, kPlace), kPlace + (float)(kBins - 1)); };
     const auto bin_at = [](float place) { return __float_as_uint(place) & (kBins - 1); };
     const auto each = [&](auto f) {   // f(index, logit), all entries of this lane in ascending order
 #pragma unroll 1
@@ -426,33 +520,40 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         __syncthreads();
     };
     // Counts are kept in units that make them masses of the nucleus' kind.
-    const auto add_one = [&](uint32_t bin) { atomicAdd(&sm.low[bin], 1); };
-    // Entries for which `in` holds, sorted, in every CTA; their number (over kList: there is no list).
-    const auto gather = [&](auto in) {
-        each([&](int i, float x) {
-            if (in(x, (uint32_t)i)) {
-                const uint32_t at = atomicAdd(&sm.n_list, 1u);
-                if (at < kList) sm.list[at] = (uint64_t)key_of(x) << 32 | (uint32_t)~i;
+    const auto add_one = [&](uint32_t bin, bool really) { add_shared(&sm.low[bin], 1, really); };
+    // Entries for which `in` holds, in every CTA, sorted where that is asked for; their number (over kList: there is no list).
+    const auto gather = [&](bool sort, auto in) {
+#pragma unroll 1
+        for (int j = 0; j < words; ++j) {   // (four entries, a branch for all of them)
+            const int at = w0 + j * 128;
+            const float4 v = held4(at);
+            uint32_t found = (uint32_t)in(v.x, first + at) | (uint32_t)in(v.y, first + at + 1) << 1 | (uint32_t)in(v.z, first + at + 2) << 2 |
+                             (uint32_t)in(v.w, first + at + 3) << 3;
+#pragma unroll 1
+            for (; found; found &= found - 1) {
+                const int e = __ffs(found) - 1;
+                const uint32_t to = atomicAdd(&sm.n_list, 1u);
+                if (to < kList) sm.list[to] = (Mass)key_of(held1(at + e)) << 32 | (uint32_t)~(first + at + e);
             }
-        });
-        return collect(sm, turn ^= 1, mine);
+        }
+        return collect(sm, turn ^= 1, mine, sort);
     };
 
     Boundary last{-FLT_MAX, 0xffffffffu};   // all of them
     const bool by_count = k > 0 && k < p.V, by_mass = top_p < 1.f;
     bool listed = false;   // the sorted list begins with all entries that stay
     uint32_t n_listed = 0;
-    bool drawn = false;    // of_cta[turn] is what stays of the CTAs but for the list, and `sorted` up to `last` the rest, in masses of the nucleus
+    bool drawn = false;    // of_cta[turn] is what stays of the CTAs but for the list, and the list up to `last` the rest, in masses of the nucleus
     for (int step = 0; step < 2 && !listed; ++step) {
         if (!(step ? by_mass : by_count)) continue;
         Found found;
         if (step == 0) {
             // the k-th largest of the threads' maxima
-            if (most > -INFINITY) add_one(bin_at(place_of(bits_of(most))));
+            add_one(bin_at(place_of(bits_of(most))), most > -INFINITY);
             found = find_bin((Mass)k, 0.f);
             if (found.bin >= 0) {
                 const float place = kPlace + found.bin;
-                const uint32_t n = gather([&](float x, uint32_t) { return x > -INFINITY && place_of(bits_of(x)) <= place; });
+                const uint32_t n = gather(true, [&](float x, uint32_t) { return (x > -INFINITY) & (place_of(bits_of(x)) <= place); });
                 if (n <= kList) {
                     listed = true, n_listed = n;
                     break;
@@ -461,14 +562,14 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         }
         const Boundary within = last;
         const auto weight = [&](float x) { return step ? mass_of<kNucleus>(e_of(x)) : 1ull; };
-        const auto add = [&](uint32_t bin, float bits) {
+        const auto add = [&](uint32_t bin, float bits, bool really) {
             if (step == 0) {
-                add_one(bin);
+                add_one(bin, really);
                 return;
             }
             const Parts q = parts_of<kNucleus>(svk::fast_exp2(-bits));
-            if (q.high) atomicAdd(&sm.high[bin], q.high);
-            if (q.low) atomicAdd(&sm.low[bin], q.low);
+            add_shared(reinterpret_cast<int *>(&sm.high[bin]), (int)q.high, really & (q.high != 0));
+            add_shared(&sm.low[bin], q.low, really & (q.low != 0));
         };
         // first histogram: by the distance from the maximum
         if (by_count) {   // (else it still is clear)
@@ -477,13 +578,12 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         }
         if (step == 0) {
             each([&](int, float x) {
-                if (x > -INFINITY) add_one(bin_at(place_of(bits_of(x))));
+                add_one(bin_at(place_of(bits_of(x))), x > -INFINITY);
             });
         } else {
             each([&](int i, float x) {   // (an entry that is not there has no mass)
-                if (by_count && !within.keeps(x, i)) return;
                 const float bits = bits_of(x);
-                add(bin_at(place_of(bits)), bits);
+                add(bin_at(place_of(bits)), bits, !by_count || within.keeps(x, i));
             });
         }
         found = find_bin(step ? 0 : (Mass)k, top_p);
@@ -502,7 +602,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         __syncthreads();
         if (tid == 0) sm.n_list = 0;
         __syncthreads();
-        uint32_t n = gather([&](float x, uint32_t i) { return place_of(bits_of(x)) == place && within.keeps(x, i); });
+        uint32_t n = gather(false, [&](float x, uint32_t i) { return (place_of(bits_of(x)) == place) & within.keeps(x, i); });
         drawn = drawn && n <= kList;
         // too many: the keys of the bin, then of a part of them, divided evenly
         uint32_t lo = 0, hi = 0;
@@ -526,10 +626,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         }
         while (n > kList && lo < hi) {
             const int shift = max(0, 32 - __clz(hi - lo) - 11);   // (hi - lo) >> shift < kBins
-            const auto in = [&](float x, uint32_t i) { return x > -INFINITY && key_of(x) >= lo && key_of(x) <= hi && within.keeps(x, i); };
+            const auto in = [&](float x, uint32_t i) { return (x > -INFINITY) & (key_of(x) >= lo) & (key_of(x) <= hi) & within.keeps(x, i); };
             clear();
             each([&](int i, float x) {
-                if (in(x, i)) add((hi - key_of(x)) >> shift, bits_of(x));
+                const bool is = in(x, i);
+                add(is ? (hi - key_of(x)) >> shift : 0u, bits_of(x), is);
             });
             found = find_bin(goal - ahead, 0.f);
             const int b = found.bin;
@@ -539,26 +640,15 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
             __syncthreads();
             if (tid == 0) sm.n_list = 0;
             __syncthreads();
-            n = gather(in);
+            n = gather(false, in);
         }
         const auto is_last = [&](float x, uint32_t i) {
 #pragma unroll 1
             for (int c = 0; c < CL; ++c) *cluster.map_shared_rank(&sm.boundary, c) = Boundary{x, i};
         };
-        if (n <= kList) {   // by the sorted list, which every CTA has
-            Mass sum = ahead;
-#pragma unroll 1
-            for (uint32_t base = 0; base < n; base += kThreads) {
-                const bool in = base + tid < n;
-                const uint64_t me = in ? sm.sorted[base + tid] : 0;
-                const Mass w = in ? weight(logit_of((uint32_t)(me >> 32))) : 0;
-                const Scan scan = scan_block(sm, w);
-                const Mass before = sum + scan.before;
-                if (in && before < goal && before + w >= goal) sm.boundary = Boundary{logit_of((uint32_t)(me >> 32)), ~(uint32_t)me};
-                sum += scan.total;
-            }
+        if (n <= kList) {   // by the list, which every CTA has
+            last = pick(sm, n, goal - ahead, step != 0, peak, rate);
             n_listed = n;
-            __syncthreads();
         } else {   // all equal: counted off in the order of the vocabulary
             const float x_all = logit_of(hi);
             const Mass one = weight(x_all), nth = (goal - ahead + one - 1) / one;   // the nth of them (from 1) is the last
@@ -582,11 +672,15 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
                 before += __shfl_sync(0xffffffffu, upto, 31);
             }
             cluster.sync();
+            last = sm.boundary;
         }
-        last = sm.boundary;
     }
     if (listed || drawn) svk::cluster_arrive();   // nobody leaves while another CTA reads its list
 
+    const auto stays = [&](float x, uint32_t i) {   // e of an entry that stays, 0 of others
+        const float e = e_of(x);
+        return last.keeps(x, i) & ((e >= min_e) | (x == peak)) ? e : 0.f;
+    };
     Mass total;   // of the draw
     float scale = 1099511627776.f;   // ... and what the largest entry counts
     if (listed) {
@@ -637,19 +731,14 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     } else {
         // the mass that stays, by CTA; of the CTA in which the target lies by warp, word and entry
         const auto mass = [&](float x, uint32_t i) -> Mass {
-            if (!last.keeps(x, i)) return 0;
-            const float e = e_of(x);
-            if (!(e >= min_e || x == peak)) return 0;
+            const float e = stays(x, i);
             return drawn ? mass_of<kNucleus>(e) : mass_of<kDraw>(e);
         };
         if (!drawn) {
             uint32_t high = 0;   // (a lane has at most 96 entries)
             int low = 0;
             each([&](int i, float x) {
-                if (!last.keeps(x, i)) return;
-                const float e = e_of(x);
-                if (!(e >= min_e || x == peak)) return;
-                const Parts q = parts_of<kDraw>(e);
+                const Parts q = parts_of<kDraw>(stays(x, i));
                 high += q.high, low += q.low;
             });
             mine = whole<kDraw>(high, low);
@@ -661,9 +750,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
                 Mass m = 0;
 #pragma unroll 1
                 for (uint32_t i = lane; i < n_listed; i += 32) {
-                    const uint64_t entry = sm.sorted[i];
+                    const uint64_t entry = sm.list[i];
                     const uint32_t index = ~(uint32_t)entry;
-                    if ((int)(index / (uint32_t)p.part) == warp) m += mass(logit_of((uint32_t)(entry >> 32)), index);
+                    if (index - (uint32_t)(warp * p.part) < (uint32_t)p.part) m += mass(logit_of((uint32_t)(entry >> 32)), index);
                 }
                 m = sum_over_warp(m);
                 if (lane == 0) sm.sums[warp] = sm.of_cta[turn][warp] + m;
@@ -690,7 +779,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
                     uint32_t high = 0;
                     int low = 0;
                     each([&](int i, float x) {
-                        const Parts q = last.keeps(x, i) ? parts_of<kNucleus>(e_of(x)) : Parts{0u, 0};
+                        const Parts q = parts_of<kNucleus>(stays(x, i));
                         high += q.high, low += q.low;
                     });
                     mine = sum_over_warp(whole<kNucleus>(high, low));
@@ -727,20 +816,22 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         return;
     }
     const float inv = scale / (float)total;
-    const auto prob = [&](float x, uint32_t i) {
-        if (!last.keeps(x, i)) return 0.f;
-        const float e = e_of(x);
-        return e >= min_e || x == peak ? e * inv : 0.f;
-    };
+    const auto prob = [&](float x, uint32_t i) { return stays(x, i) * inv; };
     float *const to = p.probs + (size_t)r * p.V + first;
     const int n_wide = (reinterpret_cast<uintptr_t>(to) & 15) == 0 ? max(0, n_here) / 4 * 4 : 0;
 #pragma unroll 2
     for (int at = tid * 4; at < n_wide; at += kThreads * 4) {
         const float4 v = held4(at);
-        *reinterpret_cast<float4 *>(to + at) = make_float4(prob(v.x, first + at), prob(v.y, first + at + 1), prob(v.z, first + at + 2), prob(v.w, first + at + 3));
+        float4 out = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)) >= last.x)   // (of a short top-k hardly any)
+            out = make_float4(prob(v.x, first + at), prob(v.y, first + at + 1), prob(v.z, first + at + 2), prob(v.w, first + at + 3));
+        *reinterpret_cast<float4 *>(to + at) = out;
     }
 #pragma unroll 4
-    for (int at = n_wide + tid; at < n_here; at += kThreads) to[at] = prob(held1(at), first + at);
+    for (int at = n_wide + tid; at < n_here; at += kThreads) {
+        const float x = held1(at);
+        to[at] = x >= last.x ? prob(x, first + at) : 0.f;
+    }
     if (listed || drawn) svk::cluster_wait();
 }
 
