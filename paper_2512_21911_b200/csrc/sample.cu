@@ -3,9 +3,10 @@
 // Mathematics: e(x) = 2^((x - max) log2 e / temperature).  The entries are never sorted: what stays is everything up to one entry, the
 // boundary (logit, index), in the order "larger logit first, then smaller index".  Search for the boundary by count (top-k) or mass
 // (top-p): a histogram of the entries by their distance from the maximum, the bin in which the goal is reached, and the few entries of
-// that bin, divided again in the same way until a warp has them.  A bin with too many of them is divided again by the bits of its keys; entries that are all equal are counted
-// off by index.  For a short top-k the histogram holds the threads' maxima only: the k-th largest of these bounds the k-th entry from
-// below, all entries up to its bin are ranked at once, and top-p, min-p and the token follow from that list.
+// that bin, divided again in the same way until a warp has them.  A bin with too many of them is divided again by the bits of its keys;
+// entries that are all equal are counted off by index.  For a short top-k the histogram holds the threads' maxima only: the k-th largest
+// of these bounds the k-th entry from below, all entries up to its bin are ranked at once, and top-p, min-p and the token follow from
+// that list.
 //
 // Sums of masses are sums of whole numbers, exact in any order.  Of the nucleus: multiples of 2^-32 of the largest entry's mass, so that a
 // bin is two 32-bit words that shared-memory atomics add to (2^-32 is less than fp32 sums keep; what is lost are entries below 2^-33 of
@@ -248,8 +249,8 @@ __device__ __noinline__ Found find_in_bins(Smem &sm, Mass goal, float of_all)
     __syncthreads();
     return {sm.found_bin, sm.found_goal, sm.found_ahead};
 }
-// All CTAs' lists behind this one's own, and sorted where that is asked for; their length (over kList: there is no list).  mine: what the CTA tells the others,
-// into of_cta[turn].  The lists have to stay until the cluster's next barrier.
+// All CTAs' lists behind this one's own, and sorted where that is asked for; their length (over kList: there is no list).  mine: what the
+// CTA tells the others, into of_cta[turn].  The lists have to stay until the cluster's next barrier.
 __device__ __noinline__ uint32_t collect(Smem &sm, int turn, Mass mine, bool sort)
 {
     const cg::cluster_group cluster = cg::this_cluster();
@@ -293,9 +294,9 @@ __device__ __noinline__ uint32_t collect(Smem &sm, int turn, Mass mine, bool sor
     return n;
 }
 
-// Of the list's n entries, in their order, the one that brings the sum of their weights to the goal (it exists): divided into 256 parts of
-// their range by sums as in the large histogram, the part of the goal divided again until a warp has what is left of it.  (Ranked one against
-// another by all CTAs, 300 to 700 entries were most of a row's instructions.)
+// Of the list's n entries, in their order, the one that brings the sum of their weights to the goal (it exists): divided into 256 parts
+// of their range by sums as in the large histogram, the part of the goal divided again until a warp has what is left of it.  (Ranked one
+// against another by all CTAs, 300 to 700 entries were most of a row's instructions.)
 __device__ __noinline__ Boundary pick(Smem &sm, uint32_t n, Mass goal, bool by_mass, float peak, float rate)
 {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;

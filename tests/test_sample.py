@@ -197,6 +197,36 @@ def test_many_entries_of_nearly_the_same_logit():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("half", [False, True])
+@pytest.mark.parametrize("n", [1, 31, 32, 33, 255, 300, 512, 513, 767, 768, 769, 1500])
+def test_the_boundary_lies_among_n_neighbours(n, half):
+    """2,000 entries ahead, n of nearly or exactly the same logit, 5,000 behind; the boundary at the first, inside and at the last of the n."""
+    V = 9000
+    g = np.random.default_rng(n)
+    places = np.stack([g.permutation(V) for _ in range(9)])
+    x = np.full((9, V), -9.0, np.float32)
+    step = np.float32(2.0 ** -20)
+    for i in range(9):
+        near = [np.arange(n) * step, np.zeros(n), (np.arange(n) % 3 == 0) * step][i // 3].astype(np.float32)
+        x[i, places[i, :2000]] = g.uniform(-1, 2, 2000)
+        x[i, places[i, 2000:2000 + n]] = np.float32(-3) + near
+        x[i, places[i, 2000 + n:2000 + n + 5000]] = g.uniform(-8, -4, 5000)
+    logits = torch.from_numpy(x).cuda()
+    if half:
+        logits = logits.bfloat16()
+        x = logits.float().cpu().numpy()
+    u = g.random(9).astype(np.float32)
+    k = np.int32([2000 + m for m in (1, (n + 1) // 2, n)] * 3)
+    tokens, p = _sample(logits, u, k=k)
+    _check_rows(x, u, tokens, p, k=k)
+    for kw in (dict(), dict(k=np.full(9, 2000 + n, np.int32))):
+        _, ahead = zip(*[_rule(row, k=None if not kw else 2000 + n) for row in x])
+        top_p = np.float32([(a[at - 1] + a[at]) / 2 for a, at in zip(ahead, k)])   # (entry number k is the last that begins below it)
+        tokens, p = _sample(logits, u, top_p=top_p, **kw)
+        _check_rows(x, u, tokens, p, top_p=top_p, **kw)
+
+
+@pytest.mark.gpu
 def test_tokens_follow_the_distribution_and_u_of_zero_and_one():
     V, R = 50, 4000
     logits = _logits(1, V, 3).expand(R, V).contiguous()
