@@ -16,13 +16,14 @@
 // A cluster of 1 to 8 CTAs per row; a CTA keeps its part of the row in shared memory, so the logits are read once from HBM (19.5 MB of 19.4
 // for 64 bfloat16 rows of 151,936).  Warps own contiguous parts: a token is found by sums per CTA, warp and lane.
 //
-// Bound by the instructions of the passes (some 30 an entry for the histogram, 14 to gather a bin, 18 for the probabilities) and by the
+// Bound by the instructions of the passes (some 26 an entry for the histogram, 10 to gather a bin, 18 for the probabilities) and by the
 // steps between them (a barrier of the cluster is 1.8 us), two CTAs an SM overlapping one's steps with the other's passes: warps issue in
 // half of the cycles, and HBM, whose floor for these cases is 3 to 12 us, idles.  Measured: one row of 128,256 with a top-k of 50 12.8 us;
-// 64 bfloat16 rows of 151,936 with a nucleus 50 us, one round of clusters of four; 80 rows of 128,256 with a nucleus and their
-// distributions 77 us, three rounds of clusters of eight (12 of them the load, 10 the probabilities); 256 rows of 32,003 with top-k, min-p
-// and distributions 38 us.  Tests of an entry are written without branches, of which a pass had 20 an entry before (one row 13.7, then
-// 57, 84 and 40 us, with lists ranked entry against entry by every CTA).
+// 64 bfloat16 rows of 151,936 with a nucleus 48 us, one round of clusters of four; 80 rows of 128,256 with a nucleus and their
+// distributions 75 us, three rounds of clusters of eight (12 of them the load, 10 the probabilities); 256 rows of 32,003 with top-k, min-p
+// and distributions 37.5 us.  Tests of an entry are written without branches, of which a pass had 20 an entry before (one row 13.7, then
+// 57, 84 and 40 us, with lists ranked entry against entry by every CTA).  A histogram of its own for rows without a top-k takes 46 us for
+// the 64 rows and 13.7 for the one, by more code to fetch.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <float.h>
@@ -141,10 +142,9 @@ __device__ __forceinline__ T scan_warp(T v)   // inclusive
 }
 
 // (one instruction with a predicate: as a branch it was a quarter of a pass)
-__device__ __forceinline__ void add_shared(int *at, int v, bool really)
+__device__ __forceinline__ void add_shared(uint32_t at, int v)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\t@p red.shared.add.u32 [%0], %1;\n\t}" ::"r"(svk::smem_u32(at)), "r"(v), "r"((int)really)
-                 : "memory");
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %1, 0;\n\t@p red.shared.add.u32 [%0], %1;\n\t}" ::"r"(at), "r"(v) : "memory");
 }
 
 // The cluster's CTAs, and a word of this CTA's shared memory in each of them (one warp).
@@ -328,8 +328,7 @@ __device__ __noinline__ Boundary pick(Smem &sm, uint32_t n, Mass goal, bool by_m
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const uint32_t part = me[i] ? (uint32_t)((most - me[i]) >> shift) : 0u;
-            add_shared(reinterpret_cast<int *>(&sm.high[part]), (int)w[i].high, me[i] && w[i].high);
-            add_shared(&sm.low[part], w[i].low, me[i] && w[i].low);
+            if (me[i]) add_shared(svk::smem_u32(&sm.high[part]), (int)w[i].high), add_shared(svk::smem_u32(&sm.low[part]), w[i].low);
         }
         __syncthreads();
         if (warp == 0) {
@@ -521,7 +520,12 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         __syncthreads();
     };
     // Counts are kept in units that make them masses of the nucleus' kind.
-    const auto add_one = [&](uint32_t bin, bool really) { add_shared(&sm.low[bin], 1, really); };
+    const uint32_t bins = svk::smem_u32(sm.high), lows = svk::smem_u32(sm.low);
+    const auto add_one = [&](uint32_t bin, bool really) { add_shared(lows + 4 * bin, really); };
+    const auto add_mass = [&](uint32_t bin, float bits, bool really) {
+        const Parts q = parts_of<kNucleus>(really ? svk::fast_exp2(-bits) : 0.f);
+        add_shared(bins + 4 * bin, (int)q.high), add_shared(lows + 4 * bin, q.low);
+    };
     // Entries for which `in` holds, in every CTA, sorted where that is asked for; their number (over kList: there is no list).
     const auto gather = [&](bool sort, auto in) {
 #pragma unroll 1
@@ -564,13 +568,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         const Boundary within = last;
         const auto weight = [&](float x) { return step ? mass_of<kNucleus>(e_of(x)) : 1ull; };
         const auto add = [&](uint32_t bin, float bits, bool really) {
-            if (step == 0) {
-                add_one(bin, really);
-                return;
-            }
-            const Parts q = parts_of<kNucleus>(svk::fast_exp2(-bits));
-            add_shared(reinterpret_cast<int *>(&sm.high[bin]), (int)q.high, really & (q.high != 0));
-            add_shared(&sm.low[bin], q.low, really & (q.low != 0));
+            if (step == 0) add_one(bin, really);
+            else add_mass(bin, bits, really);
         };
         // first histogram: by the distance from the maximum
         if (by_count) {   // (else it still is clear)
@@ -584,7 +583,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         } else {
             each([&](int i, float x) {   // (an entry that is not there has no mass)
                 const float bits = bits_of(x);
-                add(bin_at(place_of(bits)), bits, !by_count || within.keeps(x, i));
+                add_mass(bin_at(place_of(bits)), bits, !by_count || within.keeps(x, i));
             });
         }
         found = find_bin(step ? 0 : (Mass)k, top_p);
@@ -603,7 +602,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         __syncthreads();
         if (tid == 0) sm.n_list = 0;
         __syncthreads();
-        uint32_t n = gather(false, [&](float x, uint32_t i) { return (place_of(bits_of(x)) == place) & within.keeps(x, i); });
+        uint32_t n = step && by_count ? gather(false, [&](float x, uint32_t i) { return (place_of(bits_of(x)) == place) & within.keeps(x, i); })
+                                      : gather(false, [&](float x, uint32_t) { return (place_of(bits_of(x)) == place) & (x > -INFINITY); });
         drawn = drawn && n <= kList;
         // too many: the keys of the bin, then of a part of them, divided evenly
         uint32_t lo = 0, hi = 0;
