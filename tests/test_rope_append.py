@@ -131,6 +131,18 @@ def test_ragged_batches(B, rot, interleaved):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rot,interleaved", [(128, False), (64, True)])
+@pytest.mark.parametrize("last", [1, 2, 9])
+def test_on_either_side_of_the_size_that_changes_the_tiles(last, rot, interleaved):
+    """1,024 tokens and a few more, of sequences that begin inside a tile of tokens; odd numbers of heads."""
+    import paper_2512_21911_b200 as sv
+    before, new = [10, 0, 64, 3, 700], [501, 5, 1, 516, last]
+    for Hq, Hkv in ((1, 1), (5, 1), (33, 3)):
+        t = _batch(sv, before, new, Hq, Hkv, 64, rot, interleaved, True, seed=last + Hq)
+        _check(sv, t, before, new)
+
+
+@pytest.mark.gpu
 def test_many_sequences_of_one_token():
     """More sequences than a CTA has threads, lengths at and around the ends of blocks, some of them empty."""
     import paper_2512_21911_b200 as sv
