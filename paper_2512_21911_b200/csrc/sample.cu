@@ -399,6 +399,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int first = rank * p.part, n_here = min(p.part, p.V - first);   // entries of this CTA (possibly none), from `first` on
     const int words = p.part / kGrain, w0 = warp * (p.part / kWarps) + lane * 4;   // a lane's words of four entries: w0, w0 + 128, ...
+    svk::cluster_arrive();   // (waited for behind the load, which hides it)
     svk::grid_dependency_wait();
     svk::grid_launch_dependents();
 
@@ -472,6 +473,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     for (int i = tid; i < kBins; i += kThreads) sm.high[i] = 0, sm.low[i] = 0;
     if (tid == 0) sm.n_list = 0;
     __syncthreads();
+    svk::cluster_wait();   // every CTA of the cluster is running: its shared memory may be written from here on
     if (warp == 0) {
         const float top = over_warp(sm.of_warp[lane & (kWarps - 1)], [](float a, float b) { return fmaxf(a, b); });
         everywhere(&sm.top_of_cta[rank], top);
