@@ -1,0 +1,51 @@
+"""sv_sample where an entry stays or goes by little: goals next to an edge between two entries, limits of the parameters, the largest
+vocabularies."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+def _draw(x, u=None, **parameters):
+    """Tokens and distributions of rows x (a CUDA tensor), parameters one a row."""
+    import paper_2512_21911_b200 as sv
+    R, V = x.shape
+    tokens, probs = torch.full((R,), -9, dtype=torch.int32, device="cuda"), torch.full((R, V), 7.0, device="cuda")
+    types = dict(top_k=torch.int32)
+    sv.sv_sample(x, torch.full((R,), 0.5, device="cuda") if u is None else u, tokens, probs=probs,
+                 **{k: torch.as_tensor(v, dtype=types.get(k, torch.float32), device="cuda") for k, v in parameters.items()})
+    return tokens, probs
+
+
+def test_the_rate_keeps_more_bits_than_a_float():
+    """Half of the mass in one entry, half in 2^17 of them 16 to 18 powers of two below, and temperatures whose log2 e / T is half a unit of
+    its last place away from a float.  A rate rounded to a float is off by up to 2^-24, which changes the 2^17 by 17 ln 2 2^-24 = 7e-7 of
+    themselves and the sums between them by a quarter of that, 1.8e-7 of the whole.  Exponentials good to 2^-22 change the sums by 6e-8 at
+    most (all of them off the same way); the other roundings are a hundred thousand independent ones.  So goals from 9e-8 on beside an edge
+    between entries have to fall on the right side of it."""
+    rng = np.random.default_rng(0)
+    rate = lambda T: math.log2(math.e) / float(T)
+    off = lambda T: float(np.float32(rate(T))) / rate(T) - 1
+    Ts = [T for T in rng.uniform(0.5, 1.5, 4000).astype(np.float32) if abs(off(T)) > 0.85 * 2.0 ** -24]
+    Ts = [T for T in Ts if off(T) > 0][:8] + [T for T in Ts if off(T) < 0][:8]
+    assert len(Ts) == 16
+    rows, top_p, want = [], [], []
+    for T in Ts:
+        x = np.concatenate([[0.0], -(16 + 2 * rng.random(1 << 17)) * math.log(2) * float(T)]).astype(np.float32)
+        order = np.argsort(-x, kind="stable")
+        edge = np.cumsum(np.exp(x[order].astype(np.float64) / float(T)))
+        edge /= edge[-1]
+        for side in (-1, 1):
+            p = np.float32(edge + side * 1.05e-7)     # a float next to every edge, the first of them that is as near as wanted
+            far = side * (p.astype(np.float64) - edge)
+            n = int(np.nonzero((far >= 0.9e-7) & (far <= 1.2e-7) & (edge > 0.6) & (edge < 0.9))[0][0])
+            keep = order[:n + 1 + (side > 0)]         # the entries that begin below the goal
+            rows.append(x), top_p.append(p[n]), want.append(np.sort(keep))
+    logits = torch.from_numpy(np.stack(rows)).cuda()
+    _, probs = _draw(logits, temperature=np.repeat(np.float32(Ts), 2), top_p=np.float32(top_p))
+    kept = (probs > 0).cpu().numpy()
+    wrong = [(i, int(kept[i].sum()) - len(w)) for i, w in enumerate(want) if not np.array_equal(np.nonzero(kept[i])[0], w)]
+    assert not wrong, wrong
