@@ -502,7 +502,9 @@ SV_API sv_status sv_rope_append(const sv_geom *geom, void *k_pool, void *v_pool,
  * Attention of such a batch over the cache that holds its own keys and values already (sv_rope_append): kv->seq_lens counts the new
  * tokens too, so that row i of sequence s, of n rows, is at position p = seq_lens[s] - n + i and sees the cached tokens 0 .. p:
  * softmax(softmax_scale * q . k) . v.  fp32 softmax and accumulation; probabilities are rounded to bf16 for the PV product.  A row that
- * sees nothing (p < 0) has an output of zeros and an lse of -infinity.  Single tokens, chunks and whole prompts may share a batch: the
+ * sees nothing (p < 0) has an output of zeros and an lse of -infinity; one that sees a NaN or an infinite score, or scores of -infinity
+ * alone, has the NaN that softmax gives.  Keys behind a row, and everything in slots that hold no token, may be anything; the values of
+ * later tokens of the same call enter with a weight of zero and have to be finite.  Single tokens, chunks and whole prompts may share a batch: the
  * keys of long sequences are split over the SMs and merged, so that a batch costs what its tokens cost however they are distributed.
  *   q               dev bf16 [N][Hq][D] contiguous
  *   q_start         dev int32 [S + 1], as above

@@ -91,7 +91,8 @@ struct Params {
     float *lse;
     float *ws_o;      // [2 * gridDim.x][slot_rows][128]: of a CTA, the share of an item that began before and of one that goes on behind
     float2 *ws_ml;    // [2 * gridDim.x][slot_rows]
-    int4 *cuts;       // [gridDim.x] the cut item that begins in a CTA's share: first row, tokens, KV head, parts (0: none)
+    int4 *cuts;       // [gridDim.x] the cut item that begins in a CTA's share: first row, tokens, KV head and (in the upper half) how many of
+                      // the tokens see no key, parts (0: none)
     int32_t *status;
     int Hq, Hkv, G, TT, B, NBmax, n_pages, slot_rows;
     float scale_log2;
@@ -656,7 +657,7 @@ __device__ __forceinline__ void softmax(const Params &p, const Shared sh, uint32
             }
             const int tokens = sh.item(n, kTokens), u0 = sh.item(n, kU0);
             const bool whole = u0 == 0 && sh.item(n, kU1) == sh.item(n, kUnits);
-            bool real[2];
+            bool real[2], blind[2];   // (blind: no key; a row that sees keys keeps what their scores made of it, a NaN too)
             size_t row[2], part[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -664,7 +665,8 @@ __device__ __forceinline__ void softmax(const Params &p, const Shared sh, uint32
                 real[h] = r < p.G * p.TT && token < tokens;
                 row[h] = (size_t)(sh.item(n, kRow0) + token) * p.Hq + sh.item(n, kHead) * p.G + r % p.G;
                 part[h] = ((size_t)blockIdx.x * 2 + (u0 == 0)) * p.slot_rows + (two ? g * 128 : 0) + r;
-                const float inv = !whole ? 1.f : l[h] > 0.f ? 1.f / l[h] : 0.f;
+                blind[h] = sees[h] + 2 * q <= 0;
+                const float inv = !whole ? 1.f : 1.f / l[h];
                 w0[h] *= inv, w1[h] *= inv;
             }
 #pragma unroll 1
@@ -691,7 +693,7 @@ __device__ __forceinline__ void softmax(const Params &p, const Shared sh, uint32
                     if (whole) {   // 16 bytes a lane, 64 consecutive ones a row
                         uint32_t w[4];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) w[i] = l[h] > 0.f ? pack_bf16(o[4 * i + 2 * h], o[4 * i + 2 * h + 1]) : 0u;
+                        for (int i = 0; i < 4; ++i) w[i] = blind[h] ? 0u : pack_bf16(o[4 * i + 2 * h], o[4 * i + 2 * h + 1]);
                         transpose_4(w, q);
                         if (real[h]) *reinterpret_cast<uint4 *>(p.out + row[h] * 128 + o0 + 8 * q) = make_uint4(w[0], w[1], w[2], w[3]);
                     } else if (real[h]) {
@@ -706,10 +708,10 @@ __device__ __forceinline__ void softmax(const Params &p, const Shared sh, uint32
             for (int h = 0; h < 2; ++h) {
                 if (q || !real[h]) continue;
                 if (!whole) p.ws_ml[part[h]] = make_float2(m[h], l[h]);
-                else if (p.lse) p.lse[row[h]] = l[h] > 0.f ? (m[h] + log2f(l[h])) * 0.69314718055994531f : -INFINITY;
+                else if (p.lse) p.lse[row[h]] = blind[h] ? -INFINITY : (m[h] + log2f(l[h])) * 0.69314718055994531f;
             }
             const int parts = sh.item(n, kParts);
-            if (threadIdx.x == 0 && parts) p.cuts[blockIdx.x] = make_int4(sh.item(n, kRow0), tokens, sh.item(n, kHead), parts);
+            if (threadIdx.x == 0 && parts) p.cuts[blockIdx.x] = make_int4(sh.item(n, kRow0), tokens, sh.item(n, kHead) | min(max(-sh.item(n, kPos0), 0), tokens) << 16, parts);
         }
         tc_fence_before_sync();
         taken(sh, n);
@@ -795,9 +797,10 @@ __global__ void __launch_bounds__(kMergeRows * 32) chunk_merge_kernel(const __gr
         }
         sum.add(ml, o);
     }
-    const size_t row = (size_t)(cut.x + token) * p.Hq + cut.z * p.G + r % p.G;
-    reinterpret_cast<uint2 *>(p.out + row * 128)[lane] = sum.l > 0.f ? sum.out() : make_uint2(0u, 0u);
-    if (p.lse && lane == 0) p.lse[row] = sum.l > 0.f ? sum.lse() : -INFINITY;
+    const bool blind = token < (int)((unsigned)cut.z >> 16);
+    const size_t row = (size_t)(cut.x + token) * p.Hq + (cut.z & 0xffff) * p.G + r % p.G;
+    reinterpret_cast<uint2 *>(p.out + row * 128)[lane] = blind ? make_uint2(0u, 0u) : sum.out();
+    if (p.lse && lane == 0) p.lse[row] = blind ? -INFINITY : sum.lse();
 }
 
 // Rows of a partial: the rows of the batch where these are one tile at most.
