@@ -83,7 +83,7 @@ SV_API const char *sv_strerror(sv_status st);
  *                         that never completed); the CTA drained and returned
  *   SV_STATUS_INDEX       a block index in sel_idx or a page id in block_table lay outside its table; it was
  *                         clamped into the table before any address was formed, so nothing out of range
- *                         was read
+ *                         was read; or sv_rope_append had no pages for some of its tokens
  *   SV_STATUS_NO_LIST     a count in sel_cnt was negative: sv_select_blocks writes -1 there when it had to
  *                         give up on a list; the attention then covered the draft tokens only
  * sv_status_word_check maps a word read back by the caller to a status: SV_OK, SV_ERR_INDEX
@@ -486,7 +486,9 @@ SV_API sv_status sv_verify_step_from_host_direct(const sv_geom *geom, const sv_l
  *                   position outside the table takes its nearest row and sets SV_STATUS_INDEX
  *   q_out           dev bf16 [N][Hq][D] contiguous; may be q itself
  *   k_pool, v_pool  as in sv_kv_append, modified in place; block_table must hold pages for the blocks that are entered: tokens behind the
- *                   last page of the table, or from a block on whose entry is not a page of the pool, are dropped
+ *                   last page of the table, or from a block on whose entry is not a page of the pool, are dropped (so are those of a
+ *                   sequence of negative length) and set SV_STATUS_INDEX: seq_lens_out then counts fewer tokens than the batch has, and
+ *                   sv_chunk_attn on it would place the batch's rows too far ahead
  *   seq_lens_out    dev int32 [S], a different buffer than seq_lens: the lengths with the tokens that were written
  *   reps            dev fp32 [S][Hkv][NBmax][D] or NULL: the representatives of the blocks that received tokens, bit for bit those of
  *                   sv_block_reps

@@ -142,7 +142,10 @@ __device__ __forceinline__ void append_block(const Params &p, int slot, int h)
             const int end = (int)min((long long)L + n_all, (long long)p.NBmax * B);
             Ln = end <= L ? L : max(L, min(end, room((end - 1) / B) * B));
         }
-        if (tid == 0) p.seq_lens_out[s] = Ln;
+        if (tid == 0) {
+            p.seq_lens_out[s] = Ln;
+            if (p.status && Ln != (long long)L + n_all) atomicOr(p.status, svk::kStatusIndex);   // tokens were dropped
+        }
     }
     const int b = b0 + j;
     if (L < 0 || n_all == 0 || b >= p.NBmax || (long long)b * B >= (long long)L + n_all || room(b) <= b) return;

@@ -380,8 +380,8 @@ class SparseVerifier:
 
     def check_status(self) -> None:
         """Read the device status word back (this synchronises with the stream) and raise if a kernel gave up
-        on a bounded wait, clamped a block index or page id, or met a list that block selection marked invalid
-        (count -1).  The outputs written since the word was last zero are then invalid."""
+        on a bounded wait, clamped a block index or page id, had no pages for new tokens (prefill_layer), or met a
+        list that block selection marked invalid (count -1).  The outputs written since the word was last zero are then invalid."""
         st = sv.sv_status_word_check(int(self.status.item()))
         if st == sv.SV_OK and int(self._lists_cnt.min().item()) < 0:
             st = 9   # SV_ERR_INDEX: a list marked invalid that no attention call has consumed yet
