@@ -47,10 +47,16 @@ class Decoder:
         return torch.cat([a * cos - b * sin, b * cos + a * sin], -1).to(torch.bfloat16)
 
 
+def most_tokens(prompts, new):
+    """Room that the longest sequence may need.  A step gives every sequence one token at least, so there are at most new - 1 of them; the
+    sequence behind the longest prompt may keep all DRAFT rows of each, and the last step's rows are written behind those."""
+    return max(map(len, prompts)) + max(0, new - 1) * DRAFT
+
+
 def generate(prompts, new, layers=4, chunk=512, seed=0, temperature=0.8, top_p=0.95):
     """Token lists of the prompts' continuations, at least `new` each, and the mean number of tokens a step keeps."""
     gen = torch.Generator(device="cuda").manual_seed(seed)
-    S, longest = len(prompts), max(map(len, prompts)) + new + 3 * DRAFT
+    S, longest = len(prompts), most_tokens(prompts, new)
     blocks = -(-longest // BLOCK)
     model = Decoder(layers, longest, gen)
     pools = [torch.zeros((layers, S * blocks, KV_HEADS, BLOCK, DIM), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
