@@ -113,6 +113,7 @@ class SparseVerifier:
         self._grown = torch.zeros(n_seq, dtype=torch.int32, device=dev)   # lengths with the new tokens, between prefill_layer and end_prefill
         self._grown_kv: List[Optional[sv.sv_kv]] = [None] * n_layers
         self._turned = self._chunk_workspace = None
+        self._outgrown: List[torch.Tensor] = []   # earlier, smaller _turned: captured graphs go on using them
 
     def _make_lists(self, flags: bytes, dev) -> None:
         """One block list per anchor layer; sel_idx / sel_cnt is the last one, which is also what verify_layer keeps its
@@ -327,12 +328,18 @@ class SparseVerifier:
         s's) in one layer: rotary positions on q and k, k and v into the cache behind its seq_lens tokens, the representatives of
         the grown blocks, and causal attention of the new tokens over everything up to them.  q, out [N][Hq][D], k, v [N][Hkv][D],
         tokens of q, k and v any distance apart (sv_rope_append, sv_chunk_attn).  The block table must hold pages for the blocks that
-        are entered.  Every layer sees the old lengths; end_prefill advances them when all layers are through."""
+        are entered (check_status reports it where it does not).  Every layer sees the old lengths; end_prefill advances them when
+        all layers are through.  Can be captured: what a graph has used of the engine's own buffers stays, also when larger batches
+        follow."""
         n = int(k.shape[0])
         if self._turned is None or self._turned.shape[0] < n:
-            self._turned = torch.empty((n, self.geom.n_q_heads, self.geom.head_dim), dtype=torch.bfloat16, device=k.device)
-        need = max(16, sv.sv_chunk_workspace_bytes(self.geom, n))
-        if self._chunk_workspace is None or self._chunk_workspace.numel() < need:
+            rows = n
+            if self._turned is not None:   # (at least twice as many: together the earlier ones are never larger than the last)
+                self._outgrown.append(self._turned)
+                rows = max(n, 2 * self._turned.shape[0])
+            self._turned = torch.empty((rows, self.geom.n_q_heads, self.geom.head_dim), dtype=torch.bfloat16, device=k.device)
+        if self._chunk_workspace is None:   # what any batch needs: more than 128 query rows a KV head need no more
+            need = sv.sv_chunk_workspace_bytes(self.geom, 129)
             self._chunk_workspace = torch.empty(need, dtype=torch.uint8, device=k.device)
         k_pool, v_pool = self._pools[layer]
         turned = self._turned[:n]

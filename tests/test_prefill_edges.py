@@ -1,5 +1,8 @@
 """SparseVerifier.prefill_layer and end_prefill where a serving loop can go wrong: tokens that the block table has no pages for, captured
 graphs beside larger batches, a turn of the loop without new tokens."""
+import gc
+import weakref
+
 import pytest
 import torch
 
@@ -59,3 +62,54 @@ def test_the_status_of_an_append(length, new, bad):
                       torch.empty_like(b.q), out, status_word=status)
     assert int(status) == (sv.SV_STATUS_INDEX if bad else 0)
     assert int(out) == (length if length < 0 else max(length, min(length + new, 192)))
+
+
+def test_a_buffer_that_was_used_stays_when_larger_batches_follow():
+    """What a captured graph has the address of; together the buffers stay below twice the largest."""
+    v = _verifier(1, 40)
+    used, sizes = [], []
+    for n in (1, 5, 6, 100, 20, 101, 300, 301):
+        _Batch([n], n).run(v)
+        used += [weakref.ref(v._turned), weakref.ref(v._chunk_workspace)]
+        sizes.append(v._turned.shape[0])
+    gc.collect()
+    assert all(r() is not None for r in used)
+    assert len({r().data_ptr() for r in used[1::2]}) == 1
+    assert sum(set(sizes)) <= 2 * sizes[-1] and sizes[-1] <= 2 * 301
+
+
+def test_the_workspace_does_for_every_batch():
+    import paper_2512_21911_b200 as sv
+    for Hq, Hkv in ((8, 2), (1, 1), (128, 1), (7, 1), (64, 64)):
+        g = sv.make_geom(3, Hq, Hkv, 128, B, 40, 1)
+        assert all(sv.sv_chunk_workspace_bytes(g, n) <= sv.sv_chunk_workspace_bytes(g, 129) for n in (1, 2, 31, 127, 128, 129, 130, 5000, 30000))
+
+
+def test_a_captured_batch_beside_a_larger_one():
+    """A graph of a decoding batch, captured first; a larger batch runs, memory that was given back is taken and filled, the graph runs again."""
+    v, w = _verifier(2, 20), _verifier(2, 20)
+    prompt, small, large = _Batch([70, 200], 1), _Batch([1, 3], 2), _Batch([300, 500], 3)
+    for x in (v, w):
+        prompt.run(x)
+        x.end_prefill()
+    v._turned = v._chunk_workspace = None                  # as in an engine whose first call is captured
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        small.run(v)
+        v.end_prefill()
+    large.run(v)
+    v.end_prefill()
+    taken = [torch.full((n,), 0x7f7f, dtype=torch.int16, device="cuda") for n in (512, 4096, 1 << 15, 1 << 20, 1 << 24)]
+    torch.cuda.synchronize()
+    graph.replay()
+    torch.cuda.synchronize()
+    got = [o.clone() for o in small.out]
+    assert all(bool((t == 0x7f7f).all()) for t in taken)
+    large.run(w)
+    w.end_prefill()
+    small.run(w)
+    w.end_prefill()
+    assert all(torch.equal(a, b) for a, b in zip(got, small.out)) and v.seq_lens.tolist() == w.seq_lens.tolist() == [371, 703]
+    for x in (v, w):
+        x.check_status()
