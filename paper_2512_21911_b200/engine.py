@@ -110,7 +110,8 @@ class SparseVerifier:
         self._stack_bytes = [sv._native.workspace_bytes_host_step(self.geom, n_layers, max_sel) if stackable else 0, need[1]]
         self._stack_workspace = [torch.zeros(n, dtype=torch.uint8, device=dev) if k else None for n, k in zip(self._stack_bytes, keeps)]
 
-        self._grown = torch.zeros(n_seq, dtype=torch.int32, device=dev)   # lengths with the new tokens, between prefill_layer and end_prefill
+        # lengths with the new tokens, between prefill_layer and end_prefill; else the least number there is
+        self._grown = torch.full((n_seq,), -2 ** 31, dtype=torch.int32, device=dev)
         self._grown_kv: List[Optional[sv.sv_kv]] = [None] * n_layers
         self._turned = self._chunk_workspace = None
         self._outgrown: List[torch.Tensor] = []   # earlier, smaller _turned: captured graphs go on using them
@@ -349,8 +350,10 @@ class SparseVerifier:
                          status_word=self.status)
 
     def end_prefill(self) -> None:
-        """The lengths with the tokens that prefill_layer has written become the cache's."""
-        self.seq_lens.copy_(self._grown)
+        """The lengths with the tokens that prefill_layer has written become the cache's; without a prefill_layer since the last
+        time nothing changes (which the device decides, so that either may be part of a captured graph)."""
+        torch.maximum(self.seq_lens, self._grown, out=self.seq_lens)
+        self._grown.fill_(-2 ** 31)
 
     def draw(self, logits, u, distributions: bool = True, **parameters):
         """Distributions (what accept takes) and tokens of rows of logits [S][T][V] or [R][V]: (probs, tokens), probs None unless they

@@ -113,3 +113,47 @@ def test_a_captured_batch_beside_a_larger_one():
     assert all(torch.equal(a, b) for a, b in zip(got, small.out)) and v.seq_lens.tolist() == w.seq_lens.tolist() == [371, 703]
     for x in (v, w):
         x.check_status()
+
+
+def test_the_end_of_a_prefill_that_was_not_there():
+    v = _verifier(2, 20)
+    v.seq_lens.copy_(torch.tensor([7, 0], dtype=torch.int32))
+    v.end_prefill()
+    assert v.seq_lens.tolist() == [7, 0]
+    _Batch([100, 30], 1).run(v)
+    v.end_prefill()
+    assert v.seq_lens.tolist() == [107, 30]
+    v.end_prefill()
+    assert v.seq_lens.tolist() == [107, 30]
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    draft_k, draft_v = (torch.empty((L, 2, 4, HKV, 128), dtype=torch.bfloat16, device="cuda").normal_(generator=gen) for _ in range(2))
+    v.commit(draft_k, draft_v, torch.arange(4, dtype=torch.int32, device="cuda").repeat(2, 1), torch.tensor([3, 1], dtype=torch.int32, device="cuda"))
+    assert v.seq_lens.tolist() == [110, 31]
+    v.end_prefill()
+    assert v.seq_lens.tolist() == [110, 31]
+    v.seq_lens.copy_(torch.tensor([0, 31], dtype=torch.int32))     # the first place goes to another request
+    v.end_prefill()
+    assert v.seq_lens.tolist() == [0, 31]
+    _Batch([2, 0], 3).run(v)
+    v.end_prefill()
+    assert v.seq_lens.tolist() == [2, 31]
+
+
+@pytest.mark.parametrize("end_inside", [False, True])
+def test_layers_in_a_graph_and_the_end_in_it_or_behind_it(end_inside):
+    v = _verifier(2, 20)
+    b = _Batch([3, 1], 1)
+    b.run(v)
+    v.end_prefill()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.run(v)
+        if end_inside:
+            v.end_prefill()
+    for i in range(2, 5):
+        graph.replay()
+        if not end_inside:
+            v.end_prefill()
+        assert v.seq_lens.tolist() == [3 * i, i]
+    v.check_status()
