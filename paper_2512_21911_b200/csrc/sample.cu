@@ -425,7 +425,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     svk::grid_launch_dependents();
 
     const float T = p.temperature ? p.temperature[g] : 1.f;
-    const bool greedy = !(T > 0.f);
+    // (no entry reaches more than the largest one's mass: the first one is left, as in a greedy draw)
+    const bool greedy = !(T > 0.f) || (p.min_p && p.min_p[g] > 1.f);
     const int k = greedy ? 1 : p.top_k ? p.top_k[g] : 0;
     const float top_p = p.top_p && !greedy ? p.top_p[g] : 1.f;
     float min_e = p.min_p && !greedy ? p.min_p[g] : 0.f;
@@ -703,7 +704,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
 
     const auto stays = [&](float x, uint32_t i) {   // e of an entry that stays, 0 of others
         const float e = e_of(x);
-        return last.keeps(x, i) & ((e >= min_e) | (x == peak)) ? e : 0.f;
+        return last.keeps(x, i) & (e >= min_e) ? e : 0.f;
     };
     Mass total;   // of the draw
     float scale = 1099511627776.f;   // ... and what the largest entry counts
@@ -726,7 +727,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const uint32_t at = i * kThreads + tid;
-            const bool keep = at < n_k && (at == 0 || (ahead[i] < goal && (e[i] >= min_e || logit_of((uint32_t)(sm.sorted[at] >> 32)) == peak)));
+            const bool keep = at < n_k && (at == 0 || (ahead[i] < goal && e[i] >= min_e));
             n_keep += __syncthreads_count(keep);
             kept += keep ? mass_of<kDraw>(e[i]) : 0;
         }

@@ -49,3 +49,22 @@ def test_the_rate_keeps_more_bits_than_a_float():
     kept = (probs > 0).cpu().numpy()
     wrong = [(i, int(kept[i].sum()) - len(w)) for i, w in enumerate(want) if not np.array_equal(np.nonzero(kept[i])[0], w)]
     assert not wrong, wrong
+
+
+@pytest.mark.parametrize("half", [False, True])
+@pytest.mark.parametrize("V", [5, 1000, 128256])
+def test_min_p_around_one_and_tied_maxima(V, half):
+    """Above 1 the first entry alone stays, with or without other restrictions; at 1 all that equal the largest."""
+    gen = torch.Generator(device="cuda").manual_seed(V)
+    x = torch.randn((6, V), generator=gen, device="cuda")
+    tied = [V // 3, V // 2 + 1, V - 1]
+    x[:, tied] = 9.0
+    if half:
+        x = x.bfloat16()
+    min_p = [1.5, math.inf, float(np.nextafter(np.float32(1), np.float32(2))), 1.0, float(np.nextafter(np.float32(1), np.float32(0))), 1.5]
+    kept = [tied[:1]] * 3 + [tied] * 2 + [tied[:1]]
+    for more in (dict(), dict(temperature=[0.3] * 5 + [0.0]), dict(top_k=[3, 3, 0, 7, 50, 2]), dict(top_p=[0.999999] * 6), dict(temperature=[4.0] * 6, top_p=[2.0] * 6, top_k=[0] * 6)):
+        tokens, probs = _draw(x, min_p=min_p, **more)
+        for i, want in enumerate(kept):
+            assert probs[i].nonzero().flatten().tolist() == want, (i, more)
+            assert bool((probs[i, want] - 1 / len(want)).abs().max() <= 1e-6) and int(tokens[i]) == want[(len(want) - 1) // 2]
