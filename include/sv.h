@@ -530,12 +530,12 @@ SV_API sv_status sv_chunk_attn(const sv_geom *geom, const void *q, const sv_kv *
  * first): the first top_k entries stay; of these, those whose predecessors have less than top_p of the mass of all of them; of these,
  * those with e >= min_p.  The first entry always stays.  probs = e / sum of e over the entries that stayed, zero elsewhere; the token is
  * the smallest x that stayed with sum_{y <= x} e(y) >= u * sum_y e(y), both sums over the entries that stayed in the order of the
- * vocabulary.  temperature 0: the first entry alone.  A logit of -infinity or NaN is that of an entry that is not there; +infinity
- * counts as the largest number.  A row without an entry has the token -1 and zeros.
+ * vocabulary.  temperature 0, or min_p above 1: the first entry alone.  A logit of -infinity or NaN is that of an entry that is not
+ * there; +infinity counts as the largest number, one below 2^-126 in magnitude as zero.  A row without an entry has the token -1 and zeros.
  *   logits          dev fp32 or (logits_bf16 != 0) bf16, rows row_stride elements apart, row_stride >= vocab
  *   temperature, top_k, top_p, min_p   dev fp32 / int32, one entry for each rows_per_param rows (n_rows a multiple of it), or NULL: 1, and no
- *                   restriction.  A negative or NaN temperature counts as 0; top_k <= 0, top_p >= 1 or NaN and min_p <= 0 or NaN
- *                   restrict nothing
+ *                   restriction.  A temperature that is negative, NaN or below 2^-126 counts as 0, one above 2^126 as 1.2e38;
+ *                   top_k <= 0, top_p >= 1 or NaN and min_p <= 0 or NaN restrict nothing
  *   u               dev fp32 [n_rows] in [0, 1), from the caller; may be NULL when tokens is
  *   tokens          dev int32 [n_rows] or NULL; probs: dev fp32 [n_rows][vocab] or NULL (not both NULL).  probs is what sv_accept takes
  * Masses are summed as multiples of 2^-32 (nucleus) and 2^-40 (draw) of the largest entry's, so sums do not depend on their order and

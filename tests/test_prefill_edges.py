@@ -85,14 +85,17 @@ def test_the_workspace_does_for_every_batch():
         assert all(sv.sv_chunk_workspace_bytes(g, n) <= sv.sv_chunk_workspace_bytes(g, 129) for n in (1, 2, 31, 127, 128, 129, 130, 5000, 30000))
 
 
-def test_a_captured_batch_beside_a_larger_one():
-    """A graph of a decoding batch, captured first; a larger batch runs, memory that was given back is taken and filled, the graph runs again."""
+@pytest.mark.parametrize("first", [True, False])
+def test_a_captured_batch_beside_a_larger_one(first):
+    """A graph of a decoding batch, which may be the engine's first call; a larger batch runs, memory that was given back is taken and filled, the graph runs again."""
     v, w = _verifier(2, 20), _verifier(2, 20)
     prompt, small, large = _Batch([70, 200], 1), _Batch([1, 3], 2), _Batch([300, 500], 3)
     for x in (v, w):
         prompt.run(x)
         x.end_prefill()
-    v._turned = v._chunk_workspace = None                  # as in an engine whose first call is captured
+    v._turned = v._chunk_workspace = None
+    if not first:
+        _Batch([4, 0], 4).run(v)
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):

@@ -68,3 +68,82 @@ def test_min_p_around_one_and_tied_maxima(V, half):
         for i, want in enumerate(kept):
             assert probs[i].nonzero().flatten().tolist() == want, (i, more)
             assert bool((probs[i, want] - 1 / len(want)).abs().max() <= 1e-6) and int(tokens[i]) == want[(len(want) - 1) // 2]
+
+
+def _tiny(rng, n):
+    """Numbers below the smallest normal one, of either sign, and zeros."""
+    return (rng.integers(-3, 4, n) * np.float32(2.0 ** -130)).astype(np.float32)
+
+
+@pytest.mark.parametrize("half", [False, True])
+@pytest.mark.parametrize("V", [40, 5000, 50000])
+def test_logits_below_the_smallest_normal_number_are_zeros(V, half):
+    """So that all of them are equal, and the first ones stay; as the largest entries of a row and among others."""
+    rng = np.random.default_rng(V)
+    x = np.full((4, V), -3.0, np.float32)
+    x[0] = _tiny(rng, V)
+    x[1, ::3] = _tiny(rng, len(x[1, ::3]))
+    x[2, ::2] = _tiny(rng, len(x[2, ::2]))
+    x[2, :3] = 1.0
+    x[3] = _tiny(rng, V)
+    x[3, V // 2] = np.float32(2.0 ** -120)                 # larger than all, and e is 1 as theirs
+    ahead = [np.arange(V), np.arange(0, V, 3), np.concatenate([np.arange(3), np.arange(4, V, 2)]), np.concatenate([[V // 2], np.delete(np.arange(V), V // 2)])]
+    logits = torch.from_numpy(x).cuda()
+    if half:
+        logits = logits.bfloat16()
+        assert bool((logits.float().abs().cpu() > 0).numpy()[x != 0].all())
+    for k in (1, 5, 11):
+        tokens, probs = _draw(logits, top_k=[k] * 4, u=torch.zeros(4, device="cuda"))
+        for i in range(4):
+            want = np.sort(ahead[i][:k])
+            assert probs[i].nonzero().flatten().tolist() == want.tolist(), (k, i)
+            assert abs(float(probs[i].double().sum()) - 1) <= 1e-5 and int(tokens[i]) == want[0]
+    tokens, probs = _draw(logits, temperature=[0.0] * 4)
+    assert tokens.tolist() == [0, 0, 0, V // 2] and probs.count_nonzero(1).tolist() == [1] * 4
+    n = [V // 2, len(ahead[1]) // 2]
+    top_p = [(n[0] - 0.5) / V, (n[1] - 0.5) / (len(ahead[1]) + (V - len(ahead[1])) * math.exp(-3))]
+    _, probs = _draw(logits[:2], top_p=top_p)
+    for i in range(2):
+        assert probs[i].nonzero().flatten().tolist() == ahead[i][:n[i]].tolist()
+
+
+@pytest.mark.parametrize("half", [False, True])
+@pytest.mark.parametrize("V", [217089, 262145, 300001, 350208, 393215, 393216])
+def test_the_largest_vocabularies(V, half):
+    """Parts of 14 to 24 grains of 2,048 entries: up to 192 KB of a row's fp32 entries in a CTA's shared memory, and the limit itself."""
+    rng = np.random.default_rng(V)
+    gen = torch.Generator(device="cuda").manual_seed(V)
+    x = torch.randn((5, V), generator=gen, device="cuda") * 3
+    x[:, V - 1] = 14.0                                     # the largest by far is the last entry
+    if half:
+        x = x.bfloat16()
+    rows = x.double().cpu().numpy()
+    order = np.argsort(-rows, axis=1, kind="stable")
+    e = np.exp(rows - rows.max(1, keepdims=True))
+    ranked = np.take_along_axis(e, order, 1)
+    whole = np.cumsum(ranked, 1)
+    n = [1, 40, 2000, 100000, V - 1]
+
+    def check(probs, tokens, counts, u):
+        for i, m in enumerate(counts):
+            want = np.zeros(V)
+            want[order[i, :m]] = ranked[i, :m] / whole[i, m - 1]
+            got = probs[i].double().cpu().numpy()
+            assert (np.abs(got - want) <= 1e-5 * want).all(), i
+            upto = np.cumsum(want)
+            t = int(tokens[i])
+            assert want[t] > 0 and upto[t] - want[t] <= u[i] + 1e-6 and upto[t] >= u[i] - 1e-6
+
+    u = rng.random(5).astype(np.float32)
+    draw = lambda **kw: _draw(x, u=torch.from_numpy(u).cuda(), **kw)
+    for parameters, counts in ((dict(), [V] * 5), (dict(top_k=n), n),
+                               (dict(top_p=[(whole[i, m - 1] - ranked[i, m - 1] / 2) / whole[i, -1] for i, m in enumerate([1, 40, 2000, 9000, 3])]), [1, 40, 2000, 9000, 3])):
+        tokens, probs = draw(**parameters)
+        check(probs, tokens, counts, u)
+
+
+def test_a_larger_vocabulary_is_refused():
+    import paper_2512_21911_b200 as sv
+    x = torch.zeros((1, 393217), device="cuda")
+    with pytest.raises(sv.SvError):
+        sv.sv_sample(x, torch.zeros(1, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda"))
