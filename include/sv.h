@@ -480,8 +480,8 @@ SV_API sv_status sv_verify_step_from_host_direct(const sv_geom *geom, const sv_l
  * replaced by (a cos - b sin, b cos + a sin), cos = rope[p][j], sin = rope[p][rot_dim / 2 + j]; dims from rot_dim on are copied.  Products
  * and sums are rounded to fp32 one by one, the result once to bf16.
  *   q, k, v         dev bf16 rows [N][Hq][D], [N][Hkv][D]; the heads of a token are contiguous, tokens q_stride / k_stride / v_stride
- *                   elements apart (multiples of 8), so that all three may be parts of one projection's output.  q may be NULL (then
- *                   q_out too): the cache only
+ *                   elements apart (multiples of 8; of one token anything), so that all three may be parts of one projection's output.
+ *                   q may be NULL (then q_out too): the cache only
  *   rope            dev fp32 [rope_rows][rot_dim] or NULL (no rotation; q_out is then a copy).  rot_dim: a multiple of 16, at most D.  A
  *                   position outside the table takes its nearest row and sets SV_STATUS_INDEX
  *   q_out           dev bf16 [N][Hq][D] contiguous; may be q itself

@@ -271,7 +271,7 @@ extern "C" sv_status sv_rope_append(const sv_geom *geom, void *k_pool, void *v_p
         return SV_ERR_SHAPE;
     // (a row of q_out is written by a CTA that reads other rows of q: in place only where both have the same layout)
     if (q && q_out == q && n_tokens > 1 && q_stride != (int64_t)Hq * svh::kHeadDim) return SV_ERR_SHAPE;
-    if (q_stride % 8 || k_stride % 8 || v_stride % 8) return SV_ERR_ALIGN;
+    if (n_tokens > 1 && (q_stride % 8 || k_stride % 8 || v_stride % 8)) return SV_ERR_ALIGN;
     if (!svh::aligned(k_pool, 128) || !svh::aligned(v_pool, 128) || !svh::aligned(q, 16) || !svh::aligned(k, 16) || !svh::aligned(v, 16) ||
         !svh::aligned(q_out, 16) || !svh::aligned(rope, 16) || !svh::aligned(reps, 16))
         return SV_ERR_ALIGN;
