@@ -21,10 +21,10 @@
 // tokens over long caches and any mixture of the two without a case of its own.
 //
 // Bound by, and measured (32 query and 8 KV heads; the faster and the slower of the machines it was timed on): a prompt of 8,192 tokens
-// takes 495 to 575 us for 0.55 TFLOP, 0.96 to 1.1 PFLOP/s or 58 to 68 % of a large library product, the tensor pipe active for 52 % of
+// takes 495 to 584 us for 0.55 TFLOP, 0.94 to 1.1 PFLOP/s or 57 to 68 % of a large library product, the tensor pipe active for 52 % of
 // the time: a unit of two tiles takes 3900 cycles where its MMAs take 2048, the rest being what passes a unit from S to the softmax, to
-// PV and on (issue()).  2,048 tokens behind 30,001 (64 heads): 2.0 to 2.1 ms for 2.08 TFLOP, 0.98 to 1.0 PFLOP/s.  16 single tokens over
-// 4K to 16K keys: 727 MB in 126 to 141 us, 79 to 88 % of a copy's rate.  One token over 4K keys of 2 heads: 19 us, of which 5 are the
+// PV and on (issue()).  2,048 tokens behind 30,001 (64 heads): 2.0 to 2.2 ms for 2.08 TFLOP, 0.95 to 1.0 PFLOP/s.  16 single tokens over
+// 4K to 16K keys: 727 MB in 126 to 145 us, 77 to 88 % of a copy's rate.  One token over 4K keys of 2 heads: 19 us, of which 5 are the
 // merging launch and the rest a chain of cold steps (batch, division, tensor maps, page, tile, softmax).
 //
 // All waits are on mbarriers and bounded; one that gives up sets the status word, the CTA drains its copies and MMAs, frees TMEM and

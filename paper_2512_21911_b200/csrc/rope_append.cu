@@ -3,8 +3,8 @@
 //
 // Mathematics: a pair (a, b) of a head's dims at position p becomes (a cos - b sin, b cos + a sin), cos and sin from a table.  Bound by
 // HBM: (Hq + 2 Hkv) * 256 bytes read and written per token, a table row of 512 bytes shared by all heads, no reuse.  A prompt of 32,768
-// tokens with 32 query and 8 KV heads moves 826 MB in 158 us, 5.2 TB/s, 80 % of a plain copy's rate; a token for each of 64 sequences
-// takes 7.1 us, three dependent loads (starts, length and table, rows) behind a launch.
+// tokens with 32 query and 8 KV heads moves 826 MB in 167 us, 4.9 TB/s, 76 % of a plain copy's rate; a token for each of 64 sequences
+// takes 6.9 us, three dependent loads (starts, length and table, rows) behind a launch.  (All figures here: nothing in L2 before the call.)
 //
 // One launch of two kinds of CTAs.  The first take a block of a sequence and a KV head: 16 threads hold a 256-byte row, so that the
 // partner of a dim is in the same thread (neighbours) or 2 to 8 lanes away (halves), the rows of the block go to its page, and the mean
@@ -25,9 +25,10 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kRowGroups = kThreads / 16;
 // Tokens of a CTA that rotates queries: two in calls of up to kFew tokens, where the query CTAs of many would not fill the machine and a
-// CTA's own chain of loads is what counts; many beyond, where reading the batch's starts and lengths is shared by more rows.  32 (28)
-// query heads: 64 tokens take 7.1 us with two and 8.1 us with four; 3,512 take 12.8 us with two and 12.0 us with eight; 32,768 take
-// 193 us with two, 167 us with four and 158 us with eight (156 us with sixteen, which cost the 3,512 0.6 us).
+// CTA's own chain of loads is what counts; many beyond, where reading the batch's starts and lengths is shared by more rows.  With two and
+// with eight tokens: 64 sequences of one token 6.8 and 9.2 us; chunks of four sequences, 256 tokens in all 5.1 and 6.0, 1,024 7.3 and 9.1,
+// 1,536 11.5 either way, 2,048 14.9 and 15.7, 4,096 26.4 and 24.9; a prompt of 32,768 195 and 168.  512, 1,024 and 2,048 sequences of one
+// token each: 43 and 47, 86 and 89, 191 and 190.  The edge is not sharp: the two cross between 1,536 and 4,096 tokens.
 constexpr int kFew = 1024, kTokensOfFew = 2, kTokensOfMany = 8;
 
 struct Params {
@@ -238,8 +239,9 @@ __device__ __forceinline__ void turn_queries(const Params &p, int tile)
     }
 }
 
-// Three CTAs an SM (80 registers): without the bound it takes 128, two CTAs an SM, and the 3,512 tokens 12.8 us; four CTAs (64 registers)
-// take 17 us for them, since the rows of a cache block then no longer all start to load at once.
+// Three CTAs an SM (80 registers): a ragged batch of 3,512 tokens (28 query heads, cache blocks of 128) takes 16.3 us; without the bound
+// it takes 128 registers, two CTAs an SM and 16.9 us; four CTAs (64 registers) take 23.6 us, since the rows of a cache block then no
+// longer all start to load at once.
 template <int B, bool kNeighbours, int kQTokens>
 __global__ void __launch_bounds__(kThreads, 3) rope_append_kernel(const Params p)
 {

@@ -16,14 +16,15 @@
 // A cluster of 1 to 8 CTAs per row; a CTA keeps its part of the row in shared memory, so the logits are read once from HBM (19.5 MB of 19.4
 // for 64 bfloat16 rows of 151,936).  Warps own contiguous parts: a token is found by sums per CTA, warp and lane.
 //
-// Bound by the instructions of the passes (some 26 an entry for the histogram, 10 to gather a bin, 18 for the probabilities) and by the
+// Bound by the instructions of the passes (some 27 an entry for the histogram, 11 to gather a bin, 19 for the probabilities) and by the
 // steps between them (a barrier of the cluster is 1.8 us), two CTAs an SM overlapping one's steps with the other's passes: warps issue in
-// half of the cycles, and HBM, whose floor for these cases is 3 to 12 us, idles.  Measured: one row of 128,256 with a top-k of 50 12.8 us;
-// 64 bfloat16 rows of 151,936 with a nucleus 48 us, one round of clusters of four; 80 rows of 128,256 with a nucleus and their
-// distributions 75 us, three rounds of clusters of eight (12 of them the load, 10 the probabilities); 256 rows of 32,003 with top-k, min-p
-// and distributions 37.5 us.  Tests of an entry are written without branches, of which a pass had 20 an entry before (one row 13.7, then
-// 57, 84 and 40 us, with lists ranked entry against entry by every CTA).  A histogram of its own for rows without a top-k takes 46 us for
-// the 64 rows and 13.7 for the one, by more code to fetch.
+// half of the cycles, and HBM, whose floor for these cases is 3 to 12 us, idles.  Measured, with nothing in L2 before the call: one row of
+// 128,256 with a top-k of 50 13.3 us; 64 bfloat16 rows of 151,936 with a nucleus 48.4 us, one round of clusters of four; 80 rows of
+// 128,256 with a nucleus and their distributions 77 us, three rounds of clusters of eight (12 of them the load, 10 the probabilities); 256
+// rows of 32,003 with top-k, min-p and distributions 44 us.  Of calls back to back, whose rows are in L2: tests of an entry are written
+// without branches, of which a pass had 20 an entry before (13.7, 57, 84 and 40 us, with lists ranked entry against entry by every CTA;
+// 12.8, 48, 75 and 37.5 then).  A histogram of its own for rows without a top-k takes 46 us for the 64 rows and 13.7 for the one, by
+// more code to fetch.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <float.h>
@@ -149,8 +150,8 @@ __device__ __forceinline__ void add_shared(uint32_t at, int v)
 
 // log2 e / temperature to more than the bits of a float, in two words neither of which is negative or zero (times an infinite distance the
 // sum stays infinite).  Rounded to one float, the rate acts as a temperature 2^-24 beside the one asked for, which in a vocabulary of 128K
-// moves the sums at a nucleus' edge by up to 1e-7 of the whole: 1 % of the mass of the entry there.  The second word takes 2 % of a
-// call (64 rows 48.0 -> 49.2 us, 80 rows with their distributions 77.2 -> 78.8, nothing in L2).
+// moves the sums at a nucleus' edge by up to 1e-7 of the whole: 1 % of the mass of the entry there.  The second word takes up to 2 % of a
+// call (64 rows 48.0 -> 48.4 to 49.2 us, 80 rows with their distributions 77.2 -> 76.4 to 78.8, nothing in L2).
 struct Rate {
     float high, low;
 };
