@@ -501,6 +501,16 @@ SV_API sv_status sv_rope_append(const sv_geom *geom, void *k_pool, void *v_pool,
                                 float *reps, int32_t *status_word, void *stream);
 
 /*
+ * sv_rope_append for a cache that has lost tokens (sv_kv_evict): row i of sequence s is rotated for position positions[s] + i and written
+ * behind the seq_lens[s] tokens that the cache holds.  positions: dev int32 [S], or NULL: seq_lens.
+ */
+SV_API sv_status sv_rope_append_at(const sv_geom *geom, void *k_pool, void *v_pool, int32_t n_pages, const int32_t *block_table,
+                                   const int32_t *seq_lens, const int32_t *positions, const void *q, const void *k, const void *v,
+                                   int64_t q_stride, int64_t k_stride, int64_t v_stride, const int32_t *q_start, int32_t n_tokens,
+                                   const float *rope, int32_t rope_rows, int32_t rot_dim, int32_t interleaved, void *q_out,
+                                   int32_t *seq_lens_out, float *reps, int32_t *status_word, void *stream);
+
+/*
  * Attention of such a batch over the cache that holds its own keys and values already (sv_rope_append): kv->seq_lens counts the new
  * tokens too, so that row i of sequence s, of n rows, is at position p = seq_lens[s] - n + i and sees the cached tokens 0 .. p:
  * softmax(softmax_scale * q . k) . v.  fp32 softmax and accumulation; probabilities are rounded to bf16 for the PV product.  A row that
@@ -544,6 +554,103 @@ SV_API sv_status sv_chunk_attn(const sv_geom *geom, const void *q, const sv_kv *
 SV_API sv_status sv_sample(int32_t n_rows, int32_t vocab, const void *logits, int32_t logits_bf16, int64_t row_stride,
                            int32_t rows_per_param, const float *temperature, const int32_t *top_k, const float *top_p,
                            const float *min_p, const float *u, int32_t *tokens, float *probs, void *stream);
+
+/*
+ * A paged cache held in 4 bits: 144 bytes for a token and KV head instead of 512.  The pool is [n_pages][Hkv][block_size / 64] slabs of
+ * SV_Q4_SLAB_BYTES bytes, 64 tokens of a KV head each; block table and lengths are those of sv_kv.
+ *
+ * Of a row of keys or values each group x of 64 dims has a scale D and an offset M in bf16, D = (max x - min x) / 15 * 16, M = min x - D
+ * (each step rounded to fp32, the result to bf16), and for every value a code c, (x - M) / D * 16 - 16 rounded to the nearest whole number
+ * in 0 .. 15 (0 where D is 0).  It stands for (1 + c / 16) D + M, rounded once to bf16; those are the keys and values that all calls below
+ * go by.  A group with a NaN or an infinite value, or whose D is infinite, stands for NaNs.
+ * A slab: codes of the keys [4 chunks of 32 dims][64 tokens][16 bytes]; codes of the values [2 chunks of 32 tokens][128 dims][16 bytes];
+ * bf16 scales of the keys [64 tokens][2 groups][D, M]; of the values [2 groups][D, M][64 tokens].  Of eight codes (dims, or tokens) a 32-bit word
+ * holds number 2 j in bits 4 j .. 4 j + 3 and number 2 j + 1 sixteen bits higher.  What a slab holds behind the last token of its sequence
+ * may be anything.
+ */
+#define SV_Q4_SLAB_BYTES 9216
+typedef struct {
+    const void *pool;           /* dev [n_pages][Hkv][block_size / 64][SV_Q4_SLAB_BYTES], 128-byte aligned */
+    const int32_t *block_table; /* dev int32 [S][NBmax] page ids */
+    const int32_t *seq_lens;    /* dev int32 [S] */
+    int32_t n_pages;
+} sv_kv_q4;
+
+/*
+ * sv_rope_append and sv_kv_append for such a cache: the same arguments, checks and dropped tokens, with the one pool in place of two.  Keys
+ * are rotated and rounded to bf16 as there, then coded.  reps: the means of the keys that the cache then holds; sv_select_blocks takes them
+ * as they are.  A block's tokens are written by one thread block, so that calls on one stream need nothing else; nothing but the new tokens
+ * changes.
+ */
+SV_API sv_status sv_rope_append_q4(const sv_geom *geom, void *pool, int32_t n_pages, const int32_t *block_table, const int32_t *seq_lens,
+                                   const void *q, const void *k, const void *v, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                                   const int32_t *q_start, int32_t n_tokens, const float *rope, int32_t rope_rows, int32_t rot_dim,
+                                   int32_t interleaved, void *q_out, int32_t *seq_lens_out, float *reps, int32_t *status_word, void *stream);
+SV_API sv_status sv_kv_append_q4(const sv_geom *geom, void *pool, int32_t n_pages, const int32_t *block_table, const int32_t *seq_lens,
+                                 const void *draft_k, const void *draft_v, const int32_t *accept_idx, const int32_t *n_accept,
+                                 int32_t max_accept, int32_t *seq_lens_out, float *reps, void *stream);
+
+/*
+ * What the cache holds for some of its tokens, as bf16 rows: rows q_start[s] .. q_start[s + 1] - 1 are the tokens of sequence s from
+ * position first[s] on.  Rows of positions that the sequence does not hold are zeros and set SV_STATUS_INDEX.
+ *   first           dev int32 [S]; q_start: dev int32 [S + 1], as in sv_rope_append
+ *   k_out, v_out    dev bf16 [N][Hkv][D]; rows from q_start[S] on are left alone
+ */
+SV_API sv_status sv_kv_read_q4(const sv_geom *geom, const sv_kv_q4 *kv, const int32_t *first, const int32_t *q_start, int32_t n_tokens,
+                               void *k_out, void *v_out, int32_t *status_word, void *stream);
+
+/*
+ * sv_verify_attn and sv_chunk_attn over such a cache: the same arguments and results, with the values that the codes stand for.  The draft
+ * tokens' own keys and values are bf16 tensors, as there.  Of the block lists no order is asked for.  Keys and values behind a sequence's
+ * last token have no part in either (a cached value of NaN or infinity that a row sees has, with a weight of zero too; the values of later
+ * tokens of a chunk's call have to be finite).
+ *   workspace       dev scratch of sv_workspace_bytes_q4(geom) bytes, 16-byte aligned, for any call with this geometry
+ * Up to 64 query rows of a KV head are taken at once; a draft or a chunk of more goes over the cache several times.  softmax_scale: 0
+ * selects 1 / sqrt(D), not negative (SV_ERR_SHAPE).
+ */
+SV_API size_t sv_workspace_bytes_q4(const sv_geom *geom);
+SV_API sv_status sv_verify_attn_q4(const sv_geom *geom, const void *q, const sv_kv_q4 *kv, const void *draft_k, const void *draft_v,
+                                   const int32_t *parent, const int32_t *sel_idx, const int32_t *sel_cnt, int32_t max_sel,
+                                   float softmax_scale, void *out, float *lse, void *workspace, size_t workspace_bytes, int32_t *status_word,
+                                   void *stream);
+SV_API sv_status sv_chunk_attn_q4(const sv_geom *geom, const void *q, const sv_kv_q4 *kv, const int32_t *q_start, int32_t n_tokens,
+                                  float softmax_scale, void *out, float *lse, void *workspace, size_t workspace_bytes, int32_t *status_word,
+                                  void *stream);
+
+/*
+ * The attention weight that the rows of a step give every cached token: for each sequence s, KV head h and cached token t < seq_lens[s] of
+ * the blocks that were attended,
+ *   weights_out[s][h][t] = weights[s][h][t] + sum over the rows i and the query heads g of h of exp(softmax_scale * q[s][i][g] . k_t - lse[s][i][g])
+ * and weights_out = weights for the tokens of other blocks; entries from seq_lens[s] on are left alone.  With lse from the attention
+ * over the same blocks and drafts these are its softmax weights.
+ *   q               dev bf16 [S][T][Hq][D]; lse: dev fp32 [S][T][Hq], natural logarithms (of a row with -infinity nothing is added)
+ *   sel_idx/sel_cnt the attended blocks as written by sv_select_blocks (ascending, none twice); NULL: all
+ *   path, n_path    dev int32 [S][T], [S] as written by sv_accept: the rows that count, or NULL, NULL: all T
+ *   softmax_scale   0 selects 1/sqrt(D); not negative
+ *   weights         dev fp32 [S][Hkv][NBmax * block_size]; weights_out: the same buffer, or one that does not overlap it
+ * Sums of fp32 in a fixed order.  One launch.
+ */
+SV_API sv_status sv_attn_weights(const sv_geom *geom, const void *q, const sv_kv *kv, const float *lse, const int32_t *sel_idx,
+                                 const int32_t *sel_cnt, int32_t max_sel, const int32_t *path, const int32_t *n_path, float softmax_scale,
+                                 const float *weights, float *weights_out, int32_t *status_word, void *stream);
+
+/*
+ * Eviction by such weights: of a sequence of L tokens, n = min(L, max(budget[s], n_sink + n_recent)) stay in every KV head: the first
+ * n_sink, the last n_recent, and of the others the heaviest in that head (equal ones: the earlier first; a NaN ranks between the negative
+ * numbers and zero).  They keep their order and close up: token number j of those that stay moves to position j of the sequence's
+ * pages, in place.  The pages from ceil(n / block_size) on are free afterwards.  Where L <= n nothing is touched.
+ *   weights         dev fp32 [S][Hkv][NBmax * block_size]; weights_out: the weights of the tokens at their new positions, and zeros for
+ *                   n <= t < L; the same buffer, or one that does not overlap it
+ *   budget          dev int32 [S]
+ *   seq_lens_out    dev int32 [S], a different buffer than seq_lens: layers that share the lengths all see the old ones
+ *   reps            dev fp32 [S][Hkv][NBmax][D] or NULL: of the sequences that lose tokens, bit for bit those of sv_block_reps
+ * Keys are rotated for the positions that their tokens had, and stay so; the caller counts positions itself from then on
+ * (sv_rope_append_at).  Rows of blocks whose table entry is not a page of the pool are neither read nor written and set SV_STATUS_INDEX.
+ * NBmax * block_size <= 393216 (SV_ERR_UNSUPPORTED).  One launch.
+ */
+SV_API sv_status sv_kv_evict(const sv_geom *geom, void *k_pool, void *v_pool, int32_t n_pages, const int32_t *block_table,
+                             const int32_t *seq_lens, const float *weights, const int32_t *budget, int32_t n_sink, int32_t n_recent,
+                             int32_t *seq_lens_out, float *weights_out, float *reps, int32_t *status_word, void *stream);
 
 /* Number of KV splits (CTAs per (sequence, KV head)) that the workspace of this geometry has room for.  sv_verify_attn uses as many, or
  * fewer where the CTAs of a thread-block cluster merge their splits themselves (the workspace is then not written). */

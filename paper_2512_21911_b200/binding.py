@@ -32,7 +32,9 @@ EXPORTS = ("sv_strerror", "sv_status_word_check", "sv_budget_blocks", "sv_worksp
            "sv_block_reps_bf16", "sv_select_blocks_bf16reps", "sv_layer_table_bytes", "sv_layer_table", "sv_workspace_bytes_layers",
            "sv_block_reps_layers", "sv_select_blocks_layers", "sv_verify_attn_layers", "sv_kv_append_layers", "sv_host_step_create",
            "sv_host_step_destroy", "sv_verify_step_from_host", "sv_verify_step_from_host_direct", "sv_workspace_bytes_host_step",
-           "sv_rope_append", "sv_chunk_workspace_bytes", "sv_chunk_attn", "sv_sample")
+           "sv_rope_append", "sv_chunk_workspace_bytes", "sv_chunk_attn", "sv_sample", "sv_rope_append_q4", "sv_kv_append_q4", "sv_kv_read_q4",
+           "sv_workspace_bytes_q4", "sv_verify_attn_q4", "sv_chunk_attn_q4", "sv_rope_append_at", "sv_attn_weights", "sv_kv_evict")
+SV_Q4_SLAB_BYTES = 9216   # of a 4-bit cache: 64 tokens of a KV head
 SV_MAX_LAYERS = 256
 SV_STACK_STATE_BYTES = 256   # what a stack's launches keep at the start of their workspace
 
@@ -52,6 +54,10 @@ class sv_geom(ctypes.Structure):
 class sv_kv(ctypes.Structure):
     _fields_ = [("k_pool", ctypes.c_void_p), ("v_pool", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
                 ("seq_lens", ctypes.c_void_p), ("n_pages", ctypes.c_int32)]
+
+
+class sv_kv_q4(ctypes.Structure):
+    _fields_ = [("pool", ctypes.c_void_p), ("block_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p), ("n_pages", ctypes.c_int32)]
 
 
 def _load() -> ctypes.CDLL:
@@ -104,6 +110,25 @@ def _load() -> ctypes.CDLL:
     lib.sv_chunk_workspace_bytes.argtypes = [gp, i32]
     lib.sv_chunk_attn.restype = ctypes.c_int
     lib.sv_chunk_attn.argtypes = [gp, vp, kp, vp, i32, f32, vp, vp, vp, sz, vp, vp]
+    qp = ctypes.POINTER(sv_kv_q4)
+    lib.sv_rope_append_q4.restype = ctypes.c_int
+    lib.sv_rope_append_q4.argtypes = [gp, vp, i32, vp, vp, vp, vp, vp, i64, i64, i64, vp, i32, vp, i32, i32, i32, vp, vp, vp, vp, vp]
+    lib.sv_kv_append_q4.restype = ctypes.c_int
+    lib.sv_kv_append_q4.argtypes = [gp, vp, i32, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp]
+    lib.sv_kv_read_q4.restype = ctypes.c_int
+    lib.sv_kv_read_q4.argtypes = [gp, qp, vp, vp, i32, vp, vp, vp, vp]
+    lib.sv_workspace_bytes_q4.restype = sz
+    lib.sv_workspace_bytes_q4.argtypes = [gp]
+    lib.sv_verify_attn_q4.restype = ctypes.c_int
+    lib.sv_verify_attn_q4.argtypes = [gp, vp, qp, vp, vp, vp, vp, vp, i32, f32, vp, vp, vp, sz, vp, vp]
+    lib.sv_chunk_attn_q4.restype = ctypes.c_int
+    lib.sv_chunk_attn_q4.argtypes = [gp, vp, qp, vp, i32, f32, vp, vp, vp, sz, vp, vp]
+    lib.sv_rope_append_at.restype = ctypes.c_int
+    lib.sv_rope_append_at.argtypes = [gp, vp, vp, i32, vp, vp, vp, vp, vp, vp, i64, i64, i64, vp, i32, vp, i32, i32, i32, vp, vp, vp, vp, vp]
+    lib.sv_attn_weights.restype = ctypes.c_int
+    lib.sv_attn_weights.argtypes = [gp, vp, kp, vp, vp, vp, i32, vp, vp, f32, vp, vp, vp, vp]
+    lib.sv_kv_evict.restype = ctypes.c_int
+    lib.sv_kv_evict.argtypes = [gp, vp, vp, i32, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp]
     lib.sv_sample.restype = ctypes.c_int
     lib.sv_sample.argtypes = [i32, i32, vp, i32, i64, i32, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.sv_accept.restype = ctypes.c_int
@@ -151,6 +176,12 @@ def make_kv(k_pool: torch.Tensor, v_pool: Optional[torch.Tensor], block_table: t
     return sv_kv(_ptr(k_pool, torch.bfloat16, "k_pool"), _ptr(v_pool, torch.bfloat16, "v_pool"),
                  _ptr(block_table, torch.int32, "block_table"), _ptr(seq_lens, torch.int32, "seq_lens"),
                  int(k_pool.shape[0]))
+
+
+def make_kv_q4(pool: torch.Tensor, block_table: torch.Tensor, seq_lens: torch.Tensor) -> sv_kv_q4:
+    """Descriptor of a 4-bit paged cache.  The pool is uint8 [n_pages][Hkv][B / 64][SV_Q4_SLAB_BYTES]; the tensors must outlive the calls."""
+    return sv_kv_q4(_ptr(pool, torch.uint8, "pool"), _ptr(block_table, torch.int32, "block_table"), _ptr(seq_lens, torch.int32, "seq_lens"),
+                    int(pool.shape[0]))
 
 
 def sv_status_word_check(value: int) -> int:
@@ -292,7 +323,15 @@ def sv_rope_append(geom: sv_geom, k_pool, v_pool, block_table, seq_lens, q, k, v
     output); q and q_out may be None.  q_start int32 [S + 1]: sequence s has rows q_start[s] .. q_start[s + 1] - 1.  rope float32
     [positions][rot_dim], cos then sin; interleaved: pairs are neighbouring dims, else halves of the rotated ones."""
     _check(_native.rope_append(geom, k_pool, v_pool, block_table, seq_lens, q, k, v, q_start, q_out, seq_lens_out, rope, interleaved,
-                               reps, status_word, stream), "sv_rope_append")
+                               reps, status_word, stream, None), "sv_rope_append")
+
+
+def sv_rope_append_at(geom: sv_geom, k_pool, v_pool, block_table, seq_lens, positions, q, k, v, q_start, q_out, seq_lens_out, rope=None,
+                      interleaved: bool = False, reps=None, status_word=None, stream=None) -> None:
+    """sv_rope_append for a cache that has lost tokens: positions (int32 [S], or None: seq_lens) are those of the sequences' first new
+    tokens, for the rotation; they are written behind the seq_lens tokens that the cache holds."""
+    _check(_native.rope_append(geom, k_pool, v_pool, block_table, seq_lens, q, k, v, q_start, q_out, seq_lens_out, rope, interleaved,
+                               reps, status_word, stream, positions), "sv_rope_append_at")
 
 
 def sv_chunk_workspace_bytes(geom: sv_geom, n_tokens: int) -> int:
@@ -306,6 +345,61 @@ def sv_chunk_attn(geom: sv_geom, q, kv: sv_kv, q_start, out, lse=None, workspace
     seq_lens_out of sv_rope_append).  q, out bfloat16 [N][Hq][128]; q_start int32 [S + 1]; lse optional float32 [N][Hq];
     workspace of sv_chunk_workspace_bytes bytes."""
     _check(_native.chunk_attn(geom, q, kv, q_start, out, lse, workspace, softmax_scale, status_word, stream), "sv_chunk_attn")
+
+
+def sv_rope_append_q4(geom: sv_geom, pool, block_table, seq_lens, q, k, v, q_start, q_out, seq_lens_out, rope=None, interleaved: bool = False,
+                      reps=None, status_word=None, stream=None) -> None:
+    """sv_rope_append into a 4-bit cache: pool uint8 [n_pages][Hkv][B / 64][SV_Q4_SLAB_BYTES]."""
+    _check(_native.rope_append_q4(geom, pool, None, block_table, seq_lens, q, k, v, q_start, q_out, seq_lens_out, rope, interleaved, reps,
+                                  status_word, stream, None), "sv_rope_append_q4")
+
+
+def sv_kv_append_q4(geom: sv_geom, pool, block_table, seq_lens, draft_k, draft_v, accept_idx, n_accept, seq_lens_out, reps=None,
+                    stream=None) -> None:
+    """sv_kv_append into a 4-bit cache."""
+    _check(_native.kv_append_q4(geom, pool, block_table, seq_lens, draft_k, draft_v, accept_idx, n_accept, seq_lens_out, reps, stream),
+           "sv_kv_append_q4")
+
+
+def sv_kv_read_q4(geom: sv_geom, kv: sv_kv_q4, first, q_start, k_out, v_out, status_word=None, stream=None) -> None:
+    """What a 4-bit cache holds: rows q_start[s] .. q_start[s + 1] - 1 of k_out, v_out bfloat16 [N][Hkv][128] become the tokens of
+    sequence s from position first[s] (int32 [S]) on."""
+    _check(_native.kv_read_q4(geom, kv, first, q_start, k_out, v_out, status_word, stream), "sv_kv_read_q4")
+
+
+def sv_workspace_bytes_q4(geom: sv_geom) -> int:
+    """Scratch of sv_verify_attn_q4 and sv_chunk_attn_q4, for any call with this geometry."""
+    return int(_lib.sv_workspace_bytes_q4(ctypes.byref(geom)))
+
+
+def sv_verify_attn_q4(geom: sv_geom, q, kv: sv_kv_q4, draft_k, draft_v, parent, sel_idx, sel_cnt, out, lse=None, workspace=None,
+                      softmax_scale: float = 0.0, status_word=None, stream=None) -> None:
+    """sv_verify_attn over a 4-bit cache (the draft tokens' own keys and values are bfloat16); workspace of sv_workspace_bytes_q4 bytes."""
+    _check(_native.verify_attn_q4(geom, q, kv, draft_k, draft_v, parent, sel_idx, sel_cnt, out, lse, workspace, softmax_scale, status_word,
+                                  stream), "sv_verify_attn_q4")
+
+
+def sv_chunk_attn_q4(geom: sv_geom, q, kv: sv_kv_q4, q_start, out, lse=None, workspace=None, softmax_scale: float = 0.0, status_word=None,
+                     stream=None) -> None:
+    """sv_chunk_attn over a 4-bit cache; workspace of sv_workspace_bytes_q4 bytes."""
+    _check(_native.chunk_attn_q4(geom, q, kv, q_start, out, lse, workspace, softmax_scale, status_word, stream), "sv_chunk_attn_q4")
+
+
+def sv_attn_weights(geom: sv_geom, q, kv: sv_kv, lse, weights, weights_out, sel_idx=None, sel_cnt=None, path=None, n_path=None,
+                    softmax_scale: float = 0.0, status_word=None, stream=None) -> None:
+    """The attention weight that a step's rows (those of path, n_path as sv_accept writes them, or all) give every cached token of the blocks
+    that they attended, added to weights float32 [S][Hkv][NBmax * B], into weights_out (which may be the same tensor).  lse: the
+    attention's denominators."""
+    _check(_native.attn_weights(geom, q, kv, lse, weights, weights_out, sel_idx, sel_cnt, path, n_path, softmax_scale, status_word, stream),
+           "sv_attn_weights")
+
+
+def sv_kv_evict(geom: sv_geom, k_pool, v_pool, block_table, seq_lens, weights, budget, n_sink: int, n_recent: int, seq_lens_out, weights_out,
+                reps=None, status_word=None, stream=None) -> None:
+    """Of every sequence the first n_sink, the last n_recent and the heaviest other tokens stay, budget int32 [S] in all, in their order;
+    pools in place, new lengths into seq_lens_out (a different tensor than seq_lens), weights into weights_out (which may be weights)."""
+    _check(_native.kv_evict(geom, k_pool, v_pool, block_table, seq_lens, weights, budget, n_sink, n_recent, seq_lens_out, weights_out, reps,
+                            status_word, stream), "sv_kv_evict")
 
 
 def sv_sample(logits, u, tokens, probs=None, temperature=None, top_k=None, top_p=None, min_p=None, stream=None) -> None:

@@ -15,7 +15,8 @@ LIB = os.path.join(HERE, "libsv.so")
 NATIVE = os.path.join(HERE, "_native.so")
 NATIVE_SOURCE = os.path.join(CSRC, "py_native.cpp")
 SOURCES = ["sv_api.cu", "block_reps.cu", "select_blocks.cu", "verify_attn.cu", "verify_attn_tc.cu", "kv_append.cu", "anchor_calib.cu",
-           "select_variants.cu", "accept.cu", "host_step.cu", "host_direct.cu", "rope_append.cu", "chunk_attn.cu", "sample.cu"]
+           "select_variants.cu", "accept.cu", "host_step.cu", "host_direct.cu", "rope_append.cu", "chunk_attn.cu", "sample.cu",
+           "q4_append.cu", "q4_attn.cu", "attn_weights.cu", "kv_evict.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "--use_fast_math", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
               "-I", os.path.join(ROOT, "include"), "-I", CSRC]

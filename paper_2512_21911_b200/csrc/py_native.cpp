@@ -90,6 +90,7 @@ T structure(PyObject *o, const char *name)
 }
 sv_geom geometry(PyObject *o) { return structure<sv_geom>(o, "sv_geom"); }
 sv_kv cache(PyObject *o) { return structure<sv_kv>(o, "sv_kv"); }
+sv_kv_q4 cache_q4(PyObject *o) { return structure<sv_kv_q4>(o, "sv_kv_q4"); }
 
 // The stream argument of the binding: a torch stream, or None for the current one.
 void *stream(PyObject *o)
@@ -579,19 +580,30 @@ void has(const at::Tensor &t, int64_t numel, const char *call)
 }
 
 // geom, k_pool, v_pool, block_table, seq_lens, q, k, v, q_start, q_out, seq_lens_out, rope, interleaved, reps, status_word, stream
-PyObject *rope_append(PyObject *, PyObject *const *a, Py_ssize_t n)
+// pages of a 4-bit pool [n_pages][Hkv][B / 64][SV_Q4_SLAB_BYTES]
+const at::Tensor &pool_q4(PyObject *o, const sv_geom &g, const char *call)
 {
-    return checked(n, 16, [&] {
-        constexpr const char *call = "sv_rope_append";
+    const at::Tensor &t = tensor(o, at::kByte, "pool");
+    if (t.dim() != 4 || t.size(0) > INT32_MAX || t.size(1) != g.n_kv_heads || t.size(2) * 64 != g.block_size || t.size(3) != SV_Q4_SLAB_BYTES)
+        shapes_disagree(call);
+    return t;
+}
+// k_pool, v_pool; of a 4-bit cache pool, None
+PyObject *append_rows(PyObject *const *a, Py_ssize_t n, bool q4)
+{
+    return checked(n, 17, [&] {
+        const char *const call = q4 ? "sv_rope_append_q4" : "sv_rope_append";
         const sv_geom g = geometry(a[0]);
-        const at::Tensor &kp = tensor(a[1], at::kBFloat16, "k_pool"), &vp = tensor(a[2], at::kBFloat16, "v_pool");
+        const at::Tensor &kp = q4 ? pool_q4(a[1], g, call) : tensor(a[1], at::kBFloat16, "k_pool");
+        const at::Tensor &vp = q4 ? kp : tensor(a[2], at::kBFloat16, "v_pool");
         const at::Tensor &k = head_rows(a[6], g.n_kv_heads, g.head_dim, "k"), &v = head_rows(a[7], g.n_kv_heads, g.head_dim, "v");
         const int64_t N = k.size(0);
         has(tensor(a[3], at::kInt, "block_table"), (int64_t)g.n_seq * g.max_blocks, call);
         has(tensor(a[4], at::kInt, "seq_lens"), g.n_seq, call);
         has(tensor(a[8], at::kInt, "q_start"), (int64_t)g.n_seq + 1, call);
         has(tensor(a[10], at::kInt, "seq_lens_out"), g.n_seq, call);
-        if (v.size(0) != N || N > INT32_MAX || !vp.sizes().equals(kp.sizes()) || kp.dim() != 4 || kp.size(1) != g.n_kv_heads || kp.size(2) != g.block_size)
+        if (v.size(0) != N || N > INT32_MAX ||
+            (!q4 && (!vp.sizes().equals(kp.sizes()) || kp.dim() != 4 || kp.size(1) != g.n_kv_heads || kp.size(2) != g.block_size)))
             shapes_disagree(call);
         const void *q = nullptr;
         int64_t q_stride = 0;
@@ -615,21 +627,120 @@ PyObject *rope_append(PyObject *, PyObject *const *a, Py_ssize_t n)
         int32_t *const word = i32(a[14], "status_word"), *const lens_out = i32(a[10], "seq_lens_out");
         const int32_t *const table = i32(a[3], "block_table"), *const lens = i32(a[4], "seq_lens"), *const start = i32(a[8], "q_start");
         void *const s = stream(a[15]);
+        if (a[16] != Py_None) has(tensor(a[16], at::kInt, "positions"), g.n_seq, call);
+        const int32_t *const positions = i32(a[16], "positions");
+        if (q4)
+            return status(unlocked([&] {
+                return sv_rope_append_q4(&g, kp.data_ptr(), (int32_t)kp.size(0), table, lens, q, k.data_ptr(), v.data_ptr(), q_stride, k.stride(0),
+                                         v.stride(0), start, (int32_t)N, rope, rope_rows, rot, pairs, q_out, lens_out, reps, word, s);
+            }));
         return status(unlocked([&] {
-            return sv_rope_append(&g, kp.data_ptr(), vp.data_ptr(), (int32_t)kp.size(0), table, lens, q, k.data_ptr(), v.data_ptr(), q_stride,
-                                  k.stride(0), v.stride(0), start, (int32_t)N, rope, rope_rows, rot, pairs, q_out, lens_out, reps, word, s);
+            return sv_rope_append_at(&g, kp.data_ptr(), vp.data_ptr(), (int32_t)kp.size(0), table, lens, positions, q, k.data_ptr(), v.data_ptr(),
+                                     q_stride, k.stride(0), v.stride(0), start, (int32_t)N, rope, rope_rows, rot, pairs, q_out, lens_out, reps, word, s);
         }));
     });
 }
 
 // geom, q, kv, q_start, out, lse, workspace, softmax_scale, status_word, stream
-PyObject *chunk_attn(PyObject *, PyObject *const *a, Py_ssize_t n)
+PyObject *rope_append(PyObject *, PyObject *const *a, Py_ssize_t n) { return append_rows(a, n, false); }
+PyObject *rope_append_q4(PyObject *, PyObject *const *a, Py_ssize_t n) { return append_rows(a, n, true); }
+// geom, pool, block_table, seq_lens, draft_k, draft_v, accept_idx, n_accept, seq_lens_out, reps, stream
+PyObject *kv_append_q4(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return checked(n, 11, [&] {
+        constexpr const char *call = "sv_kv_append_q4";
+        const sv_geom g = geometry(a[0]);
+        const at::Tensor &pool = pool_q4(a[1], g, call);
+        has(tensor(a[2], at::kInt, "block_table"), (int64_t)g.n_seq * g.max_blocks, call);
+        has(tensor(a[3], at::kInt, "seq_lens"), g.n_seq, call);
+        const int64_t rows = (int64_t)g.n_seq * g.n_draft * g.n_kv_heads * g.head_dim;
+        has(tensor(a[4], at::kBFloat16, "draft_k"), rows, call);
+        has(tensor(a[5], at::kBFloat16, "draft_v"), rows, call);
+        const int32_t most = row_length(a[6], "accept_idx");
+        has(tensor(a[6], at::kInt, "accept_idx"), (int64_t)g.n_seq * most, call);
+        has(tensor(a[7], at::kInt, "n_accept"), g.n_seq, call);
+        has(tensor(a[8], at::kInt, "seq_lens_out"), g.n_seq, call);
+        if (a[9] != Py_None) has(tensor(a[9], at::kFloat, "reps"), (int64_t)g.n_seq * g.n_kv_heads * g.max_blocks * g.head_dim, call);
+        const int32_t *const table = i32(a[2], "block_table"), *const lens = i32(a[3], "seq_lens"), *const idx = i32(a[6], "accept_idx"),
+                      *const cnt = i32(a[7], "n_accept");
+        const void *const dk = bf16(a[4], "draft_k"), *const dv = bf16(a[5], "draft_v");
+        int32_t *const lens_out = i32(a[8], "seq_lens_out");
+        float *const reps = f32(a[9], "reps");
+        void *const s = stream(a[10]);
+        return status(unlocked([&] {
+            return sv_kv_append_q4(&g, pool.data_ptr(), (int32_t)pool.size(0), table, lens, dk, dv, idx, cnt, most, lens_out, reps, s);
+        }));
+    });
+}
+// geom, kv, first, q_start, k_out, v_out, status_word, stream
+PyObject *kv_read_q4(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return checked(n, 8, [&] {
+        constexpr const char *call = "sv_kv_read_q4";
+        const sv_geom g = geometry(a[0]);
+        const sv_kv_q4 kv = cache_q4(a[1]);
+        const at::Tensor &k = tensor(a[4], at::kBFloat16, "k_out");
+        has(tensor(a[2], at::kInt, "first"), g.n_seq, call);
+        has(tensor(a[3], at::kInt, "q_start"), (int64_t)g.n_seq + 1, call);
+        const int64_t N = k.dim() ? k.size(0) : 0;
+        if (N > INT32_MAX || k.numel() != N * g.n_kv_heads * g.head_dim || !tensor(a[5], at::kBFloat16, "v_out").sizes().equals(k.sizes()))
+            shapes_disagree(call);
+        const int32_t *const first = i32(a[2], "first"), *const start = i32(a[3], "q_start");
+        void *const v = bf16(a[5], "v_out");
+        int32_t *const word = i32(a[6], "status_word");
+        void *const s = stream(a[7]);
+        return status(unlocked([&] { return sv_kv_read_q4(&g, &kv, first, start, (int32_t)N, k.data_ptr(), v, word, s); }));
+    });
+}
+double number(PyObject *o)
+{
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw ArgError{};
+    return v;
+}
+// geom, q, kv, draft_k, draft_v, parent, sel_idx, sel_cnt, out, lse, workspace, scale, status_word, stream
+PyObject *verify_attn_q4(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return checked(n, 14, [&] {
+        constexpr const char *call = "sv_verify_attn_q4";
+        const sv_geom g = geometry(a[0]);
+        const sv_kv_q4 kv = cache_q4(a[2]);
+        const int64_t tokens = (int64_t)g.n_seq * g.n_draft;
+        has(tensor(a[1], at::kBFloat16, "q"), tokens * g.n_q_heads * g.head_dim, call);
+        has(tensor(a[3], at::kBFloat16, "draft_k"), tokens * g.n_kv_heads * g.head_dim, call);
+        has(tensor(a[4], at::kBFloat16, "draft_v"), tokens * g.n_kv_heads * g.head_dim, call);
+        has(tensor(a[8], at::kBFloat16, "out"), tokens * g.n_q_heads * g.head_dim, call);
+        if (a[5] != Py_None) has(tensor(a[5], at::kInt, "parent"), tokens, call);
+        if (a[9] != Py_None) has(tensor(a[9], at::kFloat, "lse"), tokens * g.n_q_heads, call);
+        int32_t most = 0;
+        if (a[6] != Py_None) {
+            most = row_length(a[6], "sel_idx");
+            has(tensor(a[6], at::kInt, "sel_idx"), (int64_t)g.n_seq * g.n_kv_heads * most, call);
+            if (a[7] != Py_None) has(tensor(a[7], at::kInt, "sel_cnt"), (int64_t)g.n_seq * g.n_kv_heads, call);
+        }
+        const void *const q = bf16(a[1], "q"), *const dk = bf16(a[3], "draft_k"), *const dv = bf16(a[4], "draft_v");
+        const int32_t *const parent = i32(a[5], "parent"), *const idx = i32(a[6], "sel_idx"), *const cnt = i32(a[7], "sel_cnt");
+        void *const out = bf16(a[8], "out");
+        float *const lse = f32(a[9], "lse");
+        const Scratch ws = scratch(a[10]);
+        const double scale = number(a[11]);
+        int32_t *const word = i32(a[12], "status_word");
+        void *const s = stream(a[13]);
+        return status(unlocked([&] {
+            return sv_verify_attn_q4(&g, q, &kv, dk, dv, parent, idx, cnt, most, (float)scale, out, lse, ws.p, ws.bytes, word, s);
+        }));
+    });
+}
+PyObject *chunk_rows(PyObject *const *a, Py_ssize_t n, bool q4)
 {
     return checked(n, 10, [&] {
-        constexpr const char *call = "sv_chunk_attn";
+        const char *const call = q4 ? "sv_chunk_attn_q4" : "sv_chunk_attn";
         const sv_geom g = geometry(a[0]);
         const at::Tensor &q = tensor(a[1], at::kBFloat16, "q"), &out = tensor(a[4], at::kBFloat16, "out");
-        const sv_kv kv = cache(a[2]);
+        sv_kv kv{};
+        sv_kv_q4 kv_q4{};
+        if (q4) kv_q4 = cache_q4(a[2]);
+        else kv = cache(a[2]);
         const int64_t N = q.dim() ? q.size(0) : 0;
         if (N > INT32_MAX || q.numel() != N * g.n_q_heads * g.head_dim || !out.sizes().equals(q.sizes())) shapes_disagree(call);
         has(tensor(a[3], at::kInt, "q_start"), (int64_t)g.n_seq + 1, call);
@@ -641,8 +752,75 @@ PyObject *chunk_attn(PyObject *, PyObject *const *a, Py_ssize_t n)
         if (scale == -1.0 && PyErr_Occurred()) throw ArgError{};
         int32_t *const word = i32(a[8], "status_word");
         void *const s = stream(a[9]);
+        if (q4)
+            return status(unlocked([&] {
+                return sv_chunk_attn_q4(&g, q.data_ptr(), &kv_q4, start, (int32_t)N, (float)scale, out.data_ptr(), lse, ws.p, ws.bytes, word, s);
+            }));
         return status(unlocked([&] {
             return sv_chunk_attn(&g, q.data_ptr(), &kv, start, (int32_t)N, (float)scale, out.data_ptr(), lse, ws.p, ws.bytes, word, s);
+        }));
+    });
+}
+
+PyObject *chunk_attn(PyObject *, PyObject *const *a, Py_ssize_t n) { return chunk_rows(a, n, false); }
+PyObject *chunk_attn_q4(PyObject *, PyObject *const *a, Py_ssize_t n) { return chunk_rows(a, n, true); }
+
+// geom, q, kv, lse, weights, weights_out, sel_idx, sel_cnt, path, n_path, scale, status_word, stream
+PyObject *attn_weights(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return checked(n, 13, [&] {
+        constexpr const char *call = "sv_attn_weights";
+        const sv_geom g = geometry(a[0]);
+        const sv_kv kv = cache(a[2]);
+        const int64_t rows = (int64_t)g.n_seq * g.n_draft * g.n_q_heads, lists = (int64_t)g.n_seq * g.n_kv_heads;
+        has(tensor(a[1], at::kBFloat16, "q"), rows * g.head_dim, call);
+        has(tensor(a[3], at::kFloat, "lse"), rows, call);
+        has(tensor(a[4], at::kFloat, "weights"), lists * g.max_blocks * g.block_size, call);
+        has(tensor(a[5], at::kFloat, "weights_out"), lists * g.max_blocks * g.block_size, call);
+        int32_t most = 0;
+        if (a[6] != Py_None) {
+            most = row_length(a[6], "sel_idx");
+            has(tensor(a[6], at::kInt, "sel_idx"), lists * most, call);
+            if (a[7] != Py_None) has(tensor(a[7], at::kInt, "sel_cnt"), lists, call);
+        }
+        if (a[8] != Py_None) has(tensor(a[8], at::kInt, "path"), (int64_t)g.n_seq * g.n_draft, call);
+        if (a[9] != Py_None) has(tensor(a[9], at::kInt, "n_path"), g.n_seq, call);
+        const void *const q = bf16(a[1], "q");
+        const float *const lse = f32(a[3], "lse"), *const before = f32(a[4], "weights");
+        float *const after = f32(a[5], "weights_out");
+        const int32_t *const idx = i32(a[6], "sel_idx"), *const cnt = i32(a[7], "sel_cnt"), *const path = i32(a[8], "path"), *const n_path = i32(a[9], "n_path");
+        const double scale = number(a[10]);
+        int32_t *const word = i32(a[11], "status_word");
+        void *const s = stream(a[12]);
+        return status(unlocked([&] { return sv_attn_weights(&g, q, &kv, lse, idx, cnt, most, path, n_path, (float)scale, before, after, word, s); }));
+    });
+}
+// geom, k_pool, v_pool, block_table, seq_lens, weights, budget, n_sink, n_recent, seq_lens_out, weights_out, reps, status_word, stream
+PyObject *kv_evict(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return checked(n, 14, [&] {
+        constexpr const char *call = "sv_kv_evict";
+        const sv_geom g = geometry(a[0]);
+        const at::Tensor &kp = tensor(a[1], at::kBFloat16, "k_pool"), &vp = tensor(a[2], at::kBFloat16, "v_pool");
+        if (!vp.sizes().equals(kp.sizes()) || kp.dim() != 4 || kp.size(0) > INT32_MAX || kp.size(1) != g.n_kv_heads || kp.size(2) != g.block_size ||
+            kp.size(3) != g.head_dim)
+            shapes_disagree(call);
+        const int64_t lists = (int64_t)g.n_seq * g.n_kv_heads;
+        has(tensor(a[3], at::kInt, "block_table"), (int64_t)g.n_seq * g.max_blocks, call);
+        has(tensor(a[4], at::kInt, "seq_lens"), g.n_seq, call);
+        has(tensor(a[5], at::kFloat, "weights"), lists * g.max_blocks * g.block_size, call);
+        has(tensor(a[6], at::kInt, "budget"), g.n_seq, call);
+        has(tensor(a[9], at::kInt, "seq_lens_out"), g.n_seq, call);
+        has(tensor(a[10], at::kFloat, "weights_out"), lists * g.max_blocks * g.block_size, call);
+        if (a[11] != Py_None) has(tensor(a[11], at::kFloat, "reps"), lists * g.max_blocks * g.head_dim, call);
+        const int32_t *const table = i32(a[3], "block_table"), *const lens = i32(a[4], "seq_lens"), *const budget = i32(a[6], "budget");
+        const float *const before = f32(a[5], "weights");
+        const int32_t sink = int32(a[7]), recent = int32(a[8]);
+        int32_t *const lens_out = i32(a[9], "seq_lens_out"), *const word = i32(a[12], "status_word");
+        float *const after = f32(a[10], "weights_out"), *const reps = f32(a[11], "reps");
+        void *const s = stream(a[13]);
+        return status(unlocked([&] {
+            return sv_kv_evict(&g, kp.data_ptr(), vp.data_ptr(), (int32_t)kp.size(0), table, lens, before, budget, sink, recent, lens_out, after, reps, word, s);
         }));
     });
 }
@@ -692,7 +870,9 @@ PyObject *sample(PyObject *, PyObject *const *a, Py_ssize_t n)
 PyMethodDef methods[] = {METHOD(block_reps), METHOD(select_blocks), METHOD(verify_attn), METHOD(kv_append), METHOD(accept),
                          METHOD(verify_layer), METHOD(layer_row), METHOD(workspace_bytes_layers), METHOD(workspace_bytes_host_step), METHOD(block_reps_layers),
                          METHOD(verify_layers), METHOD(kv_append_layers), METHOD(accept_new), METHOD(host_step), METHOD(verify_step_from_host), METHOD(rope_append),
-                         METHOD(chunk_attn), METHOD(sample), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(chunk_attn), METHOD(sample), METHOD(rope_append_q4), METHOD(kv_append_q4), METHOD(kv_read_q4), METHOD(verify_attn_q4), METHOD(chunk_attn_q4),
+                         METHOD(attn_weights), METHOD(kv_evict),
+                         {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Argument marshalling for the entry points of sv.h.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,815 @@
+// sv_verify_attn_q4, sv_chunk_attn_q4: attention over a paged cache held in 4 bits (q4.cuh), of draft tokens over kept blocks and their
+// own keys, or of a ragged batch of new tokens over the cache that holds them.
+//
+// Mathematics, for a row q and the keys t that it sees: s_t = q . k_t * scale * log2 e, a reference m not far below the running maximum,
+// l = sum 2^(s_t - m), o = sum 2^(s_t - m) v_t; the output is o / l.  When the maximum outgrows the reference by more than 8, m moves and
+// l and o are multiplied by 2^(old - new).
+//
+// A quarter of the bytes of a bfloat16 cache, but every value has to be decoded: what counts is instructions per value and that decoded
+// values go nowhere but to the tensor cores.  So the cache is operand A, read from tensor memory, and the roles of rows and keys are
+// exchanged: both products are of 128 (keys, then dims) x N (query rows) with N = 16, 32 or 64,
+//   S^T[128 keys x N] = K . Q^T      a thread decodes a key's 128 dims into its lane of tensor memory
+//   O^T[128 dims x N] += V^T . P^T   a thread decodes a dim's 128 keys into its lane
+// and a few query rows cost what they are instead of a tile of 128.  A thread then has a key's scores against all rows: masks are its own
+// affair, sums of weights stay in registers until the end, and the running maximum, which would have to go across lanes, is only
+// looked for when a score outgrows the reference.
+//
+// A worker is a warpgroup that has everything it needs to itself -- a ring of slabs filled by bulk copies (one of 9216 bytes for 64 tokens,
+// no tensor maps), queries, P, tensor memory -- and takes a share of the batch (q4_shares.h), so that workers never wait for one another:
+// while one waits for a product the others decode.  An item that is cut is written as partial sums and merged by a second kernel.
+#include <cuda_bf16.h>
+
+#include <algorithm>
+
+#include "attn_common.cuh"
+#include "q4.cuh"
+#include "shares.cuh"
+#include "sv_host.h"
+#include "sv_ptx.cuh"
+
+namespace {
+
+using namespace svk;
+using svq::kSlabBytes;
+using svq::kUnit;
+
+constexpr float kLag = 8.f;   // what a score may exceed the reference by (log2)
+
+struct Params {
+    const uint8_t *pool;
+    const int32_t *block_table, *seq_lens, *sel_idx, *sel_cnt, *q_start, *parent;
+    const __nv_bfloat16 *q, *draft_k, *draft_v;
+    __nv_bfloat16 *out;
+    float *lse;
+    float *ws_o;     // [2 * workers][N][128]: of a worker, the part of an item that began before and of one that goes on behind
+    float2 *ws_ml;   // [2 * workers][N]
+    int4 *cuts;      // [workers][2] the cut item that begins in a worker's share: first token, first row, KV head and rows, parts (0: none); rows without a key
+    int32_t *status;
+    int S, Hq, Hkv, G, T, n_tokens, B, NBmax, n_pages, max_sel;
+    float scale_log2;
+};
+
+// Sizes that follow from the rows of a tile.
+template <int N>
+struct Form {
+    static constexpr int kWorkers = N == 64 ? 2 : 4;             // of a CTA
+    static constexpr int kThreads = kWorkers * 128;
+    static constexpr int kStages = N == 64 ? 4 : 2;              // units of a worker's ring
+    static constexpr int kUnitBytes = 2 * kSlabBytes;
+    static constexpr int kQBytes = N * 256;                      // [2 halves of the dims][N rows][128 bytes]
+    static constexpr int kPTile = 128 * 128;                     // [128 keys][128 bytes], of which N * 2 are one worker's
+    static constexpr int kSharers = 64 / N < kWorkers ? 64 / N : kWorkers;
+    static constexpr int kOffQ = 0;
+    static constexpr int kOffP = kWorkers * kQBytes;
+    static constexpr int kOffRing = kOffP + kWorkers / kSharers * kPTile;
+    static constexpr int kOffMisc = kOffRing + kWorkers * kStages * kUnitBytes;
+    // per worker: reference, its negative where there is one, factors, maxima and sums of four warps, row masks; barriers; valid tokens
+    static constexpr int kMRef = 0, kNeg = kMRef + N * 4, kFactor = kNeg + N * 4, kParts = kFactor + N * 4, kMasks = kParts + 4 * N * 4,
+                         kBars = kMasks + 64 * 8, kValid = kBars + (kStages + 2) * 8, kMiscBytes = (kValid + kStages * 8 + 127) / 128 * 128;
+    static constexpr int kOffShared = kOffMisc + kWorkers * kMiscBytes;   // tensor memory's address, the abort flag, the scan
+    static constexpr int kSharedBytes = 512;
+    static constexpr int kSmem = 1024 + kOffShared + kSharedBytes;
+    static constexpr int kColumns = 64 + 2 * N;                  // of tensor memory: decoded keys or values, S, O
+    static_assert(kWorkers * kColumns <= 512 && kSmem <= 232448, "");
+};
+
+// A (sequence, KV head) and what its items cost.
+struct Place {
+    int s, h;
+    int len;          // cached tokens that may be seen, at most what the table has room for
+    int slabs;        // verify: of the list, or of the sequence
+    int tok0, n;      // chunk: first new token, new tokens; verify: s * T, T
+    int pos0;         // chunk: position of the first new token
+    svq::Entry cost;
+};
+
+template <bool kChunk, int N>
+__device__ __forceinline__ Place place(const Params &p, int e)
+{
+    Place r;
+    r.s = e / p.Hkv, r.h = e - r.s * p.Hkv;
+    const int cap = (int)min((long long)p.NBmax * p.B, 0x7fffffffll);
+    const int len = __ldg(p.seq_lens + r.s);
+    r.len = min(max(len, 0), cap);
+    if constexpr (kChunk) {
+        const int first = min(max(__ldg(p.q_start + r.s), 0), p.n_tokens), end = min(max(__ldg(p.q_start + r.s + 1), 0), p.n_tokens);
+        r.tok0 = first, r.n = max(end - first, 0), r.pos0 = len - r.n;
+        r.slabs = 0;
+        const int seen = min(max(r.pos0, 0), cap);
+        r.cost.tiles = (int)(((long long)r.n * p.G + N - 1) / N);
+        r.cost.a = (long long)p.G * (seen + svq::kItemCost), r.cost.b = N;
+    } else {
+        r.tok0 = r.s * p.T, r.n = p.T, r.pos0 = 0;
+        if (p.sel_idx) {
+            const int cnt = min(max(__ldg(p.sel_cnt + e), 0), p.max_sel);
+            r.slabs = cnt * (p.B / 64);
+        } else {
+            r.slabs = (r.len + 63) / 64;
+        }
+        r.cost.tiles = (p.G * p.T + N - 1) / N;
+        r.cost.a = svq::kItemCost + (long long)kUnit * ((r.slabs + 1) / 2 + 1), r.cost.b = 0;
+    }
+    return r;
+}
+
+template <int N, bool kChunk>
+struct Worker {
+    using F = Form<N>;
+    const Params &p;
+    uint32_t q_tile, p_tile, ring, misc, shared, tmem;   // shared memory and tensor memory of this worker
+    int wg, tid, lane, warp, worker;
+    uint32_t of_s = 0, of_o = 0;    // parities
+    int taken = 0, asked = 0;       // units of the ring consumed and requested, ever
+    uint64_t policy;
+
+    __device__ uint32_t bar_full(int i) const { return misc + F::kBars + i * 8; }
+    __device__ uint32_t bar_s() const { return bar_full(F::kStages); }
+    __device__ uint32_t bar_o() const { return bar_full(F::kStages + 1); }
+    __device__ void sync() const { named_bar_sync(1 + wg, 128); }
+    __device__ bool aborted() const
+    {
+        uint32_t v;
+        asm volatile("ld.volatile.shared.b32 %0, [%1];" : "=r"(v) : "r"(shared + 4) : "memory");
+        return v != 0;
+    }
+    // Bounded.  Where it gives up it says so, later waits of the CTA look once, and everybody goes on to the end with what there is.
+    __device__ void wait(uint32_t bar, uint32_t parity, int bit) const
+    {
+#pragma unroll 1
+        for (int n = 0; n < 1 << 13; ++n) {
+#pragma unroll 1
+            for (int i = 0; i < 64; ++i)
+                if (mbar_try_wait(bar, parity)) return;
+            if (aborted()) return;
+        }
+        sts32(shared + 4, 1);
+        if (p.status) atomicOr(p.status, bit);
+    }
+
+    // Copies and products that nobody waited for, when a wait gave up: this CTA's memory stays until they are through.
+    __device__ void drain() const
+    {
+        if (!aborted()) return;
+#pragma unroll 1
+        for (int i = 0; i < F::kStages; ++i) {
+            const int n = asked > i ? (asked - i + F::kStages - 1) / F::kStages : 0;
+            if (n > 0) (void)mbar_wait_bounded(bar_full(i), (n - 1) & 1);
+        }
+        (void)mbar_wait_bounded(bar_s(), of_s ^ 1);
+        (void)mbar_wait_bounded(bar_o(), of_o ^ 1);
+    }
+
+    // ------------------------------------------------------------------ the ring
+    int list_base = -1, known = 0, known_valid = 0;   // (warp 0) a slab a lane, from list_base on: its page's slab number, its tokens
+    __device__ void look_up(const Place &pl, int end, int n_slabs, int from)
+    {
+        list_base = from;
+        const int j = from + lane, per = p.B / 64;
+        known = 0, known_valid = 0;
+        if (j >= n_slabs) return;
+        int b = j / per;
+        const int sub = j - b * per;
+        bool bad = false;
+        if (!kChunk && p.sel_idx) {
+            b = __ldg(p.sel_idx + ((size_t)pl.s * p.Hkv + pl.h) * p.max_sel + b);
+            bad = (unsigned)b >= (unsigned)p.NBmax;
+            b = min(max(b, 0), p.NBmax - 1);
+        }
+        int page = __ldg(p.block_table + (size_t)pl.s * p.NBmax + b);
+        known_valid = (int)min(max((long long)end - (long long)b * p.B - sub * 64, 0ll), 64ll);
+        if (known_valid > 0) bad = bad || (unsigned)page >= (unsigned)p.n_pages;
+        page = min(max(page, 0), p.n_pages - 1);
+        if (bad && p.status) atomicOr(p.status, kStatusIndex);
+        known = (page * p.Hkv + pl.h) * per + sub;
+    }
+    // unit u of the item (warp 0, converged)
+    __device__ void ask(const Place &pl, int end, int n_slabs, int u)
+    {
+        if (list_base < 0 || 2 * u >= list_base + 32) look_up(pl, end, n_slabs, 2 * u);
+        const int i = 2 * u - list_base;
+        const int a = __shfl_sync(0xffffffffu, known, i), b = __shfl_sync(0xffffffffu, known, (i + 1) & 31);
+        const int va = __shfl_sync(0xffffffffu, known_valid, i), vb = __shfl_sync(0xffffffffu, known_valid, (i + 1) & 31);
+        const int stage = asked % F::kStages;
+        if (elect_one()) {
+            const uint32_t full = bar_full(stage), dst = ring + stage * F::kUnitBytes, valid = misc + F::kValid + stage * 8;
+            sts32(valid, va), sts32(valid + 4, vb);
+            const bool second = 2 * u + 1 < n_slabs;
+            mbar_arrive_expect_tx(full, second ? F::kUnitBytes : kSlabBytes);
+            bulk_load(dst, p.pool + (size_t)a * kSlabBytes, kSlabBytes, full, policy);
+            if (second) bulk_load(dst + kSlabBytes, p.pool + (size_t)b * kSlabBytes, kSlabBytes, full, policy);
+        }
+        __syncwarp();
+        ++asked;
+    }
+
+    // ------------------------------------------------------------------ operands
+    __device__ void keys_of(uint32_t slot, uint32_t *x) const   // this thread's key
+    {
+        const uint32_t slab = slot + (tid >> 6) * kSlabBytes, t = tid & 63;
+        const uint2 sc = lds64(slab + svq::kOffKScale + t * 8);
+        const uint32_t d[2] = {svq::both_low(sc.x), svq::both_low(sc.y)}, m[2] = {svq::both_high(sc.x), svq::both_high(sc.y)};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const uint4 w = lds128(slab + c * 1024 + t * 16);
+            svq::decode(w.x, d[c >> 1], m[c >> 1], x + 16 * c);
+            svq::decode(w.y, d[c >> 1], m[c >> 1], x + 16 * c + 4);
+            svq::decode(w.z, d[c >> 1], m[c >> 1], x + 16 * c + 8);
+            svq::decode(w.w, d[c >> 1], m[c >> 1], x + 16 * c + 12);
+        }
+    }
+    __device__ static uint4 cut_pairs(uint4 v, int n)   // of eight numbers the first n
+    {
+        const auto one = [n](uint32_t w, int i) { return n >= i + 2 ? w : n == i + 1 ? w & 0xffffu : 0u; };
+        return make_uint4(one(v.x, 0), one(v.y, 2), one(v.z, 4), one(v.w, 6));
+    }
+    // this thread's dim of 64 tokens, of which `valid` are there (the others are zero: whatever a slab holds there, a weight of zero
+    // times it is to be zero)
+    __device__ void values_of(uint32_t slab, int valid, uint32_t *x) const
+    {
+        const uint32_t sc = slab + svq::kOffVScale + (tid >> 6) * 256;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const uint4 w = lds128(slab + svq::kOffV + c * 2048 + tid * 16);
+            const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint4 d = lds128(sc + c * 64 + i * 16), m = lds128(sc + 128 + c * 64 + i * 16);
+                if (valid < 64) d = cut_pairs(d, valid - 32 * c - 8 * i), m = cut_pairs(m, valid - 32 * c - 8 * i);
+                uint32_t *o = x + 16 * c + 4 * i;
+                o[0] = svq::fma_bf16x2(svq::steps<0>(words[i]), d.x, m.x);
+                o[1] = svq::fma_bf16x2(svq::steps<1>(words[i]), d.y, m.y);
+                o[2] = svq::fma_bf16x2(svq::steps<2>(words[i]), d.z, m.z);
+                o[3] = svq::fma_bf16x2(svq::steps<3>(words[i]), d.w, m.w);
+            }
+        }
+    }
+    __device__ void draft_keys(const Place &pl, uint32_t *x) const
+    {
+        const uint4 *row = reinterpret_cast<const uint4 *>(p.draft_k + ((size_t)(pl.tok0 + tid) * p.Hkv + pl.h) * 128);
+#pragma unroll
+        for (int c = 0; c < 16; ++c) {
+            const uint4 w = tid < p.T ? __ldg(row + c) : make_uint4(0, 0, 0, 0);
+            x[4 * c] = w.x, x[4 * c + 1] = w.y, x[4 * c + 2] = w.z, x[4 * c + 3] = w.w;
+        }
+    }
+    __device__ void draft_values(const Place &pl, uint32_t *x) const
+    {
+        const unsigned short *col = reinterpret_cast<const unsigned short *>(p.draft_v + ((size_t)pl.tok0 * p.Hkv + pl.h) * 128 + tid);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            const uint32_t a = 2 * j < p.T ? __ldg(col + (size_t)(2 * j) * p.Hkv * 128) : 0u;
+            const uint32_t b = 2 * j + 1 < p.T ? __ldg(col + (size_t)(2 * j + 1) * p.Hkv * 128) : 0u;
+            x[j] = a | b << 16;
+            x[32 + j] = 0u;
+        }
+    }
+    __device__ void store_operand(const uint32_t *x) const
+    {
+        const uint32_t at = tmem + ((uint32_t)(warp * 32) << 16);
+        tmem_st_x32(at, *reinterpret_cast<const uint32_t(*)[32]>(x));
+        tmem_st_x32(at + 32, *reinterpret_cast<const uint32_t(*)[32]>(x + 32));
+    }
+
+    // ------------------------------------------------------------------ products (one thread)
+    __device__ void issue_s() const
+    {
+        constexpr uint32_t idesc = umma_idesc_bf16(128, N, false);
+        const uint64_t dq = umma_desc_sw128(q_tile, 16, 1024);
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks)
+            tc_mma_bf16_ta(tmem + 64, tmem + ks * 8, dq + (uint64_t)((ks & 3) * 2 + (ks >> 2) * (N * 128 >> 4)), idesc, ks > 0);
+        tc_commit(bar_s());
+    }
+    __device__ void issue_o(bool more) const
+    {
+        constexpr uint32_t idesc = umma_idesc_bf16(128, N, true);
+        const uint64_t dp = umma_desc_sw128(p_tile, 8192, 1024);
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks)
+            tc_mma_bf16_ta(tmem + 64 + N, tmem + ks * 8, dp + (uint64_t)(ks * 2048 >> 4), idesc, ks > 0 || more);
+        tc_commit(bar_o());
+    }
+
+    // ------------------------------------------------------------------ a part of an item
+    __device__ void run(const Place &pl, int tile, const svq::Part &part, int units)
+    {
+        const int row0 = tile * N, rows = min(N, p.G * pl.n - row0);
+        // keys that any row sees, and the slabs that hold them
+        int end = pl.len, n_slabs = pl.slabs;
+        if constexpr (kChunk) {
+            end = min(max(pl.pos0 + (row0 + rows - 1) / p.G + 1, 0), pl.len);
+            n_slabs = (end + 63) / 64;
+        }
+        const int slab_units = (n_slabs + 1) / 2;
+        const int n_units = max(min(part.u1, slab_units) - part.u0, 0);
+        const bool drafts = !kChunk && part.u1 == units;
+        const size_t out_row = (size_t)pl.tok0 * p.Hq + pl.h * p.G;   // of row 0 of token 0
+
+        sync();   // (the last item's rows have been read)
+        if (warp == 0) {
+            list_base = -1;
+            for (int u = 0; u < min(n_units, F::kStages); ++u) ask(pl, end, n_slabs, part.u0 + u);
+        }
+#pragma unroll
+        for (int i = 0; i < N / 8; ++i) {
+            const int c = i * 128 + tid, r = c >> 4, ch = c & 15, row = row0 + r;
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (r < rows) v = __ldg(reinterpret_cast<const uint4 *>(p.q + (out_row + (size_t)(row / p.G) * p.Hq + row % p.G) * 128) + ch);
+            sts128(q_tile + (ch >> 3) * (N * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4), v);
+        }
+        if (tid < N) stsf(misc + F::kMRef + tid * 4, -INFINITY), stsf(misc + F::kNeg + tid * 4, 0.f);
+        if (drafts) {
+            // which drafts a row's token sees: itself and its ancestors, or all up to it
+            if (tid < N) {
+                unsigned long long seen = 0;
+                const int i = min((row0 + tid) / p.G, p.T - 1);
+                if (p.parent) {
+                    const int32_t *parent = p.parent + (size_t)pl.s * p.T;
+                    int j = i;
+#pragma unroll 1
+                    for (int n = 0; n < 64 && j >= 0; ++n) {
+                        seen |= 1ull << j;
+                        const int up = __ldg(parent + j);
+                        j = up < j ? up : -1;
+                    }
+                } else {
+                    seen = (2ull << i) - 1;
+                }
+                sts64(misc + F::kMasks + tid * 8, seen);
+            }
+        }
+        fence_proxy_async();
+        sync();
+
+        unsigned long long l2[N / 2];   // sums of the weights, rows 2 i and 2 i + 1
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) l2[i] = 0ull;
+        bool fresh = true, started = false;
+        const unsigned long long scale2 = f2_pack(p.scale_log2, p.scale_log2);
+        const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+
+#pragma unroll 1
+        for (int k = drafts ? -1 : 0; k < n_units; ++k) {
+            const int stage = taken % F::kStages;
+            const uint32_t slot = ring + stage * F::kUnitBytes;
+            int valid[2] = {p.T, 0};
+            uint32_t x[64];
+            if (k < 0) {
+                draft_keys(pl, x);
+            } else {
+                wait(bar_full(stage), (taken / F::kStages) & 1, 1);
+                const uint2 v = lds64(misc + F::kValid + stage * 8);
+                valid[0] = (int)v.x, valid[1] = (int)v.y;
+                keys_of(slot, x);
+            }
+            if (started) {
+                wait(bar_o(), of_o, 2);
+                of_o ^= 1;
+                tc_fence_after_sync();
+            }
+            store_operand(x);
+            tmem_st_wait();
+            tc_fence_before_sync();
+            sync();
+            if (warp == 0 && elect_one()) {
+                tc_fence_after_sync();
+                issue_s();
+            }
+            __syncwarp();
+            if (k < 0) {
+                draft_values(pl, x);
+            } else {
+                values_of(slot, valid[0], x);
+                values_of(slot + kSlabBytes, valid[1], x + 32);
+            }
+            wait(bar_s(), of_s, 4);
+            of_s ^= 1;
+            tc_fence_after_sync();
+            store_operand(x);
+            // scores of this thread's key
+            uint32_t s[N];
+#pragma unroll
+            for (int c = 0; c < N; c += 16) tmem_ld_x16(tmem + lanes + 64 + c, s + c);
+            tmem_ld_wait();
+            if (k < 0) {
+#pragma unroll
+                for (int r = 0; r < N; ++r) {
+                    const uint2 seen = lds64(misc + F::kMasks + r * 8);
+                    const uint32_t w = tid & 32 ? seen.y : seen.x;
+                    if (tid >= 64 || !(w >> (tid & 31) & 1)) s[r] = 0xff800000u;
+                }
+            } else {
+                const bool there = (tid & 63) < valid[tid >> 6];
+                int first = 0;   // row that sees the key first
+                if constexpr (kChunk) {
+                    const int t = (part.u0 + k) * kUnit + tid;
+                    first = (int)min(max((long long)(t - pl.pos0) * p.G - row0, 0ll), (long long)N);
+                }
+                if (!there) first = N;
+                if (__any_sync(0xffffffffu, first > 0)) {
+#pragma unroll
+                    for (int r = 0; r < N; ++r)
+                        if (r < first) s[r] = 0xff800000u;
+                }
+            }
+            // whether a score outgrows its row's reference
+            float top = -INFINITY;
+#pragma unroll
+            for (int r = 0; r < N; r += 4) {
+                const uint4 neg = lds128(misc + F::kNeg + r * 4);
+                float a, b, c, d;
+                f2_unpack(f2_fma(f2_pack(__uint_as_float(s[r]), __uint_as_float(s[r + 1])), scale2, f2_pack(__uint_as_float(neg.x), __uint_as_float(neg.y))), a, b);
+                f2_unpack(f2_fma(f2_pack(__uint_as_float(s[r + 2]), __uint_as_float(s[r + 3])), scale2, f2_pack(__uint_as_float(neg.z), __uint_as_float(neg.w))), c, d);
+                top = max3f(top, a, b);
+                top = max3f(top, c, d);
+            }
+            if (named_bar_or(1 + wg, 128, fresh || top > kLag)) {
+                // the maxima over the unit, of four warps, then of all; rows whose reference moves
+#pragma unroll
+                for (int r = 0; r < N; ++r) {
+                    const float m = warp_max(__uint_as_float(s[r]));
+                    if (lane == (r & 31)) stsf(misc + F::kParts + (warp * N + r) * 4, m);
+                }
+                sync();
+                bool none = false;
+                if (tid < N) {
+                    float m = ldsf(misc + F::kParts + tid * 4);
+#pragma unroll
+                    for (int w = 1; w < 4; ++w) m = fmaxf(m, ldsf(misc + F::kParts + (w * N + tid) * 4));
+                    m *= p.scale_log2;
+                    const float old = ldsf(misc + F::kMRef + tid * 4);
+                    float c = 1.f;
+                    if (m > old + kLag) {
+                        c = fast_exp2(old - m);
+                        stsf(misc + F::kMRef + tid * 4, m), stsf(misc + F::kNeg + tid * 4, -m);
+                        none = false;
+                    } else {
+                        none = old == -INFINITY;
+                    }
+                    stsf(misc + F::kFactor + tid * 4, c);
+                }
+                fresh = named_bar_or(1 + wg, 128, none);
+#pragma unroll
+                for (int r = 0; r < N; r += 2) {
+                    const uint2 c = lds64(misc + F::kFactor + r * 4);
+                    float a, b;
+                    f2_unpack(l2[r / 2], a, b);
+                    l2[r / 2] = f2_pack(a * __uint_as_float(c.x), b * __uint_as_float(c.y));
+                }
+                if (started) {
+#pragma unroll 1
+                    for (int c0 = 0; c0 < N; c0 += 16) {
+                        uint32_t o[16];
+                        tmem_ld_x16(tmem + lanes + 64 + N + c0, o);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * ldsf(misc + F::kFactor + (c0 + i) * 4));
+                        tmem_st_x16(tmem + lanes + 64 + N + c0, o);
+                    }
+                }
+            }
+            if (k >= 0) {
+                ++taken;
+                if (warp == 0 && k + F::kStages < n_units) ask(pl, end, n_slabs, part.u0 + k + F::kStages);   // (everybody has read the slot)
+            }
+            // Weights.  (bf16 because the matrix instruction takes both operands in one type; the sums are of what they were before.)
+            const uint32_t p_row = (p_tile & ~1023u) + tid * 128;
+            const int p_chunk = (p_tile >> 4) & 7;
+#pragma unroll
+            for (int r = 0; r < N; r += 8) {
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 8; i += 4) {
+                    const uint4 neg = lds128(misc + F::kNeg + (r + i) * 4);
+                    float a, b, c, d;
+                    f2_unpack(f2_fma(f2_pack(__uint_as_float(s[r + i]), __uint_as_float(s[r + i + 1])), scale2, f2_pack(__uint_as_float(neg.x), __uint_as_float(neg.y))), a, b);
+                    f2_unpack(f2_fma(f2_pack(__uint_as_float(s[r + i + 2]), __uint_as_float(s[r + i + 3])), scale2, f2_pack(__uint_as_float(neg.z), __uint_as_float(neg.w))), c, d);
+                    a = fast_exp2(a), b = fast_exp2(b), c = fast_exp2(c), d = fast_exp2(d);
+                    l2[(r + i) / 2] = f2_add(l2[(r + i) / 2], f2_pack(a, b));
+                    l2[(r + i) / 2 + 1] = f2_add(l2[(r + i) / 2 + 1], f2_pack(c, d));
+                    w[i / 2] = pack_bf16(a, b), w[i / 2 + 1] = pack_bf16(c, d);
+                }
+                sts128(p_row + (((p_chunk + r / 8) ^ (tid & 7)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
+            }
+            fence_proxy_async();
+            tmem_st_wait();
+            tc_fence_before_sync();
+            sync();
+            if (warp == 0 && elect_one()) {
+                tc_fence_after_sync();
+                issue_o(started);
+            }
+            __syncwarp();
+            started = true;
+        }
+
+        // sums of the weights over the keys: lanes, then warps
+        {
+            float v[N];
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) f2_unpack(l2[i], v[2 * i], v[2 * i + 1]);
+            int n = N;
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) {
+                if (n > 1) {
+                    n /= 2;
+#pragma unroll
+                    for (int i = 0; i < N / 2; ++i)
+                        if (i < n) {
+                            const bool up = lane & d;
+                            const float send = up ? v[i] : v[i + n], keep = up ? v[i + n] : v[i];
+                            v[i] = keep + __shfl_xor_sync(0xffffffffu, send, d);
+                        }
+                } else {
+                    v[0] += __shfl_xor_sync(0xffffffffu, v[0], d);
+                }
+            }
+            if constexpr (N == 64) stsf(misc + F::kParts + (warp * N + 2 * lane) * 4, v[0]), stsf(misc + F::kParts + (warp * N + 2 * lane + 1) * 4, v[1]);
+            else if constexpr (N == 32) stsf(misc + F::kParts + (warp * N + lane) * 4, v[0]);
+            else if (!(lane & 1)) stsf(misc + F::kParts + (warp * N + (lane >> 1)) * 4, v[0]);
+        }
+        if (started) {
+            wait(bar_o(), of_o, 2);
+            of_o ^= 1;
+            tc_fence_after_sync();
+        }
+        sync();
+        const bool whole = part.u0 == 0 && part.u1 == units;
+        const size_t slot = (size_t)2 * worker + (part.u0 == 0);
+        const int blind = kChunk ? min(max(-pl.pos0, 0), pl.n) * p.G : 0;   // rows of the sequence that see no key
+        if (tid < N) {
+            float l = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) l += ldsf(misc + F::kParts + (w * N + tid) * 4);
+            const float m = ldsf(misc + F::kMRef + tid * 4);
+            const int row = row0 + tid;
+            const bool sees = row >= blind;
+            stsf(misc + F::kFactor + tid * 4, sees ? 1.f / l : 0.f);
+            if (tid < rows) {
+                if (!whole) p.ws_ml[slot * N + tid] = make_float2(m, l);
+                else if (p.lse) p.lse[out_row + (size_t)(row / p.G) * p.Hq + row % p.G] = sees ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+            }
+        }
+        if (part.parts && tid == 0) {
+            p.cuts[2 * worker] = make_int4(pl.tok0, row0, pl.h << 8 | rows, part.parts);
+            p.cuts[2 * worker + 1] = make_int4(blind, 0, 0, 0);
+        }
+        sync();
+#pragma unroll 1
+        for (int c0 = 0; c0 < rows; c0 += 16) {
+            uint32_t o[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[i] = 0u;
+            if (started) {
+                tmem_ld_x16(tmem + lanes + 64 + N + c0, o);
+                tmem_ld_wait();
+            }
+            int row = row0 + c0, token = row / p.G, g = row - token * p.G;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                if (c0 + i < rows) {
+                    const float v = __uint_as_float(o[i]);
+                    if (whole) {
+                        const float f = ldsf(misc + F::kFactor + (c0 + i) * 4);
+                        p.out[(out_row + (size_t)token * p.Hq + g) * 128 + tid] = __float2bfloat16_rn(row + i < blind ? 0.f : v * f);
+                    } else {
+                        p.ws_o[(slot * N + c0 + i) * 128 + tid] = v;
+                    }
+                }
+                if (++g == p.G) g = 0, ++token;
+            }
+        }
+        tc_fence_before_sync();
+    }
+};
+
+template <int N, bool kChunk>
+__global__ void __launch_bounds__(Form<N>::kThreads, 1) q4_attn_kernel(const __grid_constant__ Params p)
+{
+    using F = Form<N>;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t smem0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t shared = smem0 + F::kOffShared;
+    const int tid = threadIdx.x, wg = tid >> 7, warp = tid >> 5, lane = tid & 31;
+    const int workers = gridDim.x * F::kWorkers;
+
+    if (tid == 0) {
+#pragma unroll 1
+        for (int w = 0; w < F::kWorkers; ++w)
+#pragma unroll 1
+            for (int i = 0; i < F::kStages + 2; ++i) mbar_init(smem0 + F::kOffMisc + w * F::kMiscBytes + F::kBars + i * 8, 1);
+        mbar_fence_init();
+        sts32(shared + 4, 0);
+    }
+    if (warp == 0) tmem_alloc(shared, 512);
+    grid_dependency_wait();
+
+    const int entries = p.S * p.Hkv, den = kChunk ? p.G : 1;
+    int per_cta;
+    bool no_list = false;
+    tc_fence_before_sync();
+    const svq::Line line = find_shares<F::kThreads, F::kWorkers>(entries, den, shared + 64, shared + 256, per_cta, [&](int e) {
+        if (!kChunk && p.sel_idx) no_list |= __ldg(p.sel_cnt + e) < 0;
+        return place<kChunk, N>(p, e).cost.all();
+    });
+    tc_fence_after_sync();
+    if (no_list && blockIdx.x == 0 && p.status) atomicOr(p.status, kStatusNoList);
+    const uint32_t tmem = lds32(shared);
+    // no cuts yet: of the CTA's own shares, and of those that there are not
+    if (tid < per_cta && blockIdx.x * per_cta + tid < line.shares) p.cuts[2 * (blockIdx.x * per_cta + tid)] = make_int4(0, 0, 0, 0);
+    for (int i = line.shares + blockIdx.x * F::kThreads + tid; i < workers; i += gridDim.x * F::kThreads) p.cuts[2 * i] = make_int4(0, 0, 0, 0);
+    __syncthreads();
+    const int share = blockIdx.x * per_cta + wg;
+    if (wg < per_cta && share < line.shares && line.total > 0) {
+        Worker<N, kChunk> w{p};
+        w.wg = wg, w.tid = tid & 127, w.lane = lane, w.warp = warp & 3, w.worker = share;
+        w.q_tile = smem0 + F::kOffQ + wg * F::kQBytes;
+        w.p_tile = smem0 + F::kOffP + wg / F::kSharers * F::kPTile + wg % F::kSharers * (N * 2);
+        w.ring = smem0 + F::kOffRing + wg * F::kStages * F::kUnitBytes;
+        w.misc = smem0 + F::kOffMisc + wg * F::kMiscBytes;
+        w.shared = shared;
+        w.tmem = tmem + wg * F::kColumns;
+        w.policy = policy_evict_first();
+        int e = (int)lds_ll(shared + 256 + wg * 16);
+        long long at = lds_ll(shared + 256 + wg * 16 + 8);
+        const long long lo = line.bound(share), hi = line.bound(share + 1);
+        Place pl = place<kChunk, N>(p, e);
+        int t = pl.cost.item_at(lo - at);
+        at += pl.cost.before(t);
+#pragma unroll 1
+        while (at < hi) {
+            const long long cost = pl.cost.cost(t);
+            int units = (pl.slabs + 1) / 2 + 1;
+            if constexpr (kChunk) {
+                const int rows = min(N, p.G * pl.n - t * N);
+                const int end = min(max(pl.pos0 + (t * N + rows - 1) / p.G + 1, 0), pl.len);
+                units = (end + kUnit - 1) / kUnit;
+            }
+            const svq::Part part = svq::part_of(line, share, at, cost, units, den);
+            if (part.mine) w.run(pl, t, part, units);
+            at += cost;
+            if (++t == pl.cost.tiles) {
+                t = 0;
+                do {
+                    if (++e < entries) pl = place<kChunk, N>(p, e);
+                } while (e < entries && pl.cost.tiles == 0);
+                if (e >= entries) break;
+            }
+        }
+        w.drain();
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    if (warp == 0) tmem_dealloc(tmem, 512);
+    grid_launch_dependents();
+}
+
+// A cut item: the sums of its parts, which are numbered from the worker that it begins with.  A warp a row, four dims a lane.
+constexpr int kMergeRows = 8;
+__global__ void __launch_bounds__(kMergeRows * 32) q4_merge_kernel(const __grid_constant__ Params p, int N)
+{
+    grid_dependency_wait();
+    const int worker = blockIdx.x, lane = threadIdx.x & 31;
+    const int4 cut = p.cuts[2 * worker];
+    if (cut.w == 0) return;
+    const int r = blockIdx.y * kMergeRows + (int)(threadIdx.x >> 5), rows = cut.z & 255, h = cut.z >> 8;
+    if (r >= rows) return;
+    const int blind = p.cuts[2 * worker + 1].x;
+    SplitSum sum;
+    constexpr int U = 8;
+    for (int base = 0; base < cut.w; base += U) {
+        float2 ml[U];
+        float4 o[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const size_t at = ((size_t)(worker + base + k) * 2 + (base + k == 0)) * N + r;
+            const bool in = base + k < cut.w;
+            ml[k] = in ? __ldcg(p.ws_ml + at) : make_float2(-INFINITY, 0.f);
+            o[k] = in ? __ldcg(reinterpret_cast<const float4 *>(p.ws_o + at * 128) + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        sum.add(ml, o);
+    }
+    const int row = cut.y + r;
+    const bool sees = row >= blind;
+    const size_t at = ((size_t)cut.x + row / p.G) * p.Hq + h * p.G + row % p.G;
+    reinterpret_cast<uint2 *>(p.out + at * 128)[lane] = sees ? sum.out() : make_uint2(0u, 0u);
+    if (p.lse && lane == 0) p.lse[at] = sees ? sum.lse() : -INFINITY;
+}
+
+sv_status check_kv_q4(const sv_geom *g, const sv_kv_q4 *kv)
+{
+    if (!kv || !kv->pool || !kv->block_table || !kv->seq_lens) return SV_ERR_NULL;
+    if (kv->n_pages < 1) return SV_ERR_SHAPE;
+    if ((int64_t)kv->n_pages * g->n_kv_heads * g->block_size >= (int64_t)1 << 31) return SV_ERR_SHAPE;
+    if (!svh::aligned(kv->pool, 128) || !svh::aligned(kv->block_table, 4) || !svh::aligned(kv->seq_lens, 4)) return SV_ERR_ALIGN;
+    return SV_OK;
+}
+
+// Query rows of a tile: as few as hold all rows of a KV head, at most 64.
+int tile_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
+int workers_of(int n) { return svh::sm_count() * (n == 64 ? 2 : 4); }
+
+template <int N, bool kChunk>
+sv_status launch(Params &p, void *workspace, void *stream)
+{
+    using F = Form<N>;
+    const int workers = workers_of(N);
+    p.cuts = static_cast<int4 *>(workspace);
+    p.ws_ml = reinterpret_cast<float2 *>(p.cuts + 2 * workers);
+    p.ws_o = reinterpret_cast<float *>(p.ws_ml + (size_t)2 * workers * N);
+    static svh::OncePerDevice once;
+    if (once.run([] { return cudaFuncSetAttribute(q4_attn_kernel<N, kChunk>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::kSmem); }) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return SV_ERR_CUDA;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(svh::sm_count());
+    cfg.blockDim = dim3(F::kThreads);
+    cfg.dynamicSmemBytes = F::kSmem;
+    cfg.stream = static_cast<cudaStream_t>(stream);
+    cudaLaunchAttribute attr[1];
+    svh::pdl_attribute(attr);
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, q4_attn_kernel<N, kChunk>, p) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return SV_ERR_CUDA;
+    }
+    const int64_t rows = std::min<int64_t>(N, (int64_t)p.G * (kChunk ? p.n_tokens : p.T));
+    cfg.gridDim = dim3(workers, (unsigned)((rows + kMergeRows - 1) / kMergeRows));
+    cfg.blockDim = dim3(kMergeRows * 32);
+    cfg.dynamicSmemBytes = 0;
+    return cudaLaunchKernelEx(&cfg, q4_merge_kernel, p, N) == cudaSuccess ? svh::launch_status() : SV_ERR_CUDA;
+}
+template <bool kChunk>
+sv_status launch_rows(Params &p, int64_t rows, void *workspace, void *stream)
+{
+    const int n = tile_rows(rows);
+    return n == 16 ? launch<16, kChunk>(p, workspace, stream) : n == 32 ? launch<32, kChunk>(p, workspace, stream) : launch<64, kChunk>(p, workspace, stream);
+}
+
+sv_status common(const sv_geom *g, const sv_kv_q4 *kv, const void *q, float softmax_scale, void *out, float *lse, void *workspace,
+                 size_t workspace_bytes, int32_t *status_word, Params &p)
+{
+    if (!(softmax_scale >= 0.f && softmax_scale < INFINITY)) return SV_ERR_SHAPE;
+    if (!svh::aligned(q, 16) || !svh::aligned(out, 16) || !svh::aligned(workspace, 16)) return SV_ERR_ALIGN;
+    if ((int64_t)g->n_seq * g->n_kv_heads >= (int64_t)1 << 31) return SV_ERR_SHAPE;
+    if (workspace_bytes < sv_workspace_bytes_q4(g)) return SV_ERR_WORKSPACE;
+    if (!workspace) return SV_ERR_NULL;
+    p = Params{};
+    p.pool = static_cast<const uint8_t *>(kv->pool), p.block_table = kv->block_table, p.seq_lens = kv->seq_lens, p.n_pages = kv->n_pages;
+    p.q = static_cast<const __nv_bfloat16 *>(q), p.out = static_cast<__nv_bfloat16 *>(out), p.lse = lse, p.status = status_word;
+    p.S = g->n_seq, p.Hq = g->n_q_heads, p.Hkv = g->n_kv_heads, p.G = p.Hq / p.Hkv, p.B = g->block_size, p.NBmax = g->max_blocks;
+    p.scale_log2 = (softmax_scale == 0.f ? 0.08838834764831845f : softmax_scale) * 1.4426950408889634f;
+    return SV_OK;
+}
+
+}  // namespace
+
+extern "C" size_t sv_workspace_bytes_q4(const sv_geom *geom)
+{
+    if (svh::check_ragged(geom, 0) != SV_OK) return 0;
+    size_t most = 0;
+    for (int n : {16, 32, 64}) most = std::max(most, (size_t)workers_of(n) * (2 * sizeof(int4) + 2 * (size_t)n * 130 * sizeof(float)));
+    return most;
+}
+
+extern "C" sv_status sv_verify_attn_q4(const sv_geom *geom, const void *q, const sv_kv_q4 *kv, const void *draft_k, const void *draft_v,
+                                       const int32_t *parent, const int32_t *sel_idx, const int32_t *sel_cnt, int32_t max_sel,
+                                       float softmax_scale, void *out, float *lse, void *workspace, size_t workspace_bytes, int32_t *status_word,
+                                       void *stream)
+{
+    sv_status st = svh::check_geom(geom);
+    if (st != SV_OK) return st;
+    st = svh::check_ragged(geom, 0);
+    if (st != SV_OK) return st;
+    st = check_kv_q4(geom, kv);
+    if (st != SV_OK) return st;
+    if (!q || !draft_k || !draft_v || !out || (sel_idx && !sel_cnt)) return SV_ERR_NULL;
+    if (sel_idx && max_sel < 1) return SV_ERR_SHAPE;
+    if (!svh::aligned(draft_k, 16) || !svh::aligned(draft_v, 16)) return SV_ERR_ALIGN;
+    Params p;
+    st = common(geom, kv, q, softmax_scale, out, lse, workspace, workspace_bytes, status_word, p);
+    if (st != SV_OK) return st;
+    p.draft_k = static_cast<const __nv_bfloat16 *>(draft_k), p.draft_v = static_cast<const __nv_bfloat16 *>(draft_v), p.parent = parent;
+    p.sel_idx = sel_idx, p.sel_cnt = sel_cnt, p.max_sel = std::min(max_sel, 1 << 24), p.T = geom->n_draft;
+    return launch_rows<false>(p, (int64_t)p.G * p.T, workspace, stream);
+}
+
+extern "C" sv_status sv_chunk_attn_q4(const sv_geom *geom, const void *q, const sv_kv_q4 *kv, const int32_t *q_start, int32_t n_tokens,
+                                      float softmax_scale, void *out, float *lse, void *workspace, size_t workspace_bytes,
+                                      int32_t *status_word, void *stream)
+{
+    sv_status st = svh::check_ragged(geom, n_tokens);
+    if (st != SV_OK) return st;
+    st = check_kv_q4(geom, kv);
+    if (st != SV_OK) return st;
+    if (!q_start || (n_tokens > 0 && (!q || !out))) return SV_ERR_NULL;
+    Params p;
+    st = common(geom, kv, q, softmax_scale, out, lse, workspace, workspace_bytes, status_word, p);
+    if (st != SV_OK || n_tokens == 0) return st;
+    p.q_start = q_start, p.n_tokens = n_tokens;
+    // (the mean rows of a sequence: a batch of single tokens with a few chunks is taken as chunks)
+    return launch_rows<true>(p, (int64_t)p.G * ((n_tokens + geom->n_seq - 1) / geom->n_seq), workspace, stream);
+}
