@@ -31,7 +31,16 @@ template <int j>
 __device__ __forceinline__ uint32_t steps(uint32_t w)
 {
     const uint32_t x = j == 0 ? w << 3 : w >> (4 * j - 3);
-    return (x & 0x00780078u) | 0x3f803f80u;
+    uint32_t d;
+    asm("lop3.b32 %0, %1, 0x00780078, %2, 0xEA;" : "=r"(d) : "r"(x), "r"(0x3f803f80u));   // (x & mask) | one, in one instruction
+    return d;
+}
+// ... of the pair that a turn to the right brings to bits 3 and 19 (29: pair 0, 33: pair 1, ...)
+__device__ __forceinline__ uint32_t steps_at(uint32_t w, uint32_t turn)
+{
+    uint32_t d;
+    asm("lop3.b32 %0, %1, 0x00780078, %2, 0xEA;" : "=r"(d) : "r"(__funnelshift_r(w, w, turn)), "r"(0x3f803f80u));
+    return d;
 }
 // the eight values of a word, pairs; D and M as pairs
 __device__ __forceinline__ void decode(uint32_t w, uint32_t d, uint32_t m, uint32_t *out)

@@ -14,10 +14,12 @@
 // affair, sums of weights stay in registers until the end, and the running maximum, which would have to go across lanes, is only
 // looked for when a score outgrows the reference.
 //
-// A worker is a warpgroup that has everything it needs to itself -- a ring of slabs filled by bulk copies (one of 9216 bytes for 64 tokens,
-// no tensor maps), queries, P, tensor memory -- and takes a share of the batch (q4_shares.h), so that workers never wait for one another:
-// while one waits for a product the others decode.  An item that is cut is written as partial sums and merged by a second kernel.
+// A worker is a warpgroup that decodes and does the softmax, and a warp that copies and issues its products; it has everything to itself --
+// a ring of slabs filled by bulk copies (one of 9216 bytes for 64 tokens, no tensor maps), queries, P, tensor memory -- and takes a share of
+// the batch (q4_shares.h), so that workers never wait for one another: while one waits for a product the others decode.  An item that is
+// cut is written as partial sums and merged by a second kernel.
 #include <cuda_bf16.h>
+#include <stddef.h>
 
 #include <algorithm>
 
@@ -53,7 +55,7 @@ struct Params {
 template <int N>
 struct Form {
     static constexpr int kWorkers = N == 64 ? 2 : 4;             // of a CTA
-    static constexpr int kThreads = kWorkers * 128;
+    static constexpr int kThreads = kWorkers * 128 + 128;        // (a warp of the last four for each worker)
     static constexpr int kStages = N == 64 ? 4 : 2;              // units of a worker's ring
     static constexpr int kUnitBytes = 2 * kSlabBytes;
     static constexpr int kQBytes = N * 256;                      // [2 halves of the dims][N rows][128 bytes]
@@ -63,12 +65,16 @@ struct Form {
     static constexpr int kOffP = kWorkers * kQBytes;
     static constexpr int kOffRing = kOffP + kWorkers / kSharers * kPTile;
     static constexpr int kOffMisc = kOffRing + kWorkers * kStages * kUnitBytes;
-    // per worker: reference, its negative where there is one, factors, maxima and sums of four warps, row masks; barriers; valid tokens
+    // per worker: reference, its negative where there is one, factors, maxima and sums of four warps, row masks; barriers; tokens of the
+    // slabs in the ring; the item and the next one
     static constexpr int kMRef = 0, kNeg = kMRef + N * 4, kFactor = kNeg + N * 4, kParts = kFactor + N * 4, kMasks = kParts + 4 * N * 4,
-                         kBars = kMasks + 64 * 8, kValid = kBars + (kStages + 2) * 8, kMiscBytes = (kValid + kStages * 8 + 127) / 128 * 128;
+                         kBars = kMasks + 64 * 8, kValid = kBars + (kStages + 8) * 8, kItems = (kValid + kStages * 8 + 15) / 16 * 16, kMiscBytes = (kItems + 2 * 64 + 127) / 128 * 128;
     static constexpr int kOffShared = kOffMisc + kWorkers * kMiscBytes;   // tensor memory's address, the abort flag, the scan
     static constexpr int kSharedBytes = 512;
     static constexpr int kSmem = 1024 + kOffShared + kSharedBytes;
+    // registers: the warpgroups that compute take what the warps that issue leave
+    static constexpr int kRegs = N == 64 ? 168 : 96, kRegsFew = 64, kRegsMany = N == 64 ? 216 : 104;
+    static_assert((kWorkers * kRegsMany + kRegsFew) * 128 <= kRegs * kThreads, "registers of the launch");
     static constexpr int kColumns = 64 + 2 * N;                  // of tensor memory: decoded keys or values, S, O
     static_assert(kWorkers * kColumns <= 512 && kSmem <= 232448, "");
 };
@@ -112,19 +118,39 @@ __device__ __forceinline__ Place place(const Params &p, int e)
     return r;
 }
 
+// A part of an item, as the warp that issues hands it to the warpgroup (which has no registers to walk the batch itself).
+struct Item {
+    int s, h, tok0;          // sequence, KV head, first token
+    int row0, rows;          // rows of the tile (0: there are no more items)
+    int n_units, u0;         // units of cached keys, the first of them
+    int drafts, whole;       // the draft's own keys are part of it; nothing is cut
+    int pos0, blind;         // (chunk) position of token 0; rows of the sequence that see no key
+    int parts, begins;       // parts of the cut item that begins here; whether the part is an item's first
+};
+static_assert(sizeof(Item) <= 64, "");
+
 template <int N, bool kChunk>
 struct Worker {
     using F = Form<N>;
     const Params &p;
     uint32_t q_tile, p_tile, ring, misc, shared, tmem;   // shared memory and tensor memory of this worker
+    const uint8_t *slabs;                                // the ring, for reading
+    const float *refs;                                   // minus the references
     int wg, tid, lane, warp, worker;
-    uint32_t of_s = 0, of_o = 0;    // parities
+    uint32_t parity = 0;            // of the next unit's barriers
     int taken = 0, asked = 0;       // units of the ring consumed and requested, ever
-    uint64_t policy;
+    int units_done = 0, items = 0;  // (the warp that issues) units and items so far
 
     __device__ uint32_t bar_full(int i) const { return misc + F::kBars + i * 8; }
-    __device__ uint32_t bar_s() const { return bar_full(F::kStages); }
-    __device__ uint32_t bar_o() const { return bar_full(F::kStages + 1); }
+    // of a unit: its keys are in tensor memory, its scores, its weights and values are, its product with them is through
+    __device__ uint32_t bar_k() const { return bar_full(F::kStages); }
+    __device__ uint32_t bar_s() const { return bar_full(F::kStages + 1); }
+    __device__ uint32_t bar_p() const { return bar_full(F::kStages + 2); }
+    __device__ uint32_t bar_o() const { return bar_full(F::kStages + 3); }
+    // an item has been handed out; it has been read (two places in turn)
+    __device__ uint32_t bar_item(int n) const { return bar_full(F::kStages + 4 + (n & 1)); }
+    __device__ uint32_t bar_taken(int n) const { return bar_full(F::kStages + 6 + (n & 1)); }
+    __device__ uint32_t item_at(int n) const { return misc + F::kItems + (n & 1) * 64; }
     __device__ void sync() const { named_bar_sync(1 + wg, 128); }
     __device__ bool aborted() const
     {
@@ -133,34 +159,32 @@ struct Worker {
         return v != 0;
     }
     // Bounded.  Where it gives up it says so, later waits of the CTA look once, and everybody goes on to the end with what there is.
-    __device__ void wait(uint32_t bar, uint32_t parity, int bit) const
+    __device__ __forceinline__ static void wait_long(uint32_t bar, uint32_t parity, uint32_t shared, int32_t *status, int bit)
     {
 #pragma unroll 1
-        for (int n = 0; n < 1 << 13; ++n) {
-#pragma unroll 1
-            for (int i = 0; i < 64; ++i)
-                if (mbar_try_wait(bar, parity)) return;
-            if (aborted()) return;
+        for (int n = 0; n < 1 << 19; ++n) {
+            if (mbar_try_wait(bar, parity)) return;
+            if ((n & 63) == 0) {
+                uint32_t v;
+                asm volatile("ld.volatile.shared.b32 %0, [%1];" : "=r"(v) : "r"(shared + 4) : "memory");
+                if (v) return;
+            }
         }
         sts32(shared + 4, 1);
-        if (p.status) atomicOr(p.status, bit);
+        if (status) atomicOr(status, bit);
     }
-
-    // Copies and products that nobody waited for, when a wait gave up: this CTA's memory stays until they are through.
-    __device__ void drain() const
+    __device__ void wait(uint32_t bar, uint32_t par, int bit) const
     {
-        if (!aborted()) return;
-#pragma unroll 1
-        for (int i = 0; i < F::kStages; ++i) {
-            const int n = asked > i ? (asked - i + F::kStages - 1) / F::kStages : 0;
-            if (n > 0) (void)mbar_wait_bounded(bar_full(i), (n - 1) & 1);
-        }
-        (void)mbar_wait_bounded(bar_s(), of_s ^ 1);
-        (void)mbar_wait_bounded(bar_o(), of_o ^ 1);
+        if (!mbar_try_wait(bar, par)) wait_long(bar, par, shared, p.status, bit);
+    }
+    __device__ void arrive(uint32_t bar) const
+    {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar);
     }
 
-    // ------------------------------------------------------------------ the ring
-    int list_base = -1, known = 0, known_valid = 0;   // (warp 0) a slab a lane, from list_base on: its page's slab number, its tokens
+    // ------------------------------------------------------------------ the warp that copies and issues
+    int list_base = -1, known = 0, known_valid = 0;   // a slab a lane, from list_base on: its page's slab number, its tokens
     __device__ void look_up(const Place &pl, int end, int n_slabs, int from)
     {
         list_base = from;
@@ -182,8 +206,8 @@ struct Worker {
         if (bad && p.status) atomicOr(p.status, kStatusIndex);
         known = (page * p.Hkv + pl.h) * per + sub;
     }
-    // unit u of the item (warp 0, converged)
-    __device__ void ask(const Place &pl, int end, int n_slabs, int u)
+    // unit u of the item
+    __device__ void ask(const Place &pl, int end, int n_slabs, int u, uint64_t policy)
     {
         if (list_base < 0 || 2 * u >= list_base + 32) look_up(pl, end, n_slabs, 2 * u);
         const int i = 2 * u - list_base;
@@ -191,8 +215,8 @@ struct Worker {
         const int va = __shfl_sync(0xffffffffu, known_valid, i), vb = __shfl_sync(0xffffffffu, known_valid, (i + 1) & 31);
         const int stage = asked % F::kStages;
         if (elect_one()) {
-            const uint32_t full = bar_full(stage), dst = ring + stage * F::kUnitBytes, valid = misc + F::kValid + stage * 8;
-            sts32(valid, va), sts32(valid + 4, vb);
+            const uint32_t full = bar_full(stage), dst = ring + stage * F::kUnitBytes;
+            sts64(misc + F::kValid + stage * 8, (unsigned long long)(uint32_t)vb << 32 | (uint32_t)va);
             const bool second = 2 * u + 1 < n_slabs;
             mbar_arrive_expect_tx(full, second ? F::kUnitBytes : kSlabBytes);
             bulk_load(dst, p.pool + (size_t)a * kSlabBytes, kSlabBytes, full, policy);
@@ -201,130 +225,223 @@ struct Worker {
         __syncwarp();
         ++asked;
     }
-
-    // ------------------------------------------------------------------ operands
-    __device__ void keys_of(uint32_t slot, uint32_t *x) const   // this thread's key
+    __device__ void hand_out(const Item &it)
     {
-        const uint32_t slab = slot + (tid >> 6) * kSlabBytes, t = tid & 63;
-        const uint2 sc = lds64(slab + svq::kOffKScale + t * 8);
-        const uint32_t d[2] = {svq::both_low(sc.x), svq::both_low(sc.y)}, m[2] = {svq::both_high(sc.x), svq::both_high(sc.y)};
+        if (items > 1) wait(bar_taken(items), ((items >> 1) - 1) & 1, 32);
+        if (__any_sync(0xffffffffu, aborted())) return;   // (nothing is written under the eyes of those who still read)
+        if (lane < (int)(sizeof(Item) / 4)) sts32(item_at(items) + lane * 4, reinterpret_cast<const uint32_t *>(&it)[lane]);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_item(items));
+        ++items;
+    }
+    __device__ void copy_and_issue(const Place &pl, int tile, const svq::Part &part, int units)
+    {
+        Item it{pl.s, pl.h, pl.tok0, tile * N, min(N, p.G * pl.n - tile * N), 0, part.u0, 0, part.u0 == 0 && part.u1 == units, pl.pos0, 0, part.parts, part.u0 == 0};
+        int end = pl.len, n_slabs = pl.slabs;   // keys that any of the rows sees, and the slabs that hold them
+        if constexpr (kChunk) {
+            end = min(max(pl.pos0 + (it.row0 + it.rows - 1) / p.G + 1, 0), pl.len);
+            n_slabs = (end + 63) / 64;
+            it.blind = min(max(-pl.pos0, 0), pl.n) * p.G;
+        } else {
+            it.drafts = part.u1 == units;
+        }
+        it.n_units = max(min(part.u1, (n_slabs + 1) / 2) - part.u0, 0);
+        hand_out(it);
+        const uint64_t policy = policy_evict_first();
+        constexpr uint32_t idesc_s = umma_idesc_bf16(128, N, false), idesc_o = umma_idesc_bf16(128, N, true);
+        const uint64_t dq = umma_desc_sw128(q_tile, 16, 1024), dp = umma_desc_sw128(p_tile, 8192, 1024);
+        list_base = -1;
+        for (int u = 0; u < min(it.n_units, F::kStages); ++u) ask(pl, end, n_slabs, part.u0 + u, policy);
+#pragma unroll 1
+        for (int k = it.drafts ? -1 : 0, n = 0; k < it.n_units; ++k, ++n) {
+            wait(bar_k(), units_done & 1, 4);
+            tc_fence_after_sync();
+            if (elect_one()) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            const uint4 w = lds128(slab + c * 1024 + t * 16);
-            svq::decode(w.x, d[c >> 1], m[c >> 1], x + 16 * c);
-            svq::decode(w.y, d[c >> 1], m[c >> 1], x + 16 * c + 4);
-            svq::decode(w.z, d[c >> 1], m[c >> 1], x + 16 * c + 8);
-            svq::decode(w.w, d[c >> 1], m[c >> 1], x + 16 * c + 12);
+                for (int ks = 0; ks < 8; ++ks)
+                    tc_mma_bf16_ta(tmem + 64, tmem + ks * 8, dq + (uint64_t)((ks & 3) * 2 + (ks >> 2) * (N * 128 >> 4)), idesc_s, ks > 0);
+                tc_commit(bar_s());
+            }
+            __syncwarp();
+            wait(bar_p(), units_done & 1, 8);
+            tc_fence_after_sync();
+            if (elect_one()) {
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks)
+                    tc_mma_bf16_ta(tmem + 64 + N, tmem + ks * 8, dp + (uint64_t)(ks * 2048 >> 4), idesc_o, ks > 0 || n > 0);
+                tc_commit(bar_o());
+            }
+            __syncwarp();
+            ++units_done;
+            // (the unit's slot has been read)
+            if (k >= 0 && k + F::kStages < it.n_units) ask(pl, end, n_slabs, part.u0 + k + F::kStages, policy);
         }
     }
-    __device__ static uint4 cut_pairs(uint4 v, int n)   // of eight numbers the first n
+    // Copies and products that nobody waited for, when a wait gave up: this CTA's memory stays until they are through.
+    __device__ void drain() const
     {
-        const auto one = [n](uint32_t w, int i) { return n >= i + 2 ? w : n == i + 1 ? w & 0xffffu : 0u; };
-        return make_uint4(one(v.x, 0), one(v.y, 2), one(v.z, 4), one(v.w, 6));
+        if (!aborted()) return;
+#pragma unroll 1
+        for (int i = 0; i < F::kStages; ++i) {
+            const int n = asked > i ? (asked - i + F::kStages - 1) / F::kStages : 0;
+            if (n > 0) (void)mbar_wait_bounded(bar_full(i), (n - 1) & 1);
+        }
+        if (units_done == 0) return;
+        (void)mbar_wait_bounded(bar_s(), (units_done - 1) & 1);
+        (void)mbar_wait_bounded(bar_o(), (units_done - 1) & 1);
     }
-    // this thread's dim of 64 tokens, of which `valid` are there (the others are zero: whatever a slab holds there, a weight of zero
-    // times it is to be zero)
-    __device__ void values_of(uint32_t slab, int valid, uint32_t *x) const
+
+    // ------------------------------------------------------------------ the warpgroup: operands, 16 columns of tensor memory at a time
+    // (rolled: what the four workers run through at different places is to stay in the instruction caches)
+    __device__ void put_keys(uint32_t at, int stage) const   // this thread's key
     {
-        const uint32_t sc = slab + svq::kOffVScale + (tid >> 6) * 256;
+        const uint8_t *slab = slabs + stage * F::kUnitBytes + (tid >> 6) * kSlabBytes;
+        const int t = tid & 63;
+        const uint2 sc = *reinterpret_cast<const uint2 *>(slab + svq::kOffKScale + t * 8);
+#pragma unroll 1
+        for (int g = 0; g < 2; ++g) {
+            const uint32_t w = g ? sc.y : sc.x, d = svq::both_low(w), m = svq::both_high(w);
+            uint32_t x[32];
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            const uint4 w = lds128(slab + svq::kOffV + c * 2048 + tid * 16);
-            const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+            for (int c = 0; c < 2; ++c) {
+                const uint4 v = *reinterpret_cast<const uint4 *>(slab + (2 * g + c) * 1024 + t * 16);
+                svq::decode(v.x, d, m, x + 16 * c);
+                svq::decode(v.y, d, m, x + 16 * c + 4);
+                svq::decode(v.z, d, m, x + 16 * c + 8);
+                svq::decode(v.w, d, m, x + 16 * c + 12);
+            }
+            tmem_st_x32(at + 32 * g, x);
+        }
+    }
+    // 128 tokens of the warp's 32 dims.  A thread has four dims (d0 + 8 i) and four tokens of every 16, so that it needs a quarter of the
+    // scales: a thread with a dim's 128 tokens of its own, all of whose scales come from shared memory, moves 2.5 times the bytes there, and
+    // they are what bounds the decoding.  Tokens that are not there are zero: whatever a slab holds for them, a weight of zero times it is
+    // to be zero.
+    __device__ void put_values(uint32_t at, int stage, const int (&valid)[2]) const
+    {
+        const int q = lane & 3, d0 = warp * 32 + (lane >> 2);
+        const uint32_t turn = 29 + 8 * (q & 1);   // of a word, that brings the first of the thread's two pairs to where steps() has them
+#pragma unroll 1
+        for (int b = 0; b < 2; ++b) {   // slabs
+            const uint8_t *slab = slabs + stage * F::kUnitBytes + b * kSlabBytes, *sc = slab + svq::kOffVScale + (warp >> 1) * 256 + q * 8;
+            uint2 d[4], m[4];   // of tokens 16 j + 4 q ..
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint4 d = lds128(sc + c * 64 + i * 16), m = lds128(sc + 128 + c * 64 + i * 16);
-                if (valid < 64) d = cut_pairs(d, valid - 32 * c - 8 * i), m = cut_pairs(m, valid - 32 * c - 8 * i);
-                uint32_t *o = x + 16 * c + 4 * i;
-                o[0] = svq::fma_bf16x2(svq::steps<0>(words[i]), d.x, m.x);
-                o[1] = svq::fma_bf16x2(svq::steps<1>(words[i]), d.y, m.y);
-                o[2] = svq::fma_bf16x2(svq::steps<2>(words[i]), d.z, m.z);
-                o[3] = svq::fma_bf16x2(svq::steps<3>(words[i]), d.w, m.w);
+            for (int j = 0; j < 4; ++j) d[j] = *reinterpret_cast<const uint2 *>(sc + 32 * j), m[j] = *reinterpret_cast<const uint2 *>(sc + 128 + 32 * j);
+            const int n = b ? valid[1] : valid[0];
+            if (n < 64) {
+                const auto cut = [](uint32_t w, int left) { return left >= 2 ? w : left == 1 ? w & 0xffffu : 0u; };
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int left = n - 16 * j - 4 * q;
+                    d[j] = make_uint2(cut(d[j].x, left), cut(d[j].y, left - 2)), m[j] = make_uint2(cut(m[j].x, left), cut(m[j].y, left - 2));
+                }
+            }
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {   // dims d0 + 16 half and 8 more
+                uint32_t x[16];   // word 4 j + 2 h + e: dim + 8 h, tokens 16 j + 4 q + 2 e and the next
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t w = *reinterpret_cast<const uint32_t *>(slab + svq::kOffV + (j >> 1) * 2048 + (d0 + 16 * half + 8 * h) * 16 + (2 * (j & 1) + (q >> 1)) * 4);
+                        x[4 * j + 2 * h] = svq::fma_bf16x2(svq::steps_at(w, turn), d[j].x, m[j].x);
+                        x[4 * j + 2 * h + 1] = svq::fma_bf16x2(svq::steps_at(w, turn + 4), d[j].y, m[j].y);
+                    }
+                tmem_st_16x256b_x4(at + ((uint32_t)half << 20) + 32 * b, x);   // (16 lanes further)
             }
         }
     }
-    __device__ void draft_keys(const Place &pl, uint32_t *x) const
+    __device__ void put_draft_keys(uint32_t at, int tok0, int h) const
     {
-        const uint4 *row = reinterpret_cast<const uint4 *>(p.draft_k + ((size_t)(pl.tok0 + tid) * p.Hkv + pl.h) * 128);
+        const uint4 *row = reinterpret_cast<const uint4 *>(p.draft_k + ((size_t)(tok0 + tid) * p.Hkv + h) * 128);
+#pragma unroll 1
+        for (int c = 0; c < 4; ++c) {
+            uint32_t x[16];
 #pragma unroll
-        for (int c = 0; c < 16; ++c) {
-            const uint4 w = tid < p.T ? __ldg(row + c) : make_uint4(0, 0, 0, 0);
-            x[4 * c] = w.x, x[4 * c + 1] = w.y, x[4 * c + 2] = w.z, x[4 * c + 3] = w.w;
+            for (int i = 0; i < 4; ++i) {
+                const uint4 w = tid < p.T ? __ldg(row + 4 * c + i) : make_uint4(0, 0, 0, 0);
+                x[4 * i] = w.x, x[4 * i + 1] = w.y, x[4 * i + 2] = w.z, x[4 * i + 3] = w.w;
+            }
+            tmem_st_x16(at + 16 * c, x);
         }
     }
-    __device__ void draft_values(const Place &pl, uint32_t *x) const
+    __device__ void put_draft_values(uint32_t at, int tok0, int h) const
     {
-        const unsigned short *col = reinterpret_cast<const unsigned short *>(p.draft_v + ((size_t)pl.tok0 * p.Hkv + pl.h) * 128 + tid);
+        const unsigned short *col = reinterpret_cast<const unsigned short *>(p.draft_v + ((size_t)tok0 * p.Hkv + h) * 128 + tid);
+#pragma unroll 1
+        for (int c = 0; c < 4; ++c) {
+            uint32_t x[16];
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            const uint32_t a = 2 * j < p.T ? __ldg(col + (size_t)(2 * j) * p.Hkv * 128) : 0u;
-            const uint32_t b = 2 * j + 1 < p.T ? __ldg(col + (size_t)(2 * j + 1) * p.Hkv * 128) : 0u;
-            x[j] = a | b << 16;
-            x[32 + j] = 0u;
+            for (int i = 0; i < 16; ++i) {
+                const int j = 32 * c + 2 * i;
+                const uint32_t a = j < p.T ? __ldg(col + (size_t)j * p.Hkv * 128) : 0u;
+                const uint32_t b = j + 1 < p.T ? __ldg(col + (size_t)(j + 1) * p.Hkv * 128) : 0u;
+                x[i] = a | b << 16;
+            }
+            tmem_st_x16(at + 16 * c, x);
         }
-    }
-    __device__ void store_operand(const uint32_t *x) const
-    {
-        const uint32_t at = tmem + ((uint32_t)(warp * 32) << 16);
-        tmem_st_x32(at, *reinterpret_cast<const uint32_t(*)[32]>(x));
-        tmem_st_x32(at + 32, *reinterpret_cast<const uint32_t(*)[32]>(x + 32));
     }
 
-    // ------------------------------------------------------------------ products (one thread)
-    __device__ void issue_s() const
+    // New references for the rows whose maximum over the unit's scores (of four warps, less the old ones) has outgrown theirs; the factors
+    // for what was summed by the old ones, and O by them.  fresh: whether there are rows without a reference still.
+    __device__ __forceinline__ void move_references(int rows, bool started, uint32_t t_o, bool &fresh) const
     {
-        constexpr uint32_t idesc = umma_idesc_bf16(128, N, false);
-        const uint64_t dq = umma_desc_sw128(q_tile, 16, 1024);
+        bool none = false;
+        if (tid < rows) {
+            float m = ldsf(misc + F::kParts + tid * 4);
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks)
-            tc_mma_bf16_ta(tmem + 64, tmem + ks * 8, dq + (uint64_t)((ks & 3) * 2 + (ks >> 2) * (N * 128 >> 4)), idesc, ks > 0);
-        tc_commit(bar_s());
-    }
-    __device__ void issue_o(bool more) const
-    {
-        constexpr uint32_t idesc = umma_idesc_bf16(128, N, true);
-        const uint64_t dp = umma_desc_sw128(p_tile, 8192, 1024);
+            for (int w = 1; w < 4; ++w) m = fmaxf(m, ldsf(misc + F::kParts + (w * N + tid) * 4));
+            const float old = ldsf(misc + F::kMRef + tid * 4);
+            m -= ldsf(misc + F::kNeg + tid * 4);   // (of the scores themselves)
+            float c = 1.f;
+            if (m > old + kLag) {
+                c = fast_exp2(old - m);
+                stsf(misc + F::kMRef + tid * 4, m), stsf(misc + F::kNeg + tid * 4, -m);
+            } else {
+                none = old == -INFINITY;
+            }
+            stsf(misc + F::kFactor + tid * 4, c);
+        }
+        fresh = named_bar_or(1 + wg, 128, none);
+        if (!started) return;
+        // (the last product is through, the next not issued: O is at rest)
+#pragma unroll 1
+        for (int c0 = 0; c0 < N; c0 += 16) {
+            uint32_t o[16];
+            tmem_ld_x16(t_o + c0, o);
+            tmem_ld_wait();
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks)
-            tc_mma_bf16_ta(tmem + 64 + N, tmem + ks * 8, dp + (uint64_t)(ks * 2048 >> 4), idesc, ks > 0 || more);
-        tc_commit(bar_o());
+            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * ldsf(misc + F::kFactor + (c0 + i) * 4));
+            tmem_st_x16(t_o + c0, o);
+        }
     }
 
-    // ------------------------------------------------------------------ a part of an item
-    __device__ void run(const Place &pl, int tile, const svq::Part &part, int units)
+    // ------------------------------------------------------------------ the warpgroup: a part of an item
+    __device__ int word(int n, size_t offset) const { return (int)lds32(item_at(n) + (uint32_t)offset); }
+#define ITEM(name) word(n, offsetof(Item, name))
+    __device__ void attend(int n)
     {
-        const int row0 = tile * N, rows = min(N, p.G * pl.n - row0);
-        // keys that any row sees, and the slabs that hold them
-        int end = pl.len, n_slabs = pl.slabs;
-        if constexpr (kChunk) {
-            end = min(max(pl.pos0 + (row0 + rows - 1) / p.G + 1, 0), pl.len);
-            n_slabs = (end + 63) / 64;
-        }
-        const int slab_units = (n_slabs + 1) / 2;
-        const int n_units = max(min(part.u1, slab_units) - part.u0, 0);
-        const bool drafts = !kChunk && part.u1 == units;
-        const size_t out_row = (size_t)pl.tok0 * p.Hq + pl.h * p.G;   // of row 0 of token 0
+        const int rows = ITEM(rows);
 
         sync();   // (the last item's rows have been read)
-        if (warp == 0) {
-            list_base = -1;
-            for (int u = 0; u < min(n_units, F::kStages); ++u) ask(pl, end, n_slabs, part.u0 + u);
-        }
-#pragma unroll
+        const bool drafts = ITEM(drafts) != 0;
+        {
+        const int row0 = ITEM(row0), tok0 = ITEM(tok0), h = ITEM(h);
+#pragma unroll 4
         for (int i = 0; i < N / 8; ++i) {
             const int c = i * 128 + tid, r = c >> 4, ch = c & 15, row = row0 + r;
             uint4 v = make_uint4(0, 0, 0, 0);
-            if (r < rows) v = __ldg(reinterpret_cast<const uint4 *>(p.q + (out_row + (size_t)(row / p.G) * p.Hq + row % p.G) * 128) + ch);
+            if (r < rows) v = __ldg(reinterpret_cast<const uint4 *>(p.q + ((size_t)(tok0 + row / p.G) * p.Hq + h * p.G + row % p.G) * 128) + ch);
             sts128(q_tile + (ch >> 3) * (N * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4), v);
         }
-        if (tid < N) stsf(misc + F::kMRef + tid * 4, -INFINITY), stsf(misc + F::kNeg + tid * 4, 0.f);
-        if (drafts) {
-            // which drafts a row's token sees: itself and its ancestors, or all up to it
-            if (tid < N) {
+        if (tid < N) {
+            stsf(misc + F::kMRef + tid * 4, -INFINITY), stsf(misc + F::kNeg + tid * 4, 0.f);
+            if (drafts) {
+                // which drafts the row's token sees: itself and its ancestors, or all up to it
                 unsigned long long seen = 0;
                 const int i = min((row0 + tid) / p.G, p.T - 1);
                 if (p.parent) {
-                    const int32_t *parent = p.parent + (size_t)pl.s * p.T;
+                    const int32_t *parent = p.parent + (size_t)ITEM(s) * p.T;
                     int j = i;
 #pragma unroll 1
                     for (int n = 0; n < 64 && j >= 0; ++n) {
@@ -338,6 +455,7 @@ struct Worker {
                 sts64(misc + F::kMasks + tid * 8, seen);
             }
         }
+        }
         fence_proxy_async();
         sync();
 
@@ -346,109 +464,86 @@ struct Worker {
         for (int i = 0; i < N / 2; ++i) l2[i] = 0ull;
         bool fresh = true, started = false;
         const unsigned long long scale2 = f2_pack(p.scale_log2, p.scale_log2);
-        const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+        const uint32_t t_op = tmem + ((uint32_t)(warp * 32) << 16), t_s = t_op + 64, t_o = t_s + N;
 
+        const int n_units = ITEM(n_units);
 #pragma unroll 1
         for (int k = drafts ? -1 : 0; k < n_units; ++k) {
             const int stage = taken % F::kStages;
-            const uint32_t slot = ring + stage * F::kUnitBytes;
-            int valid[2] = {p.T, 0};
-            uint32_t x[64];
-            if (k < 0) {
-                draft_keys(pl, x);
-            } else {
+            int valid[2] = {0, 0};
+            if (k >= 0) {
                 wait(bar_full(stage), (taken / F::kStages) & 1, 1);
                 const uint2 v = lds64(misc + F::kValid + stage * 8);
                 valid[0] = (int)v.x, valid[1] = (int)v.y;
-                keys_of(slot, x);
             }
-            if (started) {
-                wait(bar_o(), of_o, 2);
-                of_o ^= 1;
+            if (started) {   // the place of the operand is that of the last unit's values
+                wait(bar_o(), parity ^ 1, 2);
                 tc_fence_after_sync();
             }
-            store_operand(x);
+            if (k < 0) put_draft_keys(t_op, ITEM(tok0), ITEM(h));
+            else put_keys(t_op, stage);
             tmem_st_wait();
             tc_fence_before_sync();
-            sync();
-            if (warp == 0 && elect_one()) {
-                tc_fence_after_sync();
-                issue_s();
+            arrive(bar_k());
+            // from which row on this thread's key is seen
+            int first = N;
+            if (k >= 0 && (tid & 63) < valid[tid >> 6]) {
+                first = 0;
+                if constexpr (kChunk) first = (int)min(max((long long)((ITEM(u0) + k) * kUnit + tid - ITEM(pos0)) * p.G - ITEM(row0), 0ll), (long long)N);
             }
-            __syncwarp();
-            if (k < 0) {
-                draft_values(pl, x);
-            } else {
-                values_of(slot, valid[0], x);
-                values_of(slot + kSlabBytes, valid[1], x + 32);
-            }
-            wait(bar_s(), of_s, 4);
-            of_s ^= 1;
+            const bool some_hidden = __any_sync(0xffffffffu, first > 0);
+            wait(bar_s(), parity, 4);
             tc_fence_after_sync();
-            store_operand(x);
-            // scores of this thread's key
-            uint32_t s[N];
+            if (k < 0) put_draft_values(t_op, ITEM(tok0), ITEM(h));
+            else put_values(t_op, stage, valid);
+            // 16 rows' scores less their references; the scores are read twice, for the largest and for the weights, since there are no
+            // registers to keep those of all rows beside the sums
+            const auto scores = [&](int c, float (&y)[16]) {
+                uint32_t s[16];
+                tmem_ld_x16(t_s + c, s);
+                tmem_ld_wait();
+                if (k < 0) {
 #pragma unroll
-            for (int c = 0; c < N; c += 16) tmem_ld_x16(tmem + lanes + 64 + c, s + c);
-            tmem_ld_wait();
-            if (k < 0) {
+                    for (int i = 0; i < 16; ++i) {
+                        const uint2 seen = lds64(misc + F::kMasks + (c + i) * 8);
+                        const uint32_t w = tid & 32 ? seen.y : seen.x;
+                        if (tid >= 64 || !(w >> (tid & 31) & 1)) s[i] = 0xff800000u;
+                    }
+                } else if (some_hidden) {
 #pragma unroll
-                for (int r = 0; r < N; ++r) {
-                    const uint2 seen = lds64(misc + F::kMasks + r * 8);
-                    const uint32_t w = tid & 32 ? seen.y : seen.x;
-                    if (tid >= 64 || !(w >> (tid & 31) & 1)) s[r] = 0xff800000u;
+                    for (int i = 0; i < 16; ++i)
+                        if (c + i < first) s[i] = 0xff800000u;
                 }
-            } else {
-                const bool there = (tid & 63) < valid[tid >> 6];
-                int first = 0;   // row that sees the key first
-                if constexpr (kChunk) {
-                    const int t = (part.u0 + k) * kUnit + tid;
-                    first = (int)min(max((long long)(t - pl.pos0) * p.G - row0, 0ll), (long long)N);
-                }
-                if (!there) first = N;
-                if (__any_sync(0xffffffffu, first > 0)) {
 #pragma unroll
-                    for (int r = 0; r < N; ++r)
-                        if (r < first) s[r] = 0xff800000u;
+                for (int i = 0; i < 16; i += 4) {
+                    const float4 neg = *reinterpret_cast<const float4 *>(refs + c + i);
+                    f2_unpack(f2_fma(f2_pack(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), scale2, f2_pack(neg.x, neg.y)), y[i], y[i + 1]);
+                    f2_unpack(f2_fma(f2_pack(__uint_as_float(s[i + 2]), __uint_as_float(s[i + 3])), scale2, f2_pack(neg.z, neg.w)), y[i + 2], y[i + 3]);
                 }
-            }
-            // whether a score outgrows its row's reference
+            };
             float top = -INFINITY;
+#pragma unroll 1
+            for (int c = 0; c < rows; c += 16) {
+                float y[16];
+                scores(c, y);
 #pragma unroll
-            for (int r = 0; r < N; r += 4) {
-                const uint4 neg = lds128(misc + F::kNeg + r * 4);
-                float a, b, c, d;
-                f2_unpack(f2_fma(f2_pack(__uint_as_float(s[r]), __uint_as_float(s[r + 1])), scale2, f2_pack(__uint_as_float(neg.x), __uint_as_float(neg.y))), a, b);
-                f2_unpack(f2_fma(f2_pack(__uint_as_float(s[r + 2]), __uint_as_float(s[r + 3])), scale2, f2_pack(__uint_as_float(neg.z), __uint_as_float(neg.w))), c, d);
-                top = max3f(top, a, b);
-                top = max3f(top, c, d);
+                for (int i = 0; i < 16; i += 2) top = max3f(top, y[i], y[i + 1]);   // (rows that there are not have scores of zero)
             }
+            // a score that outgrows its row's reference, or a row without one: references move
             if (named_bar_or(1 + wg, 128, fresh || top > kLag)) {
-                // the maxima over the unit, of four warps, then of all; rows whose reference moves
+#pragma unroll 1
+                for (int c = 0; c < rows; c += 16) {
+                    float y[16], mine = 0.f;
+                    scores(c, y);
 #pragma unroll
-                for (int r = 0; r < N; ++r) {
-                    const float m = warp_max(__uint_as_float(s[r]));
-                    if (lane == (r & 31)) stsf(misc + F::kParts + (warp * N + r) * 4, m);
+                    for (int i = 0; i < 16; ++i) {
+                        const float m = warp_max(y[i]);
+                        if (lane == i) mine = m;
+                    }
+                    if (lane < 16) stsf(misc + F::kParts + (warp * N + c + lane) * 4, mine);
                 }
                 sync();
-                bool none = false;
-                if (tid < N) {
-                    float m = ldsf(misc + F::kParts + tid * 4);
-#pragma unroll
-                    for (int w = 1; w < 4; ++w) m = fmaxf(m, ldsf(misc + F::kParts + (w * N + tid) * 4));
-                    m *= p.scale_log2;
-                    const float old = ldsf(misc + F::kMRef + tid * 4);
-                    float c = 1.f;
-                    if (m > old + kLag) {
-                        c = fast_exp2(old - m);
-                        stsf(misc + F::kMRef + tid * 4, m), stsf(misc + F::kNeg + tid * 4, -m);
-                        none = false;
-                    } else {
-                        none = old == -INFINITY;
-                    }
-                    stsf(misc + F::kFactor + tid * 4, c);
-                }
-                fresh = named_bar_or(1 + wg, 128, none);
+                move_references(rows, started, t_o, fresh);
 #pragma unroll
                 for (int r = 0; r < N; r += 2) {
                     const uint2 c = lds64(misc + F::kFactor + r * 4);
@@ -456,50 +551,34 @@ struct Worker {
                     f2_unpack(l2[r / 2], a, b);
                     l2[r / 2] = f2_pack(a * __uint_as_float(c.x), b * __uint_as_float(c.y));
                 }
-                if (started) {
-#pragma unroll 1
-                    for (int c0 = 0; c0 < N; c0 += 16) {
-                        uint32_t o[16];
-                        tmem_ld_x16(tmem + lanes + 64 + N + c0, o);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * ldsf(misc + F::kFactor + (c0 + i) * 4));
-                        tmem_st_x16(tmem + lanes + 64 + N + c0, o);
-                    }
-                }
-            }
-            if (k >= 0) {
-                ++taken;
-                if (warp == 0 && k + F::kStages < n_units) ask(pl, end, n_slabs, part.u0 + k + F::kStages);   // (everybody has read the slot)
             }
             // Weights.  (bf16 because the matrix instruction takes both operands in one type; the sums are of what they were before.)
             const uint32_t p_row = (p_tile & ~1023u) + tid * 128;
             const int p_chunk = (p_tile >> 4) & 7;
 #pragma unroll
-            for (int r = 0; r < N; r += 8) {
-                uint32_t w[4];
+            for (int c = 0; c < N; c += 16) {
+                if (c >= rows) continue;   // (what is in the columns of rows that there are not is nobody's)
+                float y[16];
+                scores(c, y);
 #pragma unroll
-                for (int i = 0; i < 8; i += 4) {
-                    const uint4 neg = lds128(misc + F::kNeg + (r + i) * 4);
-                    float a, b, c, d;
-                    f2_unpack(f2_fma(f2_pack(__uint_as_float(s[r + i]), __uint_as_float(s[r + i + 1])), scale2, f2_pack(__uint_as_float(neg.x), __uint_as_float(neg.y))), a, b);
-                    f2_unpack(f2_fma(f2_pack(__uint_as_float(s[r + i + 2]), __uint_as_float(s[r + i + 3])), scale2, f2_pack(__uint_as_float(neg.z), __uint_as_float(neg.w))), c, d);
-                    a = fast_exp2(a), b = fast_exp2(b), c = fast_exp2(c), d = fast_exp2(d);
-                    l2[(r + i) / 2] = f2_add(l2[(r + i) / 2], f2_pack(a, b));
-                    l2[(r + i) / 2 + 1] = f2_add(l2[(r + i) / 2 + 1], f2_pack(c, d));
-                    w[i / 2] = pack_bf16(a, b), w[i / 2 + 1] = pack_bf16(c, d);
+                for (int r = 0; r < 16; r += 8) {
+                    if (c + r >= rows) continue;
+                    uint32_t w[4];
+#pragma unroll
+                    for (int i = 0; i < 8; i += 2) {
+                        const float a = fast_exp2(y[r + i]), b = fast_exp2(y[r + i + 1]);
+                        l2[(c + r + i) / 2] = f2_add(l2[(c + r + i) / 2], f2_pack(a, b));
+                        w[i / 2] = pack_bf16(a, b);
+                    }
+                    sts128(p_row + (((p_chunk + (c + r) / 8) ^ (tid & 7)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
                 }
-                sts128(p_row + (((p_chunk + r / 8) ^ (tid & 7)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
             }
             fence_proxy_async();
             tmem_st_wait();
             tc_fence_before_sync();
-            sync();
-            if (warp == 0 && elect_one()) {
-                tc_fence_after_sync();
-                issue_o(started);
-            }
-            __syncwarp();
+            arrive(bar_p());
+            if (k >= 0) ++taken;
+            parity ^= 1;
             started = true;
         }
 
@@ -529,14 +608,13 @@ struct Worker {
             else if (!(lane & 1)) stsf(misc + F::kParts + (warp * N + (lane >> 1)) * 4, v[0]);
         }
         if (started) {
-            wait(bar_o(), of_o, 2);
-            of_o ^= 1;
+            wait(bar_o(), parity ^ 1, 2);
             tc_fence_after_sync();
         }
         sync();
-        const bool whole = part.u0 == 0 && part.u1 == units;
-        const size_t slot = (size_t)2 * worker + (part.u0 == 0);
-        const int blind = kChunk ? min(max(-pl.pos0, 0), pl.n) * p.G : 0;   // rows of the sequence that see no key
+        const int row0 = ITEM(row0), blind = kChunk ? ITEM(blind) : 0;
+        const bool whole = ITEM(whole) != 0;
+        const size_t slot = (size_t)2 * worker + ITEM(begins), out_row = (size_t)ITEM(tok0) * p.Hq + ITEM(h) * p.G;   // (of row 0 of token 0)
         if (tid < N) {
             float l = 0.f;
 #pragma unroll
@@ -550,8 +628,8 @@ struct Worker {
                 else if (p.lse) p.lse[out_row + (size_t)(row / p.G) * p.Hq + row % p.G] = sees ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
             }
         }
-        if (part.parts && tid == 0) {
-            p.cuts[2 * worker] = make_int4(pl.tok0, row0, pl.h << 8 | rows, part.parts);
+        if (tid == 0 && ITEM(parts)) {
+            p.cuts[2 * worker] = make_int4(ITEM(tok0), row0, ITEM(h) << 8 | rows, ITEM(parts));
             p.cuts[2 * worker + 1] = make_int4(blind, 0, 0, 0);
         }
         sync();
@@ -561,7 +639,7 @@ struct Worker {
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[i] = 0u;
             if (started) {
-                tmem_ld_x16(tmem + lanes + 64 + N + c0, o);
+                tmem_ld_x16(t_o + c0, o);
                 tmem_ld_wait();
             }
             int row = row0 + c0, token = row / p.G, g = row - token * p.G;
@@ -581,6 +659,7 @@ struct Worker {
         }
         tc_fence_before_sync();
     }
+#undef ITEM
 };
 
 template <int N, bool kChunk>
@@ -590,14 +669,17 @@ __global__ void __launch_bounds__(Form<N>::kThreads, 1) q4_attn_kernel(const __g
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t shared = smem0 + F::kOffShared;
-    const int tid = threadIdx.x, wg = tid >> 7, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const bool issuer = tid >= F::kWorkers * 128;
+    const int wg = issuer ? warp & 3 : tid >> 7;   // the worker
     const int workers = gridDim.x * F::kWorkers;
 
     if (tid == 0) {
 #pragma unroll 1
         for (int w = 0; w < F::kWorkers; ++w)
 #pragma unroll 1
-            for (int i = 0; i < F::kStages + 2; ++i) mbar_init(smem0 + F::kOffMisc + w * F::kMiscBytes + F::kBars + i * 8, 1);
+            for (int i = 0; i < F::kStages + 8; ++i)   // (one lane of each warp says that keys, or weights and values, are there, and that an item is read)
+                mbar_init(smem0 + F::kOffMisc + w * F::kMiscBytes + F::kBars + i * 8, i == F::kStages || i == F::kStages + 2 || i >= F::kStages + 6 ? 4 : 1);
         mbar_fence_init();
         sts32(shared + 4, 0);
     }
@@ -620,43 +702,65 @@ __global__ void __launch_bounds__(Form<N>::kThreads, 1) q4_attn_kernel(const __g
     for (int i = line.shares + blockIdx.x * F::kThreads + tid; i < workers; i += gridDim.x * F::kThreads) p.cuts[2 * i] = make_int4(0, 0, 0, 0);
     __syncthreads();
     const int share = blockIdx.x * per_cta + wg;
-    if (wg < per_cta && share < line.shares && line.total > 0) {
+    const bool some = wg < min(per_cta, F::kWorkers) && share < line.shares && line.total > 0;
+    const auto worker = [&] {
         Worker<N, kChunk> w{p};
         w.wg = wg, w.tid = tid & 127, w.lane = lane, w.warp = warp & 3, w.worker = share;
         w.q_tile = smem0 + F::kOffQ + wg * F::kQBytes;
         w.p_tile = smem0 + F::kOffP + wg / F::kSharers * F::kPTile + wg % F::kSharers * (N * 2);
-        w.ring = smem0 + F::kOffRing + wg * F::kStages * F::kUnitBytes;
         w.misc = smem0 + F::kOffMisc + wg * F::kMiscBytes;
+        w.ring = smem0 + F::kOffRing + wg * F::kStages * F::kUnitBytes;
+        w.slabs = smem_raw + (w.ring - smem_u32(smem_raw));
+        w.refs = reinterpret_cast<const float *>(smem_raw + (w.misc + F::kNeg - smem_u32(smem_raw)));
         w.shared = shared;
         w.tmem = tmem + wg * F::kColumns;
-        w.policy = policy_evict_first();
-        int e = (int)lds_ll(shared + 256 + wg * 16);
-        long long at = lds_ll(shared + 256 + wg * 16 + 8);
-        const long long lo = line.bound(share), hi = line.bound(share + 1);
-        Place pl = place<kChunk, N>(p, e);
-        int t = pl.cost.item_at(lo - at);
-        at += pl.cost.before(t);
+        return w;
+    };
+    if (issuer) {
+        reg_dealloc<F::kRegsFew>();
+        if (some) {
+            Worker<N, kChunk> w = worker();
+            int e = (int)lds_ll(shared + 256 + wg * 16);
+            long long at = lds_ll(shared + 256 + wg * 16 + 8);
+            const long long lo = line.bound(share), hi = line.bound(share + 1);
+            Place pl = place<kChunk, N>(p, e);
+            int t = pl.cost.item_at(lo - at);
+            at += pl.cost.before(t);
 #pragma unroll 1
-        while (at < hi) {
-            const long long cost = pl.cost.cost(t);
-            int units = (pl.slabs + 1) / 2 + 1;
-            if constexpr (kChunk) {
-                const int rows = min(N, p.G * pl.n - t * N);
-                const int end = min(max(pl.pos0 + (t * N + rows - 1) / p.G + 1, 0), pl.len);
-                units = (end + kUnit - 1) / kUnit;
+            while (at < hi) {
+                const long long cost = pl.cost.cost(t);
+                int units = (pl.slabs + 1) / 2 + 1;
+                if constexpr (kChunk) {
+                    const int rows = min(N, p.G * pl.n - t * N);
+                    const int end = min(max(pl.pos0 + (t * N + rows - 1) / p.G + 1, 0), pl.len);
+                    units = (end + kUnit - 1) / kUnit;
+                }
+                const svq::Part part = svq::part_of(line, share, at, cost, units, den);
+                if (part.mine) w.copy_and_issue(pl, t, part, units);
+                at += cost;
+                if (++t == pl.cost.tiles) {
+                    t = 0;
+                    do {
+                        if (++e < entries) pl = place<kChunk, N>(p, e);
+                    } while (e < entries && pl.cost.tiles == 0);
+                    if (e >= entries) break;
+                }
             }
-            const svq::Part part = svq::part_of(line, share, at, cost, units, den);
-            if (part.mine) w.run(pl, t, part, units);
-            at += cost;
-            if (++t == pl.cost.tiles) {
-                t = 0;
-                do {
-                    if (++e < entries) pl = place<kChunk, N>(p, e);
-                } while (e < entries && pl.cost.tiles == 0);
-                if (e >= entries) break;
+            w.hand_out(Item{});
+            w.drain();
+        }
+    } else {
+        reg_alloc<F::kRegsMany>();
+        if (some) {
+            Worker<N, kChunk> w = worker();
+#pragma unroll 1
+            for (int n = 0;; ++n) {
+                w.wait(w.bar_item(n), (n >> 1) & 1, 32);
+                if (named_bar_or(1 + wg, 128, w.aborted()) || w.word(n, offsetof(Item, rows)) == 0) break;   // (all or nobody)
+                w.attend(n);
+                w.arrive(w.bar_taken(n));
             }
         }
-        w.drain();
     }
     tc_fence_before_sync();
     __syncthreads();
@@ -719,7 +823,14 @@ sv_status launch(Params &p, void *workspace, void *stream)
     p.ws_ml = reinterpret_cast<float2 *>(p.cuts + 2 * workers);
     p.ws_o = reinterpret_cast<float *>(p.ws_ml + (size_t)2 * workers * N);
     static svh::OncePerDevice once;
-    if (once.run([] { return cudaFuncSetAttribute(q4_attn_kernel<N, kChunk>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::kSmem); }) != cudaSuccess) {
+    if (once.run([] {
+            // (the warpgroups that compute wait for the registers that they ask for: there have to be as many)
+            cudaFuncAttributes a;
+            const cudaError_t e = cudaFuncGetAttributes(&a, q4_attn_kernel<N, kChunk>);
+            if (e != cudaSuccess) return e;
+            if (a.numRegs < F::kRegs) return cudaErrorInvalidConfiguration;
+            return cudaFuncSetAttribute(q4_attn_kernel<N, kChunk>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::kSmem);
+        }) != cudaSuccess) {
         (void)cudaGetLastError();
         return SV_ERR_CUDA;
     }
