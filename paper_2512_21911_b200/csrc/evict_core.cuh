@@ -10,18 +10,23 @@ namespace svev {
 
 namespace cg = cooperative_groups;
 
-constexpr int kThreads = 256, kRowGroups = kThreads / 16, kCluster = 8;
+constexpr int kRowGroups = 16;
+constexpr int kThreads = 512, kCluster = 8;
 constexpr int kBins = 2048;
-constexpr int kMostTokens = kCluster * 49152;   // that a cluster's shared memory holds the keys of
+constexpr int kSlice = 49152;                    // tokens that a CTA's shared memory holds the keys of
+constexpr int kMostTokens = kCluster * kSlice;
+constexpr int kRound = 256;                      // tokens that a CTA moves at a time
 
 struct Shared {
-    uint32_t hist[kBins];
+    union {
+        alignas(16) uint32_t hist[3][kBins];   // of the three passes
+        float part[kThreads / 16][128];        // (the moves) sums of keys
+    };
     uint32_t sums[kThreads / 32];
     uint32_t digit, above;      // what a pass found
-    uint32_t kept[2];           // of the slice: keys above the n-th largest, keys equal to it
+    alignas(8) uint32_t kept[2];   // of the slice: keys above the n-th largest, keys equal to it
     uint32_t first[kCluster + 1];   // where the slices' kept tokens begin
-    int32_t source[128];        // of a round's block
-    float part[kRowGroups][128];
+    int32_t source[kRound];     // of a round's tokens
 };
 
 // The sum over the threads below this one, and over all.
@@ -59,46 +64,44 @@ __device__ __forceinline__ void keep_heaviest(const cg::cluster_group &cluster, 
         const uint32_t key = svsel::key_of_bits(__float_as_uint(weights[t]));
         keys[i] = t < n_sink || t >= L - n_recent ? svsel::kForcedKey : key;
     }
-    // the n-th largest key, by digits from the top
+    for (int i = tid; i < 3 * kBins; i += kThreads) sh.hist[0][i] = 0;
+    __syncthreads();
+    // the n-th largest key, by digits from the top; all CTAs find the same
     uint32_t prefix = 0, wanted = n;
 #pragma unroll 1
     for (int pass = 0; pass < 3; ++pass) {
         const int low = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11, bins = 1 << bits;
-        for (int i = tid; i < kBins; i += kThreads) sh.hist[i] = 0;
-        __syncthreads();
         for (int i = tid; i < count; i += kThreads) {
             const uint32_t key = keys[i];
-            if (pass == 0 || key >> (low + bits) == prefix) atomicAdd(&sh.hist[key >> low & (bins - 1)], 1u);
+            if (pass == 0 || key >> (low + bits) == prefix) atomicAdd(&sh.hist[pass][key >> low & (bins - 1)], 1u);
         }
         cluster.sync();
-        // bins of a thread, from the top; all CTAs find the same
-        constexpr int kEach = kBins / kThreads;
-        uint32_t mine[kEach], sum = 0;
+        // Four bins of a thread, from the top.  (All peers' bins are asked for at once: one peer behind the other is a trip of half a
+        // microsecond each, three times eight of them, and was most of the time of a short cache.)
+        uint32_t mine[4] = {0, 0, 0, 0};
+        const int top = bins - 4 * tid;   // behind the highest of them
+        if (top >= 4) {
+            uint4 x[kCluster];
 #pragma unroll
-        for (int j = 0; j < kEach; ++j) mine[j] = 0;
-        const int each = bins / kThreads;
-#pragma unroll 1
-        for (int r = 0; r < kCluster; ++r) {
-            const uint32_t *hist = cluster.map_shared_rank(sh.hist, r);
+            for (int r = 0; r < kCluster; ++r) x[r] = *reinterpret_cast<const uint4 *>(cluster.map_shared_rank(sh.hist[pass], r) + top - 4);
 #pragma unroll
-            for (int j = 0; j < kEach; ++j)
-                if (j < each) mine[j] += hist[bins - 1 - (tid * each + j)];
+            for (int r = 0; r < kCluster; ++r) mine[0] += x[r].w, mine[1] += x[r].z, mine[2] += x[r].y, mine[3] += x[r].x;
         }
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) sum += mine[j];
+        const uint32_t sum = mine[0] + mine[1] + mine[2] + mine[3];
         uint32_t all, above = sum_below(sum, sh.sums, all);
         if (above < wanted && wanted <= above + sum) {
             int j = 0;
             while (above + mine[j] < wanted) above += mine[j++];
-            sh.digit = bins - 1 - (tid * each + j), sh.above = above;
+            sh.digit = top - 1 - j, sh.above = above;
         }
-        cluster.sync();   // (also: everybody has read this CTA's histogram)
+        __syncthreads();
         prefix = prefix << bits | sh.digit;
         wanted -= sh.above;
+        __syncthreads();
     }
     // prefix is the key; of those equal to it the first `wanted` of the sequence stay.  A warp has a run of the slice; lane u of it keeps the
     // ballots of the run's words u, 32 + u, ...
-    constexpr int kWords = kMostTokens / kCluster / (kThreads / 32) / 32 / 32;
+    constexpr int kWords = kSlice / (kThreads / 32) / 32 / 32;
     const int lane = tid & 31, warp = tid >> 5;
     const int run = ((count + kThreads / 32 - 1) / (kThreads / 32) + 31) & ~31, i0 = min(warp * run, count), i1 = min(i0 + run, count);
     uint32_t more[kWords], equal[kWords], n_more = 0, n_equal = 0;
@@ -121,16 +124,21 @@ __device__ __forceinline__ void keep_heaviest(const cg::cluster_group &cluster, 
     (void)sum_below(n_equal, sh.sums, all_equal);
     if (tid == 0) sh.kept[0] = all_more, sh.kept[1] = all_equal;
     cluster.sync();
-    if (tid == 0) {
-        uint32_t at = 0, ties = 0;
-        for (int r = 0; r < kCluster; ++r) {
-            const uint32_t *k = cluster.map_shared_rank(sh.kept, r);
-            sh.first[r] = at;
-            if (r == rank) sh.digit = ties;
-            const uint32_t take = min(k[1], wanted - ties);
-            at += k[0] + take, ties += take;
+    if (tid < 32) {
+        uint32_t above = 0, same = 0;   // of the slice of CTA `tid`
+        if (tid < kCluster) {
+            const uint2 k = *reinterpret_cast<const uint2 *>(cluster.map_shared_rank(sh.kept, tid));
+            above = k.x, same = k.y;
         }
-        sh.first[kCluster] = at;
+        uint32_t at = above, ties = same;   // up to and with that slice
+#pragma unroll
+        for (int d = 1; d <= kCluster; d <<= 1) {
+            const uint32_t a = __shfl_up_sync(0xffffffffu, at, d), b = __shfl_up_sync(0xffffffffu, ties, d);
+            if (tid >= d) at += a, ties += b;
+        }
+        const uint32_t before = min(ties - same, wanted);
+        if (tid <= kCluster) sh.first[tid] = at - above + before;
+        if (tid == rank) sh.digit = before;
     }
     // the warp's words in order: of word (j, lane) the equal keys ahead of it, then the kept ones
     const auto warp_below = [&](uint32_t x, uint32_t &all) {

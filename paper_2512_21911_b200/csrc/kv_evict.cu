@@ -54,29 +54,29 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const __grid_constan
     }
     keep_heaviest(cluster, p.weights + base, L, n, p.n_sink, p.n_recent, keys, sh);
 
-    // the moves
+    // The moves: 256 tokens of the result a CTA and round, a thread eight rows of them -- of the rows of a block those that sv_block_reps
+    // gives it, so that the means are the same to the last bit.
     const int *pages = p.block_table + (size_t)s * p.NBmax;
-    const int c = tid & 15, rg = tid >> 4, blocks = (n + B - 1) / B;
-    constexpr int kIter = B / kRowGroups;
+    const int c = tid & 15, g = tid >> 4 & 15, w = tid >> 8;
+    constexpr int kRows = 8, kPer = B / kRowGroups, kTurns = kRows / kPer;   // rows of a thread: kPer of a block, in kTurns blocks
+    const auto place = [&](int i) { return (w + 2 * (i / kPer)) * B + g + kRowGroups * (i % kPer); };
     bool lost = false;
     const auto slot_of = [&](int t) {   // its row of the pools, or -1
         const int page = __ldg(pages + t / B);
         return (unsigned)page < (unsigned)p.n_pages ? ((long long)page * p.Hkv + h) * B + t % B : -1ll;
     };
 #pragma unroll 1
-    for (int b0 = 0; b0 < blocks; b0 += kCluster) {
-        const int b = b0 + rank, first = b * B, rows = min(max(n - first, 0), B);
+    for (int t0 = 0; t0 < n; t0 += kCluster * kRound) {
+        const int first = t0 + rank * kRound, rows = min(max(n - first, 0), kRound);
         __syncthreads();   // (the last round's sources and sums have been read)
-        if (tid < B) {
-            sh.source[tid] = tid < rows ? source_of(cluster, keys, sh, first + tid) : -1;
-        }
+        if (tid < rows) sh.source[tid] = source_of(cluster, keys, sh, first + tid);
         __syncthreads();
-        const bool still = rows == 0 || sh.source[rows - 1] == first + rows - 1;   // nothing of the block moves
-        uint4 k[kIter], v[kIter];
+        const bool still = rows == 0 || sh.source[rows - 1] == first + rows - 1;   // nothing moves
+        uint4 k[kRows], v[kRows];
         float weight = 0.f;
 #pragma unroll
-        for (int i = 0; i < kIter; ++i) {
-            const int r = rg + i * kRowGroups;
+        for (int i = 0; i < kRows; ++i) {
+            const int r = place(i);
             k[i] = v[i] = make_uint4(0u, 0u, 0u, 0u);
             if (r < rows && (!still || p.reps)) {
                 const long long from = slot_of(sh.source[r]);
@@ -92,8 +92,8 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const __grid_constan
         if (tid < rows) p.weights_out[base + first + tid] = weight;
         if (!still) {
 #pragma unroll
-            for (int i = 0; i < kIter; ++i) {
-                const int r = rg + i * kRowGroups;
+            for (int i = 0; i < kRows; ++i) {
+                const int r = place(i);
                 if (r < rows) {
                     const long long to = slot_of(first + r);
                     lost |= to < 0;
@@ -101,25 +101,29 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const __grid_constan
                 }
             }
         }
-        if (p.reps && rows > 0) {
+        if (!p.reps) continue;
+#pragma unroll
+        for (int turn = 0; turn < kTurns; ++turn) {
             float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < kIter; ++i) {
-                const uint32_t w[4] = {k[i].x, k[i].y, k[i].z, k[i].w};
+            for (int i = turn * kPer; i < (turn + 1) * kPer; ++i) {
+                const uint32_t x[4] = {k[i].x, k[i].y, k[i].z, k[i].w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&w[e]));
+                    const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&x[e]));
                     acc[2 * e] += f.x, acc[2 * e + 1] += f.y;
                 }
             }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sh.part[rg][c * 8 + e] = acc[e];
             __syncthreads();
-            if (tid < 128) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sh.part[tid >> 4][c * 8 + e] = acc[e];
+            __syncthreads();
+            const int block = w + 2 * turn, held = min(rows - block * B, B);
+            if ((tid & 255) < 128 && held > 0) {
                 float sum = 0.f;
 #pragma unroll
-                for (int g = 0; g < kRowGroups; ++g) sum += sh.part[g][tid];
-                p.reps[(((size_t)s * p.Hkv + h) * p.NBmax + b) * 128 + tid] = sum / (float)rows;
+                for (int i = 0; i < kRowGroups; ++i) sum += sh.part[w * kRowGroups + i][tid & 127];
+                p.reps[(((size_t)s * p.Hkv + h) * p.NBmax + first / B + block) * 128 + (tid & 127)] = sum / (float)held;
             }
         }
     }
@@ -149,17 +153,16 @@ extern "C" sv_status sv_kv_evict(const sv_geom *geom, void *k_pool, void *v_pool
     p.block_table = block_table, p.seq_lens = seq_lens, p.budget = budget, p.weights = weights, p.weights_out = weights_out, p.reps = reps;
     p.seq_lens_out = seq_lens_out, p.status = status_word;
     p.Hkv = Hkv, p.NBmax = geom->max_blocks, p.n_pages = n_pages, p.n_sink = n_sink, p.n_recent = n_recent;
-    const int slice = (int)(((cap + kCluster - 1) / kCluster + 3) & ~3ll);
-    const size_t bytes = (size_t)slice * 4;
     const auto kernel = B == 64 ? kv_evict_kernel<64> : kv_evict_kernel<128>;
     static svh::OncePerDevice once;
     if (once.run([] {
-            const cudaError_t e = cudaFuncSetAttribute(kv_evict_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostTokens / kCluster * 4);
-            return e != cudaSuccess ? e : cudaFuncSetAttribute(kv_evict_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostTokens / kCluster * 4);
+            const cudaError_t e = cudaFuncSetAttribute(kv_evict_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSlice * 4);
+            return e != cudaSuccess ? e : cudaFuncSetAttribute(kv_evict_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSlice * 4);
         }) != cudaSuccess) {
         (void)cudaGetLastError();
         return SV_ERR_CUDA;
     }
+    const size_t bytes = (size_t)(((cap + kCluster - 1) / kCluster + 3) & ~3ll) * 4;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(kCluster, Hkv, geom->n_seq);
     cfg.blockDim = dim3(kThreads);
