@@ -601,12 +601,14 @@ SV_API sv_status sv_kv_read_q4(const sv_geom *geom, const sv_kv_q4 *kv, const in
 
 /*
  * sv_verify_attn and sv_chunk_attn over such a cache: the same arguments and results, with the values that the codes stand for.  The draft
- * tokens' own keys and values are bf16 tensors, as there.  Of the block lists no order is asked for.  Keys and values behind a sequence's
- * last token have no part in either (a cached value of NaN or infinity that a row sees has, with a weight of zero too; the values of later
- * tokens of a chunk's call have to be finite).
- *   workspace       dev scratch of sv_workspace_bytes_q4(geom) bytes, 16-byte aligned, for any call with this geometry
- * Up to 64 query rows of a KV head are taken at once; a draft or a chunk of more goes over the cache several times.  softmax_scale: 0
- * selects 1 / sqrt(D), not negative (SV_ERR_SHAPE).
+ * tokens' own keys and values are bf16 tensors, as there.  Keys and values behind a sequence's last token have no part in either (a cached
+ * value of NaN or infinity that a row sees has, with a weight of zero too; the values of later tokens of a chunk's call have to be finite).
+ *   workspace       dev scratch of sv_workspace_bytes_q4(geom) bytes, 16-byte aligned, for any call with this geometry.  Where a sequence has
+ *                   more than 64 query rows a KV head (drafts times query heads; of a ragged batch on average) the cache is decoded into it
+ *                   first, up to 256 MB of bf16 pages, and sv_verify_attn or sv_chunk_attn go over those; in as little as
+ *                   sv_workspace_bytes_q4 gives for a geometry of one sequence, head and block, or beyond 256 MB, every 64 rows
+ *                   decode what they go over
+ * softmax_scale: 0 selects 1 / sqrt(D), not negative (SV_ERR_SHAPE).
  */
 SV_API size_t sv_workspace_bytes_q4(const sv_geom *geom);
 SV_API sv_status sv_verify_attn_q4(const sv_geom *geom, const void *q, const sv_kv_q4 *kv, const void *draft_k, const void *draft_v,

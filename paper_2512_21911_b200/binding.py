@@ -368,7 +368,7 @@ def sv_kv_read_q4(geom: sv_geom, kv: sv_kv_q4, first, q_start, k_out, v_out, sta
 
 
 def sv_workspace_bytes_q4(geom: sv_geom) -> int:
-    """Scratch of sv_verify_attn_q4 and sv_chunk_attn_q4, for any call with this geometry."""
+    """Scratch of sv_verify_attn_q4 and sv_chunk_attn_q4, for any call with this geometry (up to 256 MB of it for a decoded cache)."""
     return int(_lib.sv_workspace_bytes_q4(ctypes.byref(geom)))
 
 

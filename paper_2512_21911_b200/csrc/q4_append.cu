@@ -277,6 +277,60 @@ __global__ void __launch_bounds__(kThreads) q4_read_kernel(const uint8_t *pool, 
     }
 }
 
+// The cache of a batch, or its listed blocks, as bfloat16 pages, block b of sequence s on page s * NBmax + b, and the table that says so: where there are many
+// query rows, whose attention is bound by its products, decoding every key once is cheaper than once for every 64 of them (q4_attn.cu).
+// A CTA has a slab; bound by HBM (144 bytes read and 512 written a token and head).
+__global__ void __launch_bounds__(kThreads) q4_spread_kernel(const uint8_t *pool, const int32_t *block_table, const int32_t *seq_lens, const int32_t *sel_idx, const int32_t *sel_cnt,
+                                                             int max_sel, uint4 *k_out, uint4 *v_out, int32_t *table_out, int Hkv, int NBmax, int B, int n_pages,
+                                                             int32_t *status)
+{
+    __shared__ __align__(16) uint8_t slab[kSlabBytes];
+    svk::grid_dependency_wait();
+    svk::grid_launch_dependents();
+    const int tid = threadIdx.x, per = B / 64, h = blockIdx.y, s = blockIdx.z, sub = blockIdx.x % per;
+    int b = blockIdx.x / per;
+    if (sel_idx) {   // a listed block; the table in turns
+        for (int i = blockIdx.x * kThreads + tid; i < NBmax && h == 0; i += gridDim.x * kThreads) table_out[(size_t)s * NBmax + i] = (int32_t)((size_t)s * NBmax + i);
+        if (b >= min(__ldg(sel_cnt + s * Hkv + h), max_sel)) return;
+        b = __ldg(sel_idx + ((size_t)s * Hkv + h) * max_sel + b);
+        b = min(max(b, 0), NBmax - 1);   // (the attention, which clamps it as well, says so)
+    } else if (h == 0 && sub == 0 && tid == 0) {
+        table_out[(size_t)s * NBmax + b] = (int32_t)((size_t)s * NBmax + b);
+    }
+    const size_t entry = (size_t)s * NBmax + b;
+    if ((long long)b * B + sub * 64 >= min((long long)max(seq_lens[s], 0), (long long)NBmax * B)) return;
+    int page = __ldg(block_table + entry);
+    if ((unsigned)page >= (unsigned)n_pages) {
+        if (tid == 0 && status) atomicOr(status, svk::kStatusIndex);
+        page = min(max(page, 0), n_pages - 1);
+    }
+    const uint4 *from = reinterpret_cast<const uint4 *>(pool + (((size_t)page * Hkv + h) * per + sub) * kSlabBytes);
+    for (int i = tid; i < kSlabBytes / 16; i += kThreads) reinterpret_cast<uint4 *>(slab)[i] = __ldg(from + i);
+    __syncthreads();
+    const uint32_t *const words = reinterpret_cast<const uint32_t *>(slab);
+    const size_t row0 = (entry * Hkv + h) * B + sub * 64;
+    for (int i = tid; i < 64 * 16; i += kThreads) {   // keys: a token, eight dims
+        const int r = i >> 4, c = i & 15;
+        const uint32_t sc = words[svq::kOffKScale / 4 + r * 2 + (c >> 3)];
+        uint32_t x[4];
+        svq::decode(words[(c >> 2) * 256 + r * 4 + (c & 3)], svq::both_low(sc), svq::both_high(sc), x);
+        k_out[(row0 + r) * 16 + c] = make_uint4(x[0], x[1], x[2], x[3]);
+    }
+    const unsigned short *const scales = reinterpret_cast<const unsigned short *>(slab + svq::kOffVScale);
+    for (int i = tid; i < 64 * 16; i += kThreads) {   // values: a token, eight dims (a nibble of each of eight words)
+        const int r = i >> 4, c = i & 15, at = shift_of(r & 7);
+        const uint32_t d = scales[(c >> 3) * 128 + r], m = scales[(c >> 3) * 128 + 64 + r];
+        const uint32_t *w = words + svq::kOffV / 4 + (r >> 5) * 512 + (r >> 3 & 3) + c * 32;
+        uint32_t x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t pair = ((w[8 * e] >> at & 15u) << 3 | (w[8 * e + 4] >> at & 15u) << 19) | 0x3f803f80u;
+            x[e] = svq::fma_bf16x2(pair, d | d << 16, m | m << 16);
+        }
+        v_out[(row0 + r) * 16 + c] = make_uint4(x[0], x[1], x[2], x[3]);
+    }
+}
+
 cudaLaunchConfig_t config(dim3 grid, void *stream, cudaLaunchAttribute *attr)
 {
     cudaLaunchConfig_t cfg = {};
@@ -290,6 +344,18 @@ cudaLaunchConfig_t config(dim3 grid, void *stream, cudaLaunchAttribute *attr)
 }
 
 }  // namespace
+
+sv_status svh::spread_q4(const sv_geom *geom, const sv_kv_q4 *kv, const int32_t *sel_idx, const int32_t *sel_cnt, int32_t max_sel, void *k_out, void *v_out,
+                         int32_t *table_out, int32_t *status_word, void *stream)
+{
+    cudaLaunchAttribute attr[1];
+    const int blocks = sel_idx ? max_sel : geom->max_blocks;
+    const cudaLaunchConfig_t cfg = config(dim3((unsigned)(blocks * (geom->block_size / 64)), geom->n_kv_heads, geom->n_seq), stream, attr);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, q4_spread_kernel, static_cast<const uint8_t *>(kv->pool), kv->block_table, kv->seq_lens, sel_idx, sel_cnt,
+                                             (int)max_sel, static_cast<uint4 *>(k_out), static_cast<uint4 *>(v_out), table_out, (int)geom->n_kv_heads,
+                                             (int)geom->max_blocks, (int)geom->block_size, (int)kv->n_pages, status_word);
+    return e == cudaSuccess ? SV_OK : SV_ERR_CUDA;
+}
 
 extern "C" sv_status sv_rope_append_q4(const sv_geom *geom, void *pool, int32_t n_pages, const int32_t *block_table, const int32_t *seq_lens,
                                        const void *q, const void *k, const void *v, int64_t q_stride, int64_t k_stride, int64_t v_stride,

@@ -2,7 +2,7 @@
 // own keys, or of a ragged batch of new tokens over the cache that holds them.
 //
 // Mathematics, for a row q and the keys t that it sees: s_t = q . k_t * scale * log2 e, a reference m not far below the running maximum,
-// l = sum 2^(s_t - m), o = sum 2^(s_t - m) v_t; the output is o / l.  When the maximum outgrows the reference by more than 8, m moves and
+// l = sum 2^(s_t - m), o = sum 2^(s_t - m) v_t; the output is o / l.  When the maximum outgrows the reference by more than 24, m moves and
 // l and o are multiplied by 2^(old - new).
 //
 // A quarter of the bytes of a bfloat16 cache, but every value has to be decoded: what counts is instructions per value and that decoded
@@ -35,7 +35,10 @@ using namespace svk;
 using svq::kSlabBytes;
 using svq::kUnit;
 
-constexpr float kLag = 8.f;   // what a score may exceed the reference by (log2)
+// What a score may exceed its reference by (log2).  Weights up to 2^24 cost no precision (o / l does not depend on the reference, and bf16 and
+// fp32 have the same exponents), and a reference that moves costs as much as a unit.
+constexpr float kLag = 24.f;
+constexpr int kSpreadRows = 64;   // query rows of a sequence and KV head, on average, beyond which the cache is decoded first
 
 struct Params {
     const uint8_t *pool;
@@ -298,19 +301,18 @@ struct Worker {
         const uint8_t *slab = slabs + stage * F::kUnitBytes + (tid >> 6) * kSlabBytes;
         const int t = tid & 63;
         const uint2 sc = *reinterpret_cast<const uint2 *>(slab + svq::kOffKScale + t * 8);
-#pragma unroll 1
-        for (int g = 0; g < 2; ++g) {
-            const uint32_t w = g ? sc.y : sc.x, d = svq::both_low(w), m = svq::both_high(w);
-            uint32_t x[32];
+        uint4 v[4];   // (all asked for at once: a store into tensor memory orders what is around it)
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const uint4 v = *reinterpret_cast<const uint4 *>(slab + (2 * g + c) * 1024 + t * 16);
-                svq::decode(v.x, d, m, x + 16 * c);
-                svq::decode(v.y, d, m, x + 16 * c + 4);
-                svq::decode(v.z, d, m, x + 16 * c + 8);
-                svq::decode(v.w, d, m, x + 16 * c + 12);
-            }
-            tmem_st_x32(at + 32 * g, x);
+        for (int c = 0; c < 4; ++c) v[c] = *reinterpret_cast<const uint4 *>(slab + c * 1024 + t * 16);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const uint32_t w = c < 2 ? sc.x : sc.y, d = svq::both_low(w), m = svq::both_high(w);
+            uint32_t x[16];
+            svq::decode(v[c].x, d, m, x);
+            svq::decode(v[c].y, d, m, x + 4);
+            svq::decode(v[c].z, d, m, x + 8);
+            svq::decode(v[c].w, d, m, x + 12);
+            tmem_st_x16(at + 16 * c, x);
         }
     }
     // 128 tokens of the warp's 32 dims.  A thread has four dims (d0 + 8 i) and four tokens of every 16, so that it needs a quarter of the
@@ -327,6 +329,10 @@ struct Worker {
             uint2 d[4], m[4];   // of tokens 16 j + 4 q ..
 #pragma unroll
             for (int j = 0; j < 4; ++j) d[j] = *reinterpret_cast<const uint2 *>(sc + 32 * j), m[j] = *reinterpret_cast<const uint2 *>(sc + 128 + 32 * j);
+            uint32_t words[16];   // of dims d0 + 8 i, then by j
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                words[i] = *reinterpret_cast<const uint32_t *>(slab + svq::kOffV + (i >> 1 & 1) * 2048 + (d0 + 8 * (i >> 2)) * 16 + (2 * (i & 1) + (q >> 1)) * 4);
             const int n = b ? valid[1] : valid[0];
             if (n < 64) {
                 const auto cut = [](uint32_t w, int left) { return left >= 2 ? w : left == 1 ? w & 0xffffu : 0u; };
@@ -343,7 +349,7 @@ struct Worker {
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const uint32_t w = *reinterpret_cast<const uint32_t *>(slab + svq::kOffV + (j >> 1) * 2048 + (d0 + 16 * half + 8 * h) * 16 + (2 * (j & 1) + (q >> 1)) * 4);
+                        const uint32_t w = words[8 * half + 4 * h + j];
                         x[4 * j + 2 * h] = svq::fma_bf16x2(svq::steps_at(w, turn), d[j].x, m[j].x);
                         x[4 * j + 2 * h + 1] = svq::fma_bf16x2(svq::steps_at(w, turn + 4), d[j].y, m[j].y);
                     }
@@ -853,6 +859,45 @@ sv_status launch(Params &p, void *workspace, void *stream)
     cfg.dynamicSmemBytes = 0;
     return cudaLaunchKernelEx(&cfg, q4_merge_kernel, p, N) == cudaSuccess ? svh::launch_status() : SV_ERR_CUDA;
 }
+// What the kernel itself needs, with the most rows.
+size_t own_bytes()
+{
+    size_t most = 0;
+    for (int n : {16, 32, 64}) most = std::max(most, (size_t)workers_of(n) * (2 * sizeof(int4) + 2 * (size_t)n * 130 * sizeof(float)));
+    return (most + 127) / 128 * 128;
+}
+// Behind that, in a workspace that has room: the cache as bfloat16 pages, their table, and what the attention over such pages needs.  Not for
+// caches of more than 256 MB of pages.
+struct Spread {
+    size_t pool, table, scratch, bytes;   // of one pool, the table, that attention's workspace; of all of it (0: there is none)
+    explicit Spread(const sv_geom *g)
+    {
+        const int64_t pages = (int64_t)g->n_seq * g->max_blocks, rows = pages * g->n_kv_heads * g->block_size;
+        pool = table = scratch = bytes = 0;
+        if (rows > ((int64_t)256 << 20) / 512) return;
+        pool = (size_t)rows * 256, table = ((size_t)pages * 4 + 127) / 128 * 128;
+        scratch = std::max(sv_chunk_workspace_bytes(g, 129), sv_workspace_bytes(g, g->max_blocks));   // (of a geometry that does not verify: 0)
+        bytes = 2 * pool + table + scratch + 128;
+    }
+};
+// Whether a call of this many query rows a sequence and KV head goes over the decoded cache, and where it is then.  A tile of 64 rows here
+// takes as long as one of 128 there, and every tile decodes all its keys: 1,024 tokens behind 30,001 (32 heads) take 1,490 us here, 540 there
+// with the decoding; 12 sequences, three of them chunks of some 500 tokens, 290 and 157; trees of 60 tokens of four sequences (420 rows,
+// 40 blocks) 98 and 63.
+struct Decoded {
+    bool use = false;
+    uint8_t *k, *v, *scratch;
+    int32_t *table;
+    Decoded(const sv_geom *g, const Spread &s, int64_t rows, void *workspace, size_t workspace_bytes, size_t need)
+    {
+        if (!s.bytes || need > s.scratch || workspace_bytes < own_bytes() + s.bytes || rows <= kSpreadRows) return;
+        use = true;
+        k = static_cast<uint8_t *>(workspace) + own_bytes();
+        k += (128 - (reinterpret_cast<uintptr_t>(k) & 127)) & 127;   // (pools stand on 128 bytes)
+        v = k + s.pool, table = reinterpret_cast<int32_t *>(v + s.pool), scratch = v + s.pool + s.table;
+    }
+};
+
 template <bool kChunk>
 sv_status launch_rows(Params &p, int64_t rows, void *workspace, void *stream)
 {
@@ -866,7 +911,7 @@ sv_status common(const sv_geom *g, const sv_kv_q4 *kv, const void *q, float soft
     if (!(softmax_scale >= 0.f && softmax_scale < INFINITY)) return SV_ERR_SHAPE;
     if (!svh::aligned(q, 16) || !svh::aligned(out, 16) || !svh::aligned(workspace, 16)) return SV_ERR_ALIGN;
     if ((int64_t)g->n_seq * g->n_kv_heads >= (int64_t)1 << 31) return SV_ERR_SHAPE;
-    if (workspace_bytes < sv_workspace_bytes_q4(g)) return SV_ERR_WORKSPACE;
+    if (workspace_bytes < own_bytes()) return SV_ERR_WORKSPACE;
     if (!workspace) return SV_ERR_NULL;
     p = Params{};
     p.pool = static_cast<const uint8_t *>(kv->pool), p.block_table = kv->block_table, p.seq_lens = kv->seq_lens, p.n_pages = kv->n_pages;
@@ -881,9 +926,7 @@ sv_status common(const sv_geom *g, const sv_kv_q4 *kv, const void *q, float soft
 extern "C" size_t sv_workspace_bytes_q4(const sv_geom *geom)
 {
     if (svh::check_ragged(geom, 0) != SV_OK) return 0;
-    size_t most = 0;
-    for (int n : {16, 32, 64}) most = std::max(most, (size_t)workers_of(n) * (2 * sizeof(int4) + 2 * (size_t)n * 130 * sizeof(float)));
-    return most;
+    return own_bytes() + Spread(geom).bytes;
 }
 
 extern "C" sv_status sv_verify_attn_q4(const sv_geom *geom, const void *q, const sv_kv_q4 *kv, const void *draft_k, const void *draft_v,
@@ -905,6 +948,15 @@ extern "C" sv_status sv_verify_attn_q4(const sv_geom *geom, const void *q, const
     if (st != SV_OK) return st;
     p.draft_k = static_cast<const __nv_bfloat16 *>(draft_k), p.draft_v = static_cast<const __nv_bfloat16 *>(draft_v), p.parent = parent;
     p.sel_idx = sel_idx, p.sel_cnt = sel_cnt, p.max_sel = std::min(max_sel, 1 << 24), p.T = geom->n_draft;
+    const Spread spread(geom);
+    const Decoded d(geom, spread, (int64_t)p.G * p.T, workspace, workspace_bytes, sv_workspace_bytes(geom, sel_idx ? max_sel : geom->max_blocks));
+    if (d.use && (!sel_idx || max_sel <= geom->max_blocks)) {
+        st = svh::spread_q4(geom, kv, sel_idx, sel_cnt, max_sel, d.k, d.v, d.table, status_word, stream);
+        if (st != SV_OK) return st;
+        const sv_kv pages = {d.k, d.v, d.table, kv->seq_lens, geom->n_seq * geom->max_blocks};
+        return sv_verify_attn(geom, q, &pages, draft_k, draft_v, parent, sel_idx, sel_cnt, max_sel, softmax_scale, out, lse, d.scratch, spread.scratch,
+                              status_word, stream);
+    }
     return launch_rows<false>(p, (int64_t)p.G * p.T, workspace, stream);
 }
 
@@ -921,6 +973,14 @@ extern "C" sv_status sv_chunk_attn_q4(const sv_geom *geom, const void *q, const 
     st = common(geom, kv, q, softmax_scale, out, lse, workspace, workspace_bytes, status_word, p);
     if (st != SV_OK || n_tokens == 0) return st;
     p.q_start = q_start, p.n_tokens = n_tokens;
+    const Spread spread(geom);
+    const Decoded d(geom, spread, (int64_t)p.G * n_tokens / geom->n_seq, workspace, workspace_bytes, sv_chunk_workspace_bytes(geom, n_tokens));
+    if (d.use) {
+        st = svh::spread_q4(geom, kv, nullptr, nullptr, 0, d.k, d.v, d.table, status_word, stream);
+        if (st != SV_OK) return st;
+        const sv_kv pages = {d.k, d.v, d.table, kv->seq_lens, geom->n_seq * geom->max_blocks};
+        return sv_chunk_attn(geom, q, &pages, q_start, n_tokens, softmax_scale, out, lse, d.scratch, spread.scratch, status_word, stream);
+    }
     // (the mean rows of a sequence: a batch of single tokens with a few chunks is taken as chunks)
     return launch_rows<true>(p, (int64_t)p.G * ((n_tokens + geom->n_seq - 1) / geom->n_seq), workspace, stream);
 }

@@ -223,6 +223,11 @@ sv_status verify_attn_from_host(const sv_geom *geom, const sv_layers *layers, co
 // Whether they are.
 bool lists_handed_out(const sv_geom *geom, const sv_layers *layers, int32_t max_sel);
 
+// A 4-bit cache, or (sel_idx) its listed blocks, as bfloat16 pages, one behind the other in the order of its table, and that order as a table
+// (q4_append.cu).
+sv_status spread_q4(const sv_geom *geom, const sv_kv_q4 *kv, const int32_t *sel_idx, const int32_t *sel_cnt, int32_t max_sel, void *k_out, void *v_out,
+                    int32_t *table_out, int32_t *status_word, void *stream);
+
 inline sv_status launch_status()
 {
     return cudaGetLastError() == cudaSuccess ? SV_OK : SV_ERR_CUDA;

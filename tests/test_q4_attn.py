@@ -111,11 +111,17 @@ def _lists(c, keep, seed, shuffled=False):
     return torch.from_numpy(idx).cuda(), torch.from_numpy(cnt).cuda()
 
 
-def _verify(sv, c, q, dk, dv, parent, lists, **over):
+def _scratch(sv, geom, little):
+    """Workspace for the geometry; or as much as any call takes, which leaves no room for a decoded cache."""
+    size = sv.sv_workspace_bytes_q4(sv.make_geom(1, 1, 1, 128, 64, 1, 1) if little else geom)
+    return torch.full((size,), 0xff, dtype=torch.uint8, device="cuda")
+
+
+def _verify(sv, c, q, dk, dv, parent, lists, little=False, **over):
     S, T, Hq = q.shape[:3]
     geom = sv.make_geom(S, Hq, c["Hkv"], 128, c["B"], c["NB"], T)
     kv = sv.make_kv_q4(c["pool"], c["table"], c["lens"])
-    ws = torch.full((sv.sv_workspace_bytes_q4(geom),), 0xff, dtype=torch.uint8, device="cuda")
+    ws = _scratch(sv, geom, little)
     out, lse = torch.full_like(q, float("nan")), torch.full((S, T, Hq), float("nan"), device="cuda")
     status = _ints([0])
     sv.sv_verify_attn_q4(geom, q, kv, dk, dv, parent, *(lists or (None, None)), out, lse=lse, workspace=ws, status_word=status, **over)
@@ -133,9 +139,11 @@ def test_verify(lens, Hq, Hkv, B, T, tree, keep):
     c = _cache(lens, Hkv, B, seed=len(lens) + T)
     q, dk, dv, parent = _drafts(len(lens), T, Hq, Hkv, T, tree)
     lists = _lists(c, keep, 1) if keep else None
-    out, lse, status = _verify(sv, c, q, dk, dv, parent, lists)
-    assert status == 0
-    _close(out, lse, *_exact_verify(c, q, dk, dv, parent, lists))
+    exact = _exact_verify(c, q, dk, dv, parent, lists)
+    for little in (False, True):
+        out, lse, status = _verify(sv, c, q, dk, dv, parent, lists, little)
+        assert status == 0
+        _close(out, lse, *exact)
 
 
 @pytest.mark.gpu
@@ -154,10 +162,11 @@ def test_lists_in_any_order_and_marked_ones():
 
 
 @pytest.mark.gpu
-def test_indices_outside_their_tables_are_clamped():
+@pytest.mark.parametrize("T", [1, 20])
+def test_indices_outside_their_tables_are_clamped(T):
     import paper_2512_21911_b200 as sv
     c = _cache([300], 1, 64, junk=0)
-    q, dk, dv, _ = _drafts(1, 1, 4, 1, 0, False)
+    q, dk, dv, _ = _drafts(1, T, 4, 1, 0, False)
     for bad in (-5, c["NB"], 1 << 30):
         out, _, status = _verify(sv, c, q, dk, dv, None, (_ints([[[0, bad]]]), _ints([[2]])))
         assert status == sv.SV_STATUS_INDEX and torch.isfinite(out.float()).all()
@@ -169,10 +178,11 @@ def test_indices_outside_their_tables_are_clamped():
 
 
 @pytest.mark.gpu
-def test_nan_and_infinite_scores_show():
+@pytest.mark.parametrize("T", [2, 40])
+def test_nan_and_infinite_scores_show(T):
     import paper_2512_21911_b200 as sv
     c = _cache([200, 200], 1, 64)
-    q, dk, dv, _ = _drafts(2, 2, 2, 1, 0, False)
+    q, dk, dv, _ = _drafts(2, T, 2, 1, 0, False)
     clean, _, _ = _verify(sv, c, q, dk, dv, None, None)
     q[0, 0, 1, 5] = float("nan")
     q[1, 1, 0, 5] = float("inf")
@@ -215,11 +225,11 @@ def test_offsets_beyond_32_bits():
 # ------------------------------------------------------------------------------------------------ ragged batches
 
 
-def _chunk(sv, c, q, new, extra=0, ws=None, **over):
+def _chunk(sv, c, q, new, little=False, **over):
     S, Hq = len(new), q.shape[1]
     geom = sv.make_geom(S, Hq, c["Hkv"], 128, c["B"], c["NB"], 1)
     kv = sv.make_kv_q4(c["pool"], c["table"], c["lens"])
-    ws = torch.full((sv.sv_workspace_bytes_q4(geom),), 0xff, dtype=torch.uint8, device="cuda") if ws is None else ws
+    ws = _scratch(sv, geom, little)
     out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device="cuda")
     status = _ints([0])
     start = _ints(np.concatenate([[0], np.cumsum(new)]).tolist())
@@ -258,13 +268,14 @@ def test_chunk(lens, new, Hq, Hkv, B):
     gen = torch.Generator(device="cuda").manual_seed(2)
     N = sum(new)
     q = torch.empty((N + 2, Hq, 128), dtype=torch.bfloat16, device="cuda").normal_(0.0, SIGMA, generator=gen)
-    out, lse, status = _chunk(sv, c, q, new)
-    assert status == 0 and (out[N:] == 7.0).all() and (lse[N:] == 7.0).all()
     want, lse_want, A = _exact_chunk(c, q[:N], lens, new)
-    out, lse = out[:N], lse[:N]
     blind = torch.isinf(lse_want)
-    assert torch.equal(torch.isneginf(lse), blind) and (out[blind] == 0).all()
-    _close(out, lse.masked_fill(blind, 0.0), want, lse_want.masked_fill(blind, 0.0), A)
+    for little in (False, True):
+        out, lse, status = _chunk(sv, c, q, new, little)
+        assert status == 0 and (out[N:] == 7.0).all() and (lse[N:] == 7.0).all()
+        out, lse = out[:N], lse[:N]
+        assert torch.equal(torch.isneginf(lse), blind) and (out[blind] == 0).all()
+        _close(out, lse.masked_fill(blind, 0.0), want, lse_want.masked_fill(blind, 0.0), A)
 
 
 @pytest.mark.gpu
