@@ -2,7 +2,10 @@
 chunks, the first token is drawn from the last prompt token's logits, and then every step drafts a few tokens, verifies them in one
 pass over the kept blocks, accepts a prefix and commits it to the cache.
 
-    python examples/generate.py [--prompt 3000 700] [--new 32] [--layers 4]
+    python examples/generate.py [--prompt 3000 700] [--new 32] [--layers 4] [--four-bits | --most-tokens 1000]
+
+With --four-bits the cache is held in 4 bits; with --most-tokens a sequence that has more loses, between steps, those that the steps gave least
+attention to, down to three quarters.
 
 The draft model is the target's embedding and head without its layers.  Prompts, weights and random numbers are seeded."""
 import argparse
@@ -53,13 +56,12 @@ def most_tokens(prompts, new):
     return max(map(len, prompts)) + max(0, new - 1) * DRAFT
 
 
-def generate(prompts, new, layers=4, chunk=512, seed=0, temperature=0.8, top_p=0.95):
+def generate(prompts, new, layers=4, chunk=512, seed=0, temperature=0.8, top_p=0.95, four_bits=False, most=0):
     """Token lists of the prompts' continuations, at least `new` each, and the mean number of tokens a step keeps."""
     gen = torch.Generator(device="cuda").manual_seed(seed)
     S, longest = len(prompts), most_tokens(prompts, new)
     blocks = -(-longest // BLOCK)
     model = Decoder(layers, longest, gen)
-    pools = [torch.zeros((layers, S * blocks, KV_HEADS, BLOCK, DIM), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
     ints = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
     per_seq = lambda v, t=torch.float32: torch.full((S,), v, dtype=t, device="cuda")
     table = torch.randperm(S * blocks, generator=torch.Generator().manual_seed(seed)).int().view(S, blocks).cuda()
@@ -67,7 +69,11 @@ def generate(prompts, new, layers=4, chunk=512, seed=0, temperature=0.8, top_p=0
     verifier = sv.SparseVerifier(n_seq=S, n_q_heads=HEADS, n_kv_heads=KV_HEADS, head_dim=DIM, block_size=BLOCK, max_blocks=blocks, n_draft=DRAFT,
                                  n_layers=layers, block_table=table, seq_lens=ints([0] * S), budget_blocks=per_seq(keep, torch.int32), max_sel=keep,
                                  anchors=[l % 2 == 0 for l in range(layers)])
-    verifier.set_kv_stack(*pools)
+    if four_bits:
+        for l in range(layers):
+            verifier.set_layer_kv_q4(l, torch.zeros((S * blocks, KV_HEADS, BLOCK // 64, sv.SV_Q4_SLAB_BYTES), dtype=torch.uint8, device="cuda"))
+    else:
+        verifier.set_kv_stack(*(torch.zeros((layers, S * blocks, KV_HEADS, BLOCK, DIM), dtype=torch.bfloat16, device="cuda") for _ in range(2)))
     rand = lambda *shape: torch.rand(shape, generator=gen, device="cuda")
     warp = dict(temperature=per_seq(temperature), top_p=per_seq(top_p))
 
@@ -101,18 +107,23 @@ def generate(prompts, new, layers=4, chunk=512, seed=0, temperature=0.8, top_p=0
             tokens.append(t)
         tokens, p_draft = torch.stack(tokens[:DRAFT], 1).contiguous(), torch.stack(p_draft, 1).contiguous()
         x = model.embedding[tokens.view(-1).long()]
-        positions = (verifier.seq_lens[:, None] + torch.arange(DRAFT, device="cuda")).view(-1).long()
+        positions = (verifier.positions()[:, None] + torch.arange(DRAFT, device="cuda")).view(-1).long()
         draft_k, draft_v = (torch.empty((layers, S, DRAFT, KV_HEADS, DIM), dtype=torch.bfloat16, device="cuda") for _ in range(2))
         for l, layer in enumerate(model.layers):
             q, k, v = model.project(layer, x)
             draft_k[l].copy_(model.turn(k, positions).view(S, DRAFT, KV_HEADS, DIM))
             draft_v[l].copy_(v.view(S, DRAFT, KV_HEADS, DIM))
             attended = torch.empty((S, DRAFT, HEADS, DIM), dtype=torch.bfloat16, device="cuda")
-            verifier.verify_layer(l, model.turn(q, positions).view(S, DRAFT, HEADS, DIM), draft_k[l], draft_v[l], attended)
+            turned, lse = model.turn(q, positions).view(S, DRAFT, HEADS, DIM), torch.empty((S, DRAFT, HEADS), device="cuda")
+            verifier.verify_layer(l, turned, draft_k[l], draft_v[l], attended, lse=lse)
+            if most:
+                verifier.weigh_layer(l, turned, lse)
             x = model.rest(layer, x, attended)
         p_target, _ = verifier.draw(model.logits(x).view(S, DRAFT, VOCAB), rand(S * DRAFT), **warp)
         path, n_path, root = verifier.accept(p_target, p_draft, tokens, rand(S, DRAFT), rand(S))
         verifier.commit(draft_k, draft_v, path, n_path)
+        if most and int(verifier.seq_lens.max()) > most:
+            verifier.evict(per_seq(most * 3 // 4, torch.int32))
         verifier.check_status()
         for s in range(S):
             texts[s] += tokens[s, 1:int(n_path[s])].tolist() + [int(root[s])]
@@ -125,9 +136,14 @@ def main():
     args.add_argument("--prompt", type=int, nargs="+", default=[3000, 700], help="tokens of the prompts")
     args.add_argument("--new", type=int, default=32)
     args.add_argument("--layers", type=int, default=4)
+    args.add_argument("--four-bits", action="store_true", help="hold the cache in 4 bits")
+    args.add_argument("--most-tokens", type=int, default=0, help="evict from sequences with more tokens than these")
     a = args.parse_args()
+    if a.four_bits and a.most_tokens:
+        args.error("tokens are evicted from a bfloat16 cache only")
     rng = torch.Generator().manual_seed(1)
-    texts, kept, _ = generate([torch.randint(0, VOCAB, (n,), generator=rng).tolist() for n in a.prompt], a.new, a.layers)
+    texts, kept, _ = generate([torch.randint(0, VOCAB, (n,), generator=rng).tolist() for n in a.prompt], a.new, a.layers, four_bits=a.four_bits,
+                              most=a.most_tokens)
     print(f"{kept:.2f} tokens kept a step")
     for n, t in zip(a.prompt, texts):
         print(f"behind {n} tokens:", " ".join(map(str, t[:a.new])))

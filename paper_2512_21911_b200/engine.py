@@ -1,7 +1,8 @@
 """SparseVerifier: runs block selection and sparse verification attention for a stack of layers.
 
 Around the verification steps of a sequence, ``prefill_layer`` / ``end_prefill`` bring its prompt into the cache and
-``draw`` makes distributions and tokens of logits.
+``draw`` makes distributions and tokens of logits.  A layer's cache may be held in 4 bits (``set_layer_kv_q4``), and one that has
+grown too long lose the tokens that the steps gave least attention to (``weigh_layer``, ``evict``).
 
 A thin driver over the C-ABI calls: it owns the per-layer representatives, the block lists,
 the split-KV workspace and the outputs.  ``verify_layer`` enqueues one layer: ``sv_select_blocks`` (anchor
@@ -116,6 +117,12 @@ class SparseVerifier:
         self._turned = self._chunk_workspace = None
         self._outgrown: List[torch.Tensor] = []   # earlier, smaller _turned: captured graphs go on using them
 
+        self.kv_q4: List[Optional[sv.sv_kv_q4]] = [None] * n_layers          # of the layers whose cache is held in 4 bits
+        self._grown_kv_q4: List[Optional[sv.sv_kv_q4]] = [None] * n_layers
+        self._q4_workspace = None
+        self.weights: List[Optional[torch.Tensor]] = [None] * n_layers       # attention weight of the cached tokens, see weigh_layer
+        self._evicted: Optional[torch.Tensor] = None                         # tokens that the sequences have lost
+
     def _make_lists(self, flags: bytes, dev) -> None:
         """One block list per anchor layer; sel_idx / sel_cnt is the last one, which is also what verify_layer keeps its
         current list in."""
@@ -137,6 +144,16 @@ class SparseVerifier:
             else:
                 self._table[layer].copy_(torch.frombuffer(bytearray(row), dtype=torch.uint8))
         self._rows_missing -= new
+
+    def set_layer_kv_q4(self, layer: int, pool: torch.Tensor) -> None:
+        """A layer's cache in 4 bits: pool uint8 [n_pages][Hkv][B / 64][SV_Q4_SLAB_BYTES].  prefill_layer and commit write it, representatives
+        included, verify_layer and dense_layer go over it; such layers run one by one."""
+        assert self.kv[layer] is None, "the layer has bfloat16 pools already"
+        self._pools[layer] = (pool,)
+        self.kv_q4[layer] = sv.make_kv_q4(pool, self.block_table, self.seq_lens)
+        self._grown_kv_q4[layer] = sv.make_kv_q4(pool, self.block_table, self._grown)
+        if self._q4_workspace is None:   # (made here and not in the first step, which may be captured)
+            self._q4_workspace = torch.empty(sv.sv_workspace_bytes_q4(self.geom), dtype=torch.uint8, device=self.workspace.device)
 
     def set_kv_stack(self, k_all: torch.Tensor, v_all: torch.Tensor) -> None:
         """All layers' pools in one allocation, bf16 [layers][n_pages][Hkv][B][D]."""
@@ -164,7 +181,7 @@ class SparseVerifier:
                       "sv_block_reps_layers")
             return
         for l in range(self.n_layers):
-            if which is None or which[l]:
+            if (which is None or which[l]) and self.kv_q4[l] is None:   # (an append to a 4-bit cache leaves its representatives up to date)
                 sv.sv_block_reps(self.geom, self.kv[l], self.reps[l], sv.SV_TAIL_BLOCK)
 
     def _anchor_flags(self) -> bytes:
@@ -194,7 +211,8 @@ class SparseVerifier:
         return True
 
     def build_reps(self, layer: int, block_begin: int = 0, block_end: int = -1) -> None:
-        """(Re)compute block representatives of a layer; a decoding loop only refreshes the tail block."""
+        """(Re)compute block representatives of a layer; a decoding loop only refreshes the tail block.  (Those of a 4-bit cache are made
+        by what writes it.)"""
         sv.sv_block_reps(self.geom, self.kv[layer], self.reps[layer], block_begin, block_end)
 
     def verify_layer(self, layer: int, q, draft_k, draft_v, out, lse=None, behind_own_layer: bool = False) -> None:
@@ -203,6 +221,12 @@ class SparseVerifier:
         behind_own_layer: the kernel just before this call in the stream is the preceding layer's attention / merge
         (as inside verify_step), which writes neither the block list nor the cache: a layer that reuses the list
         then starts its gather while that kernel drains (sv_verify_attn_reused)."""
+        if self.kv_q4[layer] is not None:
+            if self.anchors[layer]:
+                sv.sv_select_blocks(self.geom, q, self.reps[layer], self.seq_lens, self.budget, self.n_sink, self.n_local, self.sel_idx, self.sel_cnt)
+            sv.sv_verify_attn_q4(self.geom, q, self.kv_q4[layer], draft_k, draft_v, self.parent, self.sel_idx, self.sel_cnt, out, lse=lse,
+                                 workspace=self._q4_workspace, status_word=self.status)
+            return
         # a layer that reuses (Eq. 9) finds the preceding layer's list in place, so nothing is launched for it
         failed = sv._native.verify_layer(self.geom, self.kv[layer], q, self.reps, layer, self.seq_lens, self.budget, self.n_sink,
                                          self.n_local, self.sel_idx, self.sel_cnt, draft_k, draft_v, self.parent, out, lse,
@@ -212,6 +236,10 @@ class SparseVerifier:
 
     def dense_layer(self, layer: int, q, draft_k, draft_v, out, lse=None) -> None:
         """Dense ("strict") verification attention over every cached block, for comparison."""
+        if self.kv_q4[layer] is not None:
+            sv.sv_verify_attn_q4(self.geom, q, self.kv_q4[layer], draft_k, draft_v, self.parent, None, None, out, lse=lse,
+                                 workspace=self._q4_workspace, status_word=self.status)
+            return
         if self.dense_workspace is None:
             n = max(16, sv.sv_workspace_bytes(self.geom, self.geom.max_blocks))
             self.dense_workspace = torch.empty(n, dtype=torch.uint8, device=self.workspace.device)
@@ -339,13 +367,19 @@ class SparseVerifier:
                 self._outgrown.append(self._turned)
                 rows = max(n, 2 * self._turned.shape[0])
             self._turned = torch.empty((rows, self.geom.n_q_heads, self.geom.head_dim), dtype=torch.bfloat16, device=k.device)
+        turned = self._turned[:n]
+        if self.kv_q4[layer] is not None:
+            sv.sv_rope_append_q4(self.geom, self._pools[layer][0], self.block_table, self.seq_lens, q, k, v, q_start, turned, self._grown, rope=rope,
+                                 interleaved=interleaved, reps=self.reps[layer], status_word=self.status)
+            sv.sv_chunk_attn_q4(self.geom, turned, self._grown_kv_q4[layer], q_start, out, lse=lse, workspace=self._q4_workspace,
+                                status_word=self.status)
+            return
         if self._chunk_workspace is None:   # what any batch needs: more than 128 query rows a KV head need no more
             need = sv.sv_chunk_workspace_bytes(self.geom, 129)
             self._chunk_workspace = torch.empty(need, dtype=torch.uint8, device=k.device)
         k_pool, v_pool = self._pools[layer]
-        turned = self._turned[:n]
-        sv.sv_rope_append(self.geom, k_pool, v_pool, self.block_table, self.seq_lens, q, k, v, q_start, turned, self._grown, rope=rope,
-                          interleaved=interleaved, reps=self.reps[layer], status_word=self.status)
+        sv.sv_rope_append_at(self.geom, k_pool, v_pool, self.block_table, self.seq_lens, None if self._evicted is None else self.positions(), q, k, v,
+                             q_start, turned, self._grown, rope=rope, interleaved=interleaved, reps=self.reps[layer], status_word=self.status)
         sv.sv_chunk_attn(self.geom, turned, self._grown_kv[layer], q_start, out, lse=lse, workspace=self._chunk_workspace,
                          status_word=self.status)
 
@@ -354,6 +388,40 @@ class SparseVerifier:
         time nothing changes (which the device decides, so that either may be part of a captured graph)."""
         torch.maximum(self.seq_lens, self._grown, out=self.seq_lens)
         self._grown.fill_(-2 ** 31)
+
+    def positions(self) -> torch.Tensor:
+        """Position of every sequence's next token: the tokens that the cache holds and those that it has lost (int32 [S])."""
+        return self.seq_lens if self._evicted is None else self.seq_lens + self._evicted
+
+    def weigh_layer(self, layer: int, q, lse, path=None, n_path=None, dense: bool = False) -> None:
+        """Add the attention weight that a step's rows gave the cached tokens of a layer to what earlier steps gave them (weights[layer],
+        float32 [S][Hkv][max_blocks * B]).  Behind verify_layer (dense: dense_layer) of the same layer, before commit: q and lse are that
+        call's, the blocks those of the current list.  path, n_path: the rows that count, as accept returns them."""
+        if self.kv[layer] is None:
+            raise TypeError("weigh_layer: the layer has no bfloat16 pools")
+        if self.weights[layer] is None:
+            g = self.geom
+            self.weights[layer] = torch.zeros((g.n_seq, g.n_kv_heads, g.max_blocks * g.block_size), dtype=torch.float32, device=self.workspace.device)
+        w = self.weights[layer]
+        sv.sv_attn_weights(self.geom, q, self.kv[layer], lse, w, w, sel_idx=None if dense else self.sel_idx, sel_cnt=None if dense else self.sel_cnt,
+                           path=path, n_path=n_path, status_word=self.status)
+
+    def evict(self, budget_tokens: torch.Tensor, n_sink: int = 4, n_recent: int = 64) -> None:
+        """Every layer and KV head keeps budget_tokens (int32 [S]) of a sequence's tokens: the first n_sink, the last n_recent and of the others
+        those of the largest weight.  The lengths shrink, positions() does not; pages behind the new lengths are free.  Between steps (a
+        list selected before names other blocks afterwards).  Layers that were never weighed keep the earliest of the others."""
+        if any(kv is None for kv in self.kv):
+            raise TypeError("evict: a layer has no bfloat16 pools")
+        g, new_len = self.geom, torch.empty_like(self.seq_lens)
+        for l in range(self.n_layers):
+            if self.weights[l] is None:
+                self.weights[l] = torch.zeros((g.n_seq, g.n_kv_heads, g.max_blocks * g.block_size), dtype=torch.float32, device=self.workspace.device)
+            sv.sv_kv_evict(g, *self._pools[l], self.block_table, self.seq_lens, self.weights[l], budget_tokens, n_sink, n_recent, new_len,
+                           self.weights[l], reps=self.reps[l], status_word=self.status)
+        if self._evicted is None:
+            self._evicted = torch.zeros_like(self.seq_lens)
+        self._evicted += self.seq_lens - new_len
+        self.seq_lens.copy_(new_len)          # every layer has read the old lengths by now (same stream)
 
     def draw(self, logits, u, distributions: bool = True, **parameters):
         """Distributions (what accept takes) and tokens of rows of logits [S][T][V] or [R][V]: (probs, tokens), probs None unless they
@@ -383,6 +451,10 @@ class SparseVerifier:
                 return
         new_len = torch.empty_like(self.seq_lens)
         for l in range(self.n_layers):
+            if self.kv_q4[l] is not None:
+                sv.sv_kv_append_q4(self.geom, self._pools[l][0], self.block_table, self.seq_lens, draft_k[l], draft_v[l], path, n_path, new_len,
+                                   self.reps[l])
+                continue
             k_pool, v_pool = self._pools[l]
             sv.sv_kv_append(self.geom, k_pool, v_pool, self.block_table, self.seq_lens, draft_k[l], draft_v[l], path,
                             n_path, new_len, self.reps[l])
