@@ -630,7 +630,8 @@ SV_API sv_status sv_chunk_attn_q4(const sv_geom *geom, const void *q, const sv_k
  *   path, n_path    dev int32 [S][T], [S] as written by sv_accept: the rows that count, or NULL, NULL: all T
  *   softmax_scale   0 selects 1/sqrt(D); not negative
  *   weights         dev fp32 [S][Hkv][NBmax * block_size]; weights_out: the same buffer, or one that does not overlap it
- * Sums of fp32 in a fixed order.  One launch.
+ * Sums of fp32 in a fixed order.  An index of the list or the path outside its table, or a page outside the pool, is clamped into it and sets
+ * SV_STATUS_INDEX.  One launch.
  */
 SV_API sv_status sv_attn_weights(const sv_geom *geom, const void *q, const sv_kv *kv, const float *lse, const int32_t *sel_idx,
                                  const int32_t *sel_cnt, int32_t max_sel, const int32_t *path, const int32_t *n_path, float softmax_scale,
@@ -640,7 +641,8 @@ SV_API sv_status sv_attn_weights(const sv_geom *geom, const void *q, const sv_kv
  * Eviction by such weights: of a sequence of L tokens, n = min(L, max(budget[s], n_sink + n_recent)) stay in every KV head: the first
  * n_sink, the last n_recent, and of the others the heaviest in that head (equal ones: the earlier first; a NaN ranks between the negative
  * numbers and zero).  They keep their order and close up: token number j of those that stay moves to position j of the sequence's
- * pages, in place.  The pages from ceil(n / block_size) on are free afterwards.  Where L <= n nothing is touched.
+ * pages, in place.  The pages from ceil(n / block_size) on are free afterwards.  Where L <= n nothing is touched.  A page of a sequence that
+ * loses tokens stands in the block table once: no other sequence reads it.
  *   weights         dev fp32 [S][Hkv][NBmax * block_size]; weights_out: the weights of the tokens at their new positions, and zeros for
  *                   n <= t < L; the same buffer, or one that does not overlap it
  *   budget          dev int32 [S]

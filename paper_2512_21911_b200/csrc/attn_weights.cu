@@ -175,11 +175,11 @@ struct Worker {
         }
         __syncwarp();
     }
-    // tokens from .. to - 1 keep what they had
+    // tokens from .. to - 1 (of a list that may be bad) keep what they had
     __device__ void keep(const Place &pl, long long from, long long to) const
     {
         const size_t base = ((size_t)pl.s * p.Hkv + pl.h) * p.NBmax * p.B;
-        for (long long t = from + tid; t < min(to, (long long)pl.len); t += 128) p.after[base + t] = p.before[base + t];
+        for (long long t = max(from, 0ll) + tid; t < min(to, (long long)pl.len); t += 128) p.after[base + t] = p.before[base + t];
     }
 
     __device__ void run(const Place &pl, const svq::Part &part)
@@ -269,7 +269,16 @@ struct Worker {
                 }
                 float a, b;
                 f2_unpack(f2_add(sum2[0], sum2[1]), a, b);
-                if (there) p.after[at] = had + (a + b);
+                float sum = a + b;
+                if (sum != sum) {   // a key that is not finite: rows that do not count give nothing all the same
+                    sum = 0.f;
+#pragma unroll
+                    for (int r = 0; r < N; ++r) {
+                        const float neg = __uint_as_float(lds32(misc + F::kNeg + r * 4));
+                        if (neg != -INFINITY) sum += fast_exp2(fmaf(__uint_as_float(s[r]), p.scale_log2, neg));
+                    }
+                }
+                if (there) p.after[at] = had + sum;
                 tc_fence_before_sync();
             }
         }

@@ -124,9 +124,32 @@ def test_rows_without_a_denominator_and_bad_indices():
     t["idx"][0, 0, 0] = -1
     t["cnt"][0, 0] = 1
     assert _run(sv, t)[1] == sv.SV_STATUS_INDEX
+    t["idx"][0, 0, 0] = -(2 ** 31)              # (what is kept as it was begins behind an index that is clamped too)
+    out, status = _run(sv, t)
+    assert status == sv.SV_STATUS_INDEX and bool((out[0, 0, 64:200] == t["w"][0, 0, 64:200]).all())
     t["cnt"][0, 0] = -1
     out, status = _run(sv, t)
     assert status == sv.SV_STATUS_NO_LIST and torch.equal(out[0, 0, :200], t["w"][0, 0, :200])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("odd", [float("nan"), float("inf"), -float("inf")])
+def test_a_key_that_is_not_finite_concerns_rows_that_count(odd):
+    """Of three rows (the tile has room for 16) one has no denominator: without it, or with no row at all, an odd key gets nothing."""
+    import paper_2512_21911_b200 as sv
+    t = _inputs([200], 3, 1, 64, 1)
+    t["k"][int(t["table"][0, 1]), 0, 7] = odd   # token 71
+    t["lse"].fill_(-math.inf)
+    out, _ = _run(sv, t)
+    assert torch.equal(out[0, 0, :200], t["w"][0, 0, :200])
+    t = _inputs([200], 3, 1, 64, 1)
+    t["q"].abs_()
+    want, _ = _run(sv, t)
+    t["k"][int(t["table"][0, 1]), 0, 7] = odd
+    out, _ = _run(sv, t)
+    got, others = float(out[0, 0, 71]), torch.arange(200, device="cuda") != 71
+    assert torch.equal(out[0, 0, :200][others], want[0, 0, :200][others])
+    assert got == float(t["w"][0, 0, 71]) if odd == -math.inf else got == math.inf if odd == math.inf else math.isnan(got)
 
 
 @pytest.mark.gpu
