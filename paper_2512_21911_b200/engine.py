@@ -121,7 +121,7 @@ class SparseVerifier:
         self._grown_kv_q4: List[Optional[sv.sv_kv_q4]] = [None] * n_layers
         self._q4_workspace = None
         self.weights: List[Optional[torch.Tensor]] = [None] * n_layers       # attention weight of the cached tokens, see weigh_layer
-        self._evicted: Optional[torch.Tensor] = None                         # tokens that the sequences have lost
+        self.evicted: Optional[torch.Tensor] = None                         # tokens that the sequences have lost
 
     def _make_lists(self, flags: bytes, dev) -> None:
         """One block list per anchor layer; sel_idx / sel_cnt is the last one, which is also what verify_layer keeps its
@@ -378,7 +378,7 @@ class SparseVerifier:
             need = sv.sv_chunk_workspace_bytes(self.geom, 129)
             self._chunk_workspace = torch.empty(need, dtype=torch.uint8, device=k.device)
         k_pool, v_pool = self._pools[layer]
-        sv.sv_rope_append_at(self.geom, k_pool, v_pool, self.block_table, self.seq_lens, None if self._evicted is None else self.positions(), q, k, v,
+        sv.sv_rope_append_at(self.geom, k_pool, v_pool, self.block_table, self.seq_lens, None if self.evicted is None else self.positions(), q, k, v,
                              q_start, turned, self._grown, rope=rope, interleaved=interleaved, reps=self.reps[layer], status_word=self.status)
         sv.sv_chunk_attn(self.geom, turned, self._grown_kv[layer], q_start, out, lse=lse, workspace=self._chunk_workspace,
                          status_word=self.status)
@@ -391,36 +391,48 @@ class SparseVerifier:
 
     def positions(self) -> torch.Tensor:
         """Position of every sequence's next token: the tokens that the cache holds and those that it has lost (int32 [S])."""
-        return self.seq_lens if self._evicted is None else self.seq_lens + self._evicted
+        return self.seq_lens if self.evicted is None else self.seq_lens + self.evicted
+
+    @staticmethod
+    def _outside_of_capture() -> None:
+        if torch.cuda.is_current_stream_capturing():   # what a graph zeroes it zeroes whenever it is replayed
+            raise RuntimeError("the first weigh_layer of a layer, and the first evict, come before what is captured")
+
+    def _weights_of(self, layer: int) -> torch.Tensor:
+        if self.weights[layer] is None:
+            self._outside_of_capture()
+            g = self.geom
+            self.weights[layer] = torch.zeros((g.n_seq, g.n_kv_heads, g.max_blocks * g.block_size), dtype=torch.float32, device=self.workspace.device)
+        return self.weights[layer]
 
     def weigh_layer(self, layer: int, q, lse, path=None, n_path=None, dense: bool = False) -> None:
         """Add the attention weight that a step's rows gave the cached tokens of a layer to what earlier steps gave them (weights[layer],
         float32 [S][Hkv][max_blocks * B]).  Behind verify_layer (dense: dense_layer) of the same layer, before commit: q and lse are that
-        call's, the blocks those of the current list.  path, n_path: the rows that count, as accept returns them."""
+        call's, the blocks those of the current list.  path, n_path: the rows that count, as accept returns them.  The first call for a
+        layer makes the buffer and is not captured into a graph; whoever begins a sequence anew zeroes its part."""
         if self.kv[layer] is None:
             raise TypeError("weigh_layer: the layer has no bfloat16 pools")
-        if self.weights[layer] is None:
-            g = self.geom
-            self.weights[layer] = torch.zeros((g.n_seq, g.n_kv_heads, g.max_blocks * g.block_size), dtype=torch.float32, device=self.workspace.device)
-        w = self.weights[layer]
+        w = self._weights_of(layer)
         sv.sv_attn_weights(self.geom, q, self.kv[layer], lse, w, w, sel_idx=None if dense else self.sel_idx, sel_cnt=None if dense else self.sel_cnt,
                            path=path, n_path=n_path, status_word=self.status)
 
     def evict(self, budget_tokens: torch.Tensor, n_sink: int = 4, n_recent: int = 64) -> None:
         """Every layer and KV head keeps budget_tokens (int32 [S]) of a sequence's tokens: the first n_sink, the last n_recent and of the others
         those of the largest weight.  The lengths shrink, positions() does not; pages behind the new lengths are free.  Between steps (a
-        list selected before names other blocks afterwards).  Layers that were never weighed keep the earliest of the others."""
+        list selected before names other blocks afterwards; prefill_layer calls captured before the first eviction are captured anew).
+        Layers that were never weighed keep the earliest of the others.  A page belongs to one sequence.  Whoever begins a sequence anew
+        zeroes its entry of evicted."""
         if any(kv is None for kv in self.kv):
             raise TypeError("evict: a layer has no bfloat16 pools")
         g, new_len = self.geom, torch.empty_like(self.seq_lens)
         for l in range(self.n_layers):
-            if self.weights[l] is None:
-                self.weights[l] = torch.zeros((g.n_seq, g.n_kv_heads, g.max_blocks * g.block_size), dtype=torch.float32, device=self.workspace.device)
-            sv.sv_kv_evict(g, *self._pools[l], self.block_table, self.seq_lens, self.weights[l], budget_tokens, n_sink, n_recent, new_len,
-                           self.weights[l], reps=self.reps[l], status_word=self.status)
-        if self._evicted is None:
-            self._evicted = torch.zeros_like(self.seq_lens)
-        self._evicted += self.seq_lens - new_len
+            w = self._weights_of(l)
+            sv.sv_kv_evict(g, *self._pools[l], self.block_table, self.seq_lens, w, budget_tokens, n_sink, n_recent, new_len, w, reps=self.reps[l],
+                           status_word=self.status)
+        if self.evicted is None:
+            self._outside_of_capture()
+            self.evicted = torch.zeros_like(self.seq_lens)
+        self.evicted += self.seq_lens - new_len
         self.seq_lens.copy_(new_len)          # every layer has read the old lengths by now (same stream)
 
     def draw(self, logits, u, distributions: bool = True, **parameters):

@@ -186,6 +186,63 @@ def test_the_example(how):
 
 
 @pytest.mark.gpu
+def test_layers_of_both_kinds():
+    """Layer 1 in 4 bits between two of bfloat16: what the layers give alone."""
+    import paper_2512_21911_b200 as sv
+    lens, blocks, keep = [700, 130], 13, 4
+    res = []
+    for kinds in ([0, 0, 0], [1, 1, 1], [0, 1, 0]):
+        gen = torch.Generator(device="cuda").manual_seed(6)
+        v, _ = _verifier(2, blocks, True, keep, anchors=[True, False, True])
+        v.kv_q4, v._grown_kv_q4 = [None] * L, [None] * L
+        for l, kind in enumerate(kinds):
+            if kind:
+                v.set_layer_kv_q4(l, torch.zeros((2 * blocks, HKV, 1, sv.SV_Q4_SLAB_BYTES), dtype=torch.uint8, device="cuda"))
+            else:
+                v.set_layer_kv(l, *(torch.zeros((2 * blocks, HKV, B, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2)))
+        outs = _prefill(v, gen, lens, _rope(800))
+        q, dk, dv = _normal(gen, L, 2, T, HQ, 128), _normal(gen, L, 2, T, HKV, 128), _normal(gen, L, 2, T, HKV, 128)
+        out = torch.empty((L, 2, T, HQ, 128), dtype=torch.bfloat16, device="cuda")
+        v.verify_step(q, dk, dv, out)
+        v.commit(dk, dv, _ints([[0, 2, -1, -1], [0, 1, 2, 3]]), _ints([2, 4]))
+        again = torch.empty_like(out)
+        v.verify_step(q, dk, dv, again, refresh_tail=True)
+        res.append([torch.stack(outs), out, again, v.reps])
+        assert v.seq_lens.tolist() == [702, 134]
+    bf16, q4, both = res
+    assert all(torch.equal(b[l], (a, c)[l % 2][l]) for a, c, b in zip(bf16[:1] + bf16[3:], q4[:1] + q4[3:], both[:1] + both[3:]) for l in range(L))
+    for i in (1, 2):                            # layer 1 reuses the list of layer 0, whose representatives differ between the two alone
+        assert torch.equal(both[i][0], bf16[i][0]) and torch.equal(both[i][2], bf16[i][2])
+
+
+@pytest.mark.gpu
+def test_weights_over_replays():
+    """The first call makes the buffer and is not captured; a captured one adds to it at every replay."""
+    lens, gen = [300, 64], torch.Generator(device="cuda").manual_seed(7)
+    v, _ = _verifier(2, 7, False, 3)
+    _prefill(v, gen, lens, _rope(400))
+    q, dk, dv = _normal(gen, 2, T, HQ, 128), _normal(gen, 2, T, HKV, 128), _normal(gen, 2, T, HKV, 128)
+    out, lse = torch.empty_like(q), torch.empty((2, T, HQ), device="cuda")
+    v.verify_layer(0, q, dk, dv, out, lse=lse)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(RuntimeError):
+            v.weigh_layer(0, q, lse)
+        v.verify_layer(0, q, dk, dv, out, lse=lse)
+    v.weigh_layer(0, q, lse)
+    once = v.weights[0].clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        v.verify_layer(0, q, dk, dv, out, lse=lse)
+        v.weigh_layer(0, q, lse)
+    graph.replay()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(v.weights[0], (once + once) + once)
+
+
+@pytest.mark.gpu
 def test_what_the_engine_refuses():
     v, _ = _verifier(1, 3, True, 2)
     with pytest.raises(TypeError):
