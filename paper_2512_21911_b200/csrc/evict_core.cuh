@@ -12,21 +12,21 @@ namespace cg = cooperative_groups;
 
 constexpr int kRowGroups = 16;
 constexpr int kThreads = 512, kCluster = 8;
-constexpr int kBins = 2048;
+constexpr int kPasses = 4, kBins = 256;          // of a key's digits
 constexpr int kSlice = 49152;                    // tokens that a CTA's shared memory holds the keys of
 constexpr int kMostTokens = kCluster * kSlice;
 constexpr int kRound = 256;                      // tokens that a CTA moves at a time
 
 struct Shared {
     union {
-        alignas(16) uint32_t hist[3][kBins];   // of the three passes
-        float part[kThreads / 16][128];        // (the moves) sums of keys
+        uint32_t hist[kPasses][kBins];
+        alignas(16) float part[4][kRowGroups][128];   // (the moves) of four blocks sums of keys
     };
     uint32_t sums[kThreads / 32];
     uint32_t digit, above;      // what a pass found
     alignas(8) uint32_t kept[2];   // of the slice: keys above the n-th largest, keys equal to it
     uint32_t first[kCluster + 1];   // where the slices' kept tokens begin
-    int32_t source[kRound];     // of a round's tokens
+    int32_t source[2][kRound];     // of a round's tokens and the next one's
 };
 
 // The sum over the threads below this one, and over all.
@@ -64,38 +64,32 @@ __device__ __forceinline__ void keep_heaviest(const cg::cluster_group &cluster, 
         const uint32_t key = svsel::key_of_bits(__float_as_uint(weights[t]));
         keys[i] = t < n_sink || t >= L - n_recent ? svsel::kForcedKey : key;
     }
-    for (int i = tid; i < 3 * kBins; i += kThreads) sh.hist[0][i] = 0;
+    for (int i = tid; i < kPasses * kBins; i += kThreads) sh.hist[0][i] = 0;
     __syncthreads();
-    // the n-th largest key, by digits from the top; all CTAs find the same
+    // The n-th largest key, by digits from the top; all CTAs find the same.  (Three passes over 11, 11 and 10 bits have eight times the bins to
+    // fetch from the peers, 2.3 us a pass.)
     uint32_t prefix = 0, wanted = n;
 #pragma unroll 1
-    for (int pass = 0; pass < 3; ++pass) {
-        const int low = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11, bins = 1 << bits;
+    for (int pass = 0; pass < kPasses; ++pass) {
+        const int low = 24 - 8 * pass;
         for (int i = tid; i < count; i += kThreads) {
             const uint32_t key = keys[i];
-            if (pass == 0 || key >> (low + bits) == prefix) atomicAdd(&sh.hist[pass][key >> low & (bins - 1)], 1u);
+            if (pass == 0 || key >> (low + 8) == prefix) atomicAdd(&sh.hist[pass][key >> low & (kBins - 1)], 1u);
         }
         cluster.sync();
-        // Four bins of a thread, from the top.  (All peers' bins are asked for at once: one peer behind the other is a trip of half a
-        // microsecond each, three times eight of them, and was most of the time of a short cache.)
-        uint32_t mine[4] = {0, 0, 0, 0};
-        const int top = bins - 4 * tid;   // behind the highest of them
-        if (top >= 4) {
-            uint4 x[kCluster];
+        // A thread a bin, from the top.  (All peers' are asked for at once: one peer behind the other is a trip of half a microsecond each.)
+        uint32_t sum = 0;
+        if (tid < kBins) {
+            uint32_t x[kCluster];
 #pragma unroll
-            for (int r = 0; r < kCluster; ++r) x[r] = *reinterpret_cast<const uint4 *>(cluster.map_shared_rank(sh.hist[pass], r) + top - 4);
+            for (int r = 0; r < kCluster; ++r) x[r] = cluster.map_shared_rank(sh.hist[pass], r)[kBins - 1 - tid];
 #pragma unroll
-            for (int r = 0; r < kCluster; ++r) mine[0] += x[r].w, mine[1] += x[r].z, mine[2] += x[r].y, mine[3] += x[r].x;
+            for (int r = 0; r < kCluster; ++r) sum += x[r];
         }
-        const uint32_t sum = mine[0] + mine[1] + mine[2] + mine[3];
         uint32_t all, above = sum_below(sum, sh.sums, all);
-        if (above < wanted && wanted <= above + sum) {
-            int j = 0;
-            while (above + mine[j] < wanted) above += mine[j++];
-            sh.digit = top - 1 - j, sh.above = above;
-        }
+        if (above < wanted && wanted <= above + sum) sh.digit = kBins - 1 - tid, sh.above = above;
         __syncthreads();
-        prefix = prefix << bits | sh.digit;
+        prefix = prefix << 8 | sh.digit;
         wanted -= sh.above;
         __syncthreads();
     }
@@ -109,8 +103,9 @@ __device__ __forceinline__ void keep_heaviest(const cg::cluster_group &cluster, 
     for (int j = 0; j < kWords; ++j) {
         more[j] = equal[j] = 0;
         if (i0 + j * 1024 < i1) {
+            const int words = min((i1 - i0 - j * 1024 + 31) / 32, 32);
 #pragma unroll 4
-            for (int u = 0; u < 32; ++u) {
+            for (int u = 0; u < words; ++u) {
                 const int i = i0 + (j * 32 + u) * 32 + lane;
                 const uint32_t key = i < i1 ? keys[i] : 0u;
                 const uint32_t m = __ballot_sync(0xffffffffu, i < i1 && key > prefix), e = __ballot_sync(0xffffffffu, i < i1 && key == prefix);
@@ -184,8 +179,9 @@ __device__ __forceinline__ void keep_heaviest(const cg::cluster_group &cluster, 
         uint32_t all;
         const uint32_t ahead = at + warp_below(__popc(more[j]), all);
         at += all;
+        const int words = min((i1 - i0 - j * 1024 + 31) / 32, 32);
 #pragma unroll 4
-        for (int u = 0; u < 32; ++u) {
+        for (int u = 0; u < words; ++u) {
             const uint32_t word = __shfl_sync(0xffffffffu, more[j], u), first = __shfl_sync(0xffffffffu, ahead, u);
             if (word >> lane & 1) keys[first + __popc(word & ((1u << lane) - 1))] = t0 + i0 + (j * 32 + u) * 32 + lane;
         }

@@ -14,6 +14,7 @@
 #include <cuda_bf16.h>
 
 #include <type_traits>
+#include <utility>
 
 #include "attn_common.cuh"
 #include "evict_core.cuh"
@@ -65,13 +66,21 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const __grid_constan
         const int page = __ldg(pages + t / B);
         return (unsigned)page < (unsigned)p.n_pages ? ((long long)page * p.Hkv + h) * B + t % B : -1ll;
     };
+    // A thread arrives at the cluster's barrier when its rows are there, finds the next round's sources and sums up the keys meanwhile, and
+    // writes behind it; the next round's reads follow at once.  (One behind the other: 49.8 us instead of 47.2 for 8 K
+    // of 32 K tokens.)
+    const auto find_sources = [&](int t0, int turn) {
+        const int first = t0 + rank * kRound;
+        if (tid < min(n - first, kRound)) sh.source[turn][tid] = source_of(cluster, keys, sh, first + tid);
+    };
+    find_sources(0, 0);
+    __syncthreads();
+    int turn = 0;
 #pragma unroll 1
-    for (int t0 = 0; t0 < n; t0 += kCluster * kRound) {
+    for (int t0 = 0; t0 < n; t0 += kCluster * kRound, turn ^= 1) {
         const int first = t0 + rank * kRound, rows = min(max(n - first, 0), kRound);
-        __syncthreads();   // (the last round's sources and sums have been read)
-        if (tid < rows) sh.source[tid] = source_of(cluster, keys, sh, first + tid);
-        __syncthreads();
-        const bool still = rows == 0 || sh.source[rows - 1] == first + rows - 1;   // nothing moves
+        const int32_t *source = sh.source[turn];
+        const bool still = rows == 0 || source[rows - 1] == first + rows - 1;   // nothing moves
         uint4 k[kRows], v[kRows];
         float weight = 0.f;
 #pragma unroll
@@ -79,7 +88,7 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const __grid_constan
             const int r = place(i);
             k[i] = v[i] = make_uint4(0u, 0u, 0u, 0u);
             if (r < rows && (!still || p.reps)) {
-                const long long from = slot_of(sh.source[r]);
+                const long long from = slot_of(source[r]);
                 lost |= from < 0;
                 if (from >= 0) {
                     k[i] = p.k_pool[from * 16 + c];
@@ -87,8 +96,35 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const __grid_constan
                 }
             }
         }
-        if (tid < rows) weight = p.weights[base + sh.source[tid]];
-        cluster.sync();
+        if (tid < rows) weight = p.weights[base + source[tid]];
+        auto arrived = cluster.barrier_arrive();
+        find_sources(t0 + kCluster * kRound, turn ^ 1);
+        if (p.reps) {
+#pragma unroll
+            for (int half = 0; half < kTurns; ++half) {
+                float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = half * kPer; i < (half + 1) * kPer; ++i) {
+                    const uint32_t x[4] = {k[i].x, k[i].y, k[i].z, k[i].w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&x[e]));
+                        acc[2 * e] += f.x, acc[2 * e + 1] += f.y;
+                    }
+                }
+                float4 *part = reinterpret_cast<float4 *>(&sh.part[w + 2 * half][g][c * 8]);
+                part[0] = make_float4(acc[0], acc[1], acc[2], acc[3]), part[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+            }
+            __syncthreads();
+            const int block = tid >> 7, dim = tid & 127, held = min(rows - block * B, B);
+            if (block < kRound / B && held > 0) {
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < kRowGroups; ++i) sum += sh.part[block][i][dim];
+                p.reps[(((size_t)s * p.Hkv + h) * p.NBmax + first / B + block) * 128 + dim] = sum / (float)held;
+            }
+        }
+        cluster.barrier_wait(std::move(arrived));
         if (tid < rows) p.weights_out[base + first + tid] = weight;
         if (!still) {
 #pragma unroll
@@ -99,31 +135,6 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const __grid_constan
                     lost |= to < 0;
                     if (to >= 0) p.k_pool[to * 16 + c] = k[i], p.v_pool[to * 16 + c] = v[i];
                 }
-            }
-        }
-        if (!p.reps) continue;
-#pragma unroll
-        for (int turn = 0; turn < kTurns; ++turn) {
-            float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int i = turn * kPer; i < (turn + 1) * kPer; ++i) {
-                const uint32_t x[4] = {k[i].x, k[i].y, k[i].z, k[i].w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&x[e]));
-                    acc[2 * e] += f.x, acc[2 * e + 1] += f.y;
-                }
-            }
-            __syncthreads();
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sh.part[tid >> 4][c * 8 + e] = acc[e];
-            __syncthreads();
-            const int block = w + 2 * turn, held = min(rows - block * B, B);
-            if ((tid & 255) < 128 && held > 0) {
-                float sum = 0.f;
-#pragma unroll
-                for (int i = 0; i < kRowGroups; ++i) sum += sh.part[w * kRowGroups + i][tid & 127];
-                p.reps[(((size_t)s * p.Hkv + h) * p.NBmax + first / B + block) * 128 + (tid & 127)] = sum / (float)held;
             }
         }
     }
