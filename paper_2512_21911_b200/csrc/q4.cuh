@@ -104,5 +104,28 @@ __device__ __forceinline__ uint32_t code_of(float x, float d, float m)
     const float c = rintf(sub_rn(mul_rn(div_rn(sub_rn(x, m), d), 16.f), 16.f));
     return (uint32_t)fminf(fmaxf(c, 0.f), 15.f);
 }
+// The codes of eight values, value e in nibble e / 2 of the lower (even) or upper half of a word.  One division for the eight: a product with
+// 16 / D is off by less than 2^-17, so that what it rounds to is the code wherever it is further than that from the middle between two;
+// the others, and scales near the ends of the exponents, take the divisions.  (A number of 2^23 and half as many more has no fraction: adding it rounds.)
+__device__ __forceinline__ uint32_t codes_of(const float (&v)[8], float d, float m)
+{
+    const float kRound = 12582912.f;
+    uint32_t word = 0;
+    float worst = 0.f;
+    const bool plain = d >= 0x1p-100f && d <= 0x1p100f;
+    const float by = plain ? div_rn(16.f, d) : 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float t = sub_rn(v[e], m), up = fmaf(t, by, kRound - 16.f);
+        worst = fmaxf(worst, fabsf(fmaf(t, by, -16.f) - (up - kRound)));
+        word |= (__float_as_uint(fminf(fmaxf(up, kRound), kRound + 15.f)) & 15u) << (4 * (e & 1 ? 4 + e / 2 : e / 2));
+    }
+    if (!plain || worst > 0.4999f) {
+        word = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) word |= code_of(v[e], d, m) << (4 * (e & 1 ? 4 + e / 2 : e / 2));
+    }
+    return word;
+}
 
 }  // namespace svq

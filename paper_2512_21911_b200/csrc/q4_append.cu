@@ -67,10 +67,7 @@ __device__ __forceinline__ uint32_t code_row(uint4 x, uint32_t &scale)
     if (odd) s.d = s.m = __ushort_as_bfloat16(0x7fff);
     scale = (uint32_t)__bfloat16_as_ushort(s.d) | (uint32_t)__bfloat16_as_ushort(s.m) << 16;
     const float d = __bfloat162float(s.d), m = __bfloat162float(s.m);
-    uint32_t word = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) word |= svq::code_of(v[e], d, m) << (4 * (e & 1 ? 4 + e / 2 : e / 2));
-    return word;
+    return svq::codes_of(v, d, m);
 }
 
 // Tokens [before, end) of block b of a KV head, from rows k_row(t), v_row(t) of this thread's chunk; the block's mean.
@@ -78,91 +75,88 @@ template <int B, bool kNeighbours, class Row>
 __device__ __forceinline__ void append_block(const Params &p, int s, int h, int b, int before, int end, int page, Row row)
 {
     __shared__ float part[kRowGroups][128];
-    __shared__ uint32_t codes[B][17];   // of the values (a row and a word: no two threads of a warp in one bank)
-    const int tid = threadIdx.x, c = tid & 15, rg = tid >> 4, group = c >> 3;
-    constexpr int kIter = B / kRowGroups, kSlabs = B / 64;
-    uint8_t *const slabs = p.pool + ((size_t)page * p.Hkv + h) * kSlabs * kSlabBytes;
-    const auto key_word = [&](int r) { return reinterpret_cast<uint32_t *>(slabs + (r >> 6) * kSlabBytes + (c >> 2) * 1024 + (r & 63) * 16 + (c & 3) * 4); };
-    const auto key_scale = [&](int r) { return reinterpret_cast<uint32_t *>(slabs + (r >> 6) * kSlabBytes + svq::kOffKScale + (r & 63) * 8 + group * 4); };
+    __shared__ uint32_t codes[64][17];   // of a slab's values (a row and a word: no two threads of a warp in one bank)
+    const int tid = threadIdx.x, c = tid & 15, rg = tid >> 4, group = c >> 3, dim = tid & 127;
+    constexpr int kIter = 64 / kRowGroups, kSlabs = B / 64;
     const int r0 = max(before - b * B, 0), r1 = end - b * B;   // rows of the block that are new
-    // the values' words that keep some of their nibbles
-    const int dim = tid & 127;
-    constexpr int kChunks = B / 64;                          // of 32 tokens, of this thread's dim
-    uint4 held[kChunks];
-    const auto value_words = [&](int i) {
-        const int chunk = (tid >> 7) * kChunks + i;
-        return reinterpret_cast<uint4 *>(slabs + (chunk >> 1) * kSlabBytes + svq::kOffV + (chunk & 1) * 2048 + dim * 16);
-    };
-    uint4 k[kIter], v[kIter];
-    uint32_t old_word[kIter], old_scale[kIter];
-#pragma unroll
-    for (int i = 0; i < kIter; ++i) {
-        const int r = rg + i * kRowGroups;
-        k[i] = v[i] = make_uint4(0u, 0u, 0u, 0u);
-        old_word[i] = old_scale[i] = 0u;
-        if (r < r0) {
-            if (p.reps) old_word[i] = *key_word(r), old_scale[i] = *key_scale(r);
-        } else if (r < r1) {
-            row(b * B + r, k[i], v[i]);
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < kChunks; ++i) {
-        const int t0 = ((tid >> 7) * kChunks + i) * 32;
-        held[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (t0 < r1 && t0 + 32 > r0 && (t0 < r0 || t0 + 32 > r1)) held[i] = *value_words(i);
-    }
     float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    // (slab by slab: the rows of 128 tokens in registers leave an SM one CTA, and a prompt of 16 K tokens in blocks of 128 takes 306 us
+    // instead of 161, 64 single tokens 44 instead of 32)
+#pragma unroll 1
+    for (int j = 0; j < kSlabs; ++j) {
+        const int first = j * 64;
+        if (first >= r1) break;
+        if (first + 64 <= r0 && !p.reps) continue;
+        uint8_t *const slab = p.pool + (((size_t)page * p.Hkv + h) * kSlabs + j) * kSlabBytes;
+        const auto key_word = [&](int r) { return reinterpret_cast<uint32_t *>(slab + (c >> 2) * 1024 + (r - first) * 16 + (c & 3) * 4); };
+        const auto key_scale = [&](int r) { return reinterpret_cast<uint32_t *>(slab + svq::kOffKScale + (r - first) * 8 + group * 4); };
+        // the values' words of this thread's dim and 32 tokens, some of whose nibbles may stay
+        uint4 *const value_words = reinterpret_cast<uint4 *>(slab + svq::kOffV + (tid >> 7) * 2048 + dim * 16);
+        const int t0 = first + (tid >> 7) * 32;
+        const bool touched = t0 < r1 && t0 + 32 > r0;
+        uint4 held = make_uint4(0u, 0u, 0u, 0u), k[kIter], v[kIter];
+        uint32_t old_word[kIter], old_scale[kIter];
 #pragma unroll
-    for (int i = 0; i < kIter; ++i) {
-        const int r = rg + i * kRowGroups;
-        const bool fresh = r >= r0 && r < r1;
-        if (__any_sync(0xffffffffu, fresh)) {
-            if (p.rope) {
-                const int t = b * B + r, at = min(max(t, 0), p.rope_rows - 1);
-                Turn turn;
-                if (8 * c < p.rot) turn = load_turn<kNeighbours>(p.rope + (size_t)at * p.rot, c, p.rot);
-                k[i] = rotate<kNeighbours>(k[i], turn, c, p.rot);
-                if (fresh && t >= p.rope_rows && p.status) atomicOr(p.status, svk::kStatusIndex);
+        for (int i = 0; i < kIter; ++i) {
+            const int r = first + rg + i * kRowGroups;
+            k[i] = v[i] = make_uint4(0u, 0u, 0u, 0u);
+            old_word[i] = old_scale[i] = 0u;
+            if (r < r0) {
+                if (p.reps) old_word[i] = *key_word(r), old_scale[i] = *key_scale(r);
+            } else if (r < r1) {
+                row(b * B + r, k[i], v[i]);
             }
-            uint32_t ks, vs;
-            const uint32_t kw = code_row(k[i], ks), vw = code_row(v[i], vs);
-            if (fresh) {
-                old_word[i] = kw, old_scale[i] = ks;
-                *key_word(r) = kw;
-                codes[r][c] = vw;
-                if ((c & 7) == 0) {
-                    *key_scale(r) = ks;
-                    unsigned short *const to = reinterpret_cast<unsigned short *>(slabs + (r >> 6) * kSlabBytes + svq::kOffVScale) + group * 128 + (r & 63);
-                    to[0] = (unsigned short)vs, to[64] = (unsigned short)(vs >> 16);
+        }
+        if (touched && (t0 < r0 || t0 + 32 > r1)) held = *value_words;
+#pragma unroll
+        for (int i = 0; i < kIter; ++i) {
+            const int r = first + rg + i * kRowGroups;
+            const bool fresh = r >= r0 && r < r1;
+            if (__any_sync(0xffffffffu, fresh)) {
+                if (p.rope) {
+                    const int t = b * B + r, at = min(max(t, 0), p.rope_rows - 1);
+                    Turn turn;
+                    if (8 * c < p.rot) turn = load_turn<kNeighbours>(p.rope + (size_t)at * p.rot, c, p.rot);
+                    k[i] = rotate<kNeighbours>(k[i], turn, c, p.rot);
+                    if (fresh && t >= p.rope_rows && p.status) atomicOr(p.status, svk::kStatusIndex);
+                }
+                uint32_t ks, vs;
+                const uint32_t kw = code_row(k[i], ks), vw = code_row(v[i], vs);
+                if (fresh) {
+                    old_word[i] = kw, old_scale[i] = ks;
+                    *key_word(r) = kw;
+                    codes[r - first][c] = vw;
+                    if ((c & 7) == 0) {
+                        *key_scale(r) = ks;
+                        unsigned short *const to = reinterpret_cast<unsigned short *>(slab + svq::kOffVScale) + group * 128 + (r - first);
+                        to[0] = (unsigned short)vs, to[64] = (unsigned short)(vs >> 16);
+                    }
+                }
+            }
+            if (r < r1) {
+                uint32_t x[4];
+                svq::decode(old_word[i], svq::both_low(old_scale[i]), svq::both_high(old_scale[i]), x);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float2 f = halves_of(x[e]);
+                    acc[2 * e] += f.x, acc[2 * e + 1] += f.y;
                 }
             }
         }
-        if (r < r1) {
-            uint32_t x[4];
-            svq::decode(old_word[i], svq::both_low(old_scale[i]), svq::both_high(old_scale[i]), x);
+        __syncthreads();
+        if (touched) {
+            uint32_t w[4] = {held.x, held.y, held.z, held.w};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float2 f = halves_of(x[e]);
-                acc[2 * e] += f.x, acc[2 * e + 1] += f.y;
+            for (int e = 0; e < 32; ++e) {
+                const int r = t0 + e;
+                if (r < r0 || r >= r1) continue;
+                const uint32_t nibble = codes[r - first][dim >> 3] >> shift_of(dim & 7) & 15u;
+                const int at = 4 * (e & 1 ? 4 + (e & 7) / 2 : (e & 7) / 2);
+                w[e >> 3] = (w[e >> 3] & ~(15u << at)) | nibble << at;
             }
+            *value_words = make_uint4(w[0], w[1], w[2], w[3]);
         }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kChunks; ++i) {
-        const int t0 = ((tid >> 7) * kChunks + i) * 32;
-        if (t0 >= r1 || t0 + 32 <= r0) continue;
-        uint32_t w[4] = {held[i].x, held[i].y, held[i].z, held[i].w};
-#pragma unroll
-        for (int e = 0; e < 32; ++e) {
-            const int r = t0 + e;
-            if (r < r0 || r >= r1) continue;
-            const uint32_t nibble = codes[r][dim >> 3] >> shift_of(dim & 7) & 15u;
-            const int at = 4 * (e & 1 ? 4 + (e & 7) / 2 : (e & 7) / 2);
-            w[e >> 3] = (w[e >> 3] & ~(15u << at)) | nibble << at;
-        }
-        *value_words(i) = make_uint4(w[0], w[1], w[2], w[3]);
+        if (j + 1 < kSlabs) __syncthreads();   // (the codes have been read)
     }
     if (!p.reps) return;
 #pragma unroll
@@ -176,8 +170,9 @@ __device__ __forceinline__ void append_block(const Params &p, int s, int h, int 
     }
 }
 
+// Three CTAs an SM: with two a prompt of 16 K tokens takes 175 us instead of 159 (alone, its reading back included).
 template <int B, bool kNeighbours, int kQTokens>
-__global__ void __launch_bounds__(kThreads) q4_rope_append_kernel(const __grid_constant__ Params p)
+__global__ void __launch_bounds__(kThreads, 3) q4_rope_append_kernel(const __grid_constant__ Params p)
 {
     svk::grid_dependency_wait();
     svk::grid_launch_dependents();
@@ -217,12 +212,57 @@ __global__ void __launch_bounds__(kThreads) q4_commit_kernel(const __grid_consta
     });
 }
 
+// A slab in shared memory, in 16-byte pieces, with gaps: a row's 16 threads read words that are 128 bytes apart (values) or 1024 (keys), and find
+// them in different banks.  A word of values is read for four of its tokens.  (With neither: 40 blocks of four sequences
+// in 28 us instead of 11, a cache of 30 K tokens and 8 heads in 74 instead of 33.)
+constexpr int kValues = 264, kScales = kValues + 288, kPieces = kScales + 64;
+__device__ __forceinline__ void fetch_slab(const uint4 *from, uint4 *slab)
+{
+    static_assert(kThreads == 256 && svq::kOffV == 256 * 16 && svq::kOffKScale == 512 * 16, "");
+    const int tid = threadIdx.x;
+    slab[tid + (tid >> 6) * 2] = __ldg(from + tid);                // keys: two pieces behind each chunk
+    slab[kValues + tid + (tid >> 3)] = __ldg(from + 256 + tid);    // values: one behind each eight dims
+    if (tid < 64) slab[kScales + tid] = __ldg(from + 512 + tid);
+}
+// Rows of eight dims, by key(token, eight dims, values) and value(...).  All threads of the CTA.
+template <class Key, class Value>
+__device__ __forceinline__ void decode_slab(const uint4 *slab, Key key, Value value)
+{
+    const int tid = threadIdx.x, c = tid & 15;
+    const uint32_t *const words = reinterpret_cast<const uint32_t *>(slab);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = (tid >> 4) + 16 * i;
+        const uint32_t sc = words[kScales * 4 + r * 2 + (c >> 3)];
+        uint32_t x[4];
+        svq::decode(words[(c >> 2) * 264 + r * 4 + (c & 3)], svq::both_low(sc), svq::both_high(sc), x);
+        key(r, c, make_uint4(x[0], x[1], x[2], x[3]));
+    }
+    // four tokens of eight words: codes 2 j, 2 j + 1 of eight in nibble j of the halves of a word
+    const int part = tid >> 4 & 1, o = tid >> 5, r = 8 * o + 4 * part;
+    const uint2 *const scales = reinterpret_cast<const uint2 *>(slab + kScales + 32) + (c >> 3) * 32 + r / 4;
+    const uint2 d = scales[0], m = scales[16];
+    const uint32_t *const w = words + (kValues + (o >> 2) * 144 + c * 9) * 4 + (o & 3);
+    uint32_t x[4][4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t a = w[8 * e] >> (8 * part), b = w[8 * e + 4] >> (8 * part);
+        const uint32_t even = __byte_perm(a, b, 0x5410), odd = __byte_perm(a, b, 0x7632);
+        x[0][e] = svq::fma_bf16x2(svq::steps<0>(even), svq::both_low(d.x), svq::both_low(m.x));
+        x[1][e] = svq::fma_bf16x2(svq::steps<0>(odd), svq::both_high(d.x), svq::both_high(m.x));
+        x[2][e] = svq::fma_bf16x2(svq::steps<1>(even), svq::both_low(d.y), svq::both_low(m.y));
+        x[3][e] = svq::fma_bf16x2(svq::steps<1>(odd), svq::both_high(d.y), svq::both_high(m.y));
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) value(r + t, c, make_uint4(x[t][0], x[t][1], x[t][2], x[t][3]));
+}
+
 // Tokens back: row i of sequence s is the token at first[s] + i.  A CTA has a slab of them and a KV head.
 __global__ void __launch_bounds__(kThreads) q4_read_kernel(const uint8_t *pool, const int32_t *block_table, const int32_t *seq_lens,
-                                                           const int32_t *first, const int32_t *q_start, uint32_t *k_out, uint32_t *v_out, int S,
+                                                           const int32_t *first, const int32_t *q_start, uint4 *k_out, uint4 *v_out, int S,
                                                            int N, int Hkv, int NBmax, int B, int n_pages, int32_t *status)
 {
-    __shared__ __align__(16) uint8_t slab[kSlabBytes];
+    __shared__ uint4 slab[kPieces];
     svk::grid_dependency_wait();
     svk::grid_launch_dependents();
     const int tid = threadIdx.x, h = blockIdx.y, slot = blockIdx.x;
@@ -243,38 +283,15 @@ __global__ void __launch_bounds__(kThreads) q4_read_kernel(const uint8_t *pool, 
         int page = __ldg(block_table + (size_t)s * NBmax + b);
         bad = bad || (unsigned)page >= (unsigned)n_pages;
         page = min(max(page, 0), n_pages - 1);
-        const uint4 *from = reinterpret_cast<const uint4 *>(pool + (((size_t)page * Hkv + h) * (B / 64) + (j * 64 % B) / 64) * kSlabBytes);
-        for (int i = tid; i < kSlabBytes / 16; i += kThreads) reinterpret_cast<uint4 *>(slab)[i] = __ldg(from + i);
+        fetch_slab(reinterpret_cast<const uint4 *>(pool + (((size_t)page * Hkv + h) * (B / 64) + (j * 64 % B) / 64) * kSlabBytes), slab);
     }
     if (bad && tid == 0 && status) atomicOr(status, svk::kStatusIndex);
     __syncthreads();
-    const auto seen = [&](long long t) { return there && t >= 0 && t < len; };   // (others are zeros)
-    const uint32_t *const words = reinterpret_cast<const uint32_t *>(slab);
-    for (int i = tid; i < 64 * 16; i += kThreads) {   // keys: a token, eight dims
-        const int r = i >> 4, c = i & 15;
+    const auto put = [&](uint4 *out, int r, int c, uint4 x) {   // (of positions that the sequence does not hold: zeros)
         const long long t = j * 64 + r;
-        if (t < t0 || t >= t1) continue;
-        uint32_t x[4] = {0, 0, 0, 0};
-        if (seen(t)) {
-            const uint32_t sc = words[svq::kOffKScale / 4 + r * 2 + (c >> 3)];
-            svq::decode(words[(c >> 2) * 256 + r * 4 + (c & 3)], svq::both_low(sc), svq::both_high(sc), x);
-        }
-        reinterpret_cast<uint4 *>(k_out)[((size_t)(row0 + (t - at)) * Hkv + h) * 16 + c] = make_uint4(x[0], x[1], x[2], x[3]);
-    }
-    const unsigned short *const scales = reinterpret_cast<const unsigned short *>(slab + svq::kOffVScale);
-    for (int i = tid; i < 64 * 8; i += kThreads) {   // values: two dims, eight tokens
-        const int d = (i & 63) * 2, o = i >> 6;
-        const uint32_t w0 = words[svq::kOffV / 4 + (o >> 2) * 512 + d * 4 + (o & 3)], w1 = words[svq::kOffV / 4 + (o >> 2) * 512 + d * 4 + 4 + (o & 3)];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const long long t = j * 64 + 8 * o + e;
-            if (t < t0 || t >= t1) continue;
-            const int at_bit = 4 * (e & 1 ? 4 + e / 2 : e / 2);
-            const uint32_t pair = ((w0 >> at_bit & 15u) << 3 | (w1 >> at_bit & 15u) << 19) | 0x3f803f80u;
-            const uint32_t m = scales[(d >> 6) * 128 + 64 + 8 * o + e], dd = scales[(d >> 6) * 128 + 8 * o + e];
-            v_out[((size_t)(row0 + (t - at)) * Hkv + h) * 64 + d / 2] = seen(t) ? svq::fma_bf16x2(pair, dd | dd << 16, m | m << 16) : 0u;
-        }
-    }
+        if (t >= t0 && t < t1) out[((size_t)(row0 + (t - at)) * Hkv + h) * 16 + c] = there && t >= 0 && t < len ? x : make_uint4(0u, 0u, 0u, 0u);
+    };
+    decode_slab(slab, [&](int r, int c, uint4 x) { put(k_out, r, c, x); }, [&](int r, int c, uint4 x) { put(v_out, r, c, x); });
 }
 
 // The cache of a batch, or its listed blocks, as bfloat16 pages, block b of sequence s on page s * NBmax + b, and the table that says so: where there are many
@@ -284,7 +301,7 @@ __global__ void __launch_bounds__(kThreads) q4_spread_kernel(const uint8_t *pool
                                                              int max_sel, uint4 *k_out, uint4 *v_out, int32_t *table_out, int Hkv, int NBmax, int B, int n_pages,
                                                              int32_t *status)
 {
-    __shared__ __align__(16) uint8_t slab[kSlabBytes];
+    __shared__ uint4 slab[kPieces];
     svk::grid_dependency_wait();
     svk::grid_launch_dependents();
     const int tid = threadIdx.x, per = B / 64, h = blockIdx.y, s = blockIdx.z, sub = blockIdx.x % per;
@@ -305,30 +322,10 @@ __global__ void __launch_bounds__(kThreads) q4_spread_kernel(const uint8_t *pool
         page = min(max(page, 0), n_pages - 1);
     }
     const uint4 *from = reinterpret_cast<const uint4 *>(pool + (((size_t)page * Hkv + h) * per + sub) * kSlabBytes);
-    for (int i = tid; i < kSlabBytes / 16; i += kThreads) reinterpret_cast<uint4 *>(slab)[i] = __ldg(from + i);
+    fetch_slab(from, slab);
     __syncthreads();
-    const uint32_t *const words = reinterpret_cast<const uint32_t *>(slab);
     const size_t row0 = (entry * Hkv + h) * B + sub * 64;
-    for (int i = tid; i < 64 * 16; i += kThreads) {   // keys: a token, eight dims
-        const int r = i >> 4, c = i & 15;
-        const uint32_t sc = words[svq::kOffKScale / 4 + r * 2 + (c >> 3)];
-        uint32_t x[4];
-        svq::decode(words[(c >> 2) * 256 + r * 4 + (c & 3)], svq::both_low(sc), svq::both_high(sc), x);
-        k_out[(row0 + r) * 16 + c] = make_uint4(x[0], x[1], x[2], x[3]);
-    }
-    const unsigned short *const scales = reinterpret_cast<const unsigned short *>(slab + svq::kOffVScale);
-    for (int i = tid; i < 64 * 16; i += kThreads) {   // values: a token, eight dims (a nibble of each of eight words)
-        const int r = i >> 4, c = i & 15, at = shift_of(r & 7);
-        const uint32_t d = scales[(c >> 3) * 128 + r], m = scales[(c >> 3) * 128 + 64 + r];
-        const uint32_t *w = words + svq::kOffV / 4 + (r >> 5) * 512 + (r >> 3 & 3) + c * 32;
-        uint32_t x[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint32_t pair = ((w[8 * e] >> at & 15u) << 3 | (w[8 * e + 4] >> at & 15u) << 19) | 0x3f803f80u;
-            x[e] = svq::fma_bf16x2(pair, d | d << 16, m | m << 16);
-        }
-        v_out[(row0 + r) * 16 + c] = make_uint4(x[0], x[1], x[2], x[3]);
-    }
+    decode_slab(slab, [&](int r, int c, uint4 x) { k_out[(row0 + r) * 16 + c] = x; }, [&](int r, int c, uint4 x) { v_out[(row0 + r) * 16 + c] = x; });
 }
 
 cudaLaunchConfig_t config(dim3 grid, void *stream, cudaLaunchAttribute *attr)
@@ -437,7 +434,7 @@ extern "C" sv_status sv_kv_read_q4(const sv_geom *geom, const sv_kv_q4 *kv, cons
     cudaLaunchAttribute attr[1];
     const cudaLaunchConfig_t cfg = config(dim3((unsigned)(n_tokens / 64 + 2 * geom->n_seq), geom->n_kv_heads), stream, attr);
     const cudaError_t e = cudaLaunchKernelEx(&cfg, q4_read_kernel, static_cast<const uint8_t *>(kv->pool), kv->block_table, kv->seq_lens, first, q_start,
-                                             static_cast<uint32_t *>(k_out), static_cast<uint32_t *>(v_out), (int)geom->n_seq, (int)n_tokens,
+                                             static_cast<uint4 *>(k_out), static_cast<uint4 *>(v_out), (int)geom->n_seq, (int)n_tokens,
                                              (int)geom->n_kv_heads, (int)geom->max_blocks, (int)geom->block_size, (int)kv->n_pages, status_word);
     return e == cudaSuccess ? svh::launch_status() : SV_ERR_CUDA;
 }

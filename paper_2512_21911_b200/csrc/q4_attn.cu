@@ -9,7 +9,7 @@
 // values go nowhere but to the tensor cores.  So the cache is operand A, read from tensor memory, and the roles of rows and keys are
 // exchanged: both products are of 128 (keys, then dims) x N (query rows) with N = 16, 32 or 64,
 //   S^T[128 keys x N] = K . Q^T      a thread decodes a key's 128 dims into its lane of tensor memory
-//   O^T[128 dims x N] += V^T . P^T   a thread decodes a dim's 128 keys into its lane
+//   O^T[128 dims x N] += V^T . P^T   a warp decodes 32 dims' 128 keys, a thread four dims and four keys of every 16
 // and a few query rows cost what they are instead of a tile of 128.  A thread then has a key's scores against all rows: masks are its own
 // affair, sums of weights stay in registers until the end, and the running maximum, which would have to go across lanes, is only
 // looked for when a score outgrows the reference.
@@ -881,9 +881,9 @@ struct Spread {
     }
 };
 // Whether a call of this many query rows a sequence and KV head goes over the decoded cache, and where it is then.  A tile of 64 rows here
-// takes as long as one of 128 there, and every tile decodes all its keys: 1,024 tokens behind 30,001 (32 heads) take 1,490 us here, 540 there
-// with the decoding; 12 sequences, three of them chunks of some 500 tokens, 290 and 157; trees of 60 tokens of four sequences (420 rows,
-// 40 blocks) 98 and 63.
+// takes as long as one of 128 there, and every tile decodes all its keys: 1,024 tokens behind 30,001 (32 heads) take 1,490 us here, 505 there
+// with the decoding; 12 sequences, three of them chunks of some 500 tokens, 290 and 128; trees of 60 tokens of four sequences (420 rows,
+// 40 blocks) 98 and 48.
 struct Decoded {
     bool use = false;
     uint8_t *k, *v, *scratch;
