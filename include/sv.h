@@ -21,6 +21,10 @@
  *   sv_rope_append, sv_chunk_attn, sv_sample   the serving loop around a verification
  *                     step: new tokens rotated and written to the cache, their
  *                     attention over it, and distributions and tokens from logits
+ *   sv_rope_append_q4, sv_kv_append_q4, sv_kv_read_q4, sv_verify_attn_q4,
+ *   sv_chunk_attn_q4   the same over a paged cache held in 4 bits
+ *   sv_attn_weights, sv_kv_evict, sv_rope_append_at   attention weights of the cached
+ *                     tokens, eviction of the lightest, appending after it
  *   sv_anchor_jaccard / sv_pick_anchors   anchor-layer calibration       (Eq. 7-8)
  *   sv_select_blocks_global / _tokens, sv_token_overlap, sv_block_reps_bf16,
  *   sv_select_blocks_bf16reps   retrieval variants the paper discusses but does

@@ -2,7 +2,8 @@
 //
 // Mathematics: w_t += sum over the rows r of a KV head of exp(scale * q_r . k_t - lse_r); the denominators lse are the attention's, which
 // knows them only when it is through, so that the weights take a pass over the keys of their own.  Bound by HBM: 256 bytes of keys and 8 of
-// weights a token.
+// weights a token.  A chain of eight over 32 K tokens (8 KV heads, 69 MB): 17.8 us, 60 % of a copy's rate, the rest being the beginning and the end
+// of the launch; 16 sequences over 48 kept blocks (112 MB): 28.4.
 //
 // S^T[128 keys x N rows] = K . Q^T on the tensor cores, the keys as operand A as TMA brings them (M128 N K16, N = 16, 32 or 64 rows): a thread
 // has a key's scores against all rows in its lane of tensor memory, and its weight is a sum within the thread.  A worker is a warpgroup

@@ -2,7 +2,8 @@
 //
 // Mathematics: the rotation of sv_rope_append; a row's two groups of 64 values as scale, offset and codes; the representatives are the means
 // of what the cache then holds.  Bound by HBM in a prompt (the queries, which are only rotated, are most of it), by a chain of loads in a
-// decoding step.
+// decoding step.  A prompt of 16,384 tokens (32 query heads, 8 KV heads; 450 MB) takes 154 us with its reading back, 45 % of a copy's rate; a token
+// each of 64 sequences 20 us.
 //
 // A CTA has a block of a sequence and a KV head, as in sv_rope_append: 16 threads hold a row, eight of them a group, so that its smallest
 // and largest value are three shuffles away and a thread's eight codes are one word.  The keys' words go to the page as they are; those of
@@ -213,8 +214,8 @@ __global__ void __launch_bounds__(kThreads) q4_commit_kernel(const __grid_consta
 }
 
 // A slab in shared memory, in 16-byte pieces, with gaps: a row's 16 threads read words that are 128 bytes apart (values) or 1024 (keys), and find
-// them in different banks.  A word of values is read for four of its tokens.  (With neither: 40 blocks of four sequences
-// in 28 us instead of 11, a cache of 30 K tokens and 8 heads in 74 instead of 33.)
+// them in different banks.  A word of values is read for four of its tokens.  (With neither a verification over 40
+// blocks of four sequences takes 64 us instead of 48, 1,024 tokens over a cache of 30 K 552 instead of 509.)
 constexpr int kValues = 264, kScales = kValues + 288, kPieces = kScales + 64;
 __device__ __forceinline__ void fetch_slab(const uint4 *from, uint4 *slab)
 {

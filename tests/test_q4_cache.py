@@ -184,6 +184,32 @@ def test_values_that_are_hard_to_code():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("factor", [1.0, 3.0, 0.40625, 2.0 ** -99, 2.0 ** -112, 2.0 ** 104, 1.9921875])
+def test_values_in_the_middle_of_two_codes(factor):
+    """Quarters of a step: every fourth value lies in the middle between two codes, and goes to the even one, as do their neighbours in bfloat16
+    to theirs.  (With a factor of few bits the scale stays exact.)"""
+    import paper_2512_21911_b200 as sv
+    t = _batch(sv, [0], [8], 2, 1, 64, 0, False)
+    quarters = torch.arange(64).double() / 4    # 0 .. 15.75
+    quarters[61:] = 15.0
+    k = torch.zeros((8, 1, 128), dtype=torch.float64)
+    for i in range(8):
+        x = (quarters if i % 2 else quarters - 7.0) * factor
+        k[i, 0] = torch.cat([x, x.roll(5)])
+    t["k"] = k.cuda().bfloat16()
+    bits = t["k"].view(torch.int16).clone()
+    bits[2:4] += (torch.arange(128, device="cuda") % 64 % 3 == 1) * (torch.arange(128, device="cuda") % 64 > 0)     # a step away from the middle
+    bits[4:6] -= (torch.arange(128, device="cuda") % 64 % 4 == 2).short()
+    t["k"] = bits.view(torch.bfloat16)
+    t["v"], t["reps"] = t["k"].flip(2), None
+    pool = t["pool"].cpu().numpy().copy()
+    for i in range(8):
+        put(pool[int(t["table"][0, 0]), 0, 0], i, _host(t["k"])[i, 0], _host(t["v"])[i, 0])
+    _append(sv, t)
+    assert np.array_equal(t["pool"].cpu().numpy(), pool)
+
+
+@pytest.mark.gpu
 def test_tokens_without_room_are_dropped():
     import paper_2512_21911_b200 as sv
     t = _batch(sv, [60, 100, -4], [10, 200, 5], 4, 2, 64, 0, False, spare=0)
