@@ -126,6 +126,7 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const __grid_constan
             }
         }
         cluster.barrier_wait(std::move(arrived));
+        __syncthreads();   // (the next sources are there and the sums are through: both came after the thread had arrived)
         if (tid < rows) p.weights_out[base + first + tid] = weight;
         if (!still) {
 #pragma unroll
