@@ -64,7 +64,7 @@ __device__ __forceinline__ void keep_heaviest(const cg::cluster_group &cluster, 
         const uint32_t key = svsel::key_of_bits(__float_as_uint(weights[t]));
         keys[i] = t < n_sink || t >= L - n_recent ? svsel::kForcedKey : key;
     }
-    for (int i = tid; i < kPasses * kBins; i += kThreads) sh.hist[0][i] = 0;
+    for (int i = tid; i < kPasses * kBins; i += kThreads) sh.hist[i / kBins][i % kBins] = 0;
     __syncthreads();
     // The n-th largest key, by digits from the top; all CTAs find the same.  (Three passes over 11, 11 and 10 bits have eight times the bins to
     // fetch from the peers, 2.3 us a pass.)

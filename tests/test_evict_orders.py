@@ -106,3 +106,14 @@ def test_every_order_of_the_threads_gives_the_same(lib, order, reps, L, n, B):
         held = (rows(k, i).astype(np.uint32) << 16).view(np.float32)
         want = np.stack([held[b * B:(b + 1) * B].sum(0) / np.float32(min(B, n - b * B)) for b in range(-(-n // B))])
         assert np.array_equal(means[:len(want)], want) and (means[len(want):] == 99.0).all()
+
+
+@pytest.mark.parametrize("reps", [False, True])
+@pytest.mark.parametrize("L,n,sink,recent", [(300, 200, 4, 64), (2500, 2300, 0, 0), (9, 1, 0, 0)])
+def test_nothing_is_read_that_nobody_wrote(lib, reps, L, n, sink, recent):
+    """What shared memory holds in the end is what it held in the beginning, or does not depend on it."""
+    t, left = _case(L, n, 64), [np.zeros((8, lib.shared_bytes()), np.uint8) for _ in range(2)]
+    a, b = (_run(lib, t, sink, recent, reps, "drawn", poison, x) for poison, x in zip((0, 0x5a), left))
+    assert all(np.array_equal(x, y) for x, y in zip(a, b))
+    same = left[0] == left[1]
+    assert (same | ((left[0] == 0) & (left[1] == 0x5a))).all()
