@@ -50,7 +50,7 @@ __device__ __forceinline__ uint32_t sum_below(uint32_t x, uint32_t *sums, uint32
     return upto - x;
 }
 
-// Of tokens 0 .. L - 1 with these weights n stay: the first n_sink, the last n_recent, and the heaviest others.  keys: room for the CTA's
+// Of tokens 0 .. L - 1 with these weights n > 0 stay: the first n_sink, the last n_recent, and the heaviest others.  keys: room for the CTA's
 // slice, which becomes the list of its tokens that stay; token d of all of them is source_of(d).  All threads of the cluster; peers are
 // reached behind its first barrier, and the last is up to the caller, who reaches them too.
 __device__ __forceinline__ void keep_heaviest(const cg::cluster_group &cluster, const float *weights, int L, int n, int n_sink, int n_recent,

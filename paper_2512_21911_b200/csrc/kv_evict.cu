@@ -54,7 +54,7 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(const __grid_constan
             for (int t = rank * kThreads + tid; t < L; t += kCluster * kThreads) p.weights_out[base + t] = p.weights[base + t];
         return;
     }
-    keep_heaviest(cluster, p.weights + base, L, n, p.n_sink, p.n_recent, keys, sh);
+    if (n > 0) keep_heaviest(cluster, p.weights + base, L, n, p.n_sink, p.n_recent, keys, sh);
 
     // The moves: 256 tokens of the result a CTA and round, a thread eight rows of them -- of the rows of a block those that sv_block_reps
     // gives it, so that the means are the same to the last bit.
