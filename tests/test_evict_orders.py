@@ -113,7 +113,7 @@ def test_every_order_of_the_threads_gives_the_same(lib, order, reps, L, n, B):
 def test_nothing_is_read_that_nobody_wrote(lib, reps, L, n, sink, recent):
     """What shared memory holds in the end is what it held in the beginning, or does not depend on it."""
     t, left = _case(L, n, 64), [np.zeros((8, lib.shared_bytes()), np.uint8) for _ in range(2)]
-    a, b = (_run(lib, t, sink, recent, reps, "drawn", poison, x) for poison, x in zip((0, 0x5a), left))
+    a, b = (_run(lib, t, sink, recent, reps, "drawn", poison, x) for poison, x in zip((0, 0xff), left))
     assert all(np.array_equal(x, y) for x, y in zip(a, b))
     same = left[0] == left[1]
-    assert (same | ((left[0] == 0) & (left[1] == 0x5a))).all()
+    assert (same | ((left[0] == 0) & (left[1] == 0xff))).all()
