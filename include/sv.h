@@ -643,9 +643,10 @@ SV_API sv_status sv_attn_weights(const sv_geom *geom, const void *q, const sv_kv
 
 /*
  * Eviction by such weights: of a sequence of L tokens, n = min(L, max(budget[s], n_sink + n_recent)) stay in every KV head: the first
- * n_sink, the last n_recent, and of the others the heaviest in that head (equal ones: the earlier first; a NaN ranks between the negative
- * numbers and zero).  They keep their order and close up: token number j of those that stay moves to position j of the sequence's
- * pages, in place.  The pages from ceil(n / block_size) on are free afterwards.  Where L <= n nothing is touched.  A page of a sequence that
+ * n_sink, the last n_recent, and of the others the heaviest in that head (equal ones, the two zeros among them: the earlier first; a NaN by
+ * its bits, above infinity with a clear sign and below minus infinity with a set one, but the one that GPU arithmetic makes, 0x7fffffff,
+ * between the negative numbers and zero).  They keep their order and close up: token number j of those that stay moves to position j of the
+ * sequence's pages, in place.  The pages from ceil(n / block_size) on are free afterwards.  Where L <= n nothing is touched.  A page of a sequence that
  * loses tokens stands in the block table once: no other sequence reads it.
  *   weights         dev fp32 [S][Hkv][NBmax * block_size]; weights_out: the weights of the tokens at their new positions, and zeros for
  *                   n <= t < L; the same buffer, or one that does not overlap it

@@ -61,7 +61,7 @@ __device__ __forceinline__ void keep_heaviest(const cg::cluster_group &cluster, 
     const int per = ((L + kCluster - 1) / kCluster + 3) & ~3, t0 = min(rank * per, L), count = min(t0 + per, L) - t0;
     for (int i = tid; i < count; i += kThreads) {
         const int t = t0 + i;
-        const uint32_t key = svsel::key_of_bits(__float_as_uint(weights[t]));
+        const uint32_t bits = __float_as_uint(weights[t]), key = svsel::key_of_bits(bits == 0x80000000u ? 0u : bits);   // (the zeros are equal)
         keys[i] = t < n_sink || t >= L - n_recent ? svsel::kForcedKey : key;
     }
     for (int i = tid; i < kPasses * kBins; i += kThreads) sh.hist[i / kBins][i % kBins] = 0;

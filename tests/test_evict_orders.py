@@ -117,3 +117,28 @@ def test_nothing_is_read_that_nobody_wrote(lib, reps, L, n, sink, recent):
     assert all(np.array_equal(x, y) for x, y in zip(a, b))
     same = left[0] == left[1]
     assert (same | ((left[0] == 0) & (left[1] == 0xff))).all()
+
+
+def _ranks(w):
+    """The order that sv.h states, as numbers: zeros are equal, a NaN goes by its bits, the one of GPU arithmetic stands below zero."""
+    bits = w.view(np.uint32)
+    rank = np.nan_to_num(w).astype(np.float64)
+    rank = np.where(np.isinf(w), np.where(bits >> 31, -1e200, 1e200), rank)
+    rank = np.where(np.isnan(w), np.where(bits >> 31, -1e300, 1e300) * (1 + (bits & 0x7fffff) / 2.0 ** 23), rank)
+    return np.where(bits == 0x7fffffff, -1e-300, rank)
+
+
+ODD = [0x00000000, 0x80000000, 0x7fc00000, 0xffc00000, 0x7fffffff, 0xffffffff, 0x7f800000, 0xff800000, 0x00000001, 0x80000001, 0x3f800000, 0xbf800000,
+       0x7f800001]
+
+
+@pytest.mark.parametrize("values", [ODD, ODD[:2], ODD[:2] + ODD[4:5], ODD[4:5] + ODD[9:10]])
+@pytest.mark.parametrize("n", [250, 60, 7])
+def test_order_of_odd_weights(lib, values, n):
+    t = _case(300, n, 64)
+    t["w"][:300] = np.random.default_rng(1).choice(np.array(values, np.uint32), 300).view(np.float32)
+    kept = np.sort(np.argsort(-_ranks(t["w"][:300]), kind="stable")[:n])
+    k, v, w, _ = _run(lib, t, 0, 0, False, "drawn")
+    rows = lambda pool, at: pool[t["table"][at // 64], 0, at % 64]
+    assert np.array_equal(w[:n].view(np.uint32), t["w"][kept].view(np.uint32))
+    assert np.array_equal(rows(k, np.arange(n)), rows(t["k"], kept)) and np.array_equal(rows(v, np.arange(n)), rows(t["v"], kept))

@@ -15,3 +15,14 @@ pytestmark = pytest.mark.gpu
 def test_several_rounds(lens, Hkv, B, budget, reps, in_place):
     import paper_2512_21911_b200 as sv
     _check(sv, _inputs(lens, Hkv, B, budget), 4, 64, in_place, reps)
+
+
+def test_zeros_of_both_signs_are_equal(monkeypatch):
+    import numpy as np
+
+    import paper_2512_21911_b200 as sv
+    import test_kv_evict
+    order = test_kv_evict._order
+    monkeypatch.setattr(test_kv_evict, "_order", lambda w: order(np.where(w == 0, np.float32(0), w)))
+    zeros = lambda r, s: np.where(r.random(s) < 0.5, 0.0, np.where(r.random(s) < 0.9, -0.0, -1.0))
+    _check(sv, _inputs([3000, 517], 2, 64, [1000, 100], weights=zeros), 3, 70)
