@@ -133,6 +133,7 @@ class SparseVerifier:
         self.sel_idx, self.sel_cnt = self._lists_idx[-1], self._lists_cnt[-1]
 
     def set_layer_kv(self, layer: int, k_pool: torch.Tensor, v_pool: torch.Tensor) -> None:
+        assert self.kv_q4[layer] is None, "the layer has a 4-bit pool already"
         new = self.kv[layer] is None
         self._pools[layer] = (k_pool, v_pool)
         self.kv[layer] = sv.make_kv(k_pool, v_pool, self.block_table, self.seq_lens)
@@ -159,6 +160,7 @@ class SparseVerifier:
         """All layers' pools in one allocation, bf16 [layers][n_pages][Hkv][B][D]."""
         n_layers = int(k_all.shape[0])
         assert n_layers == self.n_layers and k_all.is_contiguous() and v_all.is_contiguous()
+        assert not any(kv is not None for kv in self.kv_q4), "a layer has a 4-bit pool already"
         for l in range(n_layers):
             self.set_layer_kv(l, k_all[l], v_all[l])
         self._one_allocation = True

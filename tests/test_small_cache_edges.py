@@ -1,0 +1,23 @@
+"""SparseVerifier with 4-bit caches and evictions: what it refuses, and what the calls around them say."""
+import pytest
+import torch
+
+
+def _bare(n_layers, **attributes):
+    """A verifier without a device: what a refusal looks at."""
+    import paper_2512_21911_b200 as sv
+    v = object.__new__(sv.SparseVerifier)
+    v.n_layers, v.kv, v.kv_q4, v._pools, v._grown_kv = n_layers, [None] * n_layers, [None] * n_layers, [None] * n_layers, [None] * n_layers
+    v.__dict__.update(attributes)
+    return v
+
+
+def test_a_layer_with_a_4_bit_pool_takes_no_others():
+    """Either way of giving it bfloat16 pools, before anything of the verifier has changed."""
+    pool, kv = (torch.zeros(1),), object()
+    v = _bare(2, kv_q4=[None, kv], _pools=[None, pool])
+    with pytest.raises(AssertionError, match="4-bit"):
+        v.set_layer_kv(1, torch.zeros(1), torch.zeros(1))
+    with pytest.raises(AssertionError, match="4-bit"):
+        v.set_kv_stack(torch.zeros((2, 1)), torch.zeros((2, 1)))
+    assert v._pools == [None, pool] and v.kv == [None, None] and v.kv_q4 == [None, kv]
