@@ -214,7 +214,9 @@ class SparseVerifier:
 
     def build_reps(self, layer: int, block_begin: int = 0, block_end: int = -1) -> None:
         """(Re)compute block representatives of a layer; a decoding loop only refreshes the tail block.  (Those of a 4-bit cache are made
-        by what writes it.)"""
+        by what writes it, and not here.)"""
+        if self.kv_q4[layer] is not None:
+            raise TypeError("build_reps: the layer has a 4-bit pool, whose representatives are made by what writes it")
         sv.sv_block_reps(self.geom, self.kv[layer], self.reps[layer], block_begin, block_end)
 
     def verify_layer(self, layer: int, q, draft_k, draft_v, out, lse=None, behind_own_layer: bool = False) -> None:

@@ -21,3 +21,9 @@ def test_a_layer_with_a_4_bit_pool_takes_no_others():
     with pytest.raises(AssertionError, match="4-bit"):
         v.set_kv_stack(torch.zeros((2, 1)), torch.zeros((2, 1)))
     assert v._pools == [None, pool] and v.kv == [None, None] and v.kv_q4 == [None, kv]
+
+
+def test_representatives_of_a_4_bit_layer_are_not_rebuilt():
+    v = _bare(2, kv_q4=[None, object()], geom=None, reps=[None, None])
+    with pytest.raises(TypeError, match="build_reps: .*4-bit"):
+        v.build_reps(1)
