@@ -123,7 +123,7 @@ def generate(prompts, new, layers=4, chunk=512, seed=0, temperature=0.8, top_p=0
         path, n_path, root = verifier.accept(p_target, p_draft, tokens, rand(S, DRAFT), rand(S))
         verifier.commit(draft_k, draft_v, path, n_path)
         if most and int(verifier.seq_lens.max()) > most:
-            verifier.evict(per_seq(most * 3 // 4, torch.int32))
+            verifier.evict(torch.where(verifier.seq_lens > most, most * 3 // 4, verifier.seq_lens).int())
         verifier.check_status()
         for s in range(S):
             texts[s] += tokens[s, 1:int(n_path[s])].tolist() + [int(root[s])]

@@ -27,3 +27,15 @@ def test_representatives_of_a_4_bit_layer_are_not_rebuilt():
     v = _bare(2, kv_q4=[None, object()], geom=None, reps=[None, None])
     with pytest.raises(TypeError, match="build_reps: .*4-bit"):
         v.build_reps(1)
+
+
+@pytest.mark.gpu
+def test_the_example_evicts_from_the_sequences_that_are_too_long():
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import generate as example
+    lens = [500, 260]
+    _, _, verifier = example.generate([list(range(n)) for n in lens], new=4, layers=1, most=300)
+    assert int(verifier.evicted[0]) >= 200 and int(verifier.evicted[1]) == 0
+    assert 260 < int(verifier.seq_lens[1]) <= 300 and verifier.seq_lens.tolist() == (verifier.positions() - verifier.evicted).tolist()
