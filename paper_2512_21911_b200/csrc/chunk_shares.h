@@ -43,6 +43,7 @@ struct ChunkWalk {
     int shares, mine;
     int s, h, t, n, row, prefix, tiles;   // next item: sequence (its tokens, first row, tokens cached before, items per head), KV head, number
 
+    static constexpr int kLeast = -(1 << 30);   // further below zero than a call has tokens
     SV_HD explicit ChunkWalk(const ChunkBatch &b) : b(b) {}
     SV_HD static long long least(long long x, long long y) { return x < y ? x : y; }
     SV_HD int start(int i) const
@@ -54,7 +55,8 @@ struct ChunkWalk {
     {
         s = i, row = start(i), n = start(i + 1) - row;
         if (n < 0) n = 0;
-        prefix = b.seq_lens[i] - n, tiles = (n + 2 * b.TT - 1) / (2 * b.TT);
+        const long long ahead = (long long)b.seq_lens[i] - n;   // (what is far below zero is as good there)
+        prefix = ahead < kLeast ? kLeast : (int)ahead, tiles = (n + 2 * b.TT - 1) / (2 * b.TT);
     }
     SV_HD long long seen_before() const { return prefix < 0 ? 0 : least(prefix, b.cap); }
     // cost of a key of item i of a KV head, of the items before it (two tiles each), of itself, of all of them

@@ -105,7 +105,7 @@ __device__ __forceinline__ Place place(const Params &p, int e)
     r.len = min(max(len, 0), cap);
     if constexpr (kChunk) {
         const int first = min(max(__ldg(p.q_start + r.s), 0), p.n_tokens), end = min(max(__ldg(p.q_start + r.s + 1), 0), p.n_tokens);
-        r.tok0 = first, r.n = max(end - first, 0), r.pos0 = len - r.n;
+        r.tok0 = first, r.n = max(end - first, 0), r.pos0 = (int)max((long long)len - r.n, -(1ll << 30));   // (further below zero than a call has tokens)
         r.slabs = 0;
         const int seen = min(max(r.pos0, 0), cap);
         r.cost.tiles = (int)(((long long)r.n * p.G + N - 1) / N);
