@@ -12,8 +12,6 @@
 #include <cuda.h>
 #include <cuda_bf16.h>
 
-#include <algorithm>
-
 #include "attn_common.cuh"
 #include "shares.cuh"
 #include "sv_host.h"
@@ -58,7 +56,7 @@ __device__ __forceinline__ Place place(const Params &p, int e)
     Place r;
     r.s = e / p.Hkv, r.h = e - r.s * p.Hkv;
     r.len = min(max(__ldg(p.seq_lens + r.s), 0), (int)min((long long)p.NBmax * p.B, 0x7fffffffll));
-    r.cnt = p.sel_idx ? min(max(__ldg(p.sel_cnt + e), 0), p.max_sel) : 0;
+    r.cnt = p.sel_idx ? min(max(__ldg(p.sel_cnt + e), 0), min(p.max_sel, svq::kMostBlocks)) : 0;
     r.slabs = p.sel_idx ? r.cnt * (p.B / 64) : (r.len + 63) / 64;
     r.cost = svq::kItemCost + (long long)kUnit * ((r.slabs + 1) / 2);
     return r;
@@ -398,7 +396,7 @@ extern "C" sv_status sv_attn_weights(const sv_geom *geom, const void *q, const s
     if (!svh::aligned(q, 16) || !svh::aligned(weights, 16) || !svh::aligned(weights_out, 16)) return SV_ERR_ALIGN;
     Params p = {};
     p.block_table = kv->block_table, p.seq_lens = kv->seq_lens, p.n_pages = kv->n_pages;
-    p.sel_idx = sel_idx, p.sel_cnt = sel_cnt, p.max_sel = std::min(max_sel, 1 << 24), p.path = path, p.n_path = n_path;
+    p.sel_idx = sel_idx, p.sel_cnt = sel_cnt, p.max_sel = max_sel, p.path = path, p.n_path = n_path;
     p.q = static_cast<const __nv_bfloat16 *>(q), p.lse = lse, p.before = weights, p.after = weights_out, p.status = status_word;
     p.S = geom->n_seq, p.Hq = geom->n_q_heads, p.Hkv = geom->n_kv_heads, p.G = p.Hq / p.Hkv, p.T = geom->n_draft, p.B = geom->block_size,
     p.NBmax = geom->max_blocks;

@@ -113,7 +113,7 @@ __device__ __forceinline__ Place place(const Params &p, int e)
     } else {
         r.tok0 = r.s * p.T, r.n = p.T, r.pos0 = 0;
         if (p.sel_idx) {
-            const int cnt = min(max(__ldg(p.sel_cnt + e), 0), p.max_sel);
+            const int cnt = min(max(__ldg(p.sel_cnt + e), 0), min(p.max_sel, svq::kMostBlocks));
             r.slabs = cnt * (p.B / 64);
         } else {
             r.slabs = (r.len + 63) / 64;
@@ -950,7 +950,7 @@ extern "C" sv_status sv_verify_attn_q4(const sv_geom *geom, const void *q, const
     st = common(geom, kv, q, softmax_scale, out, lse, workspace, workspace_bytes, status_word, p);
     if (st != SV_OK) return st;
     p.draft_k = static_cast<const __nv_bfloat16 *>(draft_k), p.draft_v = static_cast<const __nv_bfloat16 *>(draft_v), p.parent = parent;
-    p.sel_idx = sel_idx, p.sel_cnt = sel_cnt, p.max_sel = std::min(max_sel, 1 << 24), p.T = geom->n_draft;
+    p.sel_idx = sel_idx, p.sel_cnt = sel_cnt, p.max_sel = max_sel, p.T = geom->n_draft;
     const Spread spread(geom);
     const Decoded d(geom, spread, (int64_t)p.G * p.T, workspace, workspace_bytes, sv_workspace_bytes(geom, sel_idx ? max_sel : geom->max_blocks));
     if (d.use && (!sel_idx || max_sel <= geom->max_blocks)) {

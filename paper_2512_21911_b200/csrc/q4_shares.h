@@ -18,6 +18,7 @@
 namespace svq {
 
 constexpr int kUnit = 128;        // keys of a unit, the grain of a cut
+constexpr int kMostBlocks = 1 << 25;   // blocks that a table of less than 2^31 tokens may have, and a list that names none twice
 constexpr int kItemCost = 128;    // keys that the beginning and the end of an item cost as much as
 
 struct Entry {
