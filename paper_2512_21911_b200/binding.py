@@ -330,8 +330,8 @@ def sv_rope_append_at(geom: sv_geom, k_pool, v_pool, block_table, seq_lens, posi
                       interleaved: bool = False, reps=None, status_word=None, stream=None) -> None:
     """sv_rope_append for a cache that has lost tokens: positions (int32 [S], or None: seq_lens) are those of the sequences' first new
     tokens, for the rotation; they are written behind the seq_lens tokens that the cache holds."""
-    _check(_native.rope_append(geom, k_pool, v_pool, block_table, seq_lens, q, k, v, q_start, q_out, seq_lens_out, rope, interleaved,
-                               reps, status_word, stream, positions), "sv_rope_append_at")
+    _check(_native.rope_append_at(geom, k_pool, v_pool, block_table, seq_lens, q, k, v, q_start, q_out, seq_lens_out, rope, interleaved,
+                                  reps, status_word, stream, positions), "sv_rope_append_at")
 
 
 def sv_chunk_workspace_bytes(geom: sv_geom, n_tokens: int) -> int:

@@ -579,7 +579,6 @@ void has(const at::Tensor &t, int64_t numel, const char *call)
     if (t.numel() != numel) shapes_disagree(call);
 }
 
-// geom, k_pool, v_pool, block_table, seq_lens, q, k, v, q_start, q_out, seq_lens_out, rope, interleaved, reps, status_word, stream
 // pages of a 4-bit pool [n_pages][Hkv][B / 64][SV_Q4_SLAB_BYTES]
 const at::Tensor &pool_q4(PyObject *o, const sv_geom &g, const char *call)
 {
@@ -588,11 +587,11 @@ const at::Tensor &pool_q4(PyObject *o, const sv_geom &g, const char *call)
         shapes_disagree(call);
     return t;
 }
-// k_pool, v_pool; of a 4-bit cache pool, None
-PyObject *append_rows(PyObject *const *a, Py_ssize_t n, bool q4)
+// geom, k_pool, v_pool (of a 4-bit cache pool, None), block_table, seq_lens, q, k, v, q_start, q_out, seq_lens_out, rope, interleaved, reps,
+// status_word, stream, positions
+PyObject *append_rows(PyObject *const *a, Py_ssize_t n, bool q4, const char *call)
 {
     return checked(n, 17, [&] {
-        const char *const call = q4 ? "sv_rope_append_q4" : "sv_rope_append";
         const sv_geom g = geometry(a[0]);
         const at::Tensor &kp = q4 ? pool_q4(a[1], g, call) : tensor(a[1], at::kBFloat16, "k_pool");
         const at::Tensor &vp = q4 ? kp : tensor(a[2], at::kBFloat16, "v_pool");
@@ -641,9 +640,10 @@ PyObject *append_rows(PyObject *const *a, Py_ssize_t n, bool q4)
     });
 }
 
-// geom, q, kv, q_start, out, lse, workspace, softmax_scale, status_word, stream
-PyObject *rope_append(PyObject *, PyObject *const *a, Py_ssize_t n) { return append_rows(a, n, false); }
-PyObject *rope_append_q4(PyObject *, PyObject *const *a, Py_ssize_t n) { return append_rows(a, n, true); }
+PyObject *rope_append(PyObject *, PyObject *const *a, Py_ssize_t n) { return append_rows(a, n, false, "sv_rope_append"); }
+PyObject *rope_append_at(PyObject *, PyObject *const *a, Py_ssize_t n) { return append_rows(a, n, false, "sv_rope_append_at"); }
+PyObject *rope_append_q4(PyObject *, PyObject *const *a, Py_ssize_t n) { return append_rows(a, n, true, "sv_rope_append_q4"); }
+
 // geom, pool, block_table, seq_lens, draft_k, draft_v, accept_idx, n_accept, seq_lens_out, reps, stream
 PyObject *kv_append_q4(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
@@ -731,6 +731,7 @@ PyObject *verify_attn_q4(PyObject *, PyObject *const *a, Py_ssize_t n)
         }));
     });
 }
+// geom, q, kv, q_start, out, lse, workspace, softmax_scale, status_word, stream
 PyObject *chunk_rows(PyObject *const *a, Py_ssize_t n, bool q4)
 {
     return checked(n, 10, [&] {
@@ -869,7 +870,7 @@ PyObject *sample(PyObject *, PyObject *const *a, Py_ssize_t n)
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(block_reps), METHOD(select_blocks), METHOD(verify_attn), METHOD(kv_append), METHOD(accept),
                          METHOD(verify_layer), METHOD(layer_row), METHOD(workspace_bytes_layers), METHOD(workspace_bytes_host_step), METHOD(block_reps_layers),
-                         METHOD(verify_layers), METHOD(kv_append_layers), METHOD(accept_new), METHOD(host_step), METHOD(verify_step_from_host), METHOD(rope_append),
+                         METHOD(verify_layers), METHOD(kv_append_layers), METHOD(accept_new), METHOD(host_step), METHOD(verify_step_from_host), METHOD(rope_append), METHOD(rope_append_at),
                          METHOD(chunk_attn), METHOD(sample), METHOD(rope_append_q4), METHOD(kv_append_q4), METHOD(kv_read_q4), METHOD(verify_attn_q4), METHOD(chunk_attn_q4),
                          METHOD(attn_weights), METHOD(kv_evict),
                          {nullptr, nullptr, 0, nullptr}};

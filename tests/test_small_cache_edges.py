@@ -39,3 +39,16 @@ def test_the_example_evicts_from_the_sequences_that_are_too_long():
     _, _, verifier = example.generate([list(range(n)) for n in lens], new=4, layers=1, most=300)
     assert int(verifier.evicted[0]) >= 200 and int(verifier.evicted[1]) == 0
     assert 260 < int(verifier.seq_lens[1]) <= 300 and verifier.seq_lens.tolist() == (verifier.positions() - verifier.evicted).tolist()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", ["sv_rope_append", "sv_rope_append_at", "sv_rope_append_q4"])
+def test_an_append_that_does_not_fit_is_named(name):
+    import paper_2512_21911_b200 as sv
+    rows, ints = (lambda *s: torch.zeros(s, dtype=torch.bfloat16, device="cuda")), (lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda"))
+    geom, pools = sv.make_geom(2, 4, 2, 128, 64, 5, 1), [rows(10, 2, 64, 128), rows(10, 2, 64, 128)]
+    if name == "sv_rope_append_q4":
+        pools = [torch.zeros((10, 2, 1, sv.SV_Q4_SLAB_BYTES), dtype=torch.uint8, device="cuda")]
+    lens = [ints(3)] + ([None] if name == "sv_rope_append_at" else [])      # lengths of three sequences for two
+    with pytest.raises(Exception, match=name + r"\b"):
+        getattr(sv, name)(geom, *pools, ints(2, 5), *lens, None, rows(1, 2, 128), rows(1, 2, 128), ints(3), None, ints(2))
