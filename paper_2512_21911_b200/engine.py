@@ -498,19 +498,36 @@ class SparseVerifier:
         splits that a cluster merges do not have; two launches where the rest of a batch goes by itself.  A sparse step's own number
         is launches_per_step."""
         splits = sv.sv_verify_attn_splits(self.geom, self.geom.max_blocks if dense else self.max_sel)
-        attn = self.n_layers * (2 if splits > 1 else 1)
+        bits4 = [kv is not None for kv in self.kv_q4]
+        attn = 2 if splits > 1 else 1
+        if not dense:
+            attn = max(attn, sv.sv_verify_attn_launches(self.geom, self.max_sel))
+        attn = (self.n_layers - sum(bits4)) * attn + sum(bits4) * self._q4_launches(dense)
         if dense:
             return attn
-        attn = max(attn, self.n_layers * sv.sv_verify_attn_launches(self.geom, self.max_sel))
-        refresh = 0 if not refresh_tail else (1 if self._stacked() else sum(self.anchors))
-        return refresh + sum(self.anchors) + attn
+        return self._refreshed(refresh_tail) + sum(map(bool, self.anchors)) + attn
+
+    def _refreshed(self, refresh_tail: bool) -> int:
+        """Launches of a tail refresh."""
+        if not refresh_tail or self._stacked():
+            return int(refresh_tail)
+        return sum(bool(a) and kv is None for a, kv in zip(self.anchors, self.kv_q4))
+
+    def _q4_launches(self, dense: bool = False) -> int:
+        """Launches of sv_verify_attn_q4: the attention and its merge, or, for more than 64 query rows and in a workspace that has room, the
+        decoding and what sv_verify_attn makes of its pages."""
+        g, n = self.geom, self.geom.max_blocks if dense else self.max_sel
+        room = sv.sv_workspace_bytes_q4(g) >= sv.sv_workspace_bytes_q4(sv.make_geom(1, 1, 1, g.head_dim, 64, 1, 1))   # (else that of no decoded cache)
+        if g.n_q_heads // g.n_kv_heads * g.n_draft <= 64 or n > g.max_blocks or not room:
+            return 2
+        return 2 if dense and sv.sv_verify_attn_splits(g, n) == 1 else 1 + sv.sv_verify_attn_launches(g, n)
 
     def launches_per_step(self, refresh_tail: bool = False) -> int:
         """Kernel launches of one sparse step taken layer by layer, each behind its own preceding layer (verify_layer with
         behind_own_layer, as in verify_step), as they are made on this device."""
-        refresh = 0 if not refresh_tail else (1 if self._stacked() else sum(self.anchors))
         selecting = sv.sv_verify_attn_launches(self.geom, self.max_sel)
         # (a reused list of more lists than SMs has no second launch for the rest, see sv_verify_attn_launches)
         reusing = 1 if sv.sv_verify_attn_splits(self.geom, self.max_sel) == 1 else selecting
-        n = sum(map(bool, self.anchors))
-        return refresh + n + n * selecting + (self.n_layers - n) * reusing
+        bits4 = self._q4_launches() if any(kv is not None for kv in self.kv_q4) else 0
+        attn = sum(bits4 if kv is not None else selecting if a else reusing for a, kv in zip(self.anchors, self.kv_q4))
+        return self._refreshed(refresh_tail) + sum(map(bool, self.anchors)) + attn
