@@ -428,14 +428,16 @@ class SparseVerifier:
         zeroes its entry of evicted."""
         if any(kv is None for kv in self.kv):
             raise TypeError("evict: a layer has no bfloat16 pools")
+        if self.evicted is None or any(w is None for w in self.weights):   # (all of this ahead of the first launch: a capture that is refused has none)
+            self._outside_of_capture()
+            for l in range(self.n_layers):
+                self._weights_of(l)
+            if self.evicted is None:
+                self.evicted = torch.zeros_like(self.seq_lens)
         g, new_len = self.geom, torch.empty_like(self.seq_lens)
-        for l in range(self.n_layers):
-            w = self._weights_of(l)
+        for l, w in enumerate(self.weights):
             sv.sv_kv_evict(g, *self._pools[l], self.block_table, self.seq_lens, w, budget_tokens, n_sink, n_recent, new_len, w, reps=self.reps[l],
                            status_word=self.status)
-        if self.evicted is None:
-            self._outside_of_capture()
-            self.evicted = torch.zeros_like(self.seq_lens)
         self.evicted += self.seq_lens - new_len
         self.seq_lens.copy_(new_len)          # every layer has read the old lengths by now (same stream)
 

@@ -52,3 +52,29 @@ def test_an_append_that_does_not_fit_is_named(name):
     lens = [ints(3)] + ([None] if name == "sv_rope_append_at" else [])      # lengths of three sequences for two
     with pytest.raises(Exception, match=name + r"\b"):
         getattr(sv, name)(geom, *pools, ints(2, 5), *lens, None, rows(1, 2, 128), rows(1, 2, 128), ints(3), None, ints(2))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("weighed", [0, 1, 3])
+def test_an_eviction_that_is_refused_in_a_capture_leaves_nothing_in_it(weighed):
+    """The first evict, whichever layers have weights already: a replay of what was captured around it changes no cache."""
+    from test_small_cache_engine import HQ, L, T, _ints, _normal, _prefill, _rope, _verifier
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    v, pools = _verifier(2, 7, False, 3)
+    _prefill(v, gen, [300, 64], _rope(400))
+    q, lse, count = _normal(gen, 2, T, HQ, 128), torch.full((2, T, HQ), 9.0, device="cuda"), torch.zeros(1, device="cuda")
+    for l in range(weighed):
+        v.weigh_layer(l, q, lse, dense=True)
+    before, budget = [p.view(torch.int16).clone() for p in pools], _ints([100, 100])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(RuntimeError):
+            v.evict(budget)
+        count += 1
+    graph.replay()
+    torch.cuda.synchronize()
+    assert float(count) == 1.0 and all(torch.equal(p.view(torch.int16), b) for p, b in zip(pools, before))
+    assert v.evicted is None and v.seq_lens.tolist() == [300, 64] and [w is None for w in v.weights] == [l >= weighed for l in range(L)]
+    v.evict(budget)
+    assert v.seq_lens.tolist() == [100, 64] and v.positions().tolist() == [300, 64]
