@@ -395,7 +395,7 @@ class SparseVerifier:
 
     def positions(self) -> torch.Tensor:
         """Position of every sequence's next token: the tokens that the cache holds and those that it has lost (int32 [S])."""
-        return self.seq_lens if self.evicted is None else self.seq_lens + self.evicted
+        return self.seq_lens.clone() if self.evicted is None else self.seq_lens + self.evicted
 
     @staticmethod
     def _outside_of_capture() -> None:

@@ -78,3 +78,12 @@ def test_an_eviction_that_is_refused_in_a_capture_leaves_nothing_in_it(weighed):
     assert v.evicted is None and v.seq_lens.tolist() == [300, 64] and [w is None for w in v.weights] == [l >= weighed for l in range(L)]
     v.evict(budget)
     assert v.seq_lens.tolist() == [100, 64] and v.positions().tolist() == [300, 64]
+
+
+def test_positions_are_the_callers_own():
+    """A step forward in place does not change the lengths of the cache, whether tokens were evicted or not."""
+    for evicted in (None, torch.tensor([5, 0], dtype=torch.int32)):
+        v = _bare(1, seq_lens=torch.tensor([3, 7], dtype=torch.int32), evicted=evicted)
+        p = v.positions()
+        p += 1
+        assert v.seq_lens.tolist() == [3, 7] and p.tolist() == ([4, 8] if evicted is None else [9, 8])
