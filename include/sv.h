@@ -609,9 +609,9 @@ SV_API sv_status sv_kv_read_q4(const sv_geom *geom, const sv_kv_q4 *kv, const in
  * value of NaN or infinity that a row sees has, with a weight of zero too; the values of later tokens of a chunk's call have to be finite).
  *   workspace       dev scratch of sv_workspace_bytes_q4(geom) bytes, 16-byte aligned, for any call with this geometry.  Where a sequence has
  *                   more than 64 query rows a KV head (drafts times query heads; of a ragged batch on average) the cache is decoded into it
- *                   first, up to 256 MB of bf16 pages, and sv_verify_attn or sv_chunk_attn go over those; in as little as
- *                   sv_workspace_bytes_q4 gives for a geometry of one sequence, head and block, or beyond 256 MB, every 64 rows
- *                   decode what they go over
+ *                   first, up to 256 MB of bf16 pages (of all blocks that the table has room for), and sv_verify_attn or sv_chunk_attn go
+ *                   over those; in as little as sv_workspace_bytes_q4 gives for a geometry of one sequence, head and block, or beyond
+ *                   256 MB, every 64 rows decode what they go over
  * softmax_scale: 0 selects 1 / sqrt(D), not negative (SV_ERR_SHAPE).
  */
 SV_API size_t sv_workspace_bytes_q4(const sv_geom *geom);

@@ -3,8 +3,8 @@
 // Mathematics: of a KV head's L tokens the first n_sink and the last n_recent stay, and of the others the heaviest until there are n of
 // them (equal ones: the earlier first).  n is the same for all heads of a sequence, so that the block table and one length stay what the
 // cache is described by.  Bound by HBM for long caches (weights once, 512 bytes of keys and values of a moved token read and written), by
-// rendezvous for short ones.  8 K of 32 K tokens, 8 KV heads (70 MB): 40.9 us, 15 of them until the tokens are known; 16 sequences of 4 K to
-// 16 K tokens halved (288 MB): 116 us, 38 % of a copy's rate.
+// rendezvous for short ones.  8 K of 32 K tokens, 8 KV heads (70 MB): 41.0 us, 15 of them until the tokens are known; 16 sequences of 4 K to
+// 16 K tokens halved (288 MB): 117 us, 38 % of a copy's rate.
 //
 // A cluster of CTAs has a (sequence, KV head).  Each CTA holds the order keys of a slice of the tokens in shared memory; the n-th largest
 // is found by four passes of a histogram over eight bits, which the CTAs add up through distributed shared memory; each CTA then

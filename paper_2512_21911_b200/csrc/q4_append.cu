@@ -1,9 +1,9 @@
 // sv_rope_append_q4, sv_kv_append_q4, sv_kv_read_q4: rows of keys and values into a paged cache held in 4 bits (q4.cuh), and back.
 //
 // Mathematics: the rotation of sv_rope_append; a row's two groups of 64 values as scale, offset and codes; the representatives are the means
-// of what the cache then holds.  Bound by HBM in a prompt (the queries, which are only rotated, are most of it), by a chain of loads in a
-// decoding step.  A prompt of 16,384 tokens (32 query heads, 8 KV heads; 450 MB) takes 154 us with its reading back, 45 % of a copy's rate; a token
-// each of 64 sequences 20 us.
+// of what the cache then holds.  A prompt of 16,384 tokens (32 query heads, 8 KV heads; 450 MB) takes 154 us with its reading back, 45 % of a
+// copy's rate: neither HBM (28 %) nor the issue slots (63 %) is full, a slab's loads, coding and turn come one behind the other.  A token each of 64
+// sequences takes 20 us, a chain of loads and of the coding's steps.
 //
 // A CTA has a block of a sequence and a KV head, as in sv_rope_append: 16 threads hold a row, eight of them a group, so that its smallest
 // and largest value are three shuffles away and a thread's eight codes are one word.  The keys' words go to the page as they are; those of

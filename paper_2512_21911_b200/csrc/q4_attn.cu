@@ -41,7 +41,10 @@ using svq::kUnit;
 // What a score may exceed its reference by (log2).  Weights up to 2^24 cost no precision (o / l does not depend on the reference, and bf16 and
 // fp32 have the same exponents), and a reference that moves costs as much as a unit.
 constexpr float kLag = 24.f;
-constexpr int kSpreadRows = 64;   // query rows of a sequence and KV head, on average, beyond which the cache is decoded first
+// Query rows of a sequence and KV head, on average, beyond which the cache is decoded first.  Both ways with nothing in L2, here and decoded first: 64 blocks of a
+// 32 K sequence, 68 rows 33 and 18 us, 256 rows 49 and 22; 256 blocks 55 and 33, 90 and 44; all of 4 K tokens 33 and 17, 49 and 21.  One tile of rows
+// is where measuring began: at 64 rows over 64 blocks 38 us here, and decoding (3.6) and the attention of its pages (13.5) are less, too.
+constexpr int kSpreadRows = 64;
 
 struct Params {
     const uint8_t *pool;
