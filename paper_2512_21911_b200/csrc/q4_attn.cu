@@ -987,6 +987,7 @@ extern "C" sv_status sv_chunk_attn_q4(const sv_geom *geom, const void *q, const 
         const sv_kv pages = {d.k, d.v, d.table, kv->seq_lens, geom->n_seq * geom->max_blocks};
         return sv_chunk_attn(geom, q, &pages, q_start, n_tokens, softmax_scale, out, lse, d.scratch, spread.scratch, status_word, stream);
     }
-    // (the mean rows of a sequence: a batch of single tokens with a few chunks is taken as chunks)
+    // (By the mean rows of a sequence, which is what the host knows: a chunk among many single tokens has their narrow tiles.  One of 513 tokens behind 30,000
+    // among 127 single tokens behind 1,000 takes 771 us, over bf16 pages 376.)
     return launch_rows<true>(p, (int64_t)p.G * ((n_tokens + geom->n_seq - 1) / geom->n_seq), workspace, stream);
 }
